@@ -217,6 +217,92 @@ int ecspmv_run_batch(const ecspmv_matrix *const *As, const void *const *d_xs, vo
  * build options produce neither), or if not even two right-hand sides fit LDS; ECSPMV_ERR_INVALID for other nb. */
 int ecspmv_run_multi(const ecspmv_matrix *A, const void *d_X, void *d_Y, int32_t nb, void *stream);
 
+/* ---- around the products: cache of keys and values, attention, drafted tokens ------------------------ */
+/* No passage of the paper: what a decoder does between and after the products with pruned weights.  FP16 throughout
+ * (an FP32 model rounds its keys, values and queries first).  Every call is asynchronous on `stream`, allocates nothing,
+ * synchronises nothing and can be captured in a graph; lengths, pages and places are read from device memory when the
+ * kernels run. */
+
+/* (token, head, element) -> data[token * token_stride + head * head_stride + element * dim_stride]; strides in elements,
+ * of any sign.  Rows of head_dim neighbouring values (dim_stride 1) that start on 16 bytes are read and written 16 bytes
+ * at a time.  The (heads * head_dim, nb) result of a product with nb right-hand sides is token_stride 1, head_stride
+ * head_dim * nb, dim_stride nb. */
+typedef struct ecspmv_view_t {
+    void    *data;                          /* device, FP16, 2-byte aligned */
+    int64_t  token_stride, head_stride, dim_stride;
+} ecspmv_view_t;
+
+/* A cache of keys and values in pages.  k, v: device, 16-byte aligned, [pages][heads][page_size][head_dim] values of
+ *   bits = 16: FP16;
+ *   bits = 8:  signed codes in [-127, 127], value = step * code, step = max|x| / 127 of the token and head;
+ *              k_step, v_step: [pages][heads][page_size] float;
+ *   bits = 4:  codes in [0, 15], two to a byte, the earlier one in the low half, value = low + step * code, low = min x,
+ *              step = (max x - min x) / 15; k_step, v_step: [pages][heads][page_size][2] FP16 (step, low).
+ * In 8 and 4 bits NaN counts as 0 and an infinity as the largest FP16 value of its sign. */
+typedef struct ecspmv_kv_cache_t {
+    uint32_t struct_size;                   /* sizeof(ecspmv_kv_cache_t) as the caller compiled it */
+    int32_t  bits;                          /* 16, 8 or 4 */
+    int64_t  pages;                         /* >= 1 */
+    int32_t  heads, page_size, head_dim;    /* page_size: a power of two in [16, 1024]; head_dim: a multiple of 16 in [16, 256] */
+    void    *k, *v, *k_step, *v_step;       /* steps: 16-byte aligned; NULL with 16 bits */
+} ecspmv_kv_cache_t;
+
+/* Write `tokens` keys and values into their places: d_slots (device, one per token) is page * page_size + place in the
+ * page; a slot outside the cache (a negative one, say) leaves its token out.  Two tokens must not have the same slot.
+ * One launch (none for no tokens). */
+int ecspmv_kv_write(const ecspmv_kv_cache_t *cache, const ecspmv_view_t *k, const ecspmv_view_t *v, const int64_t *d_slots,
+                    int64_t tokens, void *stream);
+
+/* Read them back as FP16 values; a slot outside the cache gives zeros. */
+int ecspmv_kv_read(const ecspmv_kv_cache_t *cache, const int64_t *d_slots, int64_t tokens, const ecspmv_view_t *k,
+                   const ecspmv_view_t *v, void *stream);
+
+/* Attention of the new tokens of `batch` sequences over a cache that already holds their keys and values (ecspmv_kv_write).
+ * Sequence b has the tokens q_start[b] ... q_start[b + 1] - 1 of q and out (device int32, batch + 1 entries, not decreasing)
+ * and kv_len[b] keys in all (device int32), the new tokens' own last; its key i is in page page_table[b * table_stride +
+ * i / page_size] (device int32), place i % page_size.  Token t of its n new tokens sees the keys up to kv_len - n + t and
+ *   out = sum_i softmax_i(scale * q . k_i) v_i
+ * with sums and softmax in FP32; a token that sees no key gets zeros.  Head h of q reads head h / (q_heads / heads) of the
+ * cache.  max_new is at least every sequence's number of new tokens (it shapes the launch).  Lengths beyond max_pages *
+ * page_size count as that, page numbers outside the cache as a page of it.  What lies in the cache beyond kv_len has no
+ * effect, nor have infinities and NaN in V on tokens that do not see them.  out must not overlap q.
+ * One launch, or two where long sequences are split for want of rows: then d_work (device, 16-byte aligned, at least
+ * ecspmv_attention_workspace bytes, contents of no matter before and after) is used; it may be NULL where 0 bytes are
+ * asked for.  The result has the same bits every time. */
+typedef struct ecspmv_attention_t {
+    uint32_t struct_size;                   /* sizeof(ecspmv_attention_t) as the caller compiled it */
+    int32_t  q_heads;                       /* a multiple of the cache's heads */
+    int64_t  tokens;                        /* rows of q and out */
+    int32_t  batch, max_pages, max_new;
+    float    scale;
+    int64_t  table_stride;                  /* from one sequence's pages to the next's, in entries, >= max_pages */
+    const int32_t *q_start, *kv_len, *page_table;
+    ecspmv_view_t q, out;
+} ecspmv_attention_t;
+
+int ecspmv_attention_workspace(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *a, size_t *bytes);
+int ecspmv_attention(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *a, void *d_work, size_t work_bytes, void *stream);
+
+/* The check of drafted tokens.  Sequence b has drafted[b][0 ... count[b] - 1] (device int32, `drafts` to a row; count: device
+ * int32, NULL for `drafts` each), target probabilities target[b][i][token] (device FP32, drafts + 1 rows of `vocab`), the
+ * drafts' own draft[b][i][token] (device FP32, `drafts` rows; NULL where a draft was certain, probability 1) and random
+ * numbers uniform[b][0 ... drafts] in [0, 1) (device FP32).  Draft i is accepted while
+ *   uniform[i] * draft[i][x_i] < target[i][x_i]
+ * and with n accepted the next token is the first v at which the running sum of w passes uniform[drafts] * sum(w), where
+ * w = max(target[n] - draft[n], 0) after a refusal (target[n] where that leaves nothing) and w = target[n] without one.
+ * Differences and sums are in 64 bits.  accepted[b] = n; tokens[b][0 ... drafts] (device int32) = the accepted drafts, the next token,
+ * then -1 (also in the next token's place if target[n] has nothing above 0).  A drafted token outside [0, vocab) is
+ * refused.  *_seq, *_row: strides in elements from one sequence, resp. row, to the next. */
+typedef struct ecspmv_verify_t {
+    uint32_t struct_size;                   /* sizeof(ecspmv_verify_t) as the caller compiled it */
+    int32_t  batch, drafts, vocab;          /* drafts >= 0; vocab in [1, 2^20] */
+    const float *target, *draft, *uniform;
+    int64_t  target_seq, target_row, draft_seq, draft_row;
+    const int32_t *drafted, *count;
+    int32_t *tokens, *accepted;
+} ecspmv_verify_t;
+int ecspmv_verify(const ecspmv_verify_t *a, void *stream);
+
 /* ---- comparison: plain CSR (int32 column index + FP16 value per entry, one wavefront per row) ------- */
 /* The CSR-32 format the paper's Section 8.2 measures storage against, with a kernel of its own (not one of the
  * paper's comparison libraries). */

@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, Structure, byref, c_char_p, c_double, c_int, c_int32, c_int64, c_size_t, c_uint32, c_uint64, c_void_p
+from ctypes import POINTER, Structure, byref, c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_size_t, c_uint32, c_uint64, c_void_p
 
 import numpy as np
 
@@ -26,6 +26,7 @@ EXPORTS = (
     "ecspmv_stats", "ecspmv_decode", "ecspmv_decode_f32",
     "ecspmv_block_sets", "ecspmv_device_bytes", "ecspmv_export_image", "ecspmv_upload", "ecspmv_run", "ecspmv_run_batch", "ecspmv_run_multi",
     "ecspmv_csr_build_dense", "ecspmv_csr_destroy", "ecspmv_csr_device_bytes", "ecspmv_csr_upload",
+    "ecspmv_kv_write", "ecspmv_kv_read", "ecspmv_attention_workspace", "ecspmv_attention", "ecspmv_verify",
     "ecspmv_csr_run", "ecspmv_stream_read", "ecspmv_stream_read_sliced", "ecspmv_empty_launch", "ecspmv_strerror", "ecspmv_last_hip_error",
 )
 
@@ -53,6 +54,28 @@ class Stats(Structure):
             v = getattr(self, name)
             out[name] = list(v) if hasattr(v, "__len__") else v
         return out
+
+
+class View(Structure):
+    """Where (token, head, element) lies: strides in elements."""
+    _fields_ = [("data", c_void_p), ("token_stride", c_int64), ("head_stride", c_int64), ("dim_stride", c_int64)]
+
+
+class KvCacheDesc(Structure):
+    _fields_ = [("struct_size", c_uint32), ("bits", c_int32), ("pages", c_int64), ("heads", c_int32), ("page_size", c_int32),
+                ("head_dim", c_int32), ("k", c_void_p), ("v", c_void_p), ("k_step", c_void_p), ("v_step", c_void_p)]
+
+
+class AttentionDesc(Structure):
+    _fields_ = [("struct_size", c_uint32), ("q_heads", c_int32), ("tokens", c_int64), ("batch", c_int32), ("max_pages", c_int32),
+                ("max_new", c_int32), ("scale", c_float), ("table_stride", c_int64), ("q_start", c_void_p), ("kv_len", c_void_p),
+                ("page_table", c_void_p), ("q", View), ("out", View)]
+
+
+class VerifyDesc(Structure):
+    _fields_ = [("struct_size", c_uint32), ("batch", c_int32), ("drafts", c_int32), ("vocab", c_int32), ("target", c_void_p),
+                ("draft", c_void_p), ("uniform", c_void_p), ("target_seq", c_int64), ("target_row", c_int64), ("draft_seq", c_int64),
+                ("draft_row", c_int64), ("drafted", c_void_p), ("count", c_void_p), ("tokens", c_void_p), ("accepted", c_void_p)]
 
 
 class EcspmvError(RuntimeError):
@@ -97,6 +120,11 @@ def lib() -> ctypes.CDLL:
     L.ecspmv_run.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p]
     L.ecspmv_run_batch.argtypes = [c_void_p, c_void_p, c_void_p, c_int32, c_void_p]
     L.ecspmv_run_multi.argtypes = [c_void_p, c_void_p, c_void_p, c_int32, c_void_p]
+    L.ecspmv_kv_write.argtypes = [POINTER(KvCacheDesc), POINTER(View), POINTER(View), c_void_p, c_int64, c_void_p]
+    L.ecspmv_kv_read.argtypes = [POINTER(KvCacheDesc), c_void_p, c_int64, POINTER(View), POINTER(View), c_void_p]
+    L.ecspmv_attention_workspace.argtypes = [POINTER(KvCacheDesc), POINTER(AttentionDesc), POINTER(c_size_t)]
+    L.ecspmv_attention.argtypes = [POINTER(KvCacheDesc), POINTER(AttentionDesc), c_void_p, c_size_t, c_void_p]
+    L.ecspmv_verify.argtypes = [POINTER(VerifyDesc), c_void_p]
     L.ecspmv_csr_build_dense.argtypes = [c_void_p, c_int64, c_int64, c_int64, POINTER(c_void_p)]
     L.ecspmv_csr_destroy.argtypes = [c_void_p]
     L.ecspmv_csr_destroy.restype = None
@@ -351,3 +379,27 @@ def ecspmv_stream_read_sliced(d_buf: int, nbytes: int, d_out: int, num_wg: int, 
 def ecspmv_empty_launch(d_out: int, num_wg: int, threads_per_wg: int, count: int = 1, stream: int = 0) -> None:
     _check(lib().ecspmv_empty_launch(c_void_p(d_out), num_wg, threads_per_wg, count, c_void_p(stream)),
            "ecspmv_empty_launch")
+
+
+# ---- around the products: descriptions are the structs of the C ABI, pointers and streams plain integers
+
+def ecspmv_kv_write(cache: KvCacheDesc, k: View, v: View, d_slots: int, tokens: int, stream: int = 0) -> None:
+    _check(lib().ecspmv_kv_write(cache, k, v, c_void_p(d_slots), tokens, c_void_p(stream)), "ecspmv_kv_write")
+
+
+def ecspmv_kv_read(cache: KvCacheDesc, d_slots: int, tokens: int, k: View, v: View, stream: int = 0) -> None:
+    _check(lib().ecspmv_kv_read(cache, c_void_p(d_slots), tokens, k, v, c_void_p(stream)), "ecspmv_kv_read")
+
+
+def ecspmv_attention_workspace(cache: KvCacheDesc, a: AttentionDesc) -> int:
+    n = c_size_t(0)
+    _check(lib().ecspmv_attention_workspace(cache, a, byref(n)), "ecspmv_attention_workspace")
+    return int(n.value)
+
+
+def ecspmv_attention(cache: KvCacheDesc, a: AttentionDesc, d_work: int = 0, work_bytes: int = 0, stream: int = 0) -> None:
+    _check(lib().ecspmv_attention(cache, a, c_void_p(d_work), work_bytes, c_void_p(stream)), "ecspmv_attention")
+
+
+def ecspmv_verify(a: VerifyDesc, stream: int = 0) -> None:
+    _check(lib().ecspmv_verify(a, c_void_p(stream)), "ecspmv_verify")

@@ -3,14 +3,15 @@ from __future__ import annotations
 
 import os
 import subprocess
+import tempfile
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libecspmv.so")
 TRACE_LIB = os.path.join(PKG, "libecspmv_trace.so")     # the same sources with clock stamps compiled in (timeline.py)
-SOURCES = ["api.cpp", "encoder.cpp", "kernels.hip"]
-HEADERS = ["encoder.h", "launch.h", "ecspmv_format.h", os.path.join("..", "..", "include", "ecspmv.h")]
+SOURCES = ["api.cpp", "encoder.cpp", "kernels.hip", "serve.cpp", "kv_cache.hip", "attention.hip", "verify.hip"]
+HEADERS = ["encoder.h", "launch.h", "ecspmv_format.h", "kernel_handle.h", "serve.h", "status.h", os.path.join("..", "..", "include", "ecspmv.h")]
 
 
 def lib_path() -> str:
@@ -34,22 +35,26 @@ def build_all(verbose: bool = False) -> None:
 
 
 def build(verbose: bool = False, extra_flags=(), out: str = LIB) -> str:
-    """Compile every source for gfx950 and link the shared library.  Needs hipcc; no GPU required."""
-    cmd = ["hipcc", "-O3", "-std=c++17", "-fPIC", "-shared", "--offload-arch=gfx950",
+    """Compile every source for gfx950, side by side, and link the shared library.  Needs hipcc; no GPU required."""
+    cmd = ["hipcc", "-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",
            "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
            # the first kernel arguments (count, workgroup size, first item of a launch) arrive in registers
            "-mllvm", "-amdgpu-kernarg-preload-count=16",
            "-mpopcnt", "-pthread", "-Wall", "-Wno-unused-function",
-           "-x", "hip"]
-    cmd += list(extra_flags)
-    cmd += [os.path.join(CSRC, f) for f in SOURCES]
-    cmd += ["-o", out]
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if verbose or res.returncode != 0:
-        print(res.stdout)
-        print(res.stderr)
-    if res.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + res.stderr[-4000:])
+           *extra_flags]
+
+    def run(args):
+        res = subprocess.run(args, capture_output=True, text=True)
+        if verbose or res.returncode != 0:
+            print(res.stdout)
+            print(res.stderr)
+        if res.returncode != 0:
+            raise RuntimeError("hipcc failed:\n" + res.stderr[-4000:])
+
+    with tempfile.TemporaryDirectory() as tmp, ThreadPoolExecutor(4) as pool:
+        objects = [os.path.join(tmp, f + ".o") for f in SOURCES]
+        list(pool.map(run, [cmd + ["-x", "hip", "-c", os.path.join(CSRC, f), "-o", o] for f, o in zip(SOURCES, objects)]))
+        run(cmd + ["-shared", *objects, "-o", out])
     return out
 
 

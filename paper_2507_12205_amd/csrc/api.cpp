@@ -10,6 +10,7 @@
 #include "../../include/ecspmv.h"
 #include "encoder.h"
 #include "launch.h"
+#include "status.h"
 
 struct ecspmv_matrix {
     ecs::Image image;
@@ -28,12 +29,7 @@ namespace {
 
 thread_local int g_last_hip_error = 0;
 
-int hip_status(int e)
-{
-    if (e == 0) return ECSPMV_OK;
-    g_last_hip_error = e;
-    return ECSPMV_ERR_HIP;
-}
+using ecs::hip_status;
 
 // LDS a workgroup may use on the current device, asked once per device and kept (the hot calls must not query the
 // runtime on every launch)
@@ -192,6 +188,13 @@ int decode_t(const ecspmv_matrix *A, int value_bits, int64_t *nnz, int32_t *rows
 }
 
 }  // namespace
+
+int ecs::hip_status(int e)
+{
+    if (e == 0) return ECSPMV_OK;
+    g_last_hip_error = e;
+    return ECSPMV_ERR_HIP;
+}
 
 extern "C" {
 

@@ -1,0 +1,507 @@
+// Attention of new tokens over the paged cache of keys and values.
+//
+// For a head of the cache, the rows are the (token, head of its group) pairs of a sequence's new tokens: row r is token r / group,
+// head r % group of the group.  A row sees the keys up to its own place, p = kv_len - new + token:
+//   o_r = sum_{j <= p} exp(t_j - m) v_j / sum_{j <= p} exp(t_j - m),   t_j = scale * q_r . k_j,   m = max t_j
+// in one pass over the keys: m and both sums are carried along, and what was added up under an older m is scaled by exp(m_old - m_new).
+#include <hip/hip_runtime.h>
+#include <hip/hip_fp16.h>
+#include <stdint.h>
+#include <algorithm>
+
+#include "kernel_handle.h"
+#include "serve.h"
+
+namespace {
+
+using ecs::AttentionArgs;
+
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef _Float16 half8v __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kNone = -__builtin_inff();
+
+// a register as two FP16 values and back
+__device__ __forceinline__ half2v as_half2(uint32_t w) { return __builtin_bit_cast(half2v, w); }
+__device__ __forceinline__ uint32_t as_word(half2v h) { return __builtin_bit_cast(uint32_t, h); }
+__device__ __forceinline__ half8v as_half8(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    const uint4 t = make_uint4(a, b, c, d);
+    return __builtin_bit_cast(half8v, t);
+}
+
+template <int BYTES>
+struct Raw {
+    uint32_t w[BYTES < 4 ? 1 : BYTES / 4];
+    __device__ __forceinline__ void load(const uint8_t *p)
+    {
+        if constexpr (BYTES == 2) {
+            w[0] = *reinterpret_cast<const uint16_t *>(p);
+        } else if constexpr (BYTES == 4) {
+            w[0] = *reinterpret_cast<const uint32_t *>(p);
+        } else if constexpr (BYTES == 8) {
+            const uint2 t = *reinterpret_cast<const uint2 *>(p);
+            w[0] = t.x, w[1] = t.y;
+        } else {
+#pragma unroll
+            for (int i = 0; i < BYTES / 16; ++i) {
+                const uint4 t = reinterpret_cast<const uint4 *>(p)[i];
+                w[4 * i] = t.x, w[4 * i + 1] = t.y, w[4 * i + 2] = t.z, w[4 * i + 3] = t.w;
+            }
+        }
+    }
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (uint32_t &x : w) x = 0;
+    }
+};
+
+// Codes as FP16 values, exactly: the code goes into the last bits of 1024, which is then taken off.
+__device__ __forceinline__ uint32_t minus(uint32_t w, _Float16 c) { return as_word(as_half2(w) - half2v{c, c}); }
+// two bytes (in the low halves of 16 bits each, the sign bit flipped) of 8-bit codes
+__device__ __forceinline__ uint32_t from_bytes(uint32_t w) { return minus(w | 0x64006400u, (_Float16)1152.0f); }
+// two nibbles, in bits 0-3 and 16-19; less 8, and the lowest value of a row is taken 8 steps higher (low_of): sums of products with
+// rounded weights then cancel less
+__device__ __forceinline__ uint32_t from_nibbles(uint32_t w) { return minus((w & 0x000F000Fu) | 0x64006400u, (_Float16)1032.0f); }
+
+// 8 neighbouring codes of a key as eight FP16 values.  With 4 bits in the order 0 4 1 5 2 6 3 7 (slot_dim): the values of q are put in
+// the same order, and the order of a sum's terms is free.
+template <int BITS>
+__device__ __forceinline__ half8v key_values(const uint32_t *w)
+{
+    if constexpr (BITS == 16) {
+        return as_half8(w[0], w[1], w[2], w[3]);
+    } else if constexpr (BITS == 8) {
+        const uint32_t a = w[0] ^ 0x80808080u, b = w[1] ^ 0x80808080u;
+        return as_half8(from_bytes(__builtin_amdgcn_perm(0, a, 0x0C010C00u)), from_bytes(__builtin_amdgcn_perm(0, a, 0x0C030C02u)),
+                        from_bytes(__builtin_amdgcn_perm(0, b, 0x0C010C00u)), from_bytes(__builtin_amdgcn_perm(0, b, 0x0C030C02u)));
+    } else {
+        return as_half8(from_nibbles(w[0]), from_nibbles(w[0] >> 4), from_nibbles(w[0] >> 8), from_nibbles(w[0] >> 12));
+    }
+}
+template <int BITS>
+__device__ __forceinline__ constexpr int slot_dim(int i) { return BITS == 4 ? (i >> 1) + 4 * (i & 1) : i; }
+
+// The i-th of a lane's values of eight keys as an operand: key r in slot r
+template <int BITS, class R>
+__device__ __forceinline__ half8v value_column(const R (&v)[8], int i)
+{
+    uint32_t o[4];
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        if constexpr (BITS == 16) {
+            o[p] = __builtin_amdgcn_perm(v[2 * p + 1].w[i >> 1], v[2 * p].w[i >> 1], (i & 1) ? 0x07060302u : 0x05040100u);
+        } else if constexpr (BITS == 8) {
+            const uint32_t s = 0x0C040C00u + 0x00010001u * (uint32_t)(i & 3);
+            o[p] = from_bytes(__builtin_amdgcn_perm(v[2 * p + 1].w[i >> 2], v[2 * p].w[i >> 2], s) ^ 0x00800080u);
+        } else {
+            const uint32_t s = 0x0C040C00u + 0x00010001u * (uint32_t)((i >> 1) & 3);
+            const uint32_t t = __builtin_amdgcn_perm(v[2 * p + 1].w[i >> 3], v[2 * p].w[i >> 3], s);
+            o[p] = from_nibbles((i & 1) ? t >> 4 : t);
+        }
+    }
+    return as_half8(o[0], o[1], o[2], o[3]);
+}
+
+__device__ __forceinline__ float half_to_float(uint32_t h) { return __half2float(__ushort_as_half((unsigned short)h)); }
+
+// the step of a 4-bit row, and what its code 8 stands for
+__device__ __forceinline__ float step_of(uint32_t w) { return half_to_float(w & 0xFFFFu); }
+__device__ __forceinline__ float low_of(uint32_t w) { return fmaf(8.0f, step_of(w), half_to_float(w >> 16)); }
+
+// A sequence's part of the arguments
+struct Sequence {
+    uint32_t first, new_tokens, len;      // first token in q, how many, keys in all
+    const int32_t *table;
+    __device__ __forceinline__ Sequence(const AttentionArgs &a, uint32_t b)
+    {
+        const int32_t total = (int32_t)a.tokens;
+        const int32_t s = min(max(a.q_start[b], 0), total), e = min(max(a.q_start[b + 1], s), total);
+        first = (uint32_t)s;
+        new_tokens = min((uint32_t)(e - s), a.max_new);
+        const uint64_t most = (uint64_t)a.max_pages << a.cache.page_shift;
+        len = (uint32_t)min((uint64_t)max(a.kv_len[b], 0), most);
+        behind = (int32_t)len - (e - s);
+        table = a.table + (int64_t)b * a.table_stride;
+    }
+    int32_t behind;                       // keys before the first new token (negative: the first tokens see nothing)
+};
+
+// The page of a key, a number that is one whatever the table holds
+__device__ __forceinline__ uint32_t page_of(const AttentionArgs &a, const int32_t *table, uint32_t key)
+{
+    return min((uint32_t)table[key >> a.cache.page_shift], a.cache.pages - 1u);
+}
+
+// ---- up to 16 rows per workgroup, its four wavefronts on different keys ------------------------------------------------------------
+//
+// A wavefront takes 32 keys at a time.  Keys times q: the keys are the rows of the matrix product's result and the 16 rows of q its
+// columns, so that lane l has column l % 16 and of each 16 keys the four 4 (l / 16) ... + 3.  These are what the second product, V^T
+// times the weights, reads of the weights in that lane, if its sum over 32 keys is taken in the order that the first one left: the
+// weights never leave their lane.  V comes as it lies in memory, 8 keys times DP / 16 values per lane, and is turned round in
+// registers; its columns are dealt to the products as DP / 16 per lane, the i-th product has values i of every lane.
+template <int BITS, int DP, bool PAD>
+__global__ __launch_bounds__(256) void attention_rows_kernel(const AttentionArgs a)
+{
+    constexpr int kSteps = DP / 32, VD = DP / 16;
+    constexpr int KB = BITS == 16 ? 8 : BITS == 8 || PAD || DP == 64 ? 16 : 32;       // neighbouring values of a key in a lane
+    constexpr int kLoads = DP / 4 / KB;
+    typedef Raw<KB * BITS / 8> KeyRaw;
+    typedef Raw<VD * BITS / 8> ValueRaw;
+    constexpr int kRow = DP + 4;
+    __shared__ float lds_o[4][16][kRow];
+    __shared__ float lds_ml[4][16][2];
+
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, j = lane & 15u, g = lane >> 4;
+    const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid >> 6));
+    const uint32_t tile = blockIdx.x / a.splits, split = blockIdx.x - tile * a.splits, head = blockIdx.y;
+    const Sequence s(a, blockIdx.z);
+    const uint32_t rows = s.new_tokens * a.group, row0 = 16u * tile;
+    if (row0 >= rows) return;
+    const uint32_t dim = PAD ? a.cache.dim : DP;
+
+    // this lane's row, and the keys that rows of the tile see
+    const uint32_t row = min(row0 + j, rows - 1u), token = row / a.group;
+    const int32_t seen = min(s.behind + (int32_t)token + 1, (int32_t)s.len);             // keys that this row sees
+    const uint32_t last_row = min(row0 + 15u, rows - 1u);
+    const int32_t end_i = min(s.behind + (int32_t)(last_row / a.group) + 1, (int32_t)s.len);
+    const uint32_t end = end_i > 0 ? (uint32_t)end_i : 0u;
+    const int32_t all_see = s.behind + (int32_t)(row0 / a.group) + 1;                    // keys that every row sees
+
+    half8v q[kSteps];
+    float q_sum = 0.0f;
+    {
+        const uint16_t *p = a.q.data + (int64_t)(s.first + token) * a.q.token_stride +
+                            (int64_t)(head * a.group + (row - token * a.group)) * a.q.head_stride;
+#pragma unroll
+        for (int t = 0; t < kSteps; ++t) {
+            const uint32_t d0 = (uint32_t)(t / (KB / 8)) * (4u * KB) + g * KB + 8u * (t % (KB / 8));
+            const bool in = !PAD || d0 < dim;
+            uint32_t w[4] = {0, 0, 0, 0};
+            if (in) {
+                if (a.q_wide) {
+                    const uint4 v = *reinterpret_cast<const uint4 *>(p + d0);
+                    w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) w[i >> 1] |= (uint32_t)p[(int64_t)(d0 + i) * a.q.dim_stride] << (16 * (i & 1));
+                }
+            }
+            uint32_t o[4] = {0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int d = slot_dim<BITS>(i);
+                const uint32_t h = (d & 1) ? w[d >> 1] >> 16 : w[d >> 1] & 0xFFFFu;
+                o[i >> 1] |= h << (16 * (i & 1));
+                if constexpr (BITS == 4) q_sum += half_to_float(h);
+            }
+            q[t] = as_half8(o[0], o[1], o[2], o[3]);
+        }
+        if constexpr (BITS == 4) {
+            q_sum += __shfl_xor(q_sum, 16, 64);
+            q_sum += __shfl_xor(q_sum, 32, 64);
+        }
+    }
+
+    const uint32_t tiles = (end + 31u) >> 5, per = (tiles + a.splits - 1u) / a.splits;
+    const uint32_t t0 = min(split * per, tiles), t1 = min(t0 + per, tiles);
+    const uint32_t page_mask = (1u << a.cache.page_shift) - 1u;
+    const uint64_t page_rows = (uint64_t)a.cache.heads << a.cache.page_shift, head_rows = (uint64_t)head << a.cache.page_shift;
+
+    f32x4 acc[VD];
+#pragma unroll
+    for (int i = 0; i < VD; ++i) acc[i] = f32x4{0, 0, 0, 0};
+    float m = kNone, l = 0.0f, z_acc = 0.0f, unit = 0.0f;         // unit: acc is in units of it (BITS < 16)
+
+    for (uint32_t t = t0 + wave; t < t1; t += 4u) {
+        const uint32_t key0 = 32u * t;
+        // first row of each 16 keys in the cache; keys beyond the last one are read from where the last one is
+        uint64_t at[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t key = min(key0 + 16u * h, (end - 1u) & ~15u);
+            at[h] = (uint64_t)page_of(a, s.table, key) * page_rows + head_rows + (key & page_mask);
+        }
+        KeyRaw k[2][kLoads];
+        ValueRaw v[8];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint8_t *p = a.cache.k + at[h] * a.cache.row_bytes + j * a.cache.row_bytes + g * (KB * BITS / 8);
+#pragma unroll
+            for (int x = 0; x < kLoads; ++x) {
+                if (!PAD || (uint32_t)(x * 4 * KB) + g * KB < dim)
+                    k[h][x].load(p + x * (4 * KB * BITS / 8));
+                else
+                    k[h][x].clear();
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            const uint8_t *p = a.cache.v + at[r >> 2] * a.cache.row_bytes + (4u * g + (r & 3)) * a.cache.row_bytes + j * (VD * BITS / 8);
+            if (!PAD || j * VD < dim)
+                v[r].load(p);
+            else
+                v[r].clear();
+        }
+        uint32_t ks[8] = {}, vs[8] = {};
+        if constexpr (BITS < 16) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint4 x = *reinterpret_cast<const uint4 *>(a.cache.k_step + 4u * (at[h] + 4u * g));
+                const uint4 y = *reinterpret_cast<const uint4 *>(a.cache.v_step + 4u * (at[h] + 4u * g));
+                ks[4 * h] = x.x, ks[4 * h + 1] = x.y, ks[4 * h + 2] = x.z, ks[4 * h + 3] = x.w;
+                vs[4 * h] = y.x, vs[4 * h + 1] = y.y, vs[4 * h + 2] = y.z, vs[4 * h + 3] = y.w;
+            }
+        }
+
+        float w[8];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            f32x4 c = {0, 0, 0, 0};
+#pragma unroll
+            for (int t = 0; t < kSteps; ++t) {
+                constexpr int kPer = KB / 8;                       // steps that a load feeds
+                c = __builtin_amdgcn_mfma_f32_16x16x32_f16(key_values<BITS>(&k[h][t / kPer].w[(t % kPer) * (BITS / 4)]), q[t], c, 0, 0, 0);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                float d = c[r];
+                if constexpr (BITS == 8) d *= __uint_as_float(ks[4 * h + r]);
+                if constexpr (BITS == 4) d = fmaf(d, step_of(ks[4 * h + r]), q_sum * low_of(ks[4 * h + r]));
+                w[4 * h + r] = d * a.scale_log2;
+            }
+        }
+        const bool some_hidden = (int32_t)(key0 + 32u) > all_see || key0 + 32u > end;
+        if (some_hidden) {
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                const int32_t key = (int32_t)(key0 + (r < 4 ? 0u : 16u) + 4u * g + (r & 3));
+                if (key >= seen) w[r] = kNone;
+            }
+        }
+        float most = w[0];
+#pragma unroll
+        for (int r = 1; r < 8; ++r) most = fmaxf(most, w[r]);
+        most = fmaxf(most, __shfl_xor(most, 16, 64));
+        most = fmaxf(most, __shfl_xor(most, 32, 64));
+        const float m_new = fmaxf(m, most), base = m_new == kNone ? 0.0f : m_new;
+        const float alpha = exp2f(m - base);                       // (0 where nothing was seen before)
+        m = m_new;
+        float sum = 0.0f;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            w[r] = exp2f(w[r] - base);
+            sum += w[r];
+        }
+        l = l * alpha + sum;
+
+        float shrink = alpha;
+        if constexpr (BITS < 16) {
+            // The steps of V go into the weights, as shares of the largest step so far (rounded up to a power of two), so that
+            // the weights that are rounded to FP16 stay within [0, 1] whatever the steps are.
+            float step[8], top = 0.0f;
+            z_acc *= alpha;
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                const uint32_t key = key0 + (r < 4 ? 0u : 16u) + 4u * g + (r & 3);
+                const bool in = key < end;
+                step[r] = in ? (BITS == 8 ? __uint_as_float(vs[r]) : step_of(vs[r])) : 0.0f;
+                top = fmaxf(top, step[r]);
+                if constexpr (BITS == 4) z_acc = in ? fmaf(w[r], low_of(vs[r]), z_acc) : z_acc;
+            }
+            top = fmaxf(top, __shfl_xor(top, 16, 64));
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            if (top > unit) {
+                const float up = ldexpf(1.0f, ilogbf(top) + 1);
+                shrink *= unit / up;
+                unit = up;
+            }
+            const float inv = unit > 0.0f ? 1.0f / unit : 0.0f;
+#pragma unroll
+            for (int r = 0; r < 8; ++r) w[r] *= step[r] * inv;
+        }
+#pragma unroll
+        for (int i = 0; i < VD; ++i) acc[i] *= shrink;
+
+        bool odd = false;
+        if constexpr (BITS == 16) {
+            if (some_hidden) {
+                // Keys that no row of the tile sees may hold anything; and where V is not finite, a weight of 0 has to stay without
+                // effect on the rows that do not see it: such values are left out of the product.
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    const uint32_t key = key0 + (r < 4 ? 0u : 16u) + 4u * g + (r & 3);
+#pragma unroll
+                    for (uint32_t &x : v[r].w) {
+                        x = key < end ? x : 0u;
+                        const uint32_t keep = ((x & 0x7C00u) != 0x7C00u ? 0xFFFFu : 0u) | ((x & 0x7C000000u) != 0x7C000000u ? 0xFFFF0000u : 0u);
+                        odd |= keep != 0xFFFFFFFFu;
+                        x &= keep;
+                    }
+                }
+                odd = __any((int)odd);
+            }
+        }
+        uint32_t pw[4];
+#pragma unroll
+        for (int p = 0; p < 4; ++p) pw[p] = as_word(half2v{(_Float16)w[2 * p], (_Float16)w[2 * p + 1]});
+        const half8v weights = as_half8(pw[0], pw[1], pw[2], pw[3]);
+#pragma unroll
+        for (int i = 0; i < VD; ++i) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(value_column<BITS>(v, i), weights, acc[i], 0, 0, 0);
+        if (odd) {
+            // what was left out, one key after the other, in the rows that see it
+            for (uint32_t k = 0; k < 32u && key0 + k < end; ++k) {
+                const uint32_t r = (k & 3u) + 4u * (k >> 4), from = j + 16u * ((k >> 2) & 3u);
+                float x = w[0];
+#pragma unroll
+                for (uint32_t i = 1; i < 8; ++i) x = r == i ? w[i] : x;
+                x = __shfl(x, (int)from, 64);
+                if ((int32_t)(key0 + k) >= seen) continue;
+                const uint16_t *p = reinterpret_cast<const uint16_t *>(a.cache.v + (at[k >> 4] + (k & 15u)) * a.cache.row_bytes);
+#pragma unroll
+                for (int r2 = 0; r2 < 4; ++r2)
+#pragma unroll
+                    for (int i = 0; i < VD; ++i) {
+                        const uint32_t d = VD * (4u * g + r2) + i;
+                        if (PAD && d >= dim) continue;
+                        if ((p[d] & 0x7C00u) == 0x7C00u) acc[i][r2] = fmaf(x, half_to_float(p[d]), acc[i][r2]);
+                    }
+            }
+        }
+    }
+
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    if constexpr (BITS == 4) {
+        z_acc += __shfl_xor(z_acc, 16, 64);
+        z_acc += __shfl_xor(z_acc, 32, 64);
+    }
+    // the four wavefronts' results meet in LDS
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int i = 0; i < VD; i += 4) {
+            f32x4 o = {acc[i][r], acc[i + 1][r], acc[i + 2][r], acc[i + 3][r]};
+            if constexpr (BITS < 16) o = o * unit + z_acc;
+            *reinterpret_cast<f32x4 *>(&lds_o[wave][j][VD * (4u * g + r) + i]) = o;
+        }
+    if (g == 0) lds_ml[wave][j][0] = m, lds_ml[wave][j][1] = l;
+    __syncthreads();
+
+    const uint32_t n = tid >> 4, d0 = VD * (tid & 15u);
+    if (row0 + n >= rows || d0 >= dim) return;
+    float most = kNone, total = 0.0f, share[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) most = fmaxf(most, lds_ml[x][n][0]);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+        share[x] = most == kNone ? 0.0f : exp2f(lds_ml[x][n][0] - most);
+        if (lds_ml[x][n][0] == kNone) share[x] = 0.0f;             // (what it has added up is nothing)
+        total += share[x] * lds_ml[x][n][1];
+    }
+    float o[VD];
+#pragma unroll
+    for (int i = 0; i < VD; ++i) {
+        o[i] = 0.0f;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) o[i] += share[x] * lds_o[x][n][d0 + i];
+    }
+    const uint32_t out_row = row0 + n, out_token = out_row / a.group, out_head = head * a.group + (out_row - out_token * a.group);
+    if (a.splits == 1u) {
+        const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+        uint16_t *p = a.out.data + (int64_t)(s.first + out_token) * a.out.token_stride + (int64_t)out_head * a.out.head_stride;
+#pragma unroll
+        for (int i = 0; i < VD; i += 2) {
+            const half2v h = {(_Float16)(o[i] * inv), (_Float16)(o[i + 1] * inv)};
+            if (a.out_wide) {
+                *reinterpret_cast<uint32_t *>(p + d0 + i) = as_word(h);
+            } else {
+                p[(int64_t)(d0 + i) * a.out.dim_stride] = (uint16_t)as_word(h);
+                p[(int64_t)(d0 + i + 1) * a.out.dim_stride] = (uint16_t)(as_word(h) >> 16);
+            }
+        }
+    } else {
+        const uint64_t at = ((uint64_t)split * a.tokens + s.first + out_token) * a.q_heads + out_head;
+#pragma unroll
+        for (int i = 0; i < VD; i += 4) *reinterpret_cast<f32x4 *>(a.part_o + at * dim + d0 + i) = f32x4{o[i], o[i + 1], o[i + 2], o[i + 3]};
+        if ((tid & 15u) == 0) a.part_ml[2 * at] = most, a.part_ml[2 * at + 1] = total;
+    }
+}
+
+// ---- joining the splits: a workgroup per (token, head), its wavefronts on different splits --------------------------------------------
+__global__ __launch_bounds__(256) void attention_join_kernel(const AttentionArgs a)
+{
+    __shared__ float lds_o[4][256];
+    __shared__ float lds_l[4];
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6, dim = a.cache.dim;
+    const uint32_t token = blockIdx.x / a.q_heads, head = blockIdx.x - token * a.q_heads;
+    if ((int32_t)token < a.q_start[0] || (int32_t)token >= a.q_start[a.batch]) return;      // of no sequence
+    const uint64_t row = blockIdx.x, step = (uint64_t)a.tokens * a.q_heads;
+    float m = kNone;
+    for (uint32_t s = lane; s < a.splits; s += 64u) m = fmaxf(m, a.part_ml[2 * (row + s * step)]);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+    float l = 0.0f, o[4] = {0, 0, 0, 0};
+    for (uint32_t s = wave; s < a.splits; s += 4u) {
+        const uint64_t at = row + s * step;
+        const float ms = a.part_ml[2 * at];
+        if (ms == kNone) continue;
+        const float share = exp2f(ms - m);
+        l += share * a.part_ml[2 * at + 1];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (lane + 64u * i < dim) o[i] += share * a.part_o[at * dim + lane + 64u * i];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) lds_o[wave][lane + 64u * i] = o[i];
+    if (lane == 0) lds_l[wave] = l;
+    __syncthreads();
+    if (tid >= dim) return;
+    const float total = lds_l[0] + lds_l[1] + lds_l[2] + lds_l[3];
+    const float sum = lds_o[0][tid] + lds_o[1][tid] + lds_o[2][tid] + lds_o[3][tid];
+    const _Float16 h = (_Float16)(total == 0.0f ? 0.0f : sum / total);
+    a.out.data[(int64_t)token * a.out.token_stride + (int64_t)head * a.out.head_stride + (int64_t)tid * a.out.dim_stride] = __builtin_bit_cast(uint16_t, h);
+}
+
+template <int BITS>
+int launch_rows(const AttentionArgs &a, void *stream)
+{
+    const uint32_t gx = a.row_tiles * a.splits, gy = a.cache.heads, gz = a.batch;
+    switch (a.cache.dim) {
+    case 64: return ecs::launch_args<attention_rows_kernel<BITS, 64, false>>(a, gx, gy, gz, 256, stream);
+    case 128: return ecs::launch_args<attention_rows_kernel<BITS, 128, false>>(a, gx, gy, gz, 256, stream);
+    case 256: return ecs::launch_args<attention_rows_kernel<BITS, 256, false>>(a, gx, gy, gz, 256, stream);
+    default: break;
+    }
+    if (a.cache.dim < 64) return ecs::launch_args<attention_rows_kernel<BITS, 64, true>>(a, gx, gy, gz, 256, stream);
+    if (a.cache.dim < 128) return ecs::launch_args<attention_rows_kernel<BITS, 128, true>>(a, gx, gy, gz, 256, stream);
+    return ecs::launch_args<attention_rows_kernel<BITS, 256, true>>(a, gx, gy, gz, 256, stream);
+}
+
+}  // namespace
+
+namespace ecs {
+
+AttentionPlan plan_attention(uint32_t batch, uint32_t kv_heads, uint32_t group, uint32_t dim, uint64_t tokens, uint32_t max_new, uint64_t max_kv)
+{
+    AttentionPlan p = {};
+    const uint64_t rows = (uint64_t)max_new * group;
+    p.row_tiles = (uint32_t)((rows + 15u) / 16u);
+    const uint64_t blocks = (uint64_t)p.row_tiles * kv_heads * batch;
+    // enough workgroups for the chip, and two rounds of 32 keys for each wavefront of a split
+    const uint64_t by_chip = blocks ? 1024u / blocks : 1u, by_keys = (max_kv + 255u) / 256u;
+    p.splits = (uint32_t)std::max<uint64_t>(1u, std::min(by_chip, by_keys));
+    if (p.splits > 1u) p.work_bytes = (uint64_t)p.splits * tokens * kv_heads * group * (dim + 2u) * sizeof(float);
+    return p;
+}
+
+int launch_attention(const AttentionArgs &a, void *stream)
+{
+    int e = a.cache.bits == 16 ? launch_rows<16>(a, stream) : a.cache.bits == 8 ? launch_rows<8>(a, stream) : launch_rows<4>(a, stream);
+    if (e || a.splits == 1u) return e;
+    return launch_args<attention_join_kernel>(a, a.tokens * a.q_heads, 1, 1, 256, stream);
+}
+
+}  // namespace ecs

@@ -1,6 +1,8 @@
 """PyTorch plumbing around the C ABI: device buffers and streams only, no arithmetic."""
 from __future__ import annotations
 
+from ctypes import sizeof
+
 import torch
 from torch import _C
 
@@ -57,3 +59,117 @@ def csr_run(csr: B.CsrMatrix, x: torch.Tensor, y: torch.Tensor, stream=None) -> 
     assert x.dtype == torch.float16 and y.dtype == torch.float16 and x.is_cuda and y.is_cuda
     csr.ecspmv_csr_run(x.data_ptr(), y.data_ptr(), _stream_handle(stream))
     return y
+
+
+# ---- around the products ---------------------------------------------------------------------------------
+
+_VIEW, _KV_CACHE, _ATTENTION, _VERIFY = (sizeof(t) for t in (B.View, B.KvCacheDesc, B.AttentionDesc, B.VerifyDesc))
+
+
+class KvCache:
+    """A cache of keys and values in pages.  k, v: (pages, heads, page_size, head_dim) FP16 for 16 bits, int8 for 8;
+    (pages, heads, page_size, head_dim / 2) uint8 for 4, the earlier code in the low half.  k_step, v_step: (pages, heads, page_size)
+    FP32 for 8 bits, (pages, heads, page_size, 2) FP16, step and lowest value, for 4.  The tensors are the caller's and stay in place."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_step: torch.Tensor = None, v_step: torch.Tensor = None):
+        self.bits = {torch.float16: 16, torch.int8: 8, torch.uint8: 4}[k.dtype]
+        self.pages, self.heads, self.page_size, width = k.shape
+        self.head_dim = 2 * width if self.bits == 4 else width
+        assert v.dtype is k.dtype and v.shape == k.shape and k.is_cuda and v.device == k.device
+        assert k.is_contiguous() and v.is_contiguous()
+        if self.bits == 16:
+            assert k_step is None and v_step is None
+        else:
+            want = (torch.float32, k.shape[:3]) if self.bits == 8 else (torch.float16, (*k.shape[:3], 2))
+            for t in (k_step, v_step):
+                assert t.dtype is want[0] and t.shape == want[1] and t.is_contiguous() and t.device == k.device
+        self.k, self.v, self.k_step, self.v_step = k, v, k_step, v_step
+        self.desc = B.KvCacheDesc(_KV_CACHE, self.bits, self.pages, self.heads, self.page_size, self.head_dim, k.data_ptr(), v.data_ptr(),
+                                  k_step.data_ptr() if k_step is not None else None, v_step.data_ptr() if v_step is not None else None)
+
+
+def kv_cache(pages: int, heads: int, page_size: int, head_dim: int, bits: int = 16, device="cuda:0") -> KvCache:
+    """An empty cache (all zeros)."""
+    dtype, width = {16: (torch.float16, head_dim), 8: (torch.int8, head_dim), 4: (torch.uint8, head_dim // 2)}[bits]
+    k, v = (torch.zeros((pages, heads, page_size, width), dtype=dtype, device=device) for _ in range(2))
+    if bits == 16:
+        return KvCache(k, v)
+    dtype, shape = (torch.float32, (pages, heads, page_size)) if bits == 8 else (torch.float16, (pages, heads, page_size, 2))
+    return KvCache(k, v, *(torch.zeros(shape, dtype=dtype, device=device) for _ in range(2)))
+
+
+def _view(t: torch.Tensor) -> B.View:
+    return B.View(t.data_ptr(), *t.stride())
+
+
+def _rows_of(cache: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
+    assert k.dtype is torch.float16 and v.dtype is torch.float16 and k.device == v.device == slots.device == cache.k.device
+    assert k.shape == v.shape == (slots.shape[0], cache.heads, cache.head_dim)
+    assert slots.dtype is torch.int64 and slots.dim() == 1 and slots.is_contiguous()
+
+
+def kv_write(cache: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, stream=None) -> None:
+    """Keys and values of new tokens, (tokens, heads, head_dim) FP16 with any strides, into the places slots names: page * page_size +
+    place in the page (int64, one per token; one outside the cache leaves its token out)."""
+    _rows_of(cache, k, v, slots)
+    B.ecspmv_kv_write(cache.desc, _view(k), _view(v), slots.data_ptr(), slots.shape[0], _stream_handle(stream))
+
+
+def kv_read(cache: KvCache, slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, stream=None):
+    """The same places back into k and v (zeros for a place outside the cache)."""
+    _rows_of(cache, k, v, slots)
+    B.ecspmv_kv_read(cache.desc, slots.data_ptr(), slots.shape[0], _view(k), _view(v), _stream_handle(stream))
+    return k, v
+
+
+def attention_workspace(cache: KvCache, q: torch.Tensor, batch: int, max_new: int, max_kv: int) -> torch.Tensor:
+    """The workspace of attention() calls of up to these sizes: q's shape, sequences, new tokens of one, places in their page tables."""
+    a = B.AttentionDesc(_ATTENTION, q.shape[1], q.shape[0], batch, -(-max_kv // cache.page_size), max_new)
+    return torch.empty(B.ecspmv_attention_workspace(cache.desc, a), dtype=torch.uint8, device=q.device)
+
+
+def attention(cache: KvCache, q: torch.Tensor, out: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, page_table: torch.Tensor,
+              max_new: int, scale: float = None, workspace: torch.Tensor = None, stream=None) -> torch.Tensor:
+    """out = causal attention of the new tokens q, (tokens, q_heads, head_dim) FP16 with any strides, over the cache that holds their
+    keys and values: sequence b has q[q_start[b]:q_start[b + 1]] and kv_len[b] keys in all, in the pages page_table[b] (all int32).
+    max_new: the most new tokens of a sequence; scale: 1 / sqrt(head_dim) if not given."""
+    assert q.dtype is torch.float16 and out.dtype is torch.float16 and q.shape == out.shape and q.shape[2] == cache.head_dim
+    assert q.device == out.device == q_start.device == kv_len.device == page_table.device == cache.k.device
+    assert q_start.dtype is kv_len.dtype is page_table.dtype is torch.int32
+    batch, pages = page_table.shape
+    assert kv_len.shape == (batch,) and q_start.shape == (batch + 1,) and q_start.is_contiguous() and kv_len.is_contiguous()
+    assert pages <= 1 or page_table.stride(1) == 1
+    tokens, heads, _ = q.shape
+    a = B.AttentionDesc(_ATTENTION, heads, tokens, batch, pages, max_new, cache.head_dim ** -0.5 if scale is None else scale,
+                        max(page_table.stride(0), pages), q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), _view(q), _view(out))
+    if workspace is None:
+        workspace = torch.empty(B.ecspmv_attention_workspace(cache.desc, a), dtype=torch.uint8, device=q.device)
+        if stream is not None:
+            workspace.record_stream(stream)
+    B.ecspmv_attention(cache.desc, a, workspace.data_ptr(), workspace.numel(), _stream_handle(stream))
+    return out
+
+
+def verify(target: torch.Tensor, draft, drafted: torch.Tensor, uniform: torch.Tensor, tokens: torch.Tensor, accepted: torch.Tensor,
+           count: torch.Tensor = None, stream=None):
+    """Which drafted tokens stand, and the token after them.  target: (batch, drafts + 1, vocab) probabilities, draft: (batch, drafts,
+    vocab) the drafts' own (None where a draft was certain), uniform: (batch, drafts + 1) random numbers in [0, 1), all FP32; drafted:
+    (batch, drafts) int32, count: (batch,) int32, how many of them (None: all).  tokens: (batch, drafts + 1), accepted: (batch,) int32."""
+    batch, rows, vocab = target.shape
+    drafts = rows - 1
+    assert target.dtype is uniform.dtype is torch.float32 and drafted.dtype is tokens.dtype is accepted.dtype is torch.int32
+    assert target.is_cuda and target.device == uniform.device == drafted.device == tokens.device == accepted.device
+    assert uniform.shape == tokens.shape == (batch, rows) and drafted.shape == (batch, drafts) and accepted.shape == (batch,)
+    assert uniform.is_contiguous() and tokens.is_contiguous() and drafted.is_contiguous() and accepted.is_contiguous()
+    assert target.numel() == 0 or vocab == 1 or target.stride(2) == 1
+    a = B.VerifyDesc(_VERIFY, batch, drafts, vocab, target.data_ptr(), None, uniform.data_ptr(), target.stride(0), target.stride(1), 0, 0,
+                     drafted.data_ptr() or None, None, tokens.data_ptr(), accepted.data_ptr())
+    if draft is not None:
+        assert draft.dtype is torch.float32 and draft.shape == (batch, drafts, vocab) and draft.device == target.device
+        assert draft.numel() <= 1 or vocab == 1 or draft.stride(2) == 1
+        a.draft, a.draft_seq, a.draft_row = draft.data_ptr() or None, draft.stride(0), draft.stride(1)
+    if count is not None:
+        assert count.dtype is torch.int32 and count.shape == (batch,) and count.is_contiguous() and count.device == target.device
+        a.count = count.data_ptr()
+    B.ecspmv_verify(a, _stream_handle(stream))
+    return tokens, accepted
