@@ -217,6 +217,23 @@ int ecspmv_run_batch(const ecspmv_matrix *const *As, const void *const *d_xs, vo
  * build options produce neither), or if not even two right-hand sides fit LDS; ECSPMV_ERR_INVALID for other nb. */
 int ecspmv_run_multi(const ecspmv_matrix *A, const void *d_X, void *d_Y, int32_t nb, void *stream);
 
+/* No passage of the paper: Y = act(W X + b) o G + R, the product with what a decoder does to its result, in the launch that
+ * makes it: bias, activation, an elementwise factor (a gated MLP's other half) and an addition (the residual stream), in
+ * FP32 before the result is rounded once.  bias: device, m values; gate, residual: device, laid out as Y; all of Y's type and
+ * aligned to it; NULL leaves the step out.  residual and gate may be Y itself (each value is read before it is written, by who
+ * writes it).  Everything else is as in ecspmv_run_multi, nb in {1, 2, 4, 8}. */
+#define ECSPMV_ACT_NONE 0
+#define ECSPMV_ACT_RELU 1  /* max(t, 0), NaN stays */
+#define ECSPMV_ACT_GELU 2  /* t * (1 + erf(t / sqrt 2)) / 2 */
+#define ECSPMV_ACT_SILU 3  /* t / (1 + exp(-t)) */
+typedef struct ecspmv_epilogue_t {
+    uint32_t struct_size;                   /* sizeof(ecspmv_epilogue_t) as the caller compiled it */
+    int32_t  activation;                    /* ECSPMV_ACT_* */
+    const void *bias, *gate, *residual;
+} ecspmv_epilogue_t;
+int ecspmv_run_epilogue(const ecspmv_matrix *A, const void *d_X, void *d_Y, int32_t nb, const ecspmv_epilogue_t *epilogue,
+                        void *stream);
+
 /* ---- around the products: cache of keys and values, attention, drafted tokens ------------------------ */
 /* No passage of the paper: what a decoder does between and after the products with pruned weights.  FP16 throughout
  * (an FP32 model rounds its keys, values and queries first).  Every call is asynchronous on `stream`, allocates nothing,

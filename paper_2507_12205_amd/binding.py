@@ -24,7 +24,7 @@ FLAG_CLUSTER_ROWS = 8
 EXPORTS = (
     "ecspmv_build_dense", "ecspmv_build_csr", "ecspmv_build_dense_f32", "ecspmv_build_csr_f32", "ecspmv_destroy",
     "ecspmv_stats", "ecspmv_decode", "ecspmv_decode_f32",
-    "ecspmv_block_sets", "ecspmv_device_bytes", "ecspmv_export_image", "ecspmv_upload", "ecspmv_run", "ecspmv_run_batch", "ecspmv_run_multi",
+    "ecspmv_block_sets", "ecspmv_device_bytes", "ecspmv_export_image", "ecspmv_upload", "ecspmv_run", "ecspmv_run_batch", "ecspmv_run_multi", "ecspmv_run_epilogue",
     "ecspmv_csr_build_dense", "ecspmv_csr_destroy", "ecspmv_csr_device_bytes", "ecspmv_csr_upload",
     "ecspmv_kv_write", "ecspmv_kv_read", "ecspmv_attention_workspace", "ecspmv_attention", "ecspmv_verify",
     "ecspmv_csr_run", "ecspmv_stream_read", "ecspmv_stream_read_sliced", "ecspmv_empty_launch", "ecspmv_strerror", "ecspmv_last_hip_error",
@@ -54,6 +54,13 @@ class Stats(Structure):
             v = getattr(self, name)
             out[name] = list(v) if hasattr(v, "__len__") else v
         return out
+
+
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
+
+
+class Epilogue(Structure):
+    _fields_ = [("struct_size", c_uint32), ("activation", c_int32), ("bias", c_void_p), ("gate", c_void_p), ("residual", c_void_p)]
 
 
 class View(Structure):
@@ -120,6 +127,7 @@ def lib() -> ctypes.CDLL:
     L.ecspmv_run.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p]
     L.ecspmv_run_batch.argtypes = [c_void_p, c_void_p, c_void_p, c_int32, c_void_p]
     L.ecspmv_run_multi.argtypes = [c_void_p, c_void_p, c_void_p, c_int32, c_void_p]
+    L.ecspmv_run_epilogue.argtypes = [c_void_p, c_void_p, c_void_p, c_int32, POINTER(Epilogue), c_void_p]
     L.ecspmv_kv_write.argtypes = [POINTER(KvCacheDesc), POINTER(View), POINTER(View), c_void_p, c_int64, c_void_p]
     L.ecspmv_kv_read.argtypes = [POINTER(KvCacheDesc), c_void_p, c_int64, POINTER(View), POINTER(View), c_void_p]
     L.ecspmv_attention_workspace.argtypes = [POINTER(KvCacheDesc), POINTER(AttentionDesc), POINTER(c_size_t)]
@@ -260,6 +268,13 @@ class Matrix:
         status = (_lib or lib()).ecspmv_run_multi(self._h, d_X, d_Y, nb, stream)
         if status:
             raise EcspmvError(status, "ecspmv_run_multi")
+
+    def ecspmv_run_epilogue(self, d_X: int, d_Y: int, nb: int, epilogue: Epilogue, stream: int = 0) -> None:
+        if not (type(d_X) is type(d_Y) is type(nb) is type(stream) is int):
+            d_X, d_Y, nb, stream = c_void_p(d_X), c_void_p(d_Y), c_int32(nb), c_void_p(stream)
+        status = (_lib or lib()).ecspmv_run_epilogue(self._h, d_X, d_Y, nb, epilogue, stream)
+        if status:
+            raise EcspmvError(status, "ecspmv_run_epilogue")
 
 
 class Batch:

@@ -10,7 +10,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libecspmv.so")
 TRACE_LIB = os.path.join(PKG, "libecspmv_trace.so")     # the same sources with clock stamps compiled in (timeline.py)
-SOURCES = ["api.cpp", "encoder.cpp", "kernels.hip", "serve.cpp", "kv_cache.hip", "attention.hip", "verify.hip"]
+SOURCES = ["api.cpp", "encoder.cpp", "kernels.hip", "epilogue.hip", "serve.cpp", "kv_cache.hip", "attention.hip", "verify.hip"]
 HEADERS = ["encoder.h", "launch.h", "ecspmv_format.h", "kernel_handle.h", "serve.h", "status.h", os.path.join("..", "..", "include", "ecspmv.h")]
 
 

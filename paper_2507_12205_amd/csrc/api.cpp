@@ -353,8 +353,9 @@ int ecspmv_upload(ecspmv_matrix *A, void *d_buf, size_t bytes, void *stream)
     return ECSPMV_OK;
 }
 
-int ecspmv_run_batch(const ecspmv_matrix *const *As, const void *const *d_xs, void *const *d_ys, int32_t count,
-                     void *stream)
+// `fused`: the epilogue of the only matrix, or null
+static int run_batch(const ecspmv_matrix *const *As, const void *const *d_xs, void *const *d_ys, int32_t count,
+                     const ecs::EcsEpilogue *fused, void *stream)
 {
     if (!As || !d_xs || !d_ys || count <= 0) return ECSPMV_ERR_INVALID;
     for (int32_t i = 0; i < count; ++i) {
@@ -373,8 +374,9 @@ int ecspmv_run_batch(const ecspmv_matrix *const *As, const void *const *d_xs, vo
             const ecs::Image &nx = As[base + nb]->image;
             if (nx.delta_bits != bits || nx.value_bits != vbits) break;
         }
-        ecs::EcsBatch b;
-        std::memset(&b, 0, offsetof(ecs::EcsBatch, item) + sizeof(ecs::EcsBatchItem) * (size_t)(nb == 1 ? 1 : ECS_MAX_BATCH));
+        ecs::EcsFused b;
+        std::memset(static_cast<void *>(&b), 0,
+                    offsetof(ecs::EcsBatch, item) + sizeof(ecs::EcsBatchItem) * (size_t)(nb == 1 ? 1 : ECS_MAX_BATCH));
         b.count = (uint32_t)nb;
         uint32_t blocks = 0, lds = 0, mask = 0, pieces = 0, rows = 0;
         uint64_t chunks = 0, block_chunks = 0;
@@ -404,21 +406,29 @@ int ecspmv_run_batch(const ecspmv_matrix *const *As, const void *const *d_xs, vo
             const int t = As[base + i]->image.threads_per_wg;
             if (t) threads = (uint32_t)t;                      // a build-time choice overrides
         }
-        int s = hip_status(ecs::launch_ecspmv(b, threads, lds, mask, (uint32_t)bits, (uint32_t)vbits, chunks, block_chunks, stream));
+        if (fused) b.epilogue = *fused;
+        int s = hip_status((fused ? ecs::launch_epilogue(b, threads, lds, mask, (uint32_t)bits, (uint32_t)vbits, chunks, block_chunks, stream)
+                                  : ecs::launch_ecspmv(b, threads, lds, mask, (uint32_t)bits, (uint32_t)vbits, chunks, block_chunks, stream)));
         if (s) return s;
     }
     return ECSPMV_OK;
 }
 
-int ecspmv_run(const ecspmv_matrix *A, const void *d_x, void *d_y, void *stream)
+int ecspmv_run_batch(const ecspmv_matrix *const *As, const void *const *d_xs, void *const *d_ys, int32_t count,
+                     void *stream)
 {
-    return ecspmv_run_batch(&A, &d_x, &d_y, 1, stream);
+    return run_batch(As, d_xs, d_ys, count, nullptr, stream);
 }
 
-int ecspmv_run_multi(const ecspmv_matrix *A, const void *d_X, void *d_Y, int32_t nb, void *stream)
+int ecspmv_run(const ecspmv_matrix *A, const void *d_x, void *d_y, void *stream)
+{
+    return run_batch(&A, &d_x, &d_y, 1, nullptr, stream);
+}
+
+static int run_multi(const ecspmv_matrix *A, const void *d_X, void *d_Y, int32_t nb, const ecs::EcsEpilogue *fused, void *stream)
 {
     if (!A || !d_X || !d_Y) return ECSPMV_ERR_INVALID;
-    if (nb == 1) return ecspmv_run(A, d_X, d_Y, stream);
+    if (nb == 1) return run_batch(&A, &d_X, &d_Y, 1, fused, stream);
     if (nb != 2 && nb != 4 && nb != 8) return ECSPMV_ERR_INVALID;
     const ecs::Image &im = A->image;
     const uint32_t vw = (uint32_t)im.value_bits / 8u;                 // bytes per value of W, X and Y
@@ -461,8 +471,8 @@ int ecspmv_run_multi(const ecspmv_matrix *A, const void *d_X, void *d_Y, int32_t
         for (k = 1; k < want && lds_of(per, k + 1u) <= (uint64_t)lim; ++k) {}
         break;
     }
-    ecs::EcsBatch b;
-    std::memset(&b, 0, offsetof(ecs::EcsBatch, item) + sizeof(ecs::EcsBatchItem));       // the only item
+    ecs::EcsFused b;
+    std::memset(static_cast<void *>(&b), 0, offsetof(ecs::EcsBatch, item) + sizeof(ecs::EcsBatchItem));       // the only item
     b.count = 1;
     b.per_phase = k;
     ecs::EcsBatchItem &it = b.item[0];
@@ -475,8 +485,33 @@ int ecspmv_run_multi(const ecspmv_matrix *A, const void *d_X, void *d_Y, int32_t
     it.x_bytes = (uint32_t)x_bytes_of(per);
     it.block_end = (uint32_t)im.num_panels;
     it.row_stride = (uint32_t)nb;                                       // of X and Y, in elements
+    if (fused) {
+        b.epilogue = *fused;
+        return hip_status(ecs::launch_epilogue_multi(b, threads, (uint32_t)lds_of(per, k), im.type_mask, (uint32_t)im.delta_bits,
+                                                     (uint32_t)im.value_bits, per, stream));
+    }
     return hip_status(ecs::launch_ecspmv_multi(b, threads, (uint32_t)lds_of(per, k), im.type_mask, (uint32_t)im.delta_bits,
                                                (uint32_t)im.value_bits, per, stream));
+}
+
+int ecspmv_run_multi(const ecspmv_matrix *A, const void *d_X, void *d_Y, int32_t nb, void *stream)
+{
+    return run_multi(A, d_X, d_Y, nb, nullptr, stream);
+}
+
+int ecspmv_run_epilogue(const ecspmv_matrix *A, const void *d_X, void *d_Y, int32_t nb, const ecspmv_epilogue_t *epilogue, void *stream)
+{
+    if (!A || !epilogue || epilogue->struct_size < sizeof(uint32_t)) return ECSPMV_ERR_INVALID;
+    ecspmv_epilogue_t t;
+    std::memset(&t, 0, sizeof(t));
+    std::memcpy(&t, epilogue, epilogue->struct_size < sizeof(t) ? epilogue->struct_size : sizeof(t));
+    if (t.activation < ECSPMV_ACT_NONE || t.activation > ECSPMV_ACT_SILU) return ECSPMV_ERR_UNSUPPORTED;
+    const uintptr_t align = (uintptr_t)(A->image.value_bits / 8 - 1);
+    for (const void *p : {t.bias, t.gate, t.residual})
+        if (reinterpret_cast<uintptr_t>(p) & align) return ECSPMV_ERR_INVALID;
+    const ecs::EcsEpilogue e = {static_cast<const uint16_t *>(t.bias), static_cast<const uint16_t *>(t.gate),
+                                static_cast<const uint16_t *>(t.residual), (uint32_t)t.activation, 0};
+    return run_multi(A, d_X, d_Y, nb, e.bias || e.gate || e.residual || e.activation ? &e : nullptr, stream);
 }
 
 int ecspmv_csr_build_dense(const uint16_t *W, int64_t m, int64_t n, int64_t ld, ecspmv_csr **out)

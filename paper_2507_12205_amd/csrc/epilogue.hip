@@ -1,0 +1,4 @@
+// The product kernels with an epilogue: the same source, with what kernels.hip has under ECS_EPILOGUE; a unit of its own, so that both
+// are compiled at the same time.
+#define ECS_EPILOGUE 1
+#include "kernels.hip"

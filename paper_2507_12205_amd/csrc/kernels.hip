@@ -19,7 +19,13 @@
 #include <type_traits>
 
 #include "ecspmv_format.h"
+#include "kernel_handle.h"
 #include "launch.h"
+
+// The launches of this file, or with 1 those of the same kernels with an epilogue (epilogue.hip: compiled side by side)
+#ifndef ECS_EPILOGUE
+#define ECS_EPILOGUE 0
+#endif
 
 namespace {
 
@@ -691,6 +697,47 @@ struct ResidualSet {
 // launches waits for, and it need not write 784 bytes that no one reads.
 struct NoTable {};
 constexpr bool alone(int mode) { return mode == 0 || mode >= 3; }
+// A launch with an epilogue (8 on top of the number of pieces, K) has that in the same place.
+constexpr bool with_epilogue(int k) { return k >= 8; }
+template <int MODE, int KE>
+using Extra = std::conditional_t<with_epilogue(KE), ecs::EcsEpilogue, std::conditional_t<alone(MODE), NoTable, ecs::EcsBatch>>;
+
+// What the epilogue reads for one value of y = act(sum + bias) * gate + residual.  A row's are requested before its sums are added up,
+// the first row's of each 16 lanes before the workgroup's last chunks: they come from HBM, and a workgroup has a row or two for each.
+template <int VW>
+struct EpilogueValues {
+    uint32_t bias, gate, residual;
+    static __device__ __forceinline__ uint32_t load(const uint16_t *p, size_t i)
+    {
+        if constexpr (VW == 2) return p[i];
+        return reinterpret_cast<const uint32_t *>(p)[i];
+    }
+    static __device__ __forceinline__ float value(uint32_t w)
+    {
+        if constexpr (VW == 2) return half_bits_to_float(w);
+        return __uint_as_float(w);
+    }
+    __device__ __forceinline__ void request(const ecs::EcsEpilogue &e, uint32_t row, size_t at)
+    {
+        if (e.bias) bias = load(e.bias, row);
+        if (e.gate) gate = load(e.gate, at);
+        if (e.residual) residual = load(e.residual, at);
+    }
+    // in FP32: rounded once, where y is stored
+    __device__ __forceinline__ float apply(const ecs::EcsEpilogue &e, float t) const
+    {
+        if (e.bias) t += value(bias);
+        switch (e.activation) {
+        case ecs::ECS_ACT_RELU: t = t < 0.0f ? 0.0f : t; break;                      // (NaN stays)
+        case ecs::ECS_ACT_SILU: t = t / (1.0f + expf(-t)); break;
+        case ecs::ECS_ACT_GELU: t = 0.5f * t * erfcf(-0.70710678118654752f * t); break;
+        default: break;
+        }
+        if (e.gate) t *= value(gate);
+        if (e.residual) t += value(residual);
+        return t;
+    }
+};
 
 // TM: bit t set = the image holds units of granularity 2 << t somewhere (the residual set is always handled);
 // DB: width of the delta indices in bits; MODE: 0 = a launch that carries one SpMV (nothing of the batch table is
@@ -702,16 +749,19 @@ constexpr bool alone(int mode) { return mode == 0 || mode >= 3; }
 // 16384 x 1024, 4-bit 6.5 us without it and 7.1 with it, 768 x 768 with four 3.56 and 3.76), 4 = one SpMV whose x is brought before
 // the first chunks are requested (launch_b);
 // K: 16-byte pieces of [tables | x] each thread brings to LDS before the rest follows; 5: four, and the rest directly;
+// 8 more with an epilogue;
 // NB: right-hand sides handled at once (x holds n rows of NB values, y m rows of NB values);
 // VW: bytes per value of W, x and y (2 = FP16, 4 = FP32)
-template <int TM, int DB, int MODE, int K, int NB, int VW>
+template <int TM, int DB, int MODE, int KE, int NB, int VW>
 __global__ __launch_bounds__(1024) void ecspmv_kernel(const uint32_t count, const uint32_t threads, const uint8_t *image0,
                                                       const uint16_t *x0, uint16_t *y0, const uint32_t n0,
                                                       const uint32_t panel_stride0, const uint32_t meta_stride0,
                                                       const uint32_t x_bytes0, const uint32_t block_end0,
                                                       const uint32_t row_stride0, const uint64_t trace_words,
-                                                      const std::conditional_t<alone(MODE), NoTable, ecs::EcsBatch> batch)
+                                                      const Extra<MODE, KE> batch)
 {
+    constexpr int K = KE & 7;
+    constexpr bool EPILOGUE = with_epilogue(KE);
 #ifdef ECS_TRACE
     const uint64_t t_start = __builtin_amdgcn_s_memtime(), t_start_real = __builtin_amdgcn_s_memrealtime();
 #endif
@@ -749,7 +799,7 @@ __global__ __launch_bounds__(1024) void ecspmv_kernel(const uint32_t count, cons
     // several right-hand sides: elements from one row of X (and of Y) to the next.  NB when the launch handles all
     // columns of X; larger when X has more columns than this launch takes.
     uint32_t ld = NB;
-    uint32_t panel_index = blockIdx.x - block0;
+    uint32_t panel_index = blockIdx.x - block0, first_column = 0;
     if constexpr (NB > 1) {
         ld = row_stride0;
         // Several workgroups per panel, each with NB of the columns of X (where not all fit LDS, or where there are few
@@ -762,6 +812,7 @@ __global__ __launch_bounds__(1024) void ecspmv_kernel(const uint32_t count, cons
             const uint32_t h = r / in_group;
             panel_index = 8u * g + r % in_group;
             it.x += h * (NB * VW / 2), it.y += h * (NB * VW / 2);
+            first_column = h * NB;
         }
     }
     const uint16_t *__restrict__ x = it.x;
@@ -994,6 +1045,16 @@ __global__ __launch_bounds__(1024) void ecspmv_kernel(const uint32_t count, cons
     }
     __syncthreads();
     ECS_STAMP(c, 4);            // first barrier passed
+    EpilogueValues<VW> ahead = {};
+    auto request_epilogue = [&](uint32_t r) {
+        if constexpr (EPILOGUE)
+            if (r < hdr[PH_NROWS] && (tid & 15) < (uint32_t)NB) {
+                const uint32_t row = reinterpret_cast<const uint32_t *>(meta + hdr[PH_ROWIDX_OFF])[r];
+                ahead.request(batch, row, (size_t)row * ld + first_column + (tid & 15));
+            }
+    };
+    constexpr bool AHEAD = EPILOGUE && !PHASES && TM < 8;          // (a 16-grained set leaves no registers for it)
+    if constexpr (AHEAD) request_epilogue(tid >> 4);
 
     // (eight right-hand sides with an 8-grained set, and `tight`: after the first chunk of the coarsest set, whose sums leave no
     // registers for it)
@@ -1029,6 +1090,9 @@ __global__ __launch_bounds__(1024) void ecspmv_kernel(const uint32_t count, cons
     const uint32_t j = tid & 15;
     if constexpr (NB == 1) {
         for (uint32_t r = tid >> 4; r < nrows; r += nt >> 4) {
+            if constexpr (EPILOGUE && !AHEAD) request_epilogue(r);
+            const EpilogueValues<VW> mine = ahead;
+            if constexpr (AHEAD) request_epilogue(r + (nt >> 4));
             float sum = 0.0f;
             if constexpr (TM != 0) {
                 const uint32_t s0 = rowslot[r], s1 = rowslot[r + 1];
@@ -1036,7 +1100,8 @@ __global__ __launch_bounds__(1024) void ecspmv_kernel(const uint32_t count, cons
             }
             const uint32_t l0 = rowlu[r], l1 = rowlu[r + 1];
             for (uint32_t q = l0 + j; q < l1; q += 16) sum += part[q];
-            const float t = row16_allreduce(sum);
+            float t = row16_allreduce(sum);
+            if constexpr (EPILOGUE) t = mine.apply(batch, t);
             if constexpr (VW == 2) {
                 if (j == 0) y[rowidx[r]] = __half_as_ushort(__float2half_rn(t));
             } else {
@@ -1045,8 +1110,9 @@ __global__ __launch_bounds__(1024) void ecspmv_kernel(const uint32_t count, cons
         }
     } else {
         // lane k stores the k-th total
-        auto store = [&](uint32_t r, const float (&sum)[NB]) {
-            const float out = row16_sums<NB>(sum, j);
+        auto store = [&](uint32_t r, const float (&sum)[NB], const EpilogueValues<VW> &mine) {
+            float out = row16_sums<NB>(sum, j);
+            if constexpr (EPILOGUE) out = mine.apply(batch, out);
             if (j < (uint32_t)NB) {
                 if constexpr (VW == 2)
                     y[(size_t)rowidx[r] * ld + j] = __half_as_ushort(__float2half_rn(out));
@@ -1056,6 +1122,9 @@ __global__ __launch_bounds__(1024) void ecspmv_kernel(const uint32_t count, cons
         };
         if constexpr (!PHASES) {
             for (uint32_t r = tid >> 4; r < nrows; r += nt >> 4) {
+                if constexpr (EPILOGUE && !AHEAD) request_epilogue(r);
+                const EpilogueValues<VW> mine = ahead;
+                if constexpr (AHEAD) request_epilogue(r + (nt >> 4));
                 float sum[NB] = {};
                 if constexpr (TM != 0) {
                     const uint32_t s0 = rowslot[r], s1 = rowslot[r + 1];
@@ -1063,7 +1132,7 @@ __global__ __launch_bounds__(1024) void ecspmv_kernel(const uint32_t count, cons
                 }
                 const uint32_t l0 = rowlu[r], l1 = rowlu[r + 1];
                 for (uint32_t q = l0 + j; q < l1; q += 16) Partial<NB>::add(part, c.pstride, q, sum);
-                store(r, sum);
+                store(r, sum, mine);
             }
         } else {
             // NB partial sums per lane unit are too much for LDS beside X on the larger panels, so the residual stream is
@@ -1081,6 +1150,8 @@ __global__ __launch_bounds__(1024) void ecspmv_kernel(const uint32_t count, cons
                     const uint32_t l0 = rowlu[r], l1 = rowlu[r + 1];
                     const bool done = last || l1 <= e;
                     if ((ph && l1 <= b) || (!done && l0 >= e)) continue;        // finished before, or not begun
+                    if constexpr (EPILOGUE)
+                        if (done) request_epilogue(r);
                     float sum[NB] = {};
                     uint32_t q = l0 + j;
                     if (ph && l0 < b) {
@@ -1097,7 +1168,7 @@ __global__ __launch_bounds__(1024) void ecspmv_kernel(const uint32_t count, cons
                         for (int k = 0; k < NB; ++k) carry[((ph & 1u) * 16u + j) * NB + k] = sum[k];
                         continue;
                     }
-                    store(r, sum);
+                    store(r, sum, ahead);
                 }
                 if (last) break;
                 __syncthreads();                   // the partial sums of this phase have been read
@@ -1113,6 +1184,7 @@ __global__ __launch_bounds__(1024) void ecspmv_kernel(const uint32_t count, cons
 #endif
 }
 
+#if !ECS_EPILOGUE
 // ---- plain CSR, one wavefront per row (comparison only)
 __global__ __launch_bounds__(256) void csr_kernel(const int32_t *__restrict__ rowptr, const int32_t *__restrict__ col,
                                                   const uint16_t *__restrict__ val, const uint16_t *__restrict__ x,
@@ -1182,6 +1254,8 @@ __global__ __launch_bounds__(1024) void empty_kernel(uint32_t *__restrict__ out)
     if (threadIdx.x == 0) out[blockIdx.x] = blockIdx.x;
 }
 
+#endif  // !ECS_EPILOGUE
+
 }  // namespace
 
 namespace ecs {
@@ -1220,41 +1294,14 @@ struct KernelArgs {
 };
 static_assert(offsetof(KernelArgs<EcsBatch>, table) == 64, "where the kernel reads the table");
 
-// handle of a kernel on the device of `stream` (the null stream: the current one), which need not be the current device;
-// asked for once per device and kept as long as the library is loaded
-template <auto KERNEL>
-static int kernel_handle(void *stream, hipFunction_t *f)
-{
-    constexpr int kMaxDev = 64;
-    static std::atomic<hipFunction_t> cached[kMaxDev];
-    int current = 0, dev = 0;
-    hipError_t e = hipGetDevice(&current);
-    if (e != hipSuccess) return (int)e;
-    dev = current;
-    if (stream) e = hipStreamGetDevice((hipStream_t)stream, &dev);
-    if (e != hipSuccess) return (int)e;
-    const bool keep = dev >= 0 && dev < kMaxDev;
-    if (keep) *f = cached[dev].load(std::memory_order_acquire);
-    if (*f) return 0;
-    if (dev != current) e = hipSetDevice(dev);             // symbols are looked up on the current device
-    if (e != hipSuccess) return (int)e;
-    e = hipGetFuncBySymbol(f, reinterpret_cast<const void *>(KERNEL));
-    if (dev != current) {
-        const hipError_t back = hipSetDevice(current);
-        if (e == hipSuccess) e = back;
-    }
-    if (e != hipSuccess) return (int)e;
-    if (keep) cached[dev].store(*f, std::memory_order_release);
-    return 0;
-}
-
 template <int TM, int DB, int MODE, int K, int NB, int VW = 2>
 static int launch_m(const EcsBatch &batch, uint32_t threads, uint32_t lds_bytes, void *stream)
 {
-    typedef std::conditional_t<alone(MODE), NoTable, EcsBatch> Table;
+    constexpr int KE = ECS_EPILOGUE ? K + 8 : K;
+    typedef Extra<MODE, KE> Table;
     static thread_local uint32_t attr_set_for = 0;
     if (lds_bytes > 65536 && lds_bytes > attr_set_for) {
-        hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(ecspmv_kernel<TM, DB, MODE, K, NB, VW>),
+        hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(ecspmv_kernel<TM, DB, MODE, KE, NB, VW>),
                                            hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds_bytes);
         if (e != hipSuccess) return (int)e;
         attr_set_for = lds_bytes;
@@ -1272,9 +1319,13 @@ static int launch_m(const EcsBatch &batch, uint32_t threads, uint32_t lds_bytes,
     const EcsBatchItem &it = batch.item[0];
     KernelArgs<Table> args = {first, threads, it.image, it.x, it.y, it.n, it.panel_stride, it.meta_stride, it.x_bytes,
                               it.block_end, it.row_stride, trace_words, {}};
+#if ECS_EPILOGUE
+    args.table = static_cast<const EcsFused &>(batch).epilogue;
+#else
     if constexpr (MODE == 1 || MODE == 2) args.table = batch;
+#endif
     hipFunction_t f = nullptr;
-    const int e = kernel_handle<ecspmv_kernel<TM, DB, MODE, K, NB, VW>>(stream, &f);
+    const int e = kernel_handle<ecspmv_kernel<TM, DB, MODE, KE, NB, VW>>(stream, &f);
     if (e) {
         (void)hipGetLastError();                           // as below
         return e;
@@ -1295,7 +1346,7 @@ static int launch_k(const EcsBatch &batch, uint32_t threads, uint32_t lds_bytes,
     if constexpr (NB > 2 && K == 4)           // (two right-hand sides are refused where they do not fit in one phase)
         if (batch.per_phase) return launch_m<TM, DB, 3, K, NB, VW>(batch, threads, lds_bytes, stream);
     if (batch.count == 1) return launch_m<TM, DB, 0, K, NB, VW>(batch, threads, lds_bytes, stream);
-    if constexpr (NB == 1) return launch_m<TM, DB, 1, K, NB, VW>(batch, threads, lds_bytes, stream);
+    if constexpr (NB == 1 && !ECS_EPILOGUE) return launch_m<TM, DB, 1, K, NB, VW>(batch, threads, lds_bytes, stream);
     return (int)hipErrorInvalidValue;          // several right-hand sides: one matrix per launch
 }
 
@@ -1373,8 +1424,9 @@ static int launch_tm(const EcsBatch &batch, uint32_t threads, uint32_t lds_bytes
     // 8.92 / 9.14, 8 x 4096 x 800 7.87 / 8.18, 8 x 1024 x 2600 at 30 %, 8-bit 5.11 / 5.44, 2 x 4096 x 4096 at 50 % 8.97 / 9.39.
     const uint64_t grid = batch.item[batch.count - 1].block_end;
     const bool second = TM == 0 ? grid > 512u && chunks > 45u * grid : TM == 1 && 4u * block_chunks <= 3u * grid * (threads / 64u);
-    if (batch.count > 1 && second)
-        return delta_bits == 4 ? launch_b<TM, 4, TM <= 1>(batch, threads, lds_bytes, chunks, stream)
+    if constexpr (!ECS_EPILOGUE)
+        if (batch.count > 1 && second)
+            return delta_bits == 4 ? launch_b<TM, 4, TM <= 1>(batch, threads, lds_bytes, chunks, stream)
                                : launch_b<TM, 8, TM <= 1>(batch, threads, lds_bytes, chunks, stream);
     return delta_bits == 4 ? launch_b<TM, 4, false>(batch, threads, lds_bytes, chunks, stream)
                            : launch_b<TM, 8, false>(batch, threads, lds_bytes, chunks, stream);
@@ -1411,7 +1463,12 @@ static int launch_nb(const EcsBatch &batch, uint32_t threads, uint32_t lds_bytes
     }
 }
 
-int launch_ecspmv_multi(const EcsBatch &batch, uint32_t threads, uint32_t lds_bytes, uint32_t type_mask,
+#if ECS_EPILOGUE
+int launch_epilogue_multi(const EcsFused &batch, uint32_t threads,
+#else
+int launch_ecspmv_multi(const EcsBatch &batch, uint32_t threads,
+#endif
+                         uint32_t lds_bytes, uint32_t type_mask,
                         uint32_t delta_bits, uint32_t value_bits, uint32_t nb, void *stream)
 {
     const int top = (type_mask & 4) ? 7 : (type_mask & 2) ? 3 : (type_mask & 1) ? 1 : 0;
@@ -1440,7 +1497,12 @@ int launch_ecspmv_multi(const EcsBatch &batch, uint32_t threads, uint32_t lds_by
     return launch_nb<0, 8>(batch, threads, lds_bytes, nb, stream);
 }
 
-int launch_ecspmv(const EcsBatch &batch, uint32_t threads, uint32_t lds_bytes, uint32_t type_mask, uint32_t delta_bits,
+#if ECS_EPILOGUE
+int launch_epilogue(const EcsFused &batch, uint32_t threads,
+#else
+int launch_ecspmv(const EcsBatch &batch, uint32_t threads,
+#endif
+                  uint32_t lds_bytes, uint32_t type_mask, uint32_t delta_bits,
                   uint32_t value_bits, uint64_t chunks, uint64_t block_chunks, void *stream)
 {
     // one instantiation per highest granularity present: sets that do not occur cost no registers
@@ -1454,6 +1516,7 @@ int launch_ecspmv(const EcsBatch &batch, uint32_t threads, uint32_t lds_bytes, u
     }
 }
 
+#if !ECS_EPILOGUE
 int launch_csr(const void *d_rowptr, const void *d_col, const void *d_val, const void *d_x, void *d_y, uint32_t m,
                void *stream)
 {
@@ -1498,5 +1561,7 @@ int device_lds_limit(int *bytes)
     if (e != hipSuccess) return (int)e;
     return (int)hipDeviceGetAttribute(bytes, hipDeviceAttributeMaxSharedMemoryPerBlock, dev);
 }
+
+#endif  // !ECS_EPILOGUE
 
 }  // namespace ecs

@@ -25,6 +25,16 @@ struct EcsBatch {
 };
 static_assert(sizeof(EcsBatchItem) == 48 && sizeof(EcsBatch) == 16 + 48 * ECS_MAX_BATCH, "layout the kernel reads");
 
+// y = act(sum + bias) * gate + residual, in FP32, where the pointers are not null; values of y's type, gate and residual laid out as y
+enum { ECS_ACT_NONE = 0, ECS_ACT_RELU = 1, ECS_ACT_GELU = 2, ECS_ACT_SILU = 3 };
+struct EcsEpilogue {
+    const uint16_t *bias, *gate, *residual;
+    uint32_t activation, pad_;
+};
+struct EcsFused : EcsBatch {
+    EcsEpilogue epilogue;
+};
+
 // Launches one kernel for all items (count <= ECS_MAX_BATCH, same workgroup size for all; `chunks`: what a wavefront takes at a
 // time, of all items together; `block_chunks`: those of block units).
 int launch_ecspmv(const EcsBatch &batch, uint32_t threads, uint32_t lds_bytes, uint32_t type_mask, uint32_t delta_bits,
@@ -34,6 +44,11 @@ int launch_ecspmv(const EcsBatch &batch, uint32_t threads, uint32_t lds_bytes, u
 // 8-grained set with FP32 values.
 int launch_ecspmv_multi(const EcsBatch &batch, uint32_t threads, uint32_t lds_bytes, uint32_t type_mask,
                         uint32_t delta_bits, uint32_t value_bits, uint32_t nb, void *stream);
+// The same for one matrix with an epilogue
+int launch_epilogue(const EcsFused &batch, uint32_t threads, uint32_t lds_bytes, uint32_t type_mask, uint32_t delta_bits,
+                    uint32_t value_bits, uint64_t chunks, uint64_t block_chunks, void *stream);
+int launch_epilogue_multi(const EcsFused &batch, uint32_t threads, uint32_t lds_bytes, uint32_t type_mask, uint32_t delta_bits,
+                          uint32_t value_bits, uint32_t nb, void *stream);
 int launch_csr(const void *d_rowptr, const void *d_col, const void *d_val, const void *d_x, void *d_y, uint32_t m,
                void *stream);
 int launch_stream_read(const void *d_buf, uint64_t bytes, void *d_out, uint32_t num_wg, uint32_t threads, bool sliced,

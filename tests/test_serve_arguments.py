@@ -48,7 +48,17 @@ for name, o in arg["attention"]:
     out[name] = outcome(lambda: B.ecspmv_attention(cache(), attention(**o), work, size, stream[0]))
 for name, o in arg["verify"]:
     out[name] = outcome(lambda: B.ecspmv_verify(verify(**o), stream[0]))
+A = B.ecspmv_build_dense(np.ones((16, 128), np.float16), B.make_opts())
+F = B.ecspmv_build_dense_f32(np.ones((16, 128), np.float32), B.make_opts())
+early = outcome(lambda: A.ecspmv_run_epilogue(0x100000, 0x200000, 1, B.Epilogue(ctypes.sizeof(B.Epilogue), 1, 0, 0, 0), stream[0]))
+for M in (A, F):
+    M.ecspmv_upload(0x100000, M.ecspmv_device_bytes(), 0)
+out["early"] = early
+for name, f32, nb, fields in arg["epilogue"]:
+    e = B.Epilogue(ctypes.sizeof(B.Epilogue), *fields)
+    out[name] = outcome(lambda: (F if f32 else A).ecspmv_run_epilogue(0x100000, 0x200000, nb, e, stream[0]))
 L = B.lib()
+out["no epilogue"] = [L.ecspmv_run_epilogue(A._h, 0x100000, 0x200000, 1, None, 0), L.ecspmv_run_epilogue(None, 0x100000, 0x200000, 1, B.Epilogue(32), 0)]
 short = cache()
 short.struct_size = 3
 out["short"] = [L.ecspmv_kv_write(short, view(), view(), 0x800000, 5, 0), L.ecspmv_kv_write(None, view(), view(), 0x800000, 5, 0),
@@ -85,11 +95,14 @@ VERIFY = [("v ok", {}), ("v plain", dict(draft=0, count=0)), ("no vocab", dict(v
           ("no drafts", dict(drafts=0, drafted=0, draft=0)), ("no drafted", dict(drafted=0)), ("no target", dict(target=0)),
           ("target off", dict(target=0x100002)), ("no sequences", dict(batch=0, target=0)), ("no uniform", dict(uniform=0)),
           ("no accepted", dict(accepted=0))]
+EPILOGUE = [("e ok", 0, 1, [2, 0x300000, 0x300002, 0x300004]), ("e none", 0, 1, [0, 0, 0, 0]), ("e multi", 0, 4, [1, 0, 0, 0x300000]),
+            ("e f32", 1, 8, [3, 0x300004, 0, 0]), ("e act", 0, 1, [4, 0, 0, 0]), ("e act -1", 0, 1, [-1, 0, 0, 0]), ("e nb", 0, 3, [1, 0, 0, 0]),
+            ("e off", 0, 1, [0, 0x300001, 0, 0]), ("e f32 off", 1, 1, [0, 0, 0x300002, 0]), ("e f32 off residual", 1, 2, [0, 0, 0, 0x300002])]
 INVALID, UNSUPPORTED, HIP, SMALL = -1, -2, -4, -6
 
 
 def test_refusals(tmp_path):
-    got = standin.run(tmp_path, CODE, dict(cache=CACHE, rows=ROWS, attention=ATTENTION, verify=VERIFY))
+    got = standin.run(tmp_path, CODE, dict(cache=CACHE, rows=ROWS, attention=ATTENTION, verify=VERIFY, epilogue=EPILOGUE))
     for name, _ in CACHE:
         want = {"bits": UNSUPPORTED, "page 8": UNSUPPORTED, "page 48": UNSUPPORTED, "page 2048": UNSUPPORTED, "dim 8": UNSUPPORTED,
                 "dim 72": UNSUPPORTED, "dim 272": UNSUPPORTED, "ok": 0, "16 bits": 0}.get(name, INVALID)
@@ -104,6 +117,10 @@ def test_refusals(tmp_path):
     for name, _ in VERIFY:
         want = {"v ok": 1, "v plain": 1, "no drafts": 1, "no sequences": 0, "vocab": [UNSUPPORTED, 0]}.get(name, [INVALID, 0])
         assert got[name] == want, (name, got[name])
+    for name, *_ in EPILOGUE:
+        want = {"e ok": 1, "e none": 1, "e multi": 1, "e f32": 1, "e act": [UNSUPPORTED, 0], "e act -1": [UNSUPPORTED, 0]}.get(name, [INVALID, 0])
+        assert got[name] == want, (name, got[name])
+    assert got["early"] == [-5, 0] and got["no epilogue"] == [INVALID, INVALID]
     assert got["short"] == [INVALID] * 6
     assert got["work"] > 0 and got["enough"] == [1, [SMALL, 0]] and got["grid"] == 3 * 4 and got["none"] == [INVALID, 0]
     assert got["stream"] == [[0x1000, 0x100], [0x2000, 0x200], [0, 0x100], HIP]
