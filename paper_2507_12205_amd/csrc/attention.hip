@@ -430,6 +430,368 @@ __global__ __launch_bounds__(256) void attention_rows_kernel(const AttentionArgs
     }
 }
 
+// ---- 128 rows per workgroup, 32 for each of its wavefronts, which share the keys through LDS -----------------------------------------
+//
+// Tiles of KT keys and values lie in LDS twice: one is computed with while the next one is on its way, FP16 straight from memory to LDS, 8-
+// and 4-bit codes through registers, where they become FP16 values (exact whole numbers; their steps are applied to the products'
+// results and to the weights).  As above the keys are the rows of the first product, 32 x 32 at a time, a lane has column l % 32 and of
+// each 8 keys the four 4 (l / 32) ... + 3, and the weights stay in their lane; the second product's V^T comes from LDS through its
+// transposing read, four keys of a column per lane.
+// Pieces of 16 bytes are swapped within a row by the key's number, so that a wavefront's reads spread over all banks: of K, 16 lanes
+// read the same piece of 16 rows; of V, 64 bytes of 8 rows.
+template <int RC>
+__device__ __forceinline__ uint32_t k_swap(uint32_t key) { return RC >= 16 ? key & 15u : (key / (16 / RC)) & (RC - 1u); }
+template <int RC>
+__device__ __forceinline__ uint32_t v_swap(uint32_t key) { return RC >= 16 ? (key & 3u) << 2 : RC == 8 ? (key & 2u) << 1 : 0u; }
+
+// eight 4-bit codes, less 8, in their own order
+__device__ __forceinline__ uint4 nibble_values(uint32_t w)
+{
+    const uint32_t a = from_nibbles(w), b = from_nibbles(w >> 4), c = from_nibbles(w >> 8), d = from_nibbles(w >> 12);    // 0 4, 1 5, 2 6, 3 7
+    return make_uint4(__builtin_amdgcn_perm(b, a, 0x05040100u), __builtin_amdgcn_perm(d, c, 0x05040100u),
+                      __builtin_amdgcn_perm(b, a, 0x07060302u), __builtin_amdgcn_perm(d, c, 0x07060302u));
+}
+template <int BITS>
+__device__ __forceinline__ uint4 code_values(const Raw<BITS> &r)
+{
+    if constexpr (BITS == 16) return make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
+    if constexpr (BITS == 8) return __builtin_bit_cast(uint4, key_values<8>(r.w));
+    if constexpr (BITS == 4) return nibble_values(r.w[0]);
+}
+
+template <int BITS, int DP>
+__global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(const AttentionArgs a)
+{
+    constexpr int RC = DP <= 32 ? 4 : DP <= 64 ? 8 : DP <= 128 ? 16 : 32;              // 16-byte pieces of a row in LDS
+    constexpr int KT = RC == 32 ? 32 : 64, kHalves = KT / 32, kSteps = DP / 16, kTiles = DP / 32;
+    constexpr int kGroups = KT / 16;                                                   // a wavefront brings 16 keys; with 32, of K or of V
+    constexpr int kIssues = RC / 4;                                                    // accesses per lane for 16 rows
+    __shared__ uint4 lds_k[2][KT * RC], lds_v[2][KT * RC];
+    __shared__ float lds_step[2][2][2][KT];                                            // [buffer][k, v][step, low][key]
+    __shared__ float lds_top[2][4];
+    __shared__ uint32_t lds_odd[2];
+
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, n = lane & 31u, h = lane >> 5;
+    const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid >> 6));
+    const uint32_t head = blockIdx.x, tile = a.row_tiles - 1u - blockIdx.y / a.splits, split = blockIdx.y % a.splits;
+    const Sequence s(a, blockIdx.z);
+    const uint32_t rows = s.new_tokens * a.group, row0 = 128u * tile;
+    if (row0 >= rows) return;
+    const uint32_t dim = a.cache.dim, pieces = dim / 8u;
+
+    const uint32_t row = min(row0 + 32u * wave + n, rows - 1u), token = row / a.group;
+    const int32_t seen = min(s.behind + (int32_t)token + 1, (int32_t)s.len);
+    auto sees = [&](uint32_t r) -> int32_t {                                           // keys that row r sees
+        return max(min(s.behind + (int32_t)(min(r, rows - 1u) / a.group) + 1, (int32_t)s.len), 0);
+    };
+    const uint32_t end = (uint32_t)sees(row0 + 127u), all_see = (uint32_t)sees(row0);  // of the workgroup
+    const uint32_t wave_end = row0 + 32u * wave < rows ? (uint32_t)sees(row0 + 32u * wave + 31u) : 0u;
+    const uint32_t wave_all = (uint32_t)sees(row0 + 32u * wave);
+
+    half8v q[kSteps];
+    float q_sum = 0.0f;
+    {
+        const uint16_t *p = a.q.data + (int64_t)(s.first + token) * a.q.token_stride +
+                            (int64_t)(head * a.group + (row - token * a.group)) * a.q.head_stride;
+#pragma unroll
+        for (int t = 0; t < kSteps; ++t) {
+            const uint32_t d0 = 16u * t + 8u * h;
+            uint32_t w[4] = {0, 0, 0, 0};
+            if (d0 < dim) {
+                if (a.q_wide) {
+                    const uint4 v = *reinterpret_cast<const uint4 *>(p + d0);
+                    w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) w[i >> 1] |= (uint32_t)p[(int64_t)(d0 + i) * a.q.dim_stride] << (16 * (i & 1));
+                }
+            }
+            if constexpr (BITS == 4)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) q_sum += half_to_float(w[i] & 0xFFFFu) + half_to_float(w[i] >> 16);
+            q[t] = as_half8(w[0], w[1], w[2], w[3]);
+        }
+        if constexpr (BITS == 4) q_sum += __shfl_xor(q_sum, 32, 64);
+    }
+
+    const uint32_t tiles = (end + KT - 1u) / KT, per = (tiles + a.splits - 1u) / a.splits;
+    const uint32_t t0 = min(split * per, tiles), t1 = min(t0 + per, tiles);
+    const uint32_t page_mask = (1u << a.cache.page_shift) - 1u;
+    const uint64_t page_rows = (uint64_t)a.cache.heads << a.cache.page_shift, head_rows = (uint64_t)head << a.cache.page_shift;
+    const uint32_t group16 = kGroups == 4 ? wave : wave & 1u;
+    const bool brings_k = kGroups == 4 || wave < 2u, brings_v = kGroups == 4 || wave >= 2u;
+
+    for (uint32_t i = tid; i < 2u * KT * RC; i += 256u) {          // what is beyond dim stays zero
+        lds_k[0][i] = make_uint4(0, 0, 0, 0);
+        lds_v[0][i] = make_uint4(0, 0, 0, 0);
+    }
+    if (tid < 2u) lds_odd[tid] = 0;
+    __syncthreads();
+
+    // Bringing tile t into buffer b, this wavefront's 16 keys of it: request() sends the loads off, arrive() waits for them and writes what
+    // has come through registers.
+    Raw<BITS> raw_k[BITS < 16 ? kIssues : 1], raw_v[BITS < 16 ? kIssues : 1];
+    uint32_t raw_step = 0;
+    auto request = [&](uint32_t t, uint32_t b) {
+        const uint32_t key0 = t * KT + 16u * group16;
+        const uint32_t key = min(key0, (end - 1u) & ~15u);         // (of 16 keys beyond the end, the last ones again)
+        const uint64_t at = (uint64_t)page_of(a, s.table, key) * page_rows + head_rows + (key & page_mask);
+        const uint8_t *kp = a.cache.k + at * a.cache.row_bytes, *vp = a.cache.v + at * a.cache.row_bytes;
+#pragma unroll
+        for (int i = 0; i < kIssues; ++i) {
+            const uint32_t x = 64u * i + lane, r = x / RC, c = x % RC;               // row of the 16, piece
+            if constexpr (BITS == 16) {
+                const uint32_t to = (16u * group16) * RC + 64u * i;
+                if (const uint32_t from = c ^ k_swap<RC>(16u * group16 + r); brings_k && from < pieces)
+                    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(kp + r * a.cache.row_bytes + 16u * from),
+                                                     (__attribute__((address_space(3))) void *)(&lds_k[b][to]), 16, 0, 0);
+                if (const uint32_t from = c ^ v_swap<RC>(16u * group16 + r); brings_v && from < pieces)
+                    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(vp + r * a.cache.row_bytes + 16u * from),
+                                                     (__attribute__((address_space(3))) void *)(&lds_v[b][to]), 16, 0, 0);
+            } else {
+                const uint32_t cc = min(c, pieces - 1u);
+                if (brings_k) raw_k[i].load(kp + r * a.cache.row_bytes + cc * BITS);
+                if (brings_v) raw_v[i].load(vp + r * a.cache.row_bytes + cc * BITS);
+            }
+        }
+        if constexpr (BITS < 16)                                   // lanes 0 ... 15 the steps of the keys, 16 ... 31 those of the values
+            raw_step = *reinterpret_cast<const uint32_t *>(((lane & 16u) ? a.cache.v_step : a.cache.k_step) + 4u * (at + (lane & 15u)));
+    };
+    auto arrive = [&](uint32_t t, uint32_t b) {
+        const uint32_t key0 = t * KT + 16u * group16;
+        if constexpr (BITS == 16) {
+            __builtin_amdgcn_s_waitcnt(0x0F70);                    // vmcnt(0): what went straight to LDS is there
+            asm volatile("" ::: "memory");
+            if ((t + 1u) * KT > all_see && brings_v) {
+                // Some rows do not see all of this tile.  What no row sees may be anything: zeros; and values that are not finite are
+                // left out here, so that a weight of 0 makes nothing of them (they are added below in the rows that see them).
+                bool odd = false;
+#pragma unroll
+                for (int i = 0; i < kIssues; ++i) {
+                    const uint32_t x = 64u * i + lane, at = (16u * group16) * RC + x;
+                    uint4 v = lds_v[b][at];
+                    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                    for (uint32_t &y : w) {
+                        y = key0 + x / RC < end ? y : 0u;
+                        const uint32_t keep = ((y & 0x7C00u) != 0x7C00u ? 0xFFFFu : 0u) | ((y & 0x7C000000u) != 0x7C000000u ? 0xFFFF0000u : 0u);
+                        odd |= keep != 0xFFFFFFFFu;
+                        y &= keep;
+                    }
+                    lds_v[b][at] = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+                if (odd) lds_odd[b] = 1u;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kIssues; ++i) {
+                const uint32_t x = 64u * i + lane, r = x / RC, c = x % RC, kk = 16u * group16 + r;
+                if (c < pieces) {
+                    if (brings_k) lds_k[b][kk * RC + (c ^ k_swap<RC>(kk))] = code_values<BITS>(raw_k[i]);
+                    if (brings_v) lds_v[b][kk * RC + (c ^ v_swap<RC>(kk))] = code_values<BITS>(raw_v[i]);
+                }
+            }
+            const bool in = key0 + (lane & 15u) < end;
+            const float step = !in ? 0.0f : BITS == 8 ? __uint_as_float(raw_step) : step_of(raw_step);
+            const float low = !in || BITS == 8 ? 0.0f : low_of(raw_step);
+            if (lane < 32u) {
+                lds_step[b][lane >> 4][0][16u * group16 + (lane & 15u)] = step;
+                if constexpr (BITS == 4) lds_step[b][lane >> 4][1][16u * group16 + (lane & 15u)] = low;
+            }
+            float top = step;                                      // the largest step of the 16 values
+#pragma unroll
+            for (int o = 1; o < 16; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+            if (lane == 16u) lds_top[b][wave] = top;
+        }
+    };
+
+    typedef float f32x16 __attribute__((ext_vector_type(16)));
+    f32x16 acc[kTiles];
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) acc[i][x] = 0.0f;
+    // m: the maximum that weights are taken against, of t plus `unit` (with steps: the power of two above the largest step of V, so that
+    // weights with their steps stay in FP16's range); it may lie up to 8 below the true one, weights then go to 2^8
+    float m = kNone, m_true = kNone, l = 0.0f, z_acc = 0.0f, unit = 0.0f;
+    if constexpr (BITS < 16) unit = -32.0f;           // (the smallest step is 2^-31; not so low that weights without a step overflow)
+
+    auto compute = [&](uint32_t t, uint32_t b) {
+        const uint32_t key0 = t * KT;
+        float w[16 * kHalves];
+#pragma unroll
+        for (int x = 0; x < kHalves; ++x) {
+            f32x16 c = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+            const uint32_t key = 32u * x + n;
+#pragma unroll
+            for (int t = 0; t < kSteps; ++t)
+                c = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8v, lds_k[b][key * RC + ((2u * t + h) ^ k_swap<RC>(key))]), q[t], c, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) w[16 * x + i] = c[i] * a.scale_log2;
+        }
+        if constexpr (BITS < 16) {
+#pragma unroll
+            for (int i = 0; i < 16 * kHalves; i += 4) {
+                const uint32_t key = 8u * (i / 4) + 4u * h;
+                const f32x4 step = *reinterpret_cast<const f32x4 *>(&lds_step[b][0][0][key]);
+                f32x4 low = {0, 0, 0, 0};
+                if constexpr (BITS == 4) low = *reinterpret_cast<const f32x4 *>(&lds_step[b][0][1][key]) * (q_sum * a.scale_log2);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) w[i + r] = fmaf(w[i + r], step[r], low[r]);
+            }
+        }
+        if (key0 + KT > wave_all) {
+            const int32_t left = seen - (int32_t)(key0 + 4u * h);
+#pragma unroll
+            for (int i = 0; i < 16 * kHalves; ++i)
+                if (8 * (i / 4) + (i & 3) >= left) w[i] = kNone;
+        }
+        float most = w[0];
+#pragma unroll
+        for (int i = 1; i < 16 * kHalves; ++i) most = fmaxf(most, w[i]);
+        most = fmaxf(most, __shfl_xor(most, 32, 64));
+        m_true = fmaxf(m_true, most);
+        if constexpr (BITS < 16) {
+            float top = fmaxf(lds_top[b][2], lds_top[b][3]);
+            if constexpr (kGroups == 4) top = fmaxf(top, fmaxf(lds_top[b][0], lds_top[b][1]));
+            if (top > 0.0f) unit = fmaxf(unit, (float)(ilogbf(top) + 1));
+        }
+        const float m_new = m_true + unit;
+        if (const bool far = m_new > m + 8.0f; __any((int)far)) {
+            const float alpha = far ? __builtin_amdgcn_exp2f(m - m_new) : 1.0f;       // (0 where nothing was seen before)
+            m = far ? m_new : m;                                   // a row goes by its own scores alone
+            l *= alpha;
+            z_acc *= alpha;
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i) acc[i] *= alpha;
+        }
+        const float base = m == kNone ? 0.0f : m;
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16 * kHalves; ++i) {
+            w[i] = __builtin_amdgcn_exp2f(w[i] - base);
+            sum += w[i];
+        }
+        l += sum;
+        if constexpr (BITS < 16) {
+#pragma unroll
+            for (int i = 0; i < 16 * kHalves; i += 4) {
+                const uint32_t key = 8u * (i / 4) + 4u * h;
+                const f32x4 step = *reinterpret_cast<const f32x4 *>(&lds_step[b][1][0][key]);
+                if constexpr (BITS == 4) {
+                    const f32x4 low = *reinterpret_cast<const f32x4 *>(&lds_step[b][1][1][key]);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) z_acc = fmaf(w[i + r], low[r], z_acc);
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) w[i + r] *= step[r];
+            }
+        }
+        if constexpr (BITS == 16) {
+            if (lds_odd[b]) {
+                // values that are not finite, one key after the other, in the rows that see them
+                for (uint32_t k = 0; k < (uint32_t)KT && key0 + k < end; ++k) {
+                    const uint32_t i = 4u * (k / 8u) + (k & 3u);
+                    float x = w[0];
+#pragma unroll
+                    for (uint32_t y = 1; y < 16 * kHalves; ++y) x = i == y ? w[y] : x;
+                    x = __shfl(x, (int)(n + 32u * ((k >> 2) & 1u)), 64);
+                    if ((int32_t)(key0 + k) >= seen) continue;
+                    const uint32_t kk = key0 + k;
+                    const uint64_t at = (uint64_t)page_of(a, s.table, kk) * page_rows + head_rows + (kk & page_mask);
+                    const uint16_t *p = reinterpret_cast<const uint16_t *>(a.cache.v + at * a.cache.row_bytes);
+#pragma unroll
+                    for (int y = 0; y < kTiles; ++y)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const uint32_t d = 32u * y + 8u * (i / 4) + 4u * h + (i & 3);
+                            if (d < dim && (p[d] & 0x7C00u) == 0x7C00u) acc[y][i] = fmaf(x, half_to_float(p[d]), acc[y][i]);
+                        }
+                }
+            }
+        }
+        half8v weights[2 * kHalves];
+#pragma unroll
+        for (int x = 0; x < 2 * kHalves; ++x) {
+            uint32_t o[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = as_word(half2v{(_Float16)w[8 * x + 2 * i], (_Float16)w[8 * x + 2 * i + 1]});
+            weights[x] = as_half8(o[0], o[1], o[2], o[3]);
+        }
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        const uint32_t i16 = lane & 15u, sub = (lane >> 4) & 1u;   // a lane of 16: row i16 / 4 of four keys, values 4 (i16 % 4) ... + 3
+#pragma unroll
+        for (int x = 0; x < 2 * kHalves; ++x)
+#pragma unroll
+            for (int y = 0; y < kTiles; ++y) {
+                uint64_t o[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const uint32_t key = 16u * x + 8u * e + 4u * h + i16 / 4u;
+                    const uint32_t c = 4u * y + 2u * sub + ((i16 >> 1) & 1u);
+                    const uint4 *p = &lds_v[b][key * RC + (c ^ v_swap<RC>(key))];
+                    const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (__attribute__((address_space(3))) s16x4 *)(reinterpret_cast<const uint2 *>(p) + (i16 & 1u)));
+                    o[e] = __builtin_bit_cast(uint64_t, v);
+                }
+                const half8v v = as_half8((uint32_t)o[0], (uint32_t)(o[0] >> 32), (uint32_t)o[1], (uint32_t)(o[1] >> 32));
+                acc[y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, weights[x], acc[y], 0, 0, 0);
+            }
+    };
+
+    if (t0 < t1) {
+        request(t0, 0);
+        arrive(t0, 0);
+        __syncthreads();
+        for (uint32_t t = t0; t < t1; ++t) {
+            const uint32_t b = (t - t0) & 1u;
+            if (t + 1u < t1) request(t + 1u, b ^ 1u);
+            if (t * KT < wave_end) compute(t, b);
+            if (t + 1u < t1) arrive(t + 1u, b ^ 1u);
+            __syncthreads();
+        }
+    }
+
+    l += __shfl_xor(l, 32, 64);
+    if constexpr (BITS == 4) z_acc += __shfl_xor(z_acc, 32, 64);
+    const uint32_t out_row = row0 + 32u * wave + n;
+    if (out_row >= rows) return;
+    const uint32_t out_head = head * a.group + (row - token * a.group);
+    if (a.splits == 1u) {
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        uint16_t *p = a.out.data + (int64_t)(s.first + token) * a.out.token_stride + (int64_t)out_head * a.out.head_stride;
+#pragma unroll
+        for (int y = 0; y < kTiles; ++y)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const uint32_t d = 32u * y + 8u * (i / 4) + 4u * h;
+                if (d >= dim) continue;
+                uint32_t o[2];
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+                    o[r] = as_word(half2v{(_Float16)((acc[y][i + 2 * r] + z_acc) * inv), (_Float16)((acc[y][i + 2 * r + 1] + z_acc) * inv)});
+                if (a.out_wide) {
+                    *reinterpret_cast<uint2 *>(p + d) = make_uint2(o[0], o[1]);
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) p[(int64_t)(d + r) * a.out.dim_stride] = (uint16_t)(o[r >> 1] >> (16 * (r & 1)));
+                }
+            }
+    } else {
+        const uint64_t at = ((uint64_t)split * a.tokens + s.first + token) * a.q_heads + out_head;
+#pragma unroll
+        for (int y = 0; y < kTiles; ++y)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const uint32_t d = 32u * y + 8u * (i / 4) + 4u * h;
+                if (d < dim)
+                    *reinterpret_cast<f32x4 *>(a.part_o + at * dim + d) =
+                        f32x4{acc[y][i] + z_acc, acc[y][i + 1] + z_acc, acc[y][i + 2] + z_acc, acc[y][i + 3] + z_acc};
+            }
+        if (h == 0) a.part_ml[2 * at] = m, a.part_ml[2 * at + 1] = l;
+    }
+}
+
 // ---- joining the splits: a workgroup per (token, head), its wavefronts on different splits --------------------------------------------
 __global__ __launch_bounds__(256) void attention_join_kernel(const AttentionArgs a)
 {
@@ -480,6 +842,28 @@ int launch_rows(const AttentionArgs &a, void *stream)
     return ecs::launch_args<attention_rows_kernel<BITS, 256, true>>(a, gx, gy, gz, 256, stream);
 }
 
+template <int BITS>
+int launch_chunk(const AttentionArgs &a, void *stream)
+{
+    const uint32_t gx = a.cache.heads, gy = a.row_tiles * a.splits, gz = a.batch;
+    switch ((a.cache.dim + 31u) / 32u) {
+    case 1: return ecs::launch_args<attention_chunk_kernel<BITS, 32>>(a, gx, gy, gz, 256, stream);
+    case 2: return ecs::launch_args<attention_chunk_kernel<BITS, 64>>(a, gx, gy, gz, 256, stream);
+    case 3: return ecs::launch_args<attention_chunk_kernel<BITS, 96>>(a, gx, gy, gz, 256, stream);
+    case 4: return ecs::launch_args<attention_chunk_kernel<BITS, 128>>(a, gx, gy, gz, 256, stream);
+    case 5: return ecs::launch_args<attention_chunk_kernel<BITS, 160>>(a, gx, gy, gz, 256, stream);
+    case 6: return ecs::launch_args<attention_chunk_kernel<BITS, 192>>(a, gx, gy, gz, 256, stream);
+    case 7: return ecs::launch_args<attention_chunk_kernel<BITS, 224>>(a, gx, gy, gz, 256, stream);
+    default: return ecs::launch_args<attention_chunk_kernel<BITS, 256>>(a, gx, gy, gz, 256, stream);
+    }
+}
+
+template <int BITS>
+int launch_bits(const AttentionArgs &a, void *stream)
+{
+    return a.chunk ? launch_chunk<BITS>(a, stream) : launch_rows<BITS>(a, stream);
+}
+
 }  // namespace
 
 namespace ecs {
@@ -488,10 +872,12 @@ AttentionPlan plan_attention(uint32_t batch, uint32_t kv_heads, uint32_t group, 
 {
     AttentionPlan p = {};
     const uint64_t rows = (uint64_t)max_new * group;
-    p.row_tiles = (uint32_t)((rows + 15u) / 16u);
+    p.chunk = rows > 32u;
+    const uint64_t per_tile = p.chunk ? 128u : 16u;
+    p.row_tiles = (uint32_t)((rows + per_tile - 1u) / per_tile);
     const uint64_t blocks = (uint64_t)p.row_tiles * kv_heads * batch;
-    // enough workgroups for the chip, and two rounds of 32 keys for each wavefront of a split
-    const uint64_t by_chip = blocks ? 1024u / blocks : 1u, by_keys = (max_kv + 255u) / 256u;
+    // enough workgroups for the chip, and two rounds of 32 keys for each wavefront of a split (of 64 keys for a workgroup)
+    const uint64_t by_chip = blocks ? (p.chunk ? 512u : 1024u) / blocks : 1u, by_keys = (max_kv + 255u) / 256u;
     p.splits = (uint32_t)std::max<uint64_t>(1u, std::min(by_chip, by_keys));
     if (p.splits > 1u) p.work_bytes = (uint64_t)p.splits * tokens * kv_heads * group * (dim + 2u) * sizeof(float);
     return p;
@@ -499,7 +885,7 @@ AttentionPlan plan_attention(uint32_t batch, uint32_t kv_heads, uint32_t group, 
 
 int launch_attention(const AttentionArgs &a, void *stream)
 {
-    int e = a.cache.bits == 16 ? launch_rows<16>(a, stream) : a.cache.bits == 8 ? launch_rows<8>(a, stream) : launch_rows<4>(a, stream);
+    const int e = a.cache.bits == 16 ? launch_bits<16>(a, stream) : a.cache.bits == 8 ? launch_bits<8>(a, stream) : launch_bits<4>(a, stream);
     if (e || a.splits == 1u) return e;
     return launch_args<attention_join_kernel>(a, a.tokens * a.q_heads, 1, 1, 256, stream);
 }

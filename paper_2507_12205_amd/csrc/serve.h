@@ -39,12 +39,12 @@ struct AttentionArgs {
     float *part_o, *part_ml;              // partial results of the splits (splits > 1)
     uint32_t tokens, q_heads, group;      // group: heads of q per head of the cache
     uint32_t batch, max_pages, max_new;
-    uint32_t row_tiles, splits;
+    uint32_t chunk, row_tiles, splits;    // chunk: 128 rows per workgroup instead of 16
     uint32_t q_wide, out_wide;
     float scale_log2;                     // scale * log2(e)
 };
 struct AttentionPlan {
-    uint32_t row_tiles, splits;
+    uint32_t chunk, row_tiles, splits;
     uint64_t work_bytes;
 };
 AttentionPlan plan_attention(uint32_t batch, uint32_t kv_heads, uint32_t group, uint32_t dim, uint64_t tokens, uint32_t max_new, uint64_t max_kv);
