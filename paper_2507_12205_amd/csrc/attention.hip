@@ -8,6 +8,7 @@
 #include <hip/hip_fp16.h>
 #include <stdint.h>
 #include <algorithm>
+#include <type_traits>
 
 #include "kernel_handle.h"
 #include "serve.h"
@@ -466,14 +467,22 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
     constexpr int KT = RC == 32 ? 32 : 64, kHalves = KT / 32, kSteps = DP / 16, kTiles = DP / 32;
     constexpr int kGroups = KT / 16;                                                   // a wavefront brings 16 keys; with 32, of K or of V
     constexpr int kIssues = RC / 4;                                                    // accesses per lane for 16 rows
-    __shared__ uint4 lds_k[2][KT * RC], lds_v[2][KT * RC];
+    // (four objects and not two of twice the size: a read of LDS then waits for what is on its way into the same object only)
+    __shared__ uint4 lds_k0[KT * RC], lds_k1[KT * RC], lds_v0[KT * RC], lds_v1[KT * RC];
     __shared__ float lds_step[2][2][2][KT];                                            // [buffer][k, v][step, low][key]
     __shared__ float lds_top[2][4];
     __shared__ uint32_t lds_odd[2];
 
     const uint32_t tid = threadIdx.x, lane = tid & 63u, n = lane & 31u, h = lane >> 5;
     const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid >> 6));
-    const uint32_t head = blockIdx.x, tile = a.row_tiles - 1u - blockIdx.y / a.splits, split = blockIdx.y % a.splits;
+    // the last rows see the most keys: their workgroups start first.  Where all workgroups run at once (two on a compute unit, one that
+    // starts early beside one that starts late), the second half goes the other way, so that each pair has the same to do.
+    uint32_t tile = blockIdx.y / a.splits;
+    if (tile < (a.row_tiles + 1u) / 2u || gridDim.x * gridDim.y * gridDim.z > 512u)
+        tile = a.row_tiles - 1u - tile;
+    else
+        tile -= (a.row_tiles + 1u) / 2u;
+    const uint32_t head = blockIdx.x, split = blockIdx.y % a.splits;
     const Sequence s(a, blockIdx.z);
     const uint32_t rows = s.new_tokens * a.group, row0 = 128u * tile;
     if (row0 >= rows) return;
@@ -486,7 +495,6 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
     };
     const uint32_t end = (uint32_t)sees(row0 + 127u), all_see = (uint32_t)sees(row0);  // of the workgroup
     const uint32_t wave_end = row0 + 32u * wave < rows ? (uint32_t)sees(row0 + 32u * wave + 31u) : 0u;
-    const uint32_t wave_all = (uint32_t)sees(row0 + 32u * wave);
 
     half8v q[kSteps];
     float q_sum = 0.0f;
@@ -506,6 +514,9 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
                     for (int i = 0; i < 8; ++i) w[i >> 1] |= (uint32_t)p[(int64_t)(d0 + i) * a.q.dim_stride] << (16 * (i & 1));
                 }
             }
+            if (a.scale_log2 < 0.0f)                               // the largest score is the one with the largest product
+#pragma unroll
+                for (uint32_t &x : w) x ^= 0x80008000u;
             if constexpr (BITS == 4)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) q_sum += half_to_float(w[i] & 0xFFFFu) + half_to_float(w[i] >> 16);
@@ -513,6 +524,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
         }
         if constexpr (BITS == 4) q_sum += __shfl_xor(q_sum, 32, 64);
     }
+    const float scale = fabsf(a.scale_log2), by = BITS == 16 ? scale : 1.0f;
 
     const uint32_t tiles = (end + KT - 1u) / KT, per = (tiles + a.splits - 1u) / a.splits;
     const uint32_t t0 = min(split * per, tiles), t1 = min(t0 + per, tiles);
@@ -521,10 +533,9 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
     const uint32_t group16 = kGroups == 4 ? wave : wave & 1u;
     const bool brings_k = kGroups == 4 || wave < 2u, brings_v = kGroups == 4 || wave >= 2u;
 
-    for (uint32_t i = tid; i < 2u * KT * RC; i += 256u) {          // what is beyond dim stays zero
-        lds_k[0][i] = make_uint4(0, 0, 0, 0);
-        lds_v[0][i] = make_uint4(0, 0, 0, 0);
-    }
+    if (dim < (uint32_t)DP)
+        for (uint32_t i = tid; i < KT * RC; i += 256u)             // what is beyond dim stays zero
+            lds_k0[i] = lds_k1[i] = lds_v0[i] = lds_v1[i] = make_uint4(0, 0, 0, 0);
     if (tid < 2u) lds_odd[tid] = 0;
     __syncthreads();
 
@@ -532,10 +543,15 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
     // has come through registers.
     Raw<BITS> raw_k[BITS < 16 ? kIssues : 1], raw_v[BITS < 16 ? kIssues : 1];
     uint32_t raw_step = 0;
-    auto request = [&](uint32_t t, uint32_t b) {
-        const uint32_t key0 = t * KT + 16u * group16;
-        const uint32_t key = min(key0, (end - 1u) & ~15u);         // (of 16 keys beyond the end, the last ones again)
-        const uint64_t at = (uint64_t)page_of(a, s.table, key) * page_rows + head_rows + (key & page_mask);
+    auto first_key = [&](uint32_t t) { return min(t * KT + 16u * group16, (end - 1u) & ~15u); };      // (beyond the end: the last 16 keys again)
+    uint32_t page_list = 0;                                        // lane i: the page of this wavefront's keys in the i-th tile of 64
+    auto request = [&](uint32_t t, auto buffer) {
+        constexpr int b = decltype(buffer)::value;
+        uint4 *lds_k = b ? lds_k1 : lds_k0, *lds_v = b ? lds_v1 : lds_v0;
+        if (((t - t0) & 63u) == 0) page_list = page_of(a, s.table, first_key(t + lane));
+        const uint32_t key = first_key(t);
+        const uint32_t page = (uint32_t)__builtin_amdgcn_readlane((int)page_list, (int)((t - t0) & 63u));
+        const uint64_t at = (uint64_t)page * page_rows + head_rows + (key & page_mask);
         const uint8_t *kp = a.cache.k + at * a.cache.row_bytes, *vp = a.cache.v + at * a.cache.row_bytes;
 #pragma unroll
         for (int i = 0; i < kIssues; ++i) {
@@ -544,10 +560,10 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
                 const uint32_t to = (16u * group16) * RC + 64u * i;
                 if (const uint32_t from = c ^ k_swap<RC>(16u * group16 + r); brings_k && from < pieces)
                     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(kp + r * a.cache.row_bytes + 16u * from),
-                                                     (__attribute__((address_space(3))) void *)(&lds_k[b][to]), 16, 0, 0);
+                                                     (__attribute__((address_space(3))) void *)(&lds_k[to]), 16, 0, 0);
                 if (const uint32_t from = c ^ v_swap<RC>(16u * group16 + r); brings_v && from < pieces)
                     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(vp + r * a.cache.row_bytes + 16u * from),
-                                                     (__attribute__((address_space(3))) void *)(&lds_v[b][to]), 16, 0, 0);
+                                                     (__attribute__((address_space(3))) void *)(&lds_v[to]), 16, 0, 0);
             } else {
                 const uint32_t cc = min(c, pieces - 1u);
                 if (brings_k) raw_k[i].load(kp + r * a.cache.row_bytes + cc * BITS);
@@ -557,7 +573,9 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
         if constexpr (BITS < 16)                                   // lanes 0 ... 15 the steps of the keys, 16 ... 31 those of the values
             raw_step = *reinterpret_cast<const uint32_t *>(((lane & 16u) ? a.cache.v_step : a.cache.k_step) + 4u * (at + (lane & 15u)));
     };
-    auto arrive = [&](uint32_t t, uint32_t b) {
+    auto arrive = [&](uint32_t t, auto buffer) {
+        constexpr int b = decltype(buffer)::value;
+        uint4 *lds_k = b ? lds_k1 : lds_k0, *lds_v = b ? lds_v1 : lds_v0;
         const uint32_t key0 = t * KT + 16u * group16;
         if constexpr (BITS == 16) {
             __builtin_amdgcn_s_waitcnt(0x0F70);                    // vmcnt(0): what went straight to LDS is there
@@ -569,7 +587,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
 #pragma unroll
                 for (int i = 0; i < kIssues; ++i) {
                     const uint32_t x = 64u * i + lane, at = (16u * group16) * RC + x;
-                    uint4 v = lds_v[b][at];
+                    uint4 v = lds_v[at];
                     uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
                     for (uint32_t &y : w) {
@@ -578,7 +596,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
                         odd |= keep != 0xFFFFFFFFu;
                         y &= keep;
                     }
-                    lds_v[b][at] = make_uint4(w[0], w[1], w[2], w[3]);
+                    lds_v[at] = make_uint4(w[0], w[1], w[2], w[3]);
                 }
                 if (odd) lds_odd[b] = 1u;
             }
@@ -587,16 +605,17 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
             for (int i = 0; i < kIssues; ++i) {
                 const uint32_t x = 64u * i + lane, r = x / RC, c = x % RC, kk = 16u * group16 + r;
                 if (c < pieces) {
-                    if (brings_k) lds_k[b][kk * RC + (c ^ k_swap<RC>(kk))] = code_values<BITS>(raw_k[i]);
-                    if (brings_v) lds_v[b][kk * RC + (c ^ v_swap<RC>(kk))] = code_values<BITS>(raw_v[i]);
+                    if (brings_k) lds_k[kk * RC + (c ^ k_swap<RC>(kk))] = code_values<BITS>(raw_k[i]);
+                    if (brings_v) lds_v[kk * RC + (c ^ v_swap<RC>(kk))] = code_values<BITS>(raw_v[i]);
                 }
             }
             const bool in = key0 + (lane & 15u) < end;
             const float step = !in ? 0.0f : BITS == 8 ? __uint_as_float(raw_step) : step_of(raw_step);
             const float low = !in || BITS == 8 ? 0.0f : low_of(raw_step);
             if (lane < 32u) {
-                lds_step[b][lane >> 4][0][16u * group16 + (lane & 15u)] = step;
-                if constexpr (BITS == 4) lds_step[b][lane >> 4][1][16u * group16 + (lane & 15u)] = low;
+                const float f = lane < 16u ? scale : 1.0f;
+                lds_step[b][lane >> 4][0][16u * group16 + (lane & 15u)] = f * step;
+                if constexpr (BITS == 4) lds_step[b][lane >> 4][1][16u * group16 + (lane & 15u)] = f * low;
             }
             float top = step;                                      // the largest step of the 16 values
 #pragma unroll
@@ -616,8 +635,11 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
     float m = kNone, m_true = kNone, l = 0.0f, z_acc = 0.0f, unit = 0.0f;
     if constexpr (BITS < 16) unit = -32.0f;           // (the smallest step is 2^-31; not so low that weights without a step overflow)
 
-    auto compute = [&](uint32_t t, uint32_t b) {
+    auto compute = [&](uint32_t t, auto buffer) {
+        constexpr int b = decltype(buffer)::value;
+        const uint4 *lds_k = b ? lds_k1 : lds_k0, *lds_v = b ? lds_v1 : lds_v0;
         const uint32_t key0 = t * KT;
+        const bool masked = key0 + KT > all_see;                   // not all rows see all of the tile
         float w[16 * kHalves];
 #pragma unroll
         for (int x = 0; x < kHalves; ++x) {
@@ -625,23 +647,28 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
             const uint32_t key = 32u * x + n;
 #pragma unroll
             for (int t = 0; t < kSteps; ++t)
-                c = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8v, lds_k[b][key * RC + ((2u * t + h) ^ k_swap<RC>(key))]), q[t], c, 0, 0, 0);
+                c = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8v, lds_k[key * RC + ((2u * t + h) ^ k_swap<RC>(key))]), q[t], c, 0, 0, 0);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) w[16 * x + i] = c[i] * a.scale_log2;
+            for (int i = 0; i < 16; ++i) w[16 * x + i] = c[i];
         }
         if constexpr (BITS < 16) {
 #pragma unroll
-            for (int i = 0; i < 16 * kHalves; i += 4) {
+            for (int i = 0; i < 16 * kHalves; i += 4) {            // (the steps of the keys have the scale in them)
                 const uint32_t key = 8u * (i / 4) + 4u * h;
                 const f32x4 step = *reinterpret_cast<const f32x4 *>(&lds_step[b][0][0][key]);
-                f32x4 low = {0, 0, 0, 0};
-                if constexpr (BITS == 4) low = *reinterpret_cast<const f32x4 *>(&lds_step[b][0][1][key]) * (q_sum * a.scale_log2);
+                if constexpr (BITS == 4) {
+                    const f32x4 low = *reinterpret_cast<const f32x4 *>(&lds_step[b][0][1][key]) * q_sum;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) w[i + r] = fmaf(w[i + r], step[r], low[r]);
+                    for (int r = 0; r < 4; ++r) w[i + r] = fmaf(w[i + r], step[r], low[r]);
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) w[i + r] *= step[r];
+                }
             }
         }
-        if (key0 + KT > wave_all) {
-            const int32_t left = seen - (int32_t)(key0 + 4u * h);
+        if (masked) {
+            int32_t left = seen - (int32_t)(key0 + 4u * h);
+            asm volatile("" : "+v"(left));                         // (kept a branch: few tiles take it)
 #pragma unroll
             for (int i = 0; i < 16 * kHalves; ++i)
                 if (8 * (i / 4) + (i & 3) >= left) w[i] = kNone;
@@ -650,7 +677,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
 #pragma unroll
         for (int i = 1; i < 16 * kHalves; ++i) most = fmaxf(most, w[i]);
         most = fmaxf(most, __shfl_xor(most, 32, 64));
-        m_true = fmaxf(m_true, most);
+        m_true = fmaxf(m_true, most * by);
         if constexpr (BITS < 16) {
             float top = fmaxf(lds_top[b][2], lds_top[b][3]);
             if constexpr (kGroups == 4) top = fmaxf(top, fmaxf(lds_top[b][0], lds_top[b][1]));
@@ -669,10 +696,9 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
         float sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < 16 * kHalves; ++i) {
-            w[i] = __builtin_amdgcn_exp2f(w[i] - base);
-            sum += w[i];
+            w[i] = __builtin_amdgcn_exp2f(BITS == 16 ? fmaf(w[i], by, -base) : w[i] - base);
+            if constexpr (BITS < 16) sum += w[i];                  // (with FP16 the rounded ones are added up, below)
         }
-        l += sum;
         if constexpr (BITS < 16) {
 #pragma unroll
             for (int i = 0; i < 16 * kHalves; i += 4) {
@@ -688,7 +714,9 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
             }
         }
         if constexpr (BITS == 16) {
-            if (lds_odd[b]) {
+            if (masked && lds_odd[b]) {
+                uint32_t width = dim;
+                asm volatile("" : "+s"(width));                    // (nothing of this is worth a register outside)
                 // values that are not finite, one key after the other, in the rows that see them
                 for (uint32_t k = 0; k < (uint32_t)KT && key0 + k < end; ++k) {
                     const uint32_t i = 4u * (k / 8u) + (k & 3u);
@@ -705,7 +733,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
                             const uint32_t d = 32u * y + 8u * (i / 4) + 4u * h + (i & 3);
-                            if (d < dim && (p[d] & 0x7C00u) == 0x7C00u) acc[y][i] = fmaf(x, half_to_float(p[d]), acc[y][i]);
+                            if (d < width && (p[d] & 0x7C00u) == 0x7C00u) acc[y][i] = fmaf(x, half_to_float(p[d]), acc[y][i]);
                         }
                 }
             }
@@ -715,9 +743,14 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
         for (int x = 0; x < 2 * kHalves; ++x) {
             uint32_t o[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[i] = as_word(half2v{(_Float16)w[8 * x + 2 * i], (_Float16)w[8 * x + 2 * i + 1]});
+            for (int i = 0; i < 4; ++i) {
+                const half2v p = {(_Float16)w[8 * x + 2 * i], (_Float16)w[8 * x + 2 * i + 1]};
+                if constexpr (BITS == 16) sum = __builtin_amdgcn_fdot2(p, half2v{(_Float16)1.0f, (_Float16)1.0f}, sum, false);
+                o[i] = as_word(p);
+            }
             weights[x] = as_half8(o[0], o[1], o[2], o[3]);
         }
+        l += sum;
         typedef short s16x4 __attribute__((ext_vector_type(4)));
         const uint32_t i16 = lane & 15u, sub = (lane >> 4) & 1u;   // a lane of 16: row i16 / 4 of four keys, values 4 (i16 % 4) ... + 3
 #pragma unroll
@@ -729,7 +762,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
                 for (int e = 0; e < 2; ++e) {
                     const uint32_t key = 16u * x + 8u * e + 4u * h + i16 / 4u;
                     const uint32_t c = 4u * y + 2u * sub + ((i16 >> 1) & 1u);
-                    const uint4 *p = &lds_v[b][key * RC + (c ^ v_swap<RC>(key))];
+                    const uint4 *p = &lds_v[key * RC + (c ^ v_swap<RC>(key))];
                     const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                         (__attribute__((address_space(3))) s16x4 *)(reinterpret_cast<const uint2 *>(p) + (i16 & 1u)));
                     o[e] = __builtin_bit_cast(uint64_t, v);
@@ -739,16 +772,22 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
             }
     };
 
-    if (t0 < t1) {
-        request(t0, 0);
-        arrive(t0, 0);
+    auto step = [&](uint32_t t, auto buffer) {
+        const std::integral_constant<int, 1 - decltype(buffer)::value> other;
+        if (t + 1u < t1) request(t + 1u, other);
+        if (t * KT < wave_end) compute(t, buffer);
+        if (t + 1u < t1) arrive(t + 1u, other);
         __syncthreads();
-        for (uint32_t t = t0; t < t1; ++t) {
-            const uint32_t b = (t - t0) & 1u;
-            if (t + 1u < t1) request(t + 1u, b ^ 1u);
-            if (t * KT < wave_end) compute(t, b);
-            if (t + 1u < t1) arrive(t + 1u, b ^ 1u);
-            __syncthreads();
+    };
+    if (t0 < t1) {
+        const std::integral_constant<int, 0> first;
+        const std::integral_constant<int, 1> second;
+        request(t0, first);
+        arrive(t0, first);
+        __syncthreads();
+        for (uint32_t t = t0; t < t1; t += 2u) {
+            step(t, first);
+            if (t + 1u < t1) step(t + 1u, second);
         }
     }
 
