@@ -108,6 +108,25 @@ __device__ __forceinline__ half8v value_column(const R (&v)[8], int i)
 
 __device__ __forceinline__ float half_to_float(uint32_t h) { return __half2float(__ushort_as_half((unsigned short)h)); }
 
+// A value whose further use is worked out where it stands: in a loop, what follows from it is not kept in registers from before
+__device__ __forceinline__ uint32_t here(uint32_t x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+// the larger of a lane's value and that of the lane 32 (16) away, without LDS
+__device__ __forceinline__ float max_over_32(float x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float max_over_16(float x)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
 // the step of a 4-bit row, and what its code 8 stands for
 __device__ __forceinline__ float step_of(uint32_t w) { return half_to_float(w & 0xFFFFu); }
 __device__ __forceinline__ float low_of(uint32_t w) { return fmaf(8.0f, step_of(w), half_to_float(w >> 16)); }
@@ -285,8 +304,7 @@ __global__ __launch_bounds__(256) void attention_rows_kernel(const AttentionArgs
         float most = w[0];
 #pragma unroll
         for (int r = 1; r < 8; ++r) most = fmaxf(most, w[r]);
-        most = fmaxf(most, __shfl_xor(most, 16, 64));
-        most = fmaxf(most, __shfl_xor(most, 32, 64));
+        most = max_over_32(max_over_16(most));
         const float m_new = fmaxf(m, most), base = m_new == kNone ? 0.0f : m_new;
         const float alpha = exp2f(m - base);                       // (0 where nothing was seen before)
         m = m_new;
@@ -312,8 +330,7 @@ __global__ __launch_bounds__(256) void attention_rows_kernel(const AttentionArgs
                 top = fmaxf(top, step[r]);
                 if constexpr (BITS == 4) z_acc = in ? fmaf(w[r], low_of(vs[r]), z_acc) : z_acc;
             }
-            top = fmaxf(top, __shfl_xor(top, 16, 64));
-            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            top = max_over_32(max_over_16(top));
             if (top > unit) {
                 const float up = ldexpf(1.0f, ilogbf(top) + 1);
                 shrink *= unit / up;
@@ -553,40 +570,41 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
         const uint32_t page = (uint32_t)__builtin_amdgcn_readlane((int)page_list, (int)((t - t0) & 63u));
         const uint64_t at = (uint64_t)page * page_rows + head_rows + (key & page_mask);
         const uint8_t *kp = a.cache.k + at * a.cache.row_bytes, *vp = a.cache.v + at * a.cache.row_bytes;
+        const uint32_t self = here(lane);
 #pragma unroll
         for (int i = 0; i < kIssues; ++i) {
-            const uint32_t x = 64u * i + lane, r = x / RC, c = x % RC;               // row of the 16, piece
+            const uint32_t x = 64u * i + self, r = x / RC, c = x % RC;               // row of the 16, piece
             if constexpr (BITS == 16) {
-                const uint32_t to = (16u * group16) * RC + 64u * i;
+                const uint32_t to = (16u * group16) * RC + 64u * i, row = r * a.cache.row_bytes;
                 if (const uint32_t from = c ^ k_swap<RC>(16u * group16 + r); brings_k && from < pieces)
-                    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(kp + r * a.cache.row_bytes + 16u * from),
+                    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(kp + (row + 16u * from)),
                                                      (__attribute__((address_space(3))) void *)(&lds_k[to]), 16, 0, 0);
                 if (const uint32_t from = c ^ v_swap<RC>(16u * group16 + r); brings_v && from < pieces)
-                    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(vp + r * a.cache.row_bytes + 16u * from),
+                    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(vp + (row + 16u * from)),
                                                      (__attribute__((address_space(3))) void *)(&lds_v[to]), 16, 0, 0);
             } else {
-                const uint32_t cc = min(c, pieces - 1u);
-                if (brings_k) raw_k[i].load(kp + r * a.cache.row_bytes + cc * BITS);
-                if (brings_v) raw_v[i].load(vp + r * a.cache.row_bytes + cc * BITS);
+                const uint32_t from = r * a.cache.row_bytes + min(c, pieces - 1u) * BITS;
+                if (brings_k) raw_k[i].load(kp + from);
+                if (brings_v) raw_v[i].load(vp + from);
             }
         }
         if constexpr (BITS < 16)                                   // lanes 0 ... 15 the steps of the keys, 16 ... 31 those of the values
-            raw_step = *reinterpret_cast<const uint32_t *>(((lane & 16u) ? a.cache.v_step : a.cache.k_step) + 4u * (at + (lane & 15u)));
+            raw_step = *reinterpret_cast<const uint32_t *>(((self & 16u) ? a.cache.v_step : a.cache.k_step) + 4u * (at + (self & 15u)));
     };
     auto arrive = [&](uint32_t t, auto buffer) {
         constexpr int b = decltype(buffer)::value;
         uint4 *lds_k = b ? lds_k1 : lds_k0, *lds_v = b ? lds_v1 : lds_v0;
-        const uint32_t key0 = t * KT + 16u * group16;
+        const uint32_t key0 = t * KT + 16u * group16, self = here(lane);
         if constexpr (BITS == 16) {
             __builtin_amdgcn_s_waitcnt(0x0F70);                    // vmcnt(0): what went straight to LDS is there
             asm volatile("" ::: "memory");
             if ((t + 1u) * KT > all_see && brings_v) {
                 // Some rows do not see all of this tile.  What no row sees may be anything: zeros; and values that are not finite are
-                // left out here, so that a weight of 0 makes nothing of them (they are added below in the rows that see them).
+                // left out here, so that a weight of 0 makes nothing of them (they are added at the end in the rows that see them).
                 bool odd = false;
 #pragma unroll
                 for (int i = 0; i < kIssues; ++i) {
-                    const uint32_t x = 64u * i + lane, at = (16u * group16) * RC + x;
+                    const uint32_t x = 64u * i + self, at = (16u * group16) * RC + x;
                     uint4 v = lds_v[at];
                     uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -603,7 +621,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
         } else {
 #pragma unroll
             for (int i = 0; i < kIssues; ++i) {
-                const uint32_t x = 64u * i + lane, r = x / RC, c = x % RC, kk = 16u * group16 + r;
+                const uint32_t x = 64u * i + self, r = x / RC, c = x % RC, kk = 16u * group16 + r;
                 if (c < pieces) {
                     if (brings_k) lds_k[kk * RC + (c ^ k_swap<RC>(kk))] = code_values<BITS>(raw_k[i]);
                     if (brings_v) lds_v[kk * RC + (c ^ v_swap<RC>(kk))] = code_values<BITS>(raw_v[i]);
@@ -641,16 +659,47 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
         const uint32_t key0 = t * KT;
         const bool masked = key0 + KT > all_see;                   // not all rows see all of the tile
         float w[16 * kHalves];
+        // What is read of K and V is asked for a few products ahead, V's first half before the weights are worked out.  (Left to the
+        // compiler, the reads come pair by pair right before their products, and a wavefront waits for each: 140 us in the place of XX.)
+        half8v kf[kHalves][kSteps];
+        const uint32_t key_n = here(n);
+        auto read_k = [&](int y) {
 #pragma unroll
-        for (int x = 0; x < kHalves; ++x) {
-            f32x16 c = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
-            const uint32_t key = 32u * x + n;
+            for (int x = 0; x < kHalves; ++x) {
+                const uint32_t key = 32u * x + key_n;
+                kf[x][y] = __builtin_bit_cast(half8v, lds_k[key * RC + ((2u * y + h) ^ k_swap<RC>(key))]);
+            }
+        };
+        constexpr int kAhead = kSteps < 4 ? kSteps : 4;
 #pragma unroll
-            for (int t = 0; t < kSteps; ++t)
-                c = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8v, lds_k[key * RC + ((2u * t + h) ^ k_swap<RC>(key))]), q[t], c, 0, 0, 0);
+        for (int y = 0; y < kAhead; ++y) read_k(y);
+        __builtin_amdgcn_sched_barrier(0);
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        const uint32_t i16 = lane & 15u, sub = (lane >> 4) & 1u;   // a lane of 16: row i16 / 4 of four keys, values 4 (i16 % 4) ... + 3
+        constexpr int kReads = 4 * kHalves * kTiles;               // [16 keys][8 of them][32 values]
+        s16x4 vf[kReads];
+        auto read_v = [&](int i) {
+            const int x = i / (2 * kTiles), y = i % (2 * kTiles) / 2, e = i % 2;
+            const uint32_t key = 16u * x + 8u * e + 4u * h + i16 / 4u;
+            const uint32_t c = 4u * y + 2u * sub + ((i16 >> 1) & 1u);
+            const uint4 *p = &lds_v[key * RC + (c ^ v_swap<RC>(key))];
+            vf[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(reinterpret_cast<const uint2 *>(p) + (i16 & 1u)));
+        };
+        f32x16 c[kHalves];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) w[16 * x + i] = c[i];
+        for (int x = 0; x < kHalves; ++x) c[x] = f32x16{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+        for (int y = 0; y < kSteps; ++y) {
+#pragma unroll
+            for (int x = 0; x < kHalves; ++x) c[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[x][y], q[y], c[x], 0, 0, 0);
+            if (y + kAhead < kSteps) read_k(y + kAhead);
+            if (y >= kSteps - kAhead)
+#pragma unroll
+                for (int i = (y + kAhead - kSteps) * (kReads / 2) / kAhead; i < (y + 1 + kAhead - kSteps) * (kReads / 2) / kAhead; ++i) read_v(i);
+            __builtin_amdgcn_sched_barrier(0);
         }
+#pragma unroll
+        for (int i = 0; i < 16 * kHalves; ++i) w[i] = c[i / 16][i % 16];
         if constexpr (BITS < 16) {
 #pragma unroll
             for (int i = 0; i < 16 * kHalves; i += 4) {            // (the steps of the keys have the scale in them)
@@ -676,7 +725,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
         float most = w[0];
 #pragma unroll
         for (int i = 1; i < 16 * kHalves; ++i) most = fmaxf(most, w[i]);
-        most = fmaxf(most, __shfl_xor(most, 32, 64));
+        most = max_over_32(most);
         m_true = fmaxf(m_true, most * by);
         if constexpr (BITS < 16) {
             float top = fmaxf(lds_top[b][2], lds_top[b][3]);
@@ -713,31 +762,6 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
                 for (int r = 0; r < 4; ++r) w[i + r] *= step[r];
             }
         }
-        if constexpr (BITS == 16) {
-            if (masked && lds_odd[b]) {
-                uint32_t width = dim;
-                asm volatile("" : "+s"(width));                    // (nothing of this is worth a register outside)
-                // values that are not finite, one key after the other, in the rows that see them
-                for (uint32_t k = 0; k < (uint32_t)KT && key0 + k < end; ++k) {
-                    const uint32_t i = 4u * (k / 8u) + (k & 3u);
-                    float x = w[0];
-#pragma unroll
-                    for (uint32_t y = 1; y < 16 * kHalves; ++y) x = i == y ? w[y] : x;
-                    x = __shfl(x, (int)(n + 32u * ((k >> 2) & 1u)), 64);
-                    if ((int32_t)(key0 + k) >= seen) continue;
-                    const uint32_t kk = key0 + k;
-                    const uint64_t at = (uint64_t)page_of(a, s.table, kk) * page_rows + head_rows + (kk & page_mask);
-                    const uint16_t *p = reinterpret_cast<const uint16_t *>(a.cache.v + at * a.cache.row_bytes);
-#pragma unroll
-                    for (int y = 0; y < kTiles; ++y)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const uint32_t d = 32u * y + 8u * (i / 4) + 4u * h + (i & 3);
-                            if (d < width && (p[d] & 0x7C00u) == 0x7C00u) acc[y][i] = fmaf(x, half_to_float(p[d]), acc[y][i]);
-                        }
-                }
-            }
-        }
         half8v weights[2 * kHalves];
 #pragma unroll
         for (int x = 0; x < 2 * kHalves; ++x) {
@@ -751,24 +775,18 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
             weights[x] = as_half8(o[0], o[1], o[2], o[3]);
         }
         l += sum;
-        typedef short s16x4 __attribute__((ext_vector_type(4)));
-        const uint32_t i16 = lane & 15u, sub = (lane >> 4) & 1u;   // a lane of 16: row i16 / 4 of four keys, values 4 (i16 % 4) ... + 3
 #pragma unroll
         for (int x = 0; x < 2 * kHalves; ++x)
 #pragma unroll
             for (int y = 0; y < kTiles; ++y) {
-                uint64_t o[2];
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const uint32_t key = 16u * x + 8u * e + 4u * h + i16 / 4u;
-                    const uint32_t c = 4u * y + 2u * sub + ((i16 >> 1) & 1u);
-                    const uint4 *p = &lds_v[key * RC + (c ^ v_swap<RC>(key))];
-                    const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (__attribute__((address_space(3))) s16x4 *)(reinterpret_cast<const uint2 *>(p) + (i16 & 1u)));
-                    o[e] = __builtin_bit_cast(uint64_t, v);
+                const int at = x * kTiles + y;
+                const uint2 lo = __builtin_bit_cast(uint2, vf[2 * at]), hi = __builtin_bit_cast(uint2, vf[2 * at + 1]);
+                acc[y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_half8(lo.x, lo.y, hi.x, hi.y), weights[x], acc[y], 0, 0, 0);
+                if (2 * at + 1 + kReads / 2 < kReads) {
+                    read_v(2 * at + kReads / 2);
+                    read_v(2 * at + 1 + kReads / 2);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-                const half8v v = as_half8((uint32_t)o[0], (uint32_t)(o[0] >> 32), (uint32_t)o[1], (uint32_t)(o[1] >> 32));
-                acc[y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, weights[x], acc[y], 0, 0, 0);
             }
     };
 
@@ -788,6 +806,35 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
         for (uint32_t t = t0; t < t1; t += 2u) {
             step(t, first);
             if (t + 1u < t1) step(t + 1u, second);
+        }
+    }
+
+    if constexpr (BITS == 16) {
+        if (lds_odd[0] | lds_odd[1]) {
+            // Values that are not finite and were left out: with the weights worked out once more, one key after the other, in the rows
+            // that see them.  Rare, and not fast.
+            const uint32_t last = min(t1 * KT, end);
+            for (uint32_t key = max(t0, all_see / KT) * KT; key < last; ++key) {
+                if ((int32_t)key >= seen) continue;
+                const uint64_t at = (uint64_t)page_of(a, s.table, key) * page_rows + head_rows + (key & page_mask);
+                const uint16_t *vp = reinterpret_cast<const uint16_t *>(a.cache.v + at * a.cache.row_bytes);
+                const uint16_t *kp = reinterpret_cast<const uint16_t *>(a.cache.k + at * a.cache.row_bytes);
+                const uint16_t *qp = a.q.data + (int64_t)(s.first + token) * a.q.token_stride +
+                                     (int64_t)(head * a.group + (row - token * a.group)) * a.q.head_stride;
+                bool odd = false;
+                for (uint32_t d = 0; d < dim; ++d) odd |= (vp[d] & 0x7C00u) == 0x7C00u;
+                if (!odd) continue;
+                float x = 0.0f;
+                for (uint32_t d = 0; d < dim; ++d) x = fmaf(half_to_float(kp[d]), half_to_float(qp[(int64_t)d * a.q.dim_stride]), x);
+                x = __builtin_amdgcn_exp2f(x * a.scale_log2 - m);
+#pragma unroll
+                for (int y = 0; y < kTiles; ++y)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const uint32_t d = 32u * y + 8u * (i / 4) + 4u * h + (i & 3);
+                        if (d < dim && (vp[d] & 0x7C00u) == 0x7C00u) acc[y][i] = fmaf(x, half_to_float(vp[d]), acc[y][i]);
+                    }
+            }
         }
     }
 
