@@ -478,8 +478,11 @@ __device__ __forceinline__ uint4 code_values(const Raw<BITS> &r)
     if constexpr (BITS == 4) return nibble_values(r.w[0]);
 }
 
+// Two workgroups share a compute unit where 256 registers do (codes need more: they come through registers, and their steps).
+constexpr int chunk_shared(int bits, int dim) { return dim <= 64 || (bits == 16 && dim <= 128) ? 2 : 1; }
+
 template <int BITS, int DP>
-__global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(const AttentionArgs a)
+__global__ __launch_bounds__(256, chunk_shared(BITS, DP)) void attention_chunk_kernel(const AttentionArgs a)
 {
     constexpr int RC = DP <= 32 ? 4 : DP <= 64 ? 8 : DP <= 128 ? 16 : 32;              // 16-byte pieces of a row in LDS
     constexpr int KT = 64, kSteps = DP / 16, kTiles = DP / 32;
@@ -567,18 +570,25 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
         constexpr bool V = decltype(of_v)::value;
         const uint8_t *p = (V ? a.cache.v : a.cache.k) + at * a.cache.row_bytes;
         const uint32_t self = here(lane);
+        auto bring = [&](auto whole) ALWAYS {                      // whole: dim fills the rows of LDS
 #pragma unroll
-        for (int i = 0; i < kIssues; ++i) {
-            const uint32_t x = 64u * i + self, r = x / RC, c = x % RC;               // row of the 16, piece
-            if constexpr (BITS == 16) {
-                const uint32_t from = c ^ (V ? v_swap<RC>(16u * wave + r) : k_swap<RC>(16u * wave + r));
-                if (from < pieces)
-                    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(p + (r * a.cache.row_bytes + 16u * from)),
-                                                     (__attribute__((address_space(3))) void *)(&lds[16u * wave * RC + 64u * i]), 16, 0, 0);
-            } else {
-                raw[i].load(p + (r * a.cache.row_bytes + min(c, pieces - 1u) * BITS));
+            for (int i = 0; i < kIssues; ++i) {
+                const uint32_t r = (64u * i + self) / RC, c = self % RC;             // row of the 16, piece
+                const uint32_t row = decltype(whole)::value ? (64u * i / RC) * (2u * DP) + self / RC * (2u * DP) : r * a.cache.row_bytes;
+                if constexpr (BITS == 16) {
+                    const uint32_t from = c ^ (V ? v_swap<RC>(r) : k_swap<RC>(r));
+                    if (decltype(whole)::value || from < pieces)
+                        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(p + (row + 16u * from)),
+                                                         (__attribute__((address_space(3))) void *)(&lds[16u * wave * RC + 64u * i]), 16, 0, 0);
+                } else {
+                    raw[i].load(p + (r * a.cache.row_bytes + min(c, pieces - 1u) * BITS));
+                }
             }
-        }
+        };
+        if (BITS == 16 && DP == 8 * RC && pieces == RC)
+            bring(std::true_type{});
+        else
+            bring(std::false_type{});
     };
     auto request_k = [&](uint32_t t, auto buffer) ALWAYS {
         t = min(t, t1 - 1u);
@@ -994,8 +1004,9 @@ AttentionPlan plan_attention(uint32_t batch, uint32_t kv_heads, uint32_t group, 
     const uint64_t per_tile = p.chunk ? 128u : 16u;
     p.row_tiles = (uint32_t)((rows + per_tile - 1u) / per_tile);
     const uint64_t blocks = (uint64_t)p.row_tiles * kv_heads * batch;
-    // enough workgroups for the chip, and two rounds of 32 keys for each wavefront of a split (of 64 keys for a workgroup)
-    const uint64_t by_chip = blocks ? (p.chunk ? 512u : 1024u) / blocks : 1u, by_keys = (max_kv + 255u) / 256u;
+    // enough workgroups for the chip, and two rounds of 32 keys for each wavefront of a split (four tiles of 64 for a workgroup); several
+    // sequences are likely to be of different lengths, which more and smaller workgroups even out
+    const uint64_t by_chip = blocks ? (!p.chunk || batch > 1u ? 1024u : 512u) / blocks : 1u, by_keys = (max_kv + 255u) / 256u;
     p.splits = (uint32_t)std::max<uint64_t>(1u, std::min(by_chip, by_keys));
     if (p.splits > 1u) p.work_bytes = (uint64_t)p.splits * tokens * kv_heads * group * (dim + 2u) * sizeof(float);
     return p;
