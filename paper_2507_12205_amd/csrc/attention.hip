@@ -21,7 +21,6 @@ typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef _Float16 half8v __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-#define ALWAYS __attribute__((always_inline))
 constexpr float kNone = -__builtin_inff();
 
 // a register as two FP16 values and back
@@ -478,20 +477,18 @@ __device__ __forceinline__ uint4 code_values(const Raw<BITS> &r)
     if constexpr (BITS == 4) return nibble_values(r.w[0]);
 }
 
-// Two workgroups share a compute unit where 256 registers do (codes need more: they come through registers, and their steps).
-constexpr int chunk_shared(int bits, int dim) { return dim <= 64 || (bits == 16 && dim <= 128) ? 2 : 1; }
-
 template <int BITS, int DP>
-__global__ __launch_bounds__(256, chunk_shared(BITS, DP)) void attention_chunk_kernel(const AttentionArgs a)
+__global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(const AttentionArgs a)
 {
     constexpr int RC = DP <= 32 ? 4 : DP <= 64 ? 8 : DP <= 128 ? 16 : 32;              // 16-byte pieces of a row in LDS
-    constexpr int KT = 64, kSteps = DP / 16, kTiles = DP / 32;
-    constexpr int kIssues = RC / 4;                                                    // accesses per lane for a wavefront's 16 rows of a tile
+    constexpr int KT = RC == 32 ? 32 : 64, kHalves = KT / 32, kSteps = DP / 16, kTiles = DP / 32;
+    constexpr int kGroups = KT / 16;                                                   // a wavefront brings 16 keys; with 32, of K or of V
+    constexpr int kIssues = RC / 4;                                                    // accesses per lane for 16 rows
     // (four objects and not two of twice the size: a read of LDS then waits for what is on its way into the same object only)
     __shared__ uint4 lds_k0[KT * RC], lds_k1[KT * RC], lds_v0[KT * RC], lds_v1[KT * RC];
-    __shared__ float lds_step[4][2][2][KT];                                            // [tile % 4][k, v][step, low][key]
-    __shared__ float lds_top[4][4];
-    __shared__ uint32_t lds_odd;
+    __shared__ float lds_step[2][2][2][KT];                                            // [buffer][k, v][step, low][key]
+    __shared__ float lds_top[2][4];
+    __shared__ uint32_t lds_odd[2];
 
     const uint32_t tid = threadIdx.x, lane = tid & 63u, n = lane & 31u, h = lane >> 5;
     const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid >> 6));
@@ -514,6 +511,7 @@ __global__ __launch_bounds__(256, chunk_shared(BITS, DP)) void attention_chunk_k
         return max(min(s.behind + (int32_t)(min(r, rows - 1u) / a.group) + 1, (int32_t)s.len), 0);
     };
     const uint32_t end = (uint32_t)sees(row0 + 127u), all_see = (uint32_t)sees(row0);  // of the workgroup
+    const uint32_t wave_end = row0 + 32u * wave < rows ? (uint32_t)sees(row0 + 32u * wave + 31u) : 0u;
 
     half8v q[kSteps];
     float q_sum = 0.0f;
@@ -543,45 +541,56 @@ __global__ __launch_bounds__(256, chunk_shared(BITS, DP)) void attention_chunk_k
         }
         if constexpr (BITS == 4) q_sum += __shfl_xor(q_sum, 32, 64);
     }
-    const float scale = fmaxf(fabsf(a.scale_log2), 1e-30f), by = BITS == 16 ? scale : 1.0f;      // (not 0: hidden scores stay -infinity)
+    const float scale = fabsf(a.scale_log2), by = BITS == 16 ? scale : 1.0f;
 
     const uint32_t tiles = (end + KT - 1u) / KT, per = (tiles + a.splits - 1u) / a.splits;
     const uint32_t t0 = min(split * per, tiles), t1 = min(t0 + per, tiles);
     const uint32_t page_mask = (1u << a.cache.page_shift) - 1u;
     const uint64_t page_rows = (uint64_t)a.cache.heads << a.cache.page_shift, head_rows = (uint64_t)head << a.cache.page_shift;
+    const uint32_t group16 = kGroups == 4 ? wave : wave & 1u;
+    const bool brings_k = kGroups == 4 || wave < 2u, brings_v = kGroups == 4 || wave >= 2u;
+
     if (dim < (uint32_t)DP)
         for (uint32_t i = tid; i < KT * RC; i += 256u)             // what is beyond dim stays zero
             lds_k0[i] = lds_k1[i] = lds_v0[i] = lds_v1[i] = make_uint4(0, 0, 0, 0);
-    if (tid == 0) lds_odd = 0;
+    if (tid < 2u) lds_odd[tid] = 0;
     __syncthreads();
 
-    // A wavefront brings 16 keys of each tile.  request_k() and request_v() send the loads of a tile off, arrive_k() and arrive_v() see to it
-    // that they are in LDS (and write there what has come through registers); a barrier follows.  Tiles beyond the last are the last again:
-    // the number of loads on their way is then the same everywhere.
+    // Bringing tile t into buffer b, this wavefront's 16 keys of it: request() sends the loads off, arrive() waits for them and writes what
+    // has come through registers.
     Raw<BITS> raw_k[BITS < 16 ? kIssues : 1], raw_v[BITS < 16 ? kIssues : 1];
-    uint32_t raw_step = 0, page_list = 0;                          // lane i: the page of this wavefront's keys in the i-th tile of 64
-    auto first_key = [&](uint32_t t) { return min(t * KT + 16u * wave, (end - 1u) & ~15u); };       // (beyond the end: the last 16 keys again)
-    auto place = [&](uint32_t t) -> uint64_t {
+    uint32_t raw_step = 0;
+    auto first_key = [&](uint32_t t) { return min(t * KT + 16u * group16, (end - 1u) & ~15u); };      // (beyond the end: the last 16 keys again)
+    uint32_t page_list = 0;                                        // lane i: the page of this wavefront's keys in the i-th tile of 64
+    auto request = [&](uint32_t t, auto buffer) {
+        const int b = buffer;
+        uint4 *lds_k = b ? lds_k1 : lds_k0, *lds_v = b ? lds_v1 : lds_v0;
+        if (((t - t0) & 63u) == 0) {
+            page_list = page_of(a, s.table, first_key(t + lane));
+            asm volatile("" : "+v"(page_list));                    // waited for here, where it happens, and not by every tile
+        }
         const uint32_t key = first_key(t);
         const uint32_t page = (uint32_t)__builtin_amdgcn_readlane((int)page_list, (int)((t - t0) & 63u));
-        return (uint64_t)page * page_rows + head_rows + (key & page_mask);
-    };
-    auto request = [&](auto of_v, uint64_t at, uint4 *lds, auto &raw) ALWAYS {
-        constexpr bool V = decltype(of_v)::value;
-        const uint8_t *p = (V ? a.cache.v : a.cache.k) + at * a.cache.row_bytes;
+        const uint64_t at = (uint64_t)page * page_rows + head_rows + (key & page_mask);
+        const uint8_t *kp = a.cache.k + at * a.cache.row_bytes, *vp = a.cache.v + at * a.cache.row_bytes;
         const uint32_t self = here(lane);
-        auto bring = [&](auto whole) ALWAYS {                      // whole: dim fills the rows of LDS
+        auto bring = [&](auto whole) {                             // whole: dim fills the rows of LDS
 #pragma unroll
             for (int i = 0; i < kIssues; ++i) {
                 const uint32_t r = (64u * i + self) / RC, c = self % RC;             // row of the 16, piece
-                const uint32_t row = decltype(whole)::value ? (64u * i / RC) * (2u * DP) + self / RC * (2u * DP) : r * a.cache.row_bytes;
+                const uint32_t row = decltype(whole)::value ? r * (2u * DP) : r * a.cache.row_bytes;
                 if constexpr (BITS == 16) {
-                    const uint32_t from = c ^ (V ? v_swap<RC>(r) : k_swap<RC>(r));
-                    if (decltype(whole)::value || from < pieces)
-                        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(p + (row + 16u * from)),
-                                                         (__attribute__((address_space(3))) void *)(&lds[16u * wave * RC + 64u * i]), 16, 0, 0);
+                    const uint32_t to = (16u * group16) * RC + 64u * i;
+                    if (const uint32_t from = c ^ k_swap<RC>(16u * group16 + r); brings_k && (decltype(whole)::value || from < pieces))
+                        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(kp + (row + 16u * from)),
+                                                         (__attribute__((address_space(3))) void *)(&lds_k[to]), 16, 0, 0);
+                    if (const uint32_t from = c ^ v_swap<RC>(16u * group16 + r); brings_v && (decltype(whole)::value || from < pieces))
+                        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(vp + (row + 16u * from)),
+                                                         (__attribute__((address_space(3))) void *)(&lds_v[to]), 16, 0, 0);
                 } else {
-                    raw[i].load(p + (r * a.cache.row_bytes + min(c, pieces - 1u) * BITS));
+                    const uint32_t from = row + min(c, pieces - 1u) * BITS;
+                    if (brings_k) raw_k[i].load(kp + from);
+                    if (brings_v) raw_v[i].load(vp + from);
                 }
             }
         };
@@ -589,74 +598,24 @@ __global__ __launch_bounds__(256, chunk_shared(BITS, DP)) void attention_chunk_k
             bring(std::true_type{});
         else
             bring(std::false_type{});
-    };
-    auto request_k = [&](uint32_t t, auto buffer) ALWAYS {
-        t = min(t, t1 - 1u);
-        if (((t - t0) & 63u) == 0) {
-            page_list = page_of(a, s.table, first_key(t + lane));
-            asm volatile("" : "+v"(page_list));                    // waited for here, where it happens, and not by every tile
-        }
-        const uint64_t at = place(t);
-        request(std::false_type{}, at, decltype(buffer)::value ? lds_k1 : lds_k0, raw_k);
         if constexpr (BITS < 16)                                   // lanes 0 ... 15 the steps of the keys, 16 ... 31 those of the values
-            raw_step = *reinterpret_cast<const uint32_t *>(((lane & 16u) ? a.cache.v_step : a.cache.k_step) + 4u * (at + (lane & 15u)));
+            raw_step = *reinterpret_cast<const uint32_t *>(((self & 16u) ? a.cache.v_step : a.cache.k_step) + 4u * (at + (self & 15u)));
     };
-    auto request_v = [&](uint32_t t, auto buffer) ALWAYS {
-        t = min(t, t1 - 1u);
-        request(std::true_type{}, place(t), decltype(buffer)::value ? lds_v1 : lds_v0, raw_v);
-    };
-    auto put = [&](auto of_v, uint4 *lds, const auto &raw) ALWAYS {
-        constexpr bool V = decltype(of_v)::value;
-        const uint32_t self = here(lane);
-#pragma unroll
-        for (int i = 0; i < kIssues; ++i) {
-            const uint32_t x = 64u * i + self, r = x / RC, c = x % RC, kk = 16u * wave + r;
-            if (c < pieces) lds[kk * RC + (c ^ (V ? v_swap<RC>(kk) : k_swap<RC>(kk)))] = code_values<BITS>(raw[i]);
-        }
-    };
-    auto arrive_k = [&](uint32_t t, auto buffer) ALWAYS {
+    auto arrive = [&](uint32_t t, auto buffer) {
+        const int b = buffer;
+        uint4 *lds_k = b ? lds_k1 : lds_k0, *lds_v = b ? lds_v1 : lds_v0;
+        const uint32_t key0 = t * KT + 16u * group16, self = here(lane);
         if constexpr (BITS == 16) {
-            // what went straight to LDS is there, but for the tile of V that was asked for after it
-            __builtin_amdgcn_s_waitcnt(0x0F70 | kIssues);
+            __builtin_amdgcn_s_waitcnt(0x0F70);                    // vmcnt(0): what went straight to LDS is there
             asm volatile("" ::: "memory");
-        } else {
-            put(std::false_type{}, decltype(buffer)::value ? lds_k1 : lds_k0, raw_k);
-            const uint32_t key = min(t, t1 - 1u) * KT + 16u * wave + (lane & 15u);
-            const bool in = key < end;
-            float step = !in ? 0.0f : BITS == 8 ? __uint_as_float(raw_step) : step_of(raw_step);
-            float low = !in || BITS == 8 ? 0.0f : low_of(raw_step);
-            float top = step;                                      // the largest step of the 16 values
-#pragma unroll
-            for (int o = 1; o < 16; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-            if (lane < 16u) {                                      // the keys' have the scale in them (not 0, as `scale`)
-                step = fmaxf(step * scale, 1e-30f);
-                low *= scale;
-            }
-            if (lane < 32u) {
-                lds_step[t & 3u][lane >> 4][0][16u * wave + (lane & 15u)] = step;
-                if constexpr (BITS == 4) lds_step[t & 3u][lane >> 4][1][16u * wave + (lane & 15u)] = low;
-            }
-            if (lane == 16u) lds_top[t & 3u][wave] = top;
-        }
-    };
-    auto arrive_v = [&](uint32_t t, auto buffer, int behind) ALWAYS {
-        uint4 *lds = decltype(buffer)::value ? lds_v1 : lds_v0;
-        if constexpr (BITS == 16) {
-            if (behind)
-                __builtin_amdgcn_s_waitcnt(0x0F70 | kIssues);      // all but the tile of K that was asked for after it
-            else
-                __builtin_amdgcn_s_waitcnt(0x0F70);
-            asm volatile("" ::: "memory");
-            t = min(t, t1 - 1u);
-            if ((t + 1u) * KT > all_see) {
+            if ((t + 1u) * KT > all_see && brings_v) {
                 // Some rows do not see all of this tile.  What no row sees may be anything: zeros; and values that are not finite are
                 // left out here, so that a weight of 0 makes nothing of them (they are added at the end in the rows that see them).
                 bool odd = false;
-                const uint32_t self = here(lane), key0 = t * KT + 16u * wave;
 #pragma unroll
                 for (int i = 0; i < kIssues; ++i) {
-                    const uint32_t x = 64u * i + self, at = 16u * wave * RC + x;
-                    uint4 v = lds[at];
+                    const uint32_t x = 64u * i + self, at = (16u * group16) * RC + x;
+                    uint4 v = lds_v[at];
                     uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
                     for (uint32_t &y : w) {
@@ -665,15 +624,37 @@ __global__ __launch_bounds__(256, chunk_shared(BITS, DP)) void attention_chunk_k
                         odd |= keep != 0xFFFFFFFFu;
                         y &= keep;
                     }
-                    lds[at] = make_uint4(w[0], w[1], w[2], w[3]);
+                    lds_v[at] = make_uint4(w[0], w[1], w[2], w[3]);
                 }
-                if (odd) lds_odd = 1u;
+                if (odd) lds_odd[b] = 1u;
             }
         } else {
-            put(std::true_type{}, lds, raw_v);
+#pragma unroll
+            for (int i = 0; i < kIssues; ++i) {
+                const uint32_t x = 64u * i + self, r = x / RC, c = x % RC, kk = 16u * group16 + r;
+                if (c < pieces) {
+                    if (brings_k) lds_k[kk * RC + (c ^ k_swap<RC>(kk))] = code_values<BITS>(raw_k[i]);
+                    if (brings_v) lds_v[kk * RC + (c ^ v_swap<RC>(kk))] = code_values<BITS>(raw_v[i]);
+                }
+            }
+            const bool in = key0 + (lane & 15u) < end;
+            const float step = !in ? 0.0f : BITS == 8 ? __uint_as_float(raw_step) : step_of(raw_step);
+            const float low = !in || BITS == 8 ? 0.0f : low_of(raw_step);
+            if (lane < 32u) {
+                const float f = lane < 16u ? scale : 1.0f;
+                lds_step[b][lane >> 4][0][16u * group16 + (lane & 15u)] = f * step;
+                if constexpr (BITS == 4) lds_step[b][lane >> 4][1][16u * group16 + (lane & 15u)] = f * low;
+            }
+            float top = step;                                      // the largest step of the 16 values
+#pragma unroll
+            for (int o = 1; o < 16; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+            if (lane == 16u) lds_top[b][wave] = top;
         }
     };
 
+    auto hold = []() {                                             // (with codes there are not the registers for it)
+        if constexpr (BITS == 16) __builtin_amdgcn_sched_barrier(0);
+    };
     typedef float f32x16 __attribute__((ext_vector_type(16)));
     f32x16 acc[kTiles];
 #pragma unroll
@@ -685,174 +666,167 @@ __global__ __launch_bounds__(256, chunk_shared(BITS, DP)) void attention_chunk_k
     float m = kNone, m_true = kNone, l = 0.0f, z_acc = 0.0f, unit = 0.0f;
     if constexpr (BITS < 16) unit = -32.0f;           // (the smallest step is 2^-31; not so low that weights without a step overflow)
 
-    // 32 keys at a time, three of them under way: while the weights of 32 keys are worked out, the products of the 32 before with V and
-    // those of the 32 after with K run.  Matrix instructions and the others overlap well only where a wavefront's own stream has them side
-    // by side (two wavefronts that take turns: a third less), so the order is written down: each slot is one matrix instruction, the reads
-    // of LDS for a few slots later, and a piece of the softmax.
-    // Both use of tile t: products with K while the weights of the half before are worked out, with V while those of the half after are.
-    typedef short s16x4 __attribute__((ext_vector_type(4)));
-    f32x16 c;                                                      // q . k of the next 32 keys
-    half8v kf[kSteps];
-    s16x4 vf[4 * kTiles];                                          // [16 keys][32 values][8 of the keys]
-    uint32_t weights[8], next_weights[8];                          // of the 32 keys, pairs of them
-    const uint32_t i16 = lane & 15u, sub = (lane >> 4) & 1u;       // reading V: a lane of 16 has row i16 / 4 of four keys, values 4 (i16 % 4) ... + 3
-    auto read_k = [&](const uint4 *lds, uint32_t half, int y) ALWAYS {
-        const uint32_t key = 32u * half + n;
-        kf[y] = __builtin_bit_cast(half8v, lds[key * RC + ((2u * y + h) ^ k_swap<RC>(key))]);
-    };
-    auto read_v = [&](const uint4 *lds, uint32_t half, int i) ALWAYS {
-        const int x = i / (2 * kTiles), y = i % (2 * kTiles) / 2, e = i % 2;
-        const uint32_t key = 32u * half + 16u * x + 8u * e + 4u * h + i16 / 4u;
-        const uint32_t piece = 4u * y + 2u * sub + ((i16 >> 1) & 1u);
-        const uint4 *p = &lds[key * RC + (piece ^ v_swap<RC>(key))];
-        vf[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(reinterpret_cast<const uint2 *>(p) + (i16 & 1u)));
-    };
-    auto product_k = [&](int y) ALWAYS {
-        if (y == 0) c = f32x16{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
-        c = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[y], q[y], c, 0, 0, 0);
-    };
-    auto product_v = [&](int i) ALWAYS {
-        const int x = i / kTiles, y = i % kTiles;
-        const uint2 lo = __builtin_bit_cast(uint2, vf[2 * i]), hi = __builtin_bit_cast(uint2, vf[2 * i + 1]);
-        acc[y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_half8(lo.x, lo.y, hi.x, hi.y),
-                                                        as_half8(weights[4 * x], weights[4 * x + 1], weights[4 * x + 2], weights[4 * x + 3]), acc[y], 0, 0, 0);
-    };
-    // the weights of half `half` of tile t, from c; with_v: products of the half before; K of the half after is in `k_next`, V of this one in `v_here`
-    auto work = [&](auto with_v, uint32_t t, uint32_t half, const uint4 *k_next, const uint4 *v_here) ALWAYS {
-        constexpr bool V = decltype(with_v)::value;
-        const uint32_t key0 = t * KT + 32u * half;
-        float w[16];
+    auto compute = [&](uint32_t t, auto buffer) {
+        const int b = buffer;
+        const uint4 *lds_k = b ? lds_k1 : lds_k0, *lds_v = b ? lds_v1 : lds_v0;
+        const uint32_t key0 = t * KT;
+        const bool masked = key0 + KT > all_see;                   // not all rows see all of the tile
+        float w[16 * kHalves];
+        // What is read of K and V is asked for a few products ahead, V's first half before the weights are worked out.  (Left to the
+        // compiler, the reads come pair by pair right before their products, and a wavefront waits for each: 140 us in the place of 133 for 2048 tokens over 4096 keys.)
+        half8v kf[kHalves][kSteps];
+        const uint32_t key_n = here(n);
+        auto read_k = [&](int y) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) w[i] = c[i];
-        if (key0 + 32u > all_see) {                                // not all rows see all of the 32 keys
+            for (int x = 0; x < kHalves; ++x) {
+                const uint32_t key = 32u * x + key_n;
+                kf[x][y] = __builtin_bit_cast(half8v, lds_k[key * RC + ((2u * y + h) ^ k_swap<RC>(key))]);
+            }
+        };
+        constexpr int kAhead = kSteps < 4 ? kSteps : 4;
+#pragma unroll
+        for (int y = 0; y < kAhead; ++y) read_k(y);
+        hold();
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        const uint32_t i16 = lane & 15u, sub = (lane >> 4) & 1u;   // a lane of 16: row i16 / 4 of four keys, values 4 (i16 % 4) ... + 3
+        constexpr int kReads = 4 * kHalves * kTiles;               // [16 keys][8 of them][32 values]
+        s16x4 vf[kReads];
+        auto read_v = [&](int i) {
+            const int x = i / (2 * kTiles), y = i % (2 * kTiles) / 2, e = i % 2;
+            const uint32_t key = 16u * x + 8u * e + 4u * h + i16 / 4u;
+            const uint32_t c = 4u * y + 2u * sub + ((i16 >> 1) & 1u);
+            const uint4 *p = &lds_v[key * RC + (c ^ v_swap<RC>(key))];
+            vf[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(reinterpret_cast<const uint2 *>(p) + (i16 & 1u)));
+        };
+        f32x16 c[kHalves];
+#pragma unroll
+        for (int x = 0; x < kHalves; ++x) c[x] = f32x16{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+        for (int y = 0; y < kSteps; ++y) {
+#pragma unroll
+            for (int x = 0; x < kHalves; ++x) c[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[x][y], q[y], c[x], 0, 0, 0);
+            if (y + kAhead < kSteps) read_k(y + kAhead);
+            if (y >= kSteps - kAhead)
+#pragma unroll
+                for (int i = (y + kAhead - kSteps) * (kReads / 2) / kAhead; i < (y + 1 + kAhead - kSteps) * (kReads / 2) / kAhead; ++i) read_v(i);
+            hold();
+        }
+#pragma unroll
+        for (int i = 0; i < 16 * kHalves; ++i) w[i] = c[i / 16][i % 16];
+        if constexpr (BITS < 16) {
+#pragma unroll
+            for (int i = 0; i < 16 * kHalves; i += 4) {            // (the steps of the keys have the scale in them)
+                const uint32_t key = 8u * (i / 4) + 4u * h;
+                const f32x4 step = *reinterpret_cast<const f32x4 *>(&lds_step[b][0][0][key]);
+                if constexpr (BITS == 4) {
+                    const f32x4 low = *reinterpret_cast<const f32x4 *>(&lds_step[b][0][1][key]) * q_sum;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) w[i + r] = fmaf(w[i + r], step[r], low[r]);
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) w[i + r] *= step[r];
+                }
+            }
+        }
+        if (masked) {
             int32_t left = seen - (int32_t)(key0 + 4u * h);
             asm volatile("" : "+v"(left));                         // (kept a branch: few tiles take it)
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
+            for (int i = 0; i < 16 * kHalves; ++i)
                 if (8 * (i / 4) + (i & 3) >= left) w[i] = kNone;
         }
-        float most = kNone, sum = 0.0f, z_sum = 0.0f, before = m, base = 0.0f;
-        bool far = false;
-        f32x4 step[4], low[4];
-        const float(*steps)[2][KT] = lds_step[t & 3u];
-        auto read_steps = [&](int of_v) ALWAYS {
+        float most = w[0];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                step[i] = *reinterpret_cast<const f32x4 *>(&steps[of_v][0][32u * half + 8u * i + 4u * h]);
-                if constexpr (BITS == 4) low[i] = *reinterpret_cast<const f32x4 *>(&steps[of_v][1][32u * half + 8u * i + 4u * h]);
-            }
-        };
-        // the softmax in pieces: 0 ... 2 the largest score, 3 what follows from it, then two weights each
-        auto piece = [&](int p) ALWAYS {
-            if (p < 2) {
-#pragma unroll
-                for (int i = 8 * p; i < 8 * p + 8; ++i) {
-                    if constexpr (BITS == 8) w[i] *= step[i / 4][i % 4];
-                    if constexpr (BITS == 4) w[i] = fmaf(w[i], step[i / 4][i % 4], low[i / 4][i % 4] * q_sum);
-                    most = fmaxf(most, w[i]);
-                }
-            } else if (p == 2) {
-                if constexpr (BITS < 16) read_steps(1);
-                most = max_over_32(most);
-            } else if (p == 3) {
-                m_true = fmaxf(m_true, most * by);
-                if constexpr (BITS < 16) {
-                    const f32x4 tops = *reinterpret_cast<const f32x4 *>(lds_top[t & 3u]);
-                    const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-                    if (top > 0.0f) unit = fmaxf(unit, (float)(ilogbf(top) + 1));
-                }
-                const float m_new = m_true + unit;
-                far = m_new > m + 8.0f;
-                m = far ? m_new : m;                               // a row goes by its own scores alone
-                base = m == kNone ? 0.0f : m;
-            } else {
-                const int i = 2 * (p - 4);
-                half2v o;
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    float x = __builtin_amdgcn_exp2f(BITS == 16 ? fmaf(w[i + r], by, -base) : w[i + r] - base);
-                    if constexpr (BITS < 16) sum += x;
-                    if constexpr (BITS == 4) z_sum = fmaf(x, low[i / 4][i % 4 + r], z_sum);
-                    if constexpr (BITS < 16) x *= step[i / 4][i % 4 + r];
-                    o[r] = (_Float16)x;
-                }
-                if constexpr (BITS == 16) sum = __builtin_amdgcn_fdot2(o, half2v{(_Float16)1.0f, (_Float16)1.0f}, sum, false);       // the rounded ones
-                next_weights[i / 2] = as_word(o);
-            }
-        };
-        if constexpr (BITS < 16) read_steps(0);
-        constexpr int kSlots = 2 * kSteps, kPieces = 12, kFirst = kSlots >= 16 ? 2 : 0;      // (the first slots have no piece: c is still on its way)
-#pragma unroll
-        for (int slot = 0; slot < kSlots; ++slot) {
-            if (slot < kSteps) {                                   // V's products, reads of K
-                if constexpr (V) product_v(slot);
-                read_k(k_next, 1u - half, slot);
-            } else {                                               // K's products, reads of V
-                product_k(slot - kSteps);
-                read_v(v_here, half, 2 * (slot - kSteps));
-                read_v(v_here, half, 2 * (slot - kSteps) + 1);
-            }
-            if (slot >= kFirst)
-#pragma unroll
-                for (int p = (slot - kFirst) * kPieces / (kSlots - kFirst); p < (slot + 1 - kFirst) * kPieces / (kSlots - kFirst); ++p) piece(p);
-            __builtin_amdgcn_sched_barrier(0);
+        for (int i = 1; i < 16 * kHalves; ++i) most = fmaxf(most, w[i]);
+        most = max_over_32(most);
+        m_true = fmaxf(m_true, most * by);
+        if constexpr (BITS < 16) {
+            float top = fmaxf(lds_top[b][2], lds_top[b][3]);
+            if constexpr (kGroups == 4) top = fmaxf(top, fmaxf(lds_top[b][0], lds_top[b][1]));
+            if (top > 0.0f) unit = fmaxf(unit, (float)(ilogbf(top) + 1));
         }
-        if (__any((int)far)) {
-            const float alpha = far ? __builtin_amdgcn_exp2f(before - m) : 1.0f;      // (0 where nothing was seen before)
+        const float m_new = m_true + unit;
+        if (const bool far = m_new > m + 8.0f; __any((int)far)) {
+            const float alpha = far ? __builtin_amdgcn_exp2f(m - m_new) : 1.0f;       // (0 where nothing was seen before)
+            m = far ? m_new : m;                                   // a row goes by its own scores alone
             l *= alpha;
             z_acc *= alpha;
 #pragma unroll
             for (int i = 0; i < kTiles; ++i) acc[i] *= alpha;
         }
-        l += sum;
-        z_acc += z_sum;
+        const float base = m == kNone ? 0.0f : m;
+        float sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) weights[i] = next_weights[i];
+        for (int i = 0; i < 16 * kHalves; ++i) {
+            w[i] = __builtin_amdgcn_exp2f(BITS == 16 ? fmaf(w[i], by, -base) : w[i] - base);
+            if constexpr (BITS < 16) sum += w[i];                  // (with FP16 the rounded ones are added up, below)
+        }
+        if constexpr (BITS < 16) {
+#pragma unroll
+            for (int i = 0; i < 16 * kHalves; i += 4) {
+                const uint32_t key = 8u * (i / 4) + 4u * h;
+                const f32x4 step = *reinterpret_cast<const f32x4 *>(&lds_step[b][1][0][key]);
+                if constexpr (BITS == 4) {
+                    const f32x4 low = *reinterpret_cast<const f32x4 *>(&lds_step[b][1][1][key]);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) z_acc = fmaf(w[i + r], low[r], z_acc);
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) w[i + r] *= step[r];
+            }
+        }
+        half8v weights[2 * kHalves];
+#pragma unroll
+        for (int x = 0; x < 2 * kHalves; ++x) {
+            uint32_t o[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const half2v p = {(_Float16)w[8 * x + 2 * i], (_Float16)w[8 * x + 2 * i + 1]};
+                if constexpr (BITS == 16) sum = __builtin_amdgcn_fdot2(p, half2v{(_Float16)1.0f, (_Float16)1.0f}, sum, false);
+                o[i] = as_word(p);
+            }
+            weights[x] = as_half8(o[0], o[1], o[2], o[3]);
+        }
+        l += sum;
+#pragma unroll
+        for (int x = 0; x < 2 * kHalves; ++x)
+#pragma unroll
+            for (int y = 0; y < kTiles; ++y) {
+                const int at = x * kTiles + y;
+                const uint2 lo = __builtin_bit_cast(uint2, vf[2 * at]), hi = __builtin_bit_cast(uint2, vf[2 * at + 1]);
+                acc[y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_half8(lo.x, lo.y, hi.x, hi.y), weights[x], acc[y], 0, 0, 0);
+                if (2 * at + 1 + kReads / 2 < kReads) {
+                    read_v(2 * at + kReads / 2);
+                    read_v(2 * at + 1 + kReads / 2);
+                    hold();
+                }
+            }
     };
 
+    auto step = [&](uint32_t t, auto buffer, auto other) {
+        if (t + 1u < t1) request(t + 1u, other);
+        if (t * KT < wave_end) compute(t, buffer);
+        if (t + 1u < t1) arrive(t + 1u, other);
+        __syncthreads();
+    };
     if (t0 < t1) {
         const std::integral_constant<int, 0> first;
         const std::integral_constant<int, 1> second;
-        const std::true_type with_v;
-        request_k(t0, first);
-        request_v(t0, first);
-        arrive_k(t0, first);
-        arrive_v(t0, first, 0);
+        request(t0, first);
+        arrive(t0, first);
         __syncthreads();
-        request_k(t0 + 1u, second);
-        request_v(t0 + 1u, second);
-#pragma unroll
-        for (int y = 0; y < kSteps; ++y) {
-            read_k(lds_k0, 0, y);
-            product_k(y);
+        if constexpr (BITS == 16) {
+            for (uint32_t t = t0; t < t1; t += 2u) {
+                step(t, first, second);
+                if (t + 1u < t1) step(t + 1u, second, first);
+            }
+        } else {                                                   // (nothing goes straight to LDS: one copy of the code, and fewer registers)
+            for (uint32_t t = t0, b = 0; t < t1; ++t, b ^= 1u) step(t, (int)b, (int)(b ^ 1u));
         }
-        // The two halves of a tile.  Behind the first one K of this tile has been read, and the next one's has to be there; behind the
-        // second one the same holds of V.
-        auto tile_of = [&](auto with_first, uint32_t t, auto buffer) ALWAYS {
-            const std::integral_constant<int, 1 - decltype(buffer)::value> other;
-            uint4 *k_here = decltype(buffer)::value ? lds_k1 : lds_k0, *k_other = decltype(buffer)::value ? lds_k0 : lds_k1;
-            uint4 *v_here = decltype(buffer)::value ? lds_v1 : lds_v0;
-            work(with_first, t, 0, k_here, v_here);
-            arrive_k(t + 1u, other);
-            __syncthreads();
-            request_k(t + 2u, buffer);
-            work(with_v, t, 1, k_other, v_here);
-            arrive_v(t + 1u, other, 1);
-            __syncthreads();
-            request_v(t + 2u, buffer);
-        };
-        tile_of(std::false_type{}, t0, first);
-        for (uint32_t t = t0 + 1u; t < t1; t += 2u) {
-            tile_of(with_v, t, second);
-            if (t + 1u < t1) tile_of(with_v, t + 1u, first);
-        }
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) product_v(i);
-        __builtin_amdgcn_s_waitcnt(0x0F70);                        // nothing is on its way to LDS when the workgroup ends
     }
 
     if constexpr (BITS == 16) {
-        if (lds_odd) {
+        if (lds_odd[0] | lds_odd[1]) {
             // Values that are not finite and were left out: with the weights worked out once more, one key after the other, in the rows
             // that see them.  Rare, and not fast.
             const uint32_t last = min(t1 * KT, end);
@@ -1004,9 +978,8 @@ AttentionPlan plan_attention(uint32_t batch, uint32_t kv_heads, uint32_t group, 
     const uint64_t per_tile = p.chunk ? 128u : 16u;
     p.row_tiles = (uint32_t)((rows + per_tile - 1u) / per_tile);
     const uint64_t blocks = (uint64_t)p.row_tiles * kv_heads * batch;
-    // enough workgroups for the chip, and two rounds of 32 keys for each wavefront of a split (four tiles of 64 for a workgroup); several
-    // sequences are likely to be of different lengths, which more and smaller workgroups even out
-    const uint64_t by_chip = blocks ? (!p.chunk || batch > 1u ? 1024u : 512u) / blocks : 1u, by_keys = (max_kv + 255u) / 256u;
+    // enough workgroups for the chip, and two rounds of 32 keys for each wavefront of a split (of 64 keys for a workgroup)
+    const uint64_t by_chip = blocks ? (p.chunk ? 512u : 1024u) / blocks : 1u, by_keys = (max_kv + 255u) / 256u;
     p.splits = (uint32_t)std::max<uint64_t>(1u, std::min(by_chip, by_keys));
     if (p.splits > 1u) p.work_bytes = (uint64_t)p.splits * tokens * kv_heads * group * (dim + 2u) * sizeof(float);
     return p;
