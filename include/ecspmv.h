@@ -318,7 +318,9 @@ typedef struct ecspmv_verify_t {
     const int32_t *drafted, *count;
     int32_t *tokens, *accepted;
 } ecspmv_verify_t;
-int ecspmv_verify(const ecspmv_verify_t *a, void *stream);
+/* Two launches.  d_work: device, 8-byte aligned, at least ecspmv_verify_workspace bytes, contents of no matter before and after. */
+int ecspmv_verify_workspace(const ecspmv_verify_t *a, size_t *bytes);
+int ecspmv_verify(const ecspmv_verify_t *a, void *d_work, size_t work_bytes, void *stream);
 
 /* ---- comparison: plain CSR (int32 column index + FP16 value per entry, one wavefront per row) ------- */
 /* The CSR-32 format the paper's Section 8.2 measures storage against, with a kernel of its own (not one of the

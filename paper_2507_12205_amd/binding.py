@@ -26,7 +26,8 @@ EXPORTS = (
     "ecspmv_stats", "ecspmv_decode", "ecspmv_decode_f32",
     "ecspmv_block_sets", "ecspmv_device_bytes", "ecspmv_export_image", "ecspmv_upload", "ecspmv_run", "ecspmv_run_batch", "ecspmv_run_multi", "ecspmv_run_epilogue",
     "ecspmv_csr_build_dense", "ecspmv_csr_destroy", "ecspmv_csr_device_bytes", "ecspmv_csr_upload",
-    "ecspmv_kv_write", "ecspmv_kv_read", "ecspmv_attention_workspace", "ecspmv_attention", "ecspmv_verify",
+    "ecspmv_kv_write", "ecspmv_kv_read", "ecspmv_attention_workspace", "ecspmv_attention",
+    "ecspmv_verify_workspace", "ecspmv_verify",
     "ecspmv_csr_run", "ecspmv_stream_read", "ecspmv_stream_read_sliced", "ecspmv_empty_launch", "ecspmv_strerror", "ecspmv_last_hip_error",
 )
 
@@ -132,7 +133,8 @@ def lib() -> ctypes.CDLL:
     L.ecspmv_kv_read.argtypes = [POINTER(KvCacheDesc), c_void_p, c_int64, POINTER(View), POINTER(View), c_void_p]
     L.ecspmv_attention_workspace.argtypes = [POINTER(KvCacheDesc), POINTER(AttentionDesc), POINTER(c_size_t)]
     L.ecspmv_attention.argtypes = [POINTER(KvCacheDesc), POINTER(AttentionDesc), c_void_p, c_size_t, c_void_p]
-    L.ecspmv_verify.argtypes = [POINTER(VerifyDesc), c_void_p]
+    L.ecspmv_verify_workspace.argtypes = [POINTER(VerifyDesc), POINTER(c_size_t)]
+    L.ecspmv_verify.argtypes = [POINTER(VerifyDesc), c_void_p, c_size_t, c_void_p]
     L.ecspmv_csr_build_dense.argtypes = [c_void_p, c_int64, c_int64, c_int64, POINTER(c_void_p)]
     L.ecspmv_csr_destroy.argtypes = [c_void_p]
     L.ecspmv_csr_destroy.restype = None
@@ -416,5 +418,11 @@ def ecspmv_attention(cache: KvCacheDesc, a: AttentionDesc, d_work: int = 0, work
     _check(lib().ecspmv_attention(cache, a, c_void_p(d_work), work_bytes, c_void_p(stream)), "ecspmv_attention")
 
 
-def ecspmv_verify(a: VerifyDesc, stream: int = 0) -> None:
-    _check(lib().ecspmv_verify(a, c_void_p(stream)), "ecspmv_verify")
+def ecspmv_verify_workspace(a: VerifyDesc) -> int:
+    n = c_size_t(0)
+    _check(lib().ecspmv_verify_workspace(a, byref(n)), "ecspmv_verify_workspace")
+    return int(n.value)
+
+
+def ecspmv_verify(a: VerifyDesc, d_work: int, work_bytes: int, stream: int = 0) -> None:
+    _check(lib().ecspmv_verify(a, c_void_p(d_work), work_bytes, c_void_p(stream)), "ecspmv_verify")

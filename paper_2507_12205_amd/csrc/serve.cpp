@@ -98,6 +98,15 @@ int check_attention(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *fr
     return ECSPMV_OK;
 }
 
+int check_verify(const ecspmv_verify_t *from, ecspmv_verify_t &t)
+{
+    const int s = copy_struct(from, t);
+    if (s) return s;
+    if (t.batch < 0 || t.drafts < 0 || t.vocab < 1) return ECSPMV_ERR_INVALID;
+    if (t.batch > 65535 || t.vocab > 1 << 20 || t.drafts > 1 << 20) return ECSPMV_ERR_UNSUPPORTED;
+    return ECSPMV_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -149,14 +158,24 @@ int ecspmv_attention(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *a
     return ecs::hip_status(ecs::launch_attention(args, stream));
 }
 
-int ecspmv_verify(const ecspmv_verify_t *from, void *stream)
+int ecspmv_verify_workspace(const ecspmv_verify_t *from, size_t *bytes)
 {
     ecspmv_verify_t t;
-    const int s = copy_struct(from, t);
+    const int s = check_verify(from, t);
     if (s) return s;
-    if (t.batch < 0 || t.drafts < 0 || t.vocab < 1) return ECSPMV_ERR_INVALID;
-    if (t.vocab > 1 << 20 || t.drafts > 1 << 20) return ECSPMV_ERR_UNSUPPORTED;
+    if (!bytes) return ECSPMV_ERR_INVALID;
+    *bytes = (size_t)ecs::verify_work_bytes((uint32_t)t.batch, (uint32_t)t.vocab);
+    return ECSPMV_OK;
+}
+
+int ecspmv_verify(const ecspmv_verify_t *from, void *d_work, size_t work_bytes, void *stream)
+{
+    ecspmv_verify_t t;
+    const int s = check_verify(from, t);
+    if (s) return s;
     if (t.batch == 0) return ECSPMV_OK;
+    if (!d_work || !aligned(d_work, 8)) return ECSPMV_ERR_INVALID;
+    if (work_bytes < ecs::verify_work_bytes((uint32_t)t.batch, (uint32_t)t.vocab)) return ECSPMV_ERR_TOO_SMALL;
     if (!t.target || !t.uniform || !t.tokens || !t.accepted || (t.drafts && !t.drafted)) return ECSPMV_ERR_INVALID;
     const void *all[] = {t.target, t.draft, t.uniform, t.drafted, t.count, t.tokens, t.accepted};
     for (const void *p : all)
@@ -176,6 +195,7 @@ int ecspmv_verify(const ecspmv_verify_t *from, void *stream)
     a.draft_row = t.draft_row;
     a.drafts = (uint32_t)t.drafts;
     a.vocab = (uint32_t)t.vocab;
+    a.sums = static_cast<double *>(d_work);
     return ecs::hip_status(ecs::launch_verify(a, (uint32_t)t.batch, stream));
 }
 

@@ -56,7 +56,9 @@ struct VerifyArgs {
     int32_t *tokens, *accepted;
     int64_t target_seq, target_row, draft_seq, draft_row;      // strides in elements
     uint32_t drafts, vocab;
+    double *sums;                         // verify_work_bytes
 };
+uint64_t verify_work_bytes(uint32_t batch, uint32_t vocab);
 int launch_verify(const VerifyArgs &a, uint32_t batch, void *stream);
 
 }  // namespace ecs

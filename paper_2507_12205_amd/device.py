@@ -176,11 +176,17 @@ def attention(cache: KvCache, q: torch.Tensor, out: torch.Tensor, q_start: torch
     return out
 
 
+def verify_workspace(batch: int, vocab: int) -> int:
+    """Bytes of a workspace for verify() calls of this size."""
+    return B.ecspmv_verify_workspace(B.VerifyDesc(_VERIFY, batch, 0, vocab))
+
+
 def verify(target: torch.Tensor, draft, drafted: torch.Tensor, uniform: torch.Tensor, tokens: torch.Tensor, accepted: torch.Tensor,
-           count: torch.Tensor = None, stream=None):
+           count: torch.Tensor = None, workspace: torch.Tensor = None, stream=None):
     """Which drafted tokens stand, and the token after them.  target: (batch, drafts + 1, vocab) probabilities, draft: (batch, drafts,
     vocab) the drafts' own (None where a draft was certain), uniform: (batch, drafts + 1) random numbers in [0, 1), all FP32; drafted:
-    (batch, drafts) int32, count: (batch,) int32, how many of them (None: all).  tokens: (batch, drafts + 1), accepted: (batch,) int32."""
+    (batch, drafts) int32, count: (batch,) int32, how many of them (None: all).  tokens: (batch, drafts + 1), accepted: (batch,) int32.
+    workspace: of verify_workspace(), or allocated here."""
     batch, rows, vocab = target.shape
     drafts = rows - 1
     assert target.dtype is uniform.dtype is torch.float32 and drafted.dtype is tokens.dtype is accepted.dtype is torch.int32
@@ -197,5 +203,9 @@ def verify(target: torch.Tensor, draft, drafted: torch.Tensor, uniform: torch.Te
     if count is not None:
         assert count.dtype is torch.int32 and count.shape == (batch,) and count.is_contiguous() and count.device == target.device
         a.count = count.data_ptr()
-    B.ecspmv_verify(a, _stream_handle(stream))
+    if workspace is None:
+        workspace = torch.empty(verify_workspace(batch, vocab), dtype=torch.uint8, device=target.device)
+        if stream is not None:
+            workspace.record_stream(stream)
+    B.ecspmv_verify(a, workspace.data_ptr(), workspace.numel(), _stream_handle(stream))
     return tokens, accepted

@@ -47,7 +47,7 @@ for name, o in arg["attention"]:
             o[key] = view(o[key], 256)
     out[name] = outcome(lambda: B.ecspmv_attention(cache(), attention(**o), work, size, stream[0]))
 for name, o in arg["verify"]:
-    out[name] = outcome(lambda: B.ecspmv_verify(verify(**o), stream[0]))
+    out[name] = outcome(lambda: B.ecspmv_verify(verify(**o), 0x900000, 1 << 20, stream[0]))
 A = B.ecspmv_build_dense(np.ones((16, 128), np.float16), B.make_opts())
 F = B.ecspmv_build_dense_f32(np.ones((16, 128), np.float32), B.make_opts())
 early = outcome(lambda: A.ecspmv_run_epilogue(0x100000, 0x200000, 1, B.Epilogue(ctypes.sizeof(B.Epilogue), 1, 0, 0, 0), stream[0]))
@@ -63,18 +63,22 @@ short = cache()
 short.struct_size = 3
 out["short"] = [L.ecspmv_kv_write(short, view(), view(), 0x800000, 5, 0), L.ecspmv_kv_write(None, view(), view(), 0x800000, 5, 0),
                 L.ecspmv_kv_write(cache(), None, view(), 0x800000, 5, 0), L.ecspmv_attention(cache(), None, 0, 0, 0),
-                L.ecspmv_attention_workspace(cache(), attention(), None), L.ecspmv_verify(None, 0)]
+                L.ecspmv_attention_workspace(cache(), attention(), None), L.ecspmv_verify(None, 0x900000, 1 << 20, 0)]
 long = attention(max_pages=100, table_stride=100)
 out["work"] = B.ecspmv_attention_workspace(cache(), long)
 out["enough"] = [outcome(lambda: B.ecspmv_attention(cache(), long, 0x900000, out["work"] - d, stream[0])) for d in (0, 1)]
 out["grid"] = fake.fake_launched(GRID)
 out["none"] = outcome(lambda: B.ecspmv_attention(cache(), long, 0, out["work"], stream[0]))
+need = B.ecspmv_verify_workspace(verify())
+out["verify work"] = [need, outcome(lambda: B.ecspmv_verify(verify(), 0x900000, need, stream[0])),
+                      outcome(lambda: B.ecspmv_verify(verify(), 0x900000, need - 1, stream[0])),
+                      outcome(lambda: B.ecspmv_verify(verify(), 0x900004, need, stream[0])), outcome(lambda: B.ecspmv_verify(verify(), 0, need, stream[0]))]
 out["stream"] = []
 for s in (0x1000, 0x2000, 0):
-    B.ecspmv_verify(verify(), s)
+    B.ecspmv_verify(verify(), 0x900000, 1 << 20, s)
     out["stream"].append([fake.fake_launched(STREAM), fake.fake_launched(KERNEL)])
 try:
-    B.ecspmv_verify(verify(), 0x3000)
+    B.ecspmv_verify(verify(), 0x900000, 1 << 20, 0x3000)
 except B.EcspmvError as e:
     out["stream"].append(e.status)
 print(json.dumps(out))
@@ -123,4 +127,5 @@ def test_refusals(tmp_path):
     assert got["early"] == [-5, 0] and got["no epilogue"] == [INVALID, INVALID]
     assert got["short"] == [INVALID] * 6
     assert got["work"] > 0 and got["enough"] == [1, [SMALL, 0]] and got["grid"] == 3 * 4 and got["none"] == [INVALID, 0]
+    assert got["verify work"] == [2 * 2 * 8, 1, [SMALL, 0], [INVALID, 0], [INVALID, 0]]
     assert got["stream"] == [[0x1000, 0x100], [0x2000, 0x200], [0, 0x100], HIP]
