@@ -235,20 +235,25 @@ __global__ __launch_bounds__(256) void attention_rows_kernel(const AttentionArgs
     for (int i = 0; i < VD; ++i) acc[i] = f32x4{0, 0, 0, 0};
     float m = kNone, l = 0.0f, z_acc = 0.0f, unit = 0.0f;         // unit: acc is in units of it (BITS < 16)
 
-    for (uint32_t t = t0 + wave; t < t1; t += 4u) {
-        const uint32_t key0 = 32u * t;
-        // first row of each 16 keys in the cache; keys beyond the last one are read from where the last one is
-        uint64_t at[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint32_t key = min(key0 + 16u * h, (end - 1u) & ~15u);
-            at[h] = (uint64_t)page_of(a, s.table, key) * page_rows + head_rows + (key & page_mask);
+    // The keys of the next round are asked for as soon as this round's have been multiplied, its values before that: both are on their way
+    // while the softmax is worked out.
+    uint32_t page_list = 0;                                       // lane 2 i + h: the page of the h-th 16 keys of the i-th of 32 rounds
+    uint64_t at[2], at_next[2] = {0, 0};                          // first row of each 16 keys in the cache
+    KeyRaw k[2][kLoads];
+    uint32_t ks[8] = {};
+    auto request_k = [&](uint32_t t) {
+        const uint32_t round = (t - t0 - wave) >> 2;
+        // keys beyond the last one are read from where the last one is
+        auto key_of = [&](uint32_t tile, uint32_t h) { return min(32u * tile + 16u * h, (end - 1u) & ~15u); };
+        if ((round & 31u) == 0) {
+            page_list = page_of(a, s.table, key_of(t + 4u * (lane >> 1), lane & 1u));
+            asm volatile("" : "+v"(page_list));                   // waited for here, and not by every round
         }
-        KeyRaw k[2][kLoads];
-        ValueRaw v[8];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const uint8_t *p = a.cache.k + at[h] * a.cache.row_bytes + j * a.cache.row_bytes + g * (KB * BITS / 8);
+            const uint32_t page = (uint32_t)__builtin_amdgcn_readlane((int)page_list, (int)(2u * (round & 31u) + h));
+            at_next[h] = (uint64_t)page * page_rows + head_rows + (key_of(t, h) & page_mask);
+            const uint8_t *p = a.cache.k + at_next[h] * a.cache.row_bytes + (j * a.cache.row_bytes + g * (KB * BITS / 8));
 #pragma unroll
             for (int x = 0; x < kLoads; ++x) {
                 if (!PAD || (uint32_t)(x * 4 * KB) + g * KB < dim)
@@ -256,25 +261,34 @@ __global__ __launch_bounds__(256) void attention_rows_kernel(const AttentionArgs
                 else
                     k[h][x].clear();
             }
+            if constexpr (BITS < 16) {
+                const uint4 x = *reinterpret_cast<const uint4 *>(a.cache.k_step + 4u * (at_next[h] + 4u * g));
+                ks[4 * h] = x.x, ks[4 * h + 1] = x.y, ks[4 * h + 2] = x.z, ks[4 * h + 3] = x.w;
+            }
         }
+    };
+    if (t0 + wave < t1) request_k(t0 + wave);
+    for (uint32_t t = t0 + wave; t < t1; t += 4u) {
+        const uint32_t key0 = 32u * t;
+        at[0] = at_next[0], at[1] = at_next[1];
+        ValueRaw v[8];
 #pragma unroll
         for (int r = 0; r < 8; ++r) {
-            const uint8_t *p = a.cache.v + at[r >> 2] * a.cache.row_bytes + (4u * g + (r & 3)) * a.cache.row_bytes + j * (VD * BITS / 8);
+            const uint8_t *p = a.cache.v + at[r >> 2] * a.cache.row_bytes + ((4u * g + (r & 3)) * a.cache.row_bytes + j * (VD * BITS / 8));
             if (!PAD || j * VD < dim)
                 v[r].load(p);
             else
                 v[r].clear();
         }
-        uint32_t ks[8] = {}, vs[8] = {};
+        uint32_t vs[8] = {};
         if constexpr (BITS < 16) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const uint4 x = *reinterpret_cast<const uint4 *>(a.cache.k_step + 4u * (at[h] + 4u * g));
                 const uint4 y = *reinterpret_cast<const uint4 *>(a.cache.v_step + 4u * (at[h] + 4u * g));
-                ks[4 * h] = x.x, ks[4 * h + 1] = x.y, ks[4 * h + 2] = x.z, ks[4 * h + 3] = x.w;
                 vs[4 * h] = y.x, vs[4 * h + 1] = y.y, vs[4 * h + 2] = y.z, vs[4 * h + 3] = y.w;
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
 
         float w[8];
 #pragma unroll
@@ -293,6 +307,9 @@ __global__ __launch_bounds__(256) void attention_rows_kernel(const AttentionArgs
                 w[4 * h + r] = d * a.scale_log2;
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
+        if (t + 4u < t1) request_k(t + 4u);
+        __builtin_amdgcn_sched_barrier(0);
         const bool some_hidden = (int32_t)(key0 + 32u) > all_see || key0 + 32u > end;
         if (some_hidden) {
 #pragma unroll
@@ -306,12 +323,12 @@ __global__ __launch_bounds__(256) void attention_rows_kernel(const AttentionArgs
         for (int r = 1; r < 8; ++r) most = fmaxf(most, w[r]);
         most = max_over_32(max_over_16(most));
         const float m_new = fmaxf(m, most), base = m_new == kNone ? 0.0f : m_new;
-        const float alpha = exp2f(m - base);                       // (0 where nothing was seen before)
+        const float alpha = __builtin_amdgcn_exp2f(m - base);                       // (0 where nothing was seen before)
         m = m_new;
         float sum = 0.0f;
 #pragma unroll
         for (int r = 0; r < 8; ++r) {
-            w[r] = exp2f(w[r] - base);
+            w[r] = __builtin_amdgcn_exp2f(w[r] - base);
             sum += w[r];
         }
         l = l * alpha + sum;
@@ -415,7 +432,7 @@ __global__ __launch_bounds__(256) void attention_rows_kernel(const AttentionArgs
     for (int x = 0; x < 4; ++x) most = fmaxf(most, lds_ml[x][n][0]);
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
-        share[x] = most == kNone ? 0.0f : exp2f(lds_ml[x][n][0] - most);
+        share[x] = most == kNone ? 0.0f : __builtin_amdgcn_exp2f(lds_ml[x][n][0] - most);
         if (lds_ml[x][n][0] == kNone) share[x] = 0.0f;             // (what it has added up is nothing)
         total += share[x] * lds_ml[x][n][1];
     }
@@ -903,27 +920,46 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttentionArgs
     const uint32_t token = blockIdx.x / a.q_heads, head = blockIdx.x - token * a.q_heads;
     if ((int32_t)token < a.q_start[0] || (int32_t)token >= a.q_start[a.batch]) return;      // of no sequence
     const uint64_t row = blockIdx.x, step = (uint64_t)a.tokens * a.q_heads;
-    float m = kNone;
-    for (uint32_t s = lane; s < a.splits; s += 64u) m = fmaxf(m, a.part_ml[2 * (row + s * step)]);
+    float l = 0.0f, o[4] = {0, 0, 0, 0}, top = kNone;
+    // 64 splits at a time: a lane looks at one, its share goes to the others by readlane, so that all that is waited for is two trips
+    for (uint32_t first = 0; first < a.splits; first += 64u) {
+        const uint32_t s = first + lane;
+        const float2 ml = s < a.splits ? *reinterpret_cast<const float2 *>(a.part_ml + 2 * (row + s * step)) : make_float2(kNone, 0.0f);
+        float m = ml.x;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-    float l = 0.0f, o[4] = {0, 0, 0, 0};
-    for (uint32_t s = wave; s < a.splits; s += 4u) {
-        const uint64_t at = row + s * step;
-        const float ms = a.part_ml[2 * at];
-        if (ms == kNone) continue;
-        const float share = exp2f(ms - m);
-        l += share * a.part_ml[2 * at + 1];
+        for (int x = 32; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor(m, x, 64));
+        m = fmaxf(m, top);
+        const float before = top == kNone ? 0.0f : __builtin_amdgcn_exp2f(top - m);
+        top = m;
+        const float share = ml.x == kNone ? 0.0f : __builtin_amdgcn_exp2f(ml.x - m);
+        l = l * before + share * ml.y;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (lane + 64u * i < dim) o[i] += share * a.part_o[at * dim + lane + 64u * i];
+        for (int i = 0; i < 4; ++i) o[i] *= before;
+        const uint32_t count = min(a.splits - first, 64u);
+        for (uint32_t k = wave; k < count; k += 16u) {             // four splits of this wavefront on their way
+            float x[4][4], f[4];
+#pragma unroll
+            for (uint32_t u = 0; u < 4; ++u) {
+                const uint32_t at = min(k + 4u * u, count - 1u);
+                f[u] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(share), (int)at));
+                if (k + 4u * u >= count) f[u] = 0.0f;
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) x[u][i] = lane + 64u * i < dim ? a.part_o[(row + (first + at) * step) * dim + lane + 64u * i] : 0.0f;
+            }
+#pragma unroll
+            for (uint32_t u = 0; u < 4; ++u)
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) o[i] = f[u] == 0.0f ? o[i] : fmaf(f[u], x[u][i], o[i]);
+        }
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) lds_o[wave][lane + 64u * i] = o[i];
+#pragma unroll
+    for (int x = 32; x > 0; x >>= 1) l += __shfl_xor(l, x, 64);
     if (lane == 0) lds_l[wave] = l;
     __syncthreads();
     if (tid >= dim) return;
-    const float total = lds_l[0] + lds_l[1] + lds_l[2] + lds_l[3];
+    const float total = lds_l[0];                                  // (every wavefront has looked at all of them)
     const float sum = lds_o[0][tid] + lds_o[1][tid] + lds_o[2][tid] + lds_o[3][tid];
     const _Float16 h = (_Float16)(total == 0.0f ? 0.0f : sum / total);
     a.out.data[(int64_t)token * a.out.token_stride + (int64_t)head * a.out.head_stride + (int64_t)tid * a.out.dim_stride] = __builtin_bit_cast(uint16_t, h);
