@@ -82,6 +82,23 @@ __device__ __forceinline__ half8v key_values(const uint32_t *w)
         return as_half8(from_nibbles(w[0]), from_nibbles(w[0] >> 4), from_nibbles(w[0] >> 8), from_nibbles(w[0] >> 12));
     }
 }
+// The same without taking anything off: each value is kKeyOffset too large, which is q's sum times that in a score.  (For a score's few terms
+// of V's size that costs FP32 nothing; the sums over many keys are another matter.)
+template <int BITS>
+constexpr float kKeyOffset = BITS == 8 ? 1152.0f : 1032.0f;
+template <int BITS>
+__device__ __forceinline__ half8v key_values_offset(const uint32_t *w)
+{
+    if constexpr (BITS == 16) {
+        return as_half8(w[0], w[1], w[2], w[3]);
+    } else if constexpr (BITS == 8) {
+        auto two = [](uint32_t x, uint32_t select) { return __builtin_amdgcn_perm(0, x, select) ^ 0x64806480u; };
+        return as_half8(two(w[0], 0x0C010C00u), two(w[0], 0x0C030C02u), two(w[1], 0x0C010C00u), two(w[1], 0x0C030C02u));
+    } else {
+        auto two = [](uint32_t x) { return (x & 0x000F000Fu) | 0x64006400u; };
+        return as_half8(two(w[0]), two(w[0] >> 4), two(w[0] >> 8), two(w[0] >> 12));
+    }
+}
 template <int BITS>
 __device__ __forceinline__ constexpr int slot_dim(int i) { return BITS == 4 ? (i >> 1) + 4 * (i & 1) : i; }
 
@@ -163,7 +180,7 @@ __device__ __forceinline__ uint32_t page_of(const AttentionArgs &a, const int32_
 // weights never leave their lane.  V comes as it lies in memory, 8 keys times DP / 16 values per lane, and is turned round in
 // registers; its columns are dealt to the products as DP / 16 per lane, the i-th product has values i of every lane.
 template <int BITS, int DP, bool PAD>
-__global__ __launch_bounds__(256) void attention_rows_kernel(const AttentionArgs a)
+__global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : 4) : 1) void attention_rows_kernel(const AttentionArgs a)
 {
     constexpr int kSteps = DP / 32, VD = DP / 16;
     constexpr int KB = BITS == 16 ? 8 : BITS == 8 || PAD || DP == 64 ? 16 : 32;       // neighbouring values of a key in a lane
@@ -215,11 +232,11 @@ __global__ __launch_bounds__(256) void attention_rows_kernel(const AttentionArgs
                 const int d = slot_dim<BITS>(i);
                 const uint32_t h = (d & 1) ? w[d >> 1] >> 16 : w[d >> 1] & 0xFFFFu;
                 o[i >> 1] |= h << (16 * (i & 1));
-                if constexpr (BITS == 4) q_sum += half_to_float(h);
+                if constexpr (BITS < 16) q_sum += half_to_float(h);
             }
             q[t] = as_half8(o[0], o[1], o[2], o[3]);
         }
-        if constexpr (BITS == 4) {
+        if constexpr (BITS < 16) {
             q_sum += __shfl_xor(q_sum, 16, 64);
             q_sum += __shfl_xor(q_sum, 32, 64);
         }
@@ -297,11 +314,12 @@ __global__ __launch_bounds__(256) void attention_rows_kernel(const AttentionArgs
 #pragma unroll
             for (int t = 0; t < kSteps; ++t) {
                 constexpr int kPer = KB / 8;                       // steps that a load feeds
-                c = __builtin_amdgcn_mfma_f32_16x16x32_f16(key_values<BITS>(&k[h][t / kPer].w[(t % kPer) * (BITS / 4)]), q[t], c, 0, 0, 0);
+                c = __builtin_amdgcn_mfma_f32_16x16x32_f16(key_values_offset<BITS>(&k[h][t / kPer].w[(t % kPer) * (BITS / 4)]), q[t], c, 0, 0, 0);
             }
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 float d = c[r];
+                if constexpr (BITS < 16) d = fmaf(-kKeyOffset<BITS>, q_sum, d);
                 if constexpr (BITS == 8) d *= __uint_as_float(ks[4 * h + r]);
                 if constexpr (BITS == 4) d = fmaf(d, step_of(ks[4 * h + r]), q_sum * low_of(ks[4 * h + r]));
                 w[4 * h + r] = d * a.scale_log2;
