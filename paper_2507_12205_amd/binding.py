@@ -400,12 +400,20 @@ def ecspmv_empty_launch(d_out: int, num_wg: int, threads_per_wg: int, count: int
 
 # ---- around the products: descriptions are the structs of the C ABI, pointers and streams plain integers
 
+def _plain(p):
+    return p if type(p) is int else c_void_p(p)              # (as in Matrix.ecspmv_run)
+
+
 def ecspmv_kv_write(cache: KvCacheDesc, k: View, v: View, d_slots: int, tokens: int, stream: int = 0) -> None:
-    _check(lib().ecspmv_kv_write(cache, k, v, c_void_p(d_slots), tokens, c_void_p(stream)), "ecspmv_kv_write")
+    status = (_lib or lib()).ecspmv_kv_write(cache, k, v, _plain(d_slots), tokens, _plain(stream))
+    if status:
+        raise EcspmvError(status, "ecspmv_kv_write")
 
 
 def ecspmv_kv_read(cache: KvCacheDesc, d_slots: int, tokens: int, k: View, v: View, stream: int = 0) -> None:
-    _check(lib().ecspmv_kv_read(cache, c_void_p(d_slots), tokens, k, v, c_void_p(stream)), "ecspmv_kv_read")
+    status = (_lib or lib()).ecspmv_kv_read(cache, _plain(d_slots), tokens, k, v, _plain(stream))
+    if status:
+        raise EcspmvError(status, "ecspmv_kv_read")
 
 
 def ecspmv_attention_workspace(cache: KvCacheDesc, a: AttentionDesc) -> int:
@@ -415,7 +423,9 @@ def ecspmv_attention_workspace(cache: KvCacheDesc, a: AttentionDesc) -> int:
 
 
 def ecspmv_attention(cache: KvCacheDesc, a: AttentionDesc, d_work: int = 0, work_bytes: int = 0, stream: int = 0) -> None:
-    _check(lib().ecspmv_attention(cache, a, c_void_p(d_work), work_bytes, c_void_p(stream)), "ecspmv_attention")
+    status = (_lib or lib()).ecspmv_attention(cache, a, _plain(d_work), work_bytes, _plain(stream))
+    if status:
+        raise EcspmvError(status, "ecspmv_attention")
 
 
 def ecspmv_verify_workspace(a: VerifyDesc) -> int:
@@ -425,4 +435,6 @@ def ecspmv_verify_workspace(a: VerifyDesc) -> int:
 
 
 def ecspmv_verify(a: VerifyDesc, d_work: int, work_bytes: int, stream: int = 0) -> None:
-    _check(lib().ecspmv_verify(a, c_void_p(d_work), work_bytes, c_void_p(stream)), "ecspmv_verify")
+    status = (_lib or lib()).ecspmv_verify(a, _plain(d_work), work_bytes, _plain(stream))
+    if status:
+        raise EcspmvError(status, "ecspmv_verify")

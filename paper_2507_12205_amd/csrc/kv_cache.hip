@@ -53,27 +53,31 @@ __device__ __forceinline__ void store_eight(const View &v, uint32_t wide, uint32
     }
 }
 
-// Which row a lane works on: the rows of k first, then those of v
+// Which row a lane works on.  Rows are taken 2^run_shift neighbouring tokens of one head after another: a workgroup's codes then lie side
+// by side in the cache (with the heads of one token after another every row went to a place of its own, 64 bytes of 4-bit codes and 4 of
+// steps: 8191 tokens, 8 heads of 128, written in 16.4 us).  k and v are the two halves of the grid.
 struct Row {
     bool of_v, valid;
     uint32_t token, head, at, lane;       // at: its first value
     uint64_t place;                       // row of the cache
     __device__ __forceinline__ Row(const KvArgs &a)
     {
-        const uint32_t lanes = 1u << a.lanes_shift, rows = a.tokens * a.cache.heads;
+        const uint32_t lanes = 1u << a.lanes_shift;
         const uint32_t in_block = threadIdx.x >> a.lanes_shift, per_block = blockDim.x >> a.lanes_shift;
         const uint32_t r = blockIdx.x * per_block + in_block;
         of_v = blockIdx.y != 0;
         lane = threadIdx.x & (lanes - 1u);
         at = 8u * lane;
-        const uint32_t rr = min(r, rows - 1u);
-        token = rr / a.cache.heads;
-        head = rr - token * a.cache.heads;
+        const uint32_t turn = r >> a.run_shift, first = turn / a.cache.heads;
+        head = turn - first * a.cache.heads;
+        const uint32_t mine = (first << a.run_shift) + (r & ((1u << a.run_shift) - 1u));
+        const bool some = mine < a.tokens;
+        token = min(mine, a.tokens - 1u);
         const int64_t slot = a.slots[token];
-        valid = r < rows && slot >= 0 && slot < (int64_t)a.cache.pages << a.cache.page_shift && at < a.cache.dim;
+        valid = some && slot >= 0 && slot < (int64_t)a.cache.pages << a.cache.page_shift && at < a.cache.dim;
         const uint64_t page = (uint64_t)slot >> a.cache.page_shift, off = (uint64_t)slot & ((1u << a.cache.page_shift) - 1u);
         place = ((page * a.cache.heads + head) << a.cache.page_shift) + off;
-        inside = r < rows && at < a.cache.dim;
+        inside = some && at < a.cache.dim;
     }
     bool inside;                          // this lane has values, whether or not the slot is one of the cache's
 };
@@ -164,8 +168,9 @@ __global__ __launch_bounds__(256) void kv_read_kernel(const KvArgs a)
 template <auto K16, auto K8, auto K4>
 int launch(const KvArgs &a, void *stream)
 {
-    const uint32_t per_block = 256u >> a.lanes_shift, rows = a.tokens * a.cache.heads;
-    const uint32_t grid = (rows + per_block - 1u) / per_block;
+    const uint32_t per_block = 256u >> a.lanes_shift, runs = (a.tokens + (1u << a.run_shift) - 1u) >> a.run_shift;
+    const uint64_t rows = ((uint64_t)runs * a.cache.heads) << a.run_shift;
+    const uint32_t grid = (uint32_t)((rows + per_block - 1u) / per_block);
     switch (a.cache.bits) {
     case 16: return ecs::launch_args<K16>(a, grid, 2, 1, 256, stream);
     case 8: return ecs::launch_args<K8>(a, grid, 2, 1, 256, stream);

@@ -67,10 +67,11 @@ int kv_call(const ecspmv_kv_cache_t *cache, const ecspmv_view_t *k, const ecspmv
     if (tokens == 0) return ECSPMV_OK;
     if ((s = check_view(k, a.k, a.k_wide)) || (s = check_view(v, a.v, a.v_wide))) return s;
     if (!d_slots || !aligned(d_slots, 8)) return ECSPMV_ERR_INVALID;
-    if (tokens > 0x7fffffff || (uint64_t)tokens * a.cache.heads > 0x7fffffffu) return ECSPMV_ERR_UNSUPPORTED;
+    if (tokens > 0x7fffffff || ((uint64_t)tokens + 16u) * a.cache.heads > 0x7fffffffu) return ECSPMV_ERR_UNSUPPORTED;
     a.slots = d_slots;
     a.tokens = (uint32_t)tokens;
     while ((8u << a.lanes_shift) < a.cache.dim) ++a.lanes_shift;
+    while ((1u << a.run_shift) < a.tokens && a.run_shift < 4u) ++a.run_shift;
     return ecs::hip_status(launch(a, stream));
 }
 

@@ -26,6 +26,7 @@ struct KvArgs {
     View k, v;
     const int64_t *slots;
     uint32_t tokens, lanes_shift;         // log2 of the lanes that share a row
+    uint32_t run_shift;                   // log2 of the neighbouring tokens of a head that follow one another
     uint32_t k_wide, v_wide;              // rows of k, v are 16-byte pieces
 };
 int launch_kv_write(const KvArgs &a, void *stream);

@@ -183,13 +183,21 @@ __global__ __launch_bounds__(kThreads) void verify_token_kernel(const VerifyArgs
             }
             __syncthreads();
             if (wave == 0) {
-                double v[4][4], done = before;                               // 256 tokens after another
+                double v[4][4], s[4], sums_to[4], done = before;             // 256 tokens after another
                 w.tile(tile, lane, v);
                 uint32_t token = 0xFFFFFFFFu, some = 0;
 #pragma unroll
+                for (uint32_t k = 0; k < 4; ++k) sums_to[k] = s[k] = (v[k][0] + v[k][1]) + (v[k][2] + v[k][3]);
+#pragma unroll
+                for (int o = 1; o < 64; o <<= 1)                             // the four scans side by side
+#pragma unroll
+                    for (uint32_t k = 0; k < 4; ++k) {
+                        const double t = __shfl_up(sums_to[k], o, 64);
+                        if (lane >= (uint32_t)o) sums_to[k] += t;
+                    }
+#pragma unroll
                 for (uint32_t k = 0; k < 4; ++k) {
-                    const double s = (v[k][0] + v[k][1]) + (v[k][2] + v[k][3]), sums_to = wave_incl_scan(s, lane);
-                    double cum = done + (sums_to - s);
+                    double cum = done + (sums_to[k] - s[k]);
 #pragma unroll
                     for (uint32_t i = 0; i < 4; ++i) {
                         cum += v[k][i];
@@ -197,7 +205,7 @@ __global__ __launch_bounds__(kThreads) void verify_token_kernel(const VerifyArgs
                         if (v[k][i] > 0.0) some = id + 1u;
                         if (token == 0xFFFFFFFFu && cum > bound && v[k][i] > 0.0) token = id;
                     }
-                    done += __shfl(sums_to, 63, 64);
+                    done += __shfl(sums_to[k], 63, 64);
                 }
 #pragma unroll
                 for (int o = 32; o > 0; o >>= 1) {

@@ -109,7 +109,7 @@ class KvCache:
             want = (torch.float32, k.shape[:3]) if self.bits == 8 else (torch.float16, (*k.shape[:3], 2))
             for t in (k_step, v_step):
                 assert t.dtype is want[0] and t.shape == want[1] and t.is_contiguous() and t.device == k.device
-        self.k, self.v, self.k_step, self.v_step = k, v, k_step, v_step
+        self.k, self.v, self.k_step, self.v_step, self.device = k, v, k_step, v_step, k.get_device()
         self.desc = B.KvCacheDesc(_KV_CACHE, self.bits, self.pages, self.heads, self.page_size, self.head_dim, k.data_ptr(), v.data_ptr(),
                                   k_step.data_ptr() if k_step is not None else None, v_step.data_ptr() if v_step is not None else None)
 
@@ -124,14 +124,17 @@ def kv_cache(pages: int, heads: int, page_size: int, head_dim: int, bits: int = 
     return KvCache(k, v, *(torch.zeros(shape, dtype=dtype, device=device) for _ in range(2)))
 
 
+# These calls follow one another as fast as the host makes them, so devices are compared as plain numbers (-1: not on a GPU) and the
+# structs are handed over as they are.
+
 def _view(t: torch.Tensor) -> B.View:
     return B.View(t.data_ptr(), *t.stride())
 
 
 def _rows_of(cache: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
-    assert k.dtype is torch.float16 and v.dtype is torch.float16 and k.device == v.device == slots.device == cache.k.device
-    assert k.shape == v.shape == (slots.shape[0], cache.heads, cache.head_dim)
-    assert slots.dtype is torch.int64 and slots.dim() == 1 and slots.is_contiguous()
+    assert k.dtype is v.dtype is torch.float16 and k.get_device() == v.get_device() == slots.get_device() == cache.device
+    assert k.shape == v.shape == (*slots.shape, cache.heads, cache.head_dim)
+    assert slots.dtype is torch.int64 and slots.is_contiguous()
 
 
 def kv_write(cache: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, stream=None) -> None:
@@ -159,8 +162,8 @@ def attention(cache: KvCache, q: torch.Tensor, out: torch.Tensor, q_start: torch
     """out = causal attention of the new tokens q, (tokens, q_heads, head_dim) FP16 with any strides, over the cache that holds their
     keys and values: sequence b has q[q_start[b]:q_start[b + 1]] and kv_len[b] keys in all, in the pages page_table[b] (all int32).
     max_new: the most new tokens of a sequence; scale: 1 / sqrt(head_dim) if not given."""
-    assert q.dtype is torch.float16 and out.dtype is torch.float16 and q.shape == out.shape and q.shape[2] == cache.head_dim
-    assert q.device == out.device == q_start.device == kv_len.device == page_table.device == cache.k.device
+    assert q.dtype is out.dtype is torch.float16 and q.shape == out.shape and q.shape[2] == cache.head_dim
+    assert q.get_device() == out.get_device() == q_start.get_device() == kv_len.get_device() == page_table.get_device() == cache.device
     assert q_start.dtype is kv_len.dtype is page_table.dtype is torch.int32
     batch, pages = page_table.shape
     assert kv_len.shape == (batch,) and q_start.shape == (batch + 1,) and q_start.is_contiguous() and kv_len.is_contiguous()
@@ -190,18 +193,19 @@ def verify(target: torch.Tensor, draft, drafted: torch.Tensor, uniform: torch.Te
     batch, rows, vocab = target.shape
     drafts = rows - 1
     assert target.dtype is uniform.dtype is torch.float32 and drafted.dtype is tokens.dtype is accepted.dtype is torch.int32
-    assert target.is_cuda and target.device == uniform.device == drafted.device == tokens.device == accepted.device
+    device = target.get_device()
+    assert device >= 0 and device == uniform.get_device() == drafted.get_device() == tokens.get_device() == accepted.get_device()
     assert uniform.shape == tokens.shape == (batch, rows) and drafted.shape == (batch, drafts) and accepted.shape == (batch,)
     assert uniform.is_contiguous() and tokens.is_contiguous() and drafted.is_contiguous() and accepted.is_contiguous()
     assert target.numel() == 0 or vocab == 1 or target.stride(2) == 1
     a = B.VerifyDesc(_VERIFY, batch, drafts, vocab, target.data_ptr(), None, uniform.data_ptr(), target.stride(0), target.stride(1), 0, 0,
                      drafted.data_ptr() or None, None, tokens.data_ptr(), accepted.data_ptr())
     if draft is not None:
-        assert draft.dtype is torch.float32 and draft.shape == (batch, drafts, vocab) and draft.device == target.device
+        assert draft.dtype is torch.float32 and draft.shape == (batch, drafts, vocab) and draft.get_device() == device
         assert draft.numel() <= 1 or vocab == 1 or draft.stride(2) == 1
         a.draft, a.draft_seq, a.draft_row = draft.data_ptr() or None, draft.stride(0), draft.stride(1)
     if count is not None:
-        assert count.dtype is torch.int32 and count.shape == (batch,) and count.is_contiguous() and count.device == target.device
+        assert count.dtype is torch.int32 and count.shape == (batch,) and count.is_contiguous() and count.get_device() == device
         a.count = count.data_ptr()
     if workspace is None:
         workspace = torch.empty(verify_workspace(batch, vocab), dtype=torch.uint8, device=target.device)
