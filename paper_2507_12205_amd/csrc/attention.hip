@@ -929,15 +929,16 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
     }
 }
 
-// ---- joining the splits: a workgroup per (token, head), its wavefronts on different splits --------------------------------------------
+// ---- joining the splits: W wavefronts for each (token, head), on different splits -----------------------------------------------------
+template <int W>
 __global__ __launch_bounds__(256) void attention_join_kernel(const AttentionArgs a)
 {
     __shared__ float lds_o[4][256];
-    __shared__ float lds_l[4];
-    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6, dim = a.cache.dim;
-    const uint32_t token = blockIdx.x / a.q_heads, head = blockIdx.x - token * a.q_heads;
-    if ((int32_t)token < a.q_start[0] || (int32_t)token >= a.q_start[a.batch]) return;      // of no sequence
-    const uint64_t row = blockIdx.x, step = (uint64_t)a.tokens * a.q_heads;
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = (tid >> 6) % W, dim = a.cache.dim;
+    const uint32_t r = blockIdx.x * (4u / W) + (tid >> 6) / W, token = r / a.q_heads, head = r - token * a.q_heads;
+    // of no sequence (q_start does not decrease: with one row to a workgroup all of it goes; with four nobody waits for the others)
+    if (r >= a.tokens * a.q_heads || (int32_t)token < a.q_start[0] || (int32_t)token >= a.q_start[a.batch]) return;
+    const uint64_t row = r, step = (uint64_t)a.tokens * a.q_heads;
     float l = 0.0f, o[4] = {0, 0, 0, 0}, top = kNone;
     // 64 splits at a time: a lane looks at one, its share goes to the others by readlane, so that all that is waited for is two trips
     for (uint32_t first = 0; first < a.splits; first += 64u) {
@@ -954,13 +955,13 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttentionArgs
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[i] *= before;
         const uint32_t count = min(a.splits - first, 64u);
-        for (uint32_t k = wave; k < count; k += 16u) {             // four splits of this wavefront on their way
+        for (uint32_t k = wave; k < count; k += 4u * W) {          // four splits of this wavefront on their way
             float x[4][4], f[4];
 #pragma unroll
             for (uint32_t u = 0; u < 4; ++u) {
-                const uint32_t at = min(k + 4u * u, count - 1u);
+                const uint32_t at = min(k + W * u, count - 1u);
                 f[u] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(share), (int)at));
-                if (k + 4u * u >= count) f[u] = 0.0f;
+                if (k + W * u >= count) f[u] = 0.0f;
 #pragma unroll
                 for (uint32_t i = 0; i < 4; ++i) x[u][i] = lane + 64u * i < dim ? a.part_o[(row + (first + at) * step) * dim + lane + 64u * i] : 0.0f;
             }
@@ -971,16 +972,19 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttentionArgs
         }
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) lds_o[wave][lane + 64u * i] = o[i];
+    for (int x = 32; x > 0; x >>= 1) l += __shfl_xor(l, x, 64);    // (every wavefront has looked at all of them)
+    uint16_t *out = a.out.data + (int64_t)token * a.out.token_stride + (int64_t)head * a.out.head_stride;
+    auto put = [&](uint32_t d, float sum) { out[(int64_t)d * a.out.dim_stride] = __builtin_bit_cast(uint16_t, (_Float16)(l == 0.0f ? 0.0f : sum / l)); };
+    if constexpr (W == 1) {
 #pragma unroll
-    for (int x = 32; x > 0; x >>= 1) l += __shfl_xor(l, x, 64);
-    if (lane == 0) lds_l[wave] = l;
-    __syncthreads();
-    if (tid >= dim) return;
-    const float total = lds_l[0];                                  // (every wavefront has looked at all of them)
-    const float sum = lds_o[0][tid] + lds_o[1][tid] + lds_o[2][tid] + lds_o[3][tid];
-    const _Float16 h = (_Float16)(total == 0.0f ? 0.0f : sum / total);
-    a.out.data[(int64_t)token * a.out.token_stride + (int64_t)head * a.out.head_stride + (int64_t)tid * a.out.dim_stride] = __builtin_bit_cast(uint16_t, h);
+        for (uint32_t i = 0; i < 4; ++i)
+            if (lane + 64u * i < dim) put(lane + 64u * i, o[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) lds_o[wave][lane + 64u * i] = o[i];
+        __syncthreads();
+        if (tid < dim) put(tid, lds_o[0][tid] + lds_o[1][tid] + lds_o[2][tid] + lds_o[3][tid]);
+    }
 }
 
 template <int BITS>
@@ -1043,7 +1047,9 @@ int launch_attention(const AttentionArgs &a, void *stream)
 {
     const int e = a.cache.bits == 16 ? launch_bits<16>(a, stream) : a.cache.bits == 8 ? launch_bits<8>(a, stream) : launch_bits<4>(a, stream);
     if (e || a.splits == 1u) return e;
-    return launch_args<attention_join_kernel>(a, a.tokens * a.q_heads, 1, 1, 256, stream);
+    const uint32_t rows = a.tokens * a.q_heads;                    // four wavefronts for a row where there are few
+    return rows < 2048u ? launch_args<attention_join_kernel<4>>(a, rows, 1, 1, 256, stream)
+                        : launch_args<attention_join_kernel<1>>(a, (rows + 3u) / 4u, 1, 1, 256, stream);
 }
 
 }  // namespace ecs
