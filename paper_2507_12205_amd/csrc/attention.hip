@@ -1028,16 +1028,24 @@ int launch_bits(const AttentionArgs &a, void *stream)
 
 namespace ecs {
 
-AttentionPlan plan_attention(uint32_t batch, uint32_t kv_heads, uint32_t group, uint32_t dim, uint64_t tokens, uint32_t max_new, uint64_t max_kv)
+AttentionPlan plan_attention(uint32_t batch, uint32_t kv_heads, uint32_t group, uint32_t dim, uint32_t bits, uint64_t tokens, uint32_t max_new,
+                             uint64_t max_kv)
 {
     AttentionPlan p = {};
     const uint64_t rows = (uint64_t)max_new * group;
-    p.chunk = rows > 32u;
+    // 128 rows that share their keys in LDS, or 16 a workgroup that each bring them: us by 16 / by 128, 24 rows on 8003 keys of four sequences, heads of
+    // 128, 32.3 / 29.0, in 8 bits 32.8 / 35.7, in 4 28.2 / 38.9; 48 rows 66 / 33, 45.5 / 41.5, 37.4 / 45.5; 64 rows on 564 keys 36 / 23, 29.7 /
+    // 25.6, 24.1 / 28.9; heads of 256, 32 rows, 17.5 / 27.5.
+    p.chunk = rows > (dim <= 128u && bits == 16u ? 16u : bits == 4u ? 64u : 32u);
     const uint64_t per_tile = p.chunk ? 128u : 16u;
     p.row_tiles = (uint32_t)((rows + per_tile - 1u) / per_tile);
     const uint64_t blocks = (uint64_t)p.row_tiles * kv_heads * batch;
-    // enough workgroups for the chip, and two rounds of 32 keys for each wavefront of a split (of 64 keys for a workgroup)
-    const uint64_t by_chip = blocks ? (p.chunk ? 512u : 1024u) / blocks : 1u, by_keys = (max_kv + 255u) / 256u;
+    // Enough workgroups for the chip, and two rounds of 32 keys for each wavefront of a split (four tiles of 64 for a workgroup).  More and
+    // smaller ones cost more in partial results than they gain (us by 512 / 1024 workgroups of 128 rows: 1024 tokens over 2048, heads of 128,
+    // 58 / 69, 512 over 9098 99 / 114; 1024 / 2048 of 16 rows: 8 tokens over 32768 129 / 136, in 8 bits 77 / 89), but with codes, where a tile
+    // takes longer, and several sequences of lengths of their own (five of up to 333 tokens over 3000, 8 bits 99 / 88, 4 bits 106 / 94).
+    const uint64_t wanted = !p.chunk || (bits < 16u && batch > 1u) ? 1024u : 512u;
+    const uint64_t by_chip = blocks ? wanted / blocks : 1u, by_keys = (max_kv + 255u) / 256u;
     p.splits = (uint32_t)std::max<uint64_t>(1u, std::min(by_chip, by_keys));
     if (p.splits > 1u) p.work_bytes = (uint64_t)p.splits * tokens * kv_heads * group * (dim + 2u) * sizeof(float);
     return p;

@@ -48,7 +48,8 @@ struct AttentionPlan {
     uint32_t chunk, row_tiles, splits;
     uint64_t work_bytes;
 };
-AttentionPlan plan_attention(uint32_t batch, uint32_t kv_heads, uint32_t group, uint32_t dim, uint64_t tokens, uint32_t max_new, uint64_t max_kv);
+AttentionPlan plan_attention(uint32_t batch, uint32_t kv_heads, uint32_t group, uint32_t dim, uint32_t bits, uint64_t tokens, uint32_t max_new,
+                             uint64_t max_kv);
 int launch_attention(const AttentionArgs &a, void *stream);
 
 struct VerifyArgs {
