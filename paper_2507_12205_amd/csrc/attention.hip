@@ -180,7 +180,7 @@ __device__ __forceinline__ uint32_t page_of(const AttentionArgs &a, const int32_
 // weights never leave their lane.  V comes as it lies in memory, 8 keys times DP / 16 values per lane, and is turned round in
 // registers; its columns are dealt to the products as DP / 16 per lane, the i-th product has values i of every lane.
 template <int BITS, int DP, bool PAD>
-__global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : 4) : 1) void attention_rows_kernel(const AttentionArgs a)
+__global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) : DP > 128 ? 1 : 2) void attention_rows_kernel(const AttentionArgs a)
 {
     constexpr int kSteps = DP / 32, VD = DP / 16;
     constexpr int KB = BITS == 16 ? 8 : BITS == 8 || PAD || DP == 64 ? 16 : 32;       // neighbouring values of a key in a lane
@@ -206,6 +206,53 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : 4) : 1) void atten
     const int32_t end_i = min(s.behind + (int32_t)(last_row / a.group) + 1, (int32_t)s.len);
     const uint32_t end = end_i > 0 ? (uint32_t)end_i : 0u;
     const int32_t all_see = s.behind + (int32_t)(row0 / a.group) + 1;                    // keys that every row sees
+
+    const uint32_t tiles = (end + 31u) >> 5, per = (tiles + a.splits - 1u) / a.splits;
+    const uint32_t t0 = min(split * per, tiles), t1 = min(t0 + per, tiles);
+    const uint32_t page_mask = (1u << a.cache.page_shift) - 1u;
+    const uint64_t page_rows = (uint64_t)a.cache.heads << a.cache.page_shift, head_rows = (uint64_t)head << a.cache.page_shift;
+
+    f32x4 acc[VD];
+#pragma unroll
+    for (int i = 0; i < VD; ++i) acc[i] = f32x4{0, 0, 0, 0};
+    // m: the maximum that weights are taken against, of t plus `unit` (with steps: the power of two above the largest step of V, so that
+    // weights with their steps stay in FP16's range); it may lie up to 8 below the true one, weights then go to 2^8, and what was added up
+    // is seldom scaled
+    float m = kNone, m_true = kNone, l = 0.0f, z_acc = 0.0f, unit = BITS < 16 ? -32.0f : 0.0f;   // (the smallest step is 2^-31)
+
+    // The keys of the next round are asked for as soon as this round's have been multiplied, its values before that: both are on their way
+    // while the softmax is worked out.
+    uint32_t page_list = 0;                                       // lane 2 i + h: the page of the h-th 16 keys of the i-th of 32 rounds
+    uint64_t at[2], at_next[2] = {0, 0};                          // first row of each 16 keys in the cache
+    KeyRaw k[2][kLoads];
+    uint32_t ks[8] = {};
+    auto request_k = [&](uint32_t t) {
+        const uint32_t round = (t - t0 - wave) >> 2;
+        // keys beyond the last one are read from where the last one is
+        auto key_of = [&](uint32_t tile, uint32_t h) { return min(32u * tile + 16u * h, (end - 1u) & ~15u); };
+        if ((round & 31u) == 0) {
+            page_list = page_of(a, s.table, key_of(t + 4u * (lane >> 1), lane & 1u));
+            asm volatile("" : "+v"(page_list));                   // waited for here, and not by every round
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t page = (uint32_t)__builtin_amdgcn_readlane((int)page_list, (int)(2u * (round & 31u) + h));
+            at_next[h] = (uint64_t)page * page_rows + head_rows + (key_of(t, h) & page_mask);
+            const uint8_t *p = a.cache.k + at_next[h] * a.cache.row_bytes + (j * a.cache.row_bytes + g * (KB * BITS / 8));
+#pragma unroll
+            for (int x = 0; x < kLoads; ++x) {
+                if (!PAD || (uint32_t)(x * 4 * KB) + g * KB < dim)
+                    k[h][x].load(p + x * (4 * KB * BITS / 8));
+                else
+                    k[h][x].clear();
+            }
+            if constexpr (BITS < 16) {
+                const uint4 x = *reinterpret_cast<const uint4 *>(a.cache.k_step + 4u * (at_next[h] + 4u * g));
+                ks[4 * h] = x.x, ks[4 * h + 1] = x.y, ks[4 * h + 2] = x.z, ks[4 * h + 3] = x.w;
+            }
+        }
+    };
+    if (t0 + wave < t1) request_k(t0 + wave);
 
     half8v q[kSteps];
     float q_sum = 0.0f;
@@ -242,49 +289,6 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : 4) : 1) void atten
         }
     }
 
-    const uint32_t tiles = (end + 31u) >> 5, per = (tiles + a.splits - 1u) / a.splits;
-    const uint32_t t0 = min(split * per, tiles), t1 = min(t0 + per, tiles);
-    const uint32_t page_mask = (1u << a.cache.page_shift) - 1u;
-    const uint64_t page_rows = (uint64_t)a.cache.heads << a.cache.page_shift, head_rows = (uint64_t)head << a.cache.page_shift;
-
-    f32x4 acc[VD];
-#pragma unroll
-    for (int i = 0; i < VD; ++i) acc[i] = f32x4{0, 0, 0, 0};
-    float m = kNone, l = 0.0f, z_acc = 0.0f, unit = 0.0f;         // unit: acc is in units of it (BITS < 16)
-
-    // The keys of the next round are asked for as soon as this round's have been multiplied, its values before that: both are on their way
-    // while the softmax is worked out.
-    uint32_t page_list = 0;                                       // lane 2 i + h: the page of the h-th 16 keys of the i-th of 32 rounds
-    uint64_t at[2], at_next[2] = {0, 0};                          // first row of each 16 keys in the cache
-    KeyRaw k[2][kLoads];
-    uint32_t ks[8] = {};
-    auto request_k = [&](uint32_t t) {
-        const uint32_t round = (t - t0 - wave) >> 2;
-        // keys beyond the last one are read from where the last one is
-        auto key_of = [&](uint32_t tile, uint32_t h) { return min(32u * tile + 16u * h, (end - 1u) & ~15u); };
-        if ((round & 31u) == 0) {
-            page_list = page_of(a, s.table, key_of(t + 4u * (lane >> 1), lane & 1u));
-            asm volatile("" : "+v"(page_list));                   // waited for here, and not by every round
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint32_t page = (uint32_t)__builtin_amdgcn_readlane((int)page_list, (int)(2u * (round & 31u) + h));
-            at_next[h] = (uint64_t)page * page_rows + head_rows + (key_of(t, h) & page_mask);
-            const uint8_t *p = a.cache.k + at_next[h] * a.cache.row_bytes + (j * a.cache.row_bytes + g * (KB * BITS / 8));
-#pragma unroll
-            for (int x = 0; x < kLoads; ++x) {
-                if (!PAD || (uint32_t)(x * 4 * KB) + g * KB < dim)
-                    k[h][x].load(p + x * (4 * KB * BITS / 8));
-                else
-                    k[h][x].clear();
-            }
-            if constexpr (BITS < 16) {
-                const uint4 x = *reinterpret_cast<const uint4 *>(a.cache.k_step + 4u * (at_next[h] + 4u * g));
-                ks[4 * h] = x.x, ks[4 * h + 1] = x.y, ks[4 * h + 2] = x.z, ks[4 * h + 3] = x.w;
-            }
-        }
-    };
-    if (t0 + wave < t1) request_k(t0 + wave);
     for (uint32_t t = t0 + wave; t < t1; t += 4u) {
         const uint32_t key0 = 32u * t;
         at[0] = at_next[0], at[1] = at_next[1];
@@ -340,43 +344,38 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : 4) : 1) void atten
 #pragma unroll
         for (int r = 1; r < 8; ++r) most = fmaxf(most, w[r]);
         most = max_over_32(max_over_16(most));
-        const float m_new = fmaxf(m, most), base = m_new == kNone ? 0.0f : m_new;
-        const float alpha = __builtin_amdgcn_exp2f(m - base);                       // (0 where nothing was seen before)
-        m = m_new;
+        m_true = fmaxf(m_true, most);
+        float step[8];
+        if constexpr (BITS < 16) {
+            float top = 0.0f;
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                step[r] = BITS == 8 ? __uint_as_float(vs[r]) : step_of(vs[r]);
+                if (some_hidden && key0 + (r < 4 ? 0u : 16u) + 4u * g + (r & 3) >= end) step[r] = 0.0f, vs[r] = 0u;
+                top = fmaxf(top, step[r]);
+            }
+            top = max_over_32(max_over_16(top));
+            if (top > 0.0f) unit = fmaxf(unit, (float)(ilogbf(top) + 1));
+        }
+        const float m_new = m_true + unit;
+        if (const bool far = m_new > m + 8.0f; __any((int)far)) {
+            const float alpha = far ? __builtin_amdgcn_exp2f(m - m_new) : 1.0f;       // (0 where nothing was seen before)
+            m = far ? m_new : m;                                   // a row goes by its own scores alone
+            l *= alpha;
+            z_acc *= alpha;
+#pragma unroll
+            for (int i = 0; i < VD; ++i) acc[i] *= alpha;
+        }
+        const float base = m == kNone ? 0.0f : m;
         float sum = 0.0f;
 #pragma unroll
         for (int r = 0; r < 8; ++r) {
             w[r] = __builtin_amdgcn_exp2f(w[r] - base);
             sum += w[r];
+            if constexpr (BITS == 4) z_acc = fmaf(w[r], low_of(vs[r]), z_acc);
+            if constexpr (BITS < 16) w[r] *= step[r];
         }
-        l = l * alpha + sum;
-
-        float shrink = alpha;
-        if constexpr (BITS < 16) {
-            // The steps of V go into the weights, as shares of the largest step so far (rounded up to a power of two), so that
-            // the weights that are rounded to FP16 stay within [0, 1] whatever the steps are.
-            float step[8], top = 0.0f;
-            z_acc *= alpha;
-#pragma unroll
-            for (int r = 0; r < 8; ++r) {
-                const uint32_t key = key0 + (r < 4 ? 0u : 16u) + 4u * g + (r & 3);
-                const bool in = key < end;
-                step[r] = in ? (BITS == 8 ? __uint_as_float(vs[r]) : step_of(vs[r])) : 0.0f;
-                top = fmaxf(top, step[r]);
-                if constexpr (BITS == 4) z_acc = in ? fmaf(w[r], low_of(vs[r]), z_acc) : z_acc;
-            }
-            top = max_over_32(max_over_16(top));
-            if (top > unit) {
-                const float up = ldexpf(1.0f, ilogbf(top) + 1);
-                shrink *= unit / up;
-                unit = up;
-            }
-            const float inv = unit > 0.0f ? 1.0f / unit : 0.0f;
-#pragma unroll
-            for (int r = 0; r < 8; ++r) w[r] *= step[r] * inv;
-        }
-#pragma unroll
-        for (int i = 0; i < VD; ++i) acc[i] *= shrink;
+        l += sum;
 
         bool odd = false;
         if constexpr (BITS == 16) {
@@ -437,7 +436,7 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : 4) : 1) void atten
 #pragma unroll
         for (int i = 0; i < VD; i += 4) {
             f32x4 o = {acc[i][r], acc[i + 1][r], acc[i + 2][r], acc[i + 3][r]};
-            if constexpr (BITS < 16) o = o * unit + z_acc;
+            if constexpr (BITS == 4) o = o + z_acc;
             *reinterpret_cast<f32x4 *>(&lds_o[wave][j][VD * (4u * g + r) + i]) = o;
         }
     if (g == 0) lds_ml[wave][j][0] = m, lds_ml[wave][j][1] = l;
