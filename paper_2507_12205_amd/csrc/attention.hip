@@ -396,12 +396,22 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) :
                 odd = __any((int)odd);
             }
         }
-        uint32_t pw[4];
+        // The weights as FP16 and what that leaves out, also as FP16: the matrix instructions have time for both, and the result is then as
+        // exact as sums in FP32 (rounded once its error is 1.4 times that).
+        uint32_t pw[4], pr[4];
 #pragma unroll
-        for (int p = 0; p < 4; ++p) pw[p] = as_word(half2v{(_Float16)w[2 * p], (_Float16)w[2 * p + 1]});
-        const half8v weights = as_half8(pw[0], pw[1], pw[2], pw[3]);
+        for (int p = 0; p < 4; ++p) {
+            const half2v o = {(_Float16)w[2 * p], (_Float16)w[2 * p + 1]};
+            pw[p] = as_word(o);
+            pr[p] = as_word(half2v{(_Float16)(w[2 * p] - (float)o[0]), (_Float16)(w[2 * p + 1] - (float)o[1])});
+        }
+        const half8v weights = as_half8(pw[0], pw[1], pw[2], pw[3]), rest = as_half8(pr[0], pr[1], pr[2], pr[3]);
 #pragma unroll
-        for (int i = 0; i < VD; ++i) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(value_column<BITS>(v, i), weights, acc[i], 0, 0, 0);
+        for (int i = 0; i < VD; ++i) {
+            const half8v column = value_column<BITS>(v, i);
+            acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(column, weights, acc[i], 0, 0, 0);
+            acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(column, rest, acc[i], 0, 0, 0);
+        }
         if (odd) {
             // what was left out, one key after the other, in the rows that see it
             for (uint32_t k = 0; k < 32u && key0 + k < end; ++k) {
