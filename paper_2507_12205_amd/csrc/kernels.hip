@@ -702,8 +702,12 @@ constexpr bool with_epilogue(int k) { return k >= 8; }
 template <int MODE, int KE>
 using Extra = std::conditional_t<with_epilogue(KE), ecs::EcsEpilogue, std::conditional_t<alone(MODE), NoTable, ecs::EcsBatch>>;
 
-// What the epilogue reads for one value of y = act(sum + bias) * gate + residual.  A row's are requested before its sums are added up,
-// the first row's of each 16 lanes before the workgroup's last chunks: they come from HBM, and a workgroup has a row or two for each.
+// What the epilogue reads for one value of y = act(sum + bias) * gate + residual.  It comes from HBM, and a row's is requested before its
+// sums are added up; with several right-hand sides the first row's of each 16 lanes as soon as the tables are here, among the workgroup's
+// chunks (us with the row's sums / with the chunks: four, 5120 x 13824 at 30 % with a residual 14.32 / 14.23, FP32 two, 2999 x 5003, with
+// all 8.23 / 8.07; one, 13824 x 5120 with bias, SiLU and gate 11.04 / 11.33, 5120 x 5120 with a residual 6.04 / 6.16).  What it costs beside
+// the product alone: 13824 x 5120 10.6 -> 11.0, 5120 x 5120 5.85 -> 6.04, 768 x 768 with bias and residual 2.99 -> 3.21, 4 x 5120 x 13824
+// 14.1 -> 14.2; by itself each step would be a launch of 3 us or more.
 template <int VW>
 struct EpilogueValues {
     uint32_t bias, gate, residual;
@@ -1053,7 +1057,7 @@ __global__ __launch_bounds__(1024) void ecspmv_kernel(const uint32_t count, cons
                 ahead.request(batch, row, (size_t)row * ld + first_column + (tid & 15));
             }
     };
-    constexpr bool AHEAD = EPILOGUE && !PHASES && TM < 8;          // (a 16-grained set leaves no registers for it)
+    constexpr bool AHEAD = EPILOGUE && NB > 1 && !PHASES;
     if constexpr (AHEAD) request_epilogue(tid >> 4);
 
     // (eight right-hand sides with an 8-grained set, and `tight`: after the first chunk of the coarsest set, whose sums leave no
