@@ -67,23 +67,9 @@ __device__ __forceinline__ uint32_t from_bytes(uint32_t w) { return minus(w | 0x
 // rounded weights then cancel less
 __device__ __forceinline__ uint32_t from_nibbles(uint32_t w) { return minus((w & 0x000F000Fu) | 0x64006400u, (_Float16)1032.0f); }
 
-// 8 neighbouring codes of a key as eight FP16 values.  With 4 bits in the order 0 4 1 5 2 6 3 7 (slot_dim): the values of q are put in
-// the same order, and the order of a sum's terms is free.
-template <int BITS>
-__device__ __forceinline__ half8v key_values(const uint32_t *w)
-{
-    if constexpr (BITS == 16) {
-        return as_half8(w[0], w[1], w[2], w[3]);
-    } else if constexpr (BITS == 8) {
-        const uint32_t a = w[0] ^ 0x80808080u, b = w[1] ^ 0x80808080u;
-        return as_half8(from_bytes(__builtin_amdgcn_perm(0, a, 0x0C010C00u)), from_bytes(__builtin_amdgcn_perm(0, a, 0x0C030C02u)),
-                        from_bytes(__builtin_amdgcn_perm(0, b, 0x0C010C00u)), from_bytes(__builtin_amdgcn_perm(0, b, 0x0C030C02u)));
-    } else {
-        return as_half8(from_nibbles(w[0]), from_nibbles(w[0] >> 4), from_nibbles(w[0] >> 8), from_nibbles(w[0] >> 12));
-    }
-}
-// The same without taking anything off: each value is kKeyOffset too large, which is q's sum times that in a score.  (For a score's few terms
-// of V's size that costs FP32 nothing; the sums over many keys are another matter.)
+// 8 neighbouring codes of a key as eight FP16 values, without taking anything off: each is kKeyOffset too large, which is q's sum times
+// that in a score.  (For a score's few terms that costs FP32 nothing; the sums over many keys are another matter.)  With 4 bits they come
+// in the order 0 4 1 5 2 6 3 7 (slot_dim): the values of q are put in the same order, and the order of a sum's terms is free.
 template <int BITS>
 constexpr float kKeyOffset = BITS == 8 ? 1152.0f : 1032.0f;
 template <int BITS>
@@ -179,6 +165,11 @@ __device__ __forceinline__ uint32_t page_of(const AttentionArgs &a, const int32_
 // times the weights, reads of the weights in that lane, if its sum over 32 keys is taken in the order that the first one left: the
 // weights never leave their lane.  V comes as it lies in memory, 8 keys times DP / 16 values per lane, and is turned round in
 // registers; its columns are dealt to the products as DP / 16 per lane, the i-th product has values i of every lane.
+//
+// What bounds it is reading the cache, and with one token to a sequence the two trips (lengths and pages, then keys) before the first key and
+// the join after the last, some 15 us together: one token over 200 keys, 12 heads of 64, 4.8 us; 16 sequences of up to 8192 keys, 8 heads
+// of 128 in 8 bits, 144 MB, 40 us; 8 tokens over 32768 keys, 40 heads of 128 in FP16, 671 MB, 126 us, 5.3 TB/s.  16 rows because that is
+// the least that a matrix instruction takes; four wavefronts on keys of their own need no barrier before the end.
 template <int BITS, int DP, bool PAD>
 __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) : DP > 128 ? 1 : 2) void attention_rows_kernel(const AttentionArgs a)
 {
@@ -501,6 +492,12 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) :
 // transposing read, four keys of a column per lane.
 // Pieces of 16 bytes are swapped within a row by the key's number, so that a wavefront's reads spread over all banks: of K, 16 lanes
 // read the same piece of 16 rows; of V, 64 bytes of 8 rows.
+//
+// 2048 tokens over 4096 keys, 32 heads of 128, FP16: 132 us, 780 TFLOP/s of the products that the mask leaves (a large matrix product
+// alone reaches 1229 here).  A wavefront's products and its softmax follow one another, and those of the two wavefronts of a SIMD overlap only in
+// part; without the loads it would take 98 - 107.  32 rows to a wavefront: with 64 the accumulators moved between the two halves
+// of the register file (208 us).  Softmax and products of neighbouring halves interleaved in one wavefront took 123 us here, but 122 for
+// 110 where 512 tokens see 9098 keys, 105 for 71 with five sequences in FP16 and 402 for 158 in 4 bits.
 template <int RC>
 __device__ __forceinline__ uint32_t k_swap(uint32_t key) { return RC >= 16 ? key & 15u : (key / (16 / RC)) & (RC - 1u); }
 template <int RC>
@@ -513,12 +510,17 @@ __device__ __forceinline__ uint4 nibble_values(uint32_t w)
     return make_uint4(__builtin_amdgcn_perm(b, a, 0x05040100u), __builtin_amdgcn_perm(d, c, 0x05040100u),
                       __builtin_amdgcn_perm(b, a, 0x07060302u), __builtin_amdgcn_perm(d, c, 0x07060302u));
 }
+// eight codes of 8 or 4 bits as FP16 values
 template <int BITS>
 __device__ __forceinline__ uint4 code_values(const Raw<BITS> &r)
 {
-    if constexpr (BITS == 16) return make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
-    if constexpr (BITS == 8) return __builtin_bit_cast(uint4, key_values<8>(r.w));
-    if constexpr (BITS == 4) return nibble_values(r.w[0]);
+    if constexpr (BITS == 8) {
+        const uint32_t a = r.w[0] ^ 0x80808080u, b = r.w[1] ^ 0x80808080u;
+        return make_uint4(from_bytes(__builtin_amdgcn_perm(0, a, 0x0C010C00u)), from_bytes(__builtin_amdgcn_perm(0, a, 0x0C030C02u)),
+                          from_bytes(__builtin_amdgcn_perm(0, b, 0x0C010C00u)), from_bytes(__builtin_amdgcn_perm(0, b, 0x0C030C02u)));
+    } else {
+        return nibble_values(r.w[0]);
+    }
 }
 
 template <int BITS, int DP>
@@ -585,7 +587,8 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
         }
         if constexpr (BITS == 4) q_sum += __shfl_xor(q_sum, 32, 64);
     }
-    const float scale = fabsf(a.scale_log2), by = BITS == 16 ? scale : 1.0f;
+    // (a scale of 0 as the least there is: a hidden key's score, minus infinity, stays that)
+    const float scale = a.scale_log2 == 0.0f ? 1.17549435e-38f : fabsf(a.scale_log2), by = BITS == 16 ? scale : 1.0f;
 
     const uint32_t tiles = (end + KT - 1u) / KT, per = (tiles + a.splits - 1u) / a.splits;
     const uint32_t t0 = min(split * per, tiles), t1 = min(t0 + per, tiles);
@@ -717,7 +720,8 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
         const bool masked = key0 + KT > all_see;                   // not all rows see all of the tile
         float w[16 * kHalves];
         // What is read of K and V is asked for a few products ahead, V's first half before the weights are worked out.  (Left to the
-        // compiler, the reads come pair by pair right before their products, and a wavefront waits for each: 140 us in the place of 133 for 2048 tokens over 4096 keys.)
+        // compiler, the reads come pair by pair right before their products, and a wavefront waits for each: 140 us
+        // in the place of 133 for 2048 tokens over 4096 keys.)
         half8v kf[kHalves][kSteps];
         const uint32_t key_n = here(n);
         auto read_k = [&](int y) {
@@ -1042,16 +1046,16 @@ AttentionPlan plan_attention(uint32_t batch, uint32_t kv_heads, uint32_t group, 
 {
     AttentionPlan p = {};
     const uint64_t rows = (uint64_t)max_new * group;
-    // 128 rows that share their keys in LDS, or 16 a workgroup that each bring them: us by 16 / by 128, 24 rows on 8003 keys of four sequences, heads of
-    // 128, 32.3 / 29.0, in 8 bits 32.8 / 35.7, in 4 28.2 / 38.9; 48 rows 66 / 33, 45.5 / 41.5, 37.4 / 45.5; 64 rows on 564 keys 36 / 23, 29.7 /
-    // 25.6, 24.1 / 28.9; heads of 256, 32 rows, 17.5 / 27.5.
+    // 128 rows that share their keys in LDS, or 16 a workgroup that each bring them: us by 16 / by 128, 24 rows on 8003 keys of four
+    // sequences, heads of 128, 32.3 / 29.0, in 8 bits 32.8 / 35.7, in 4 28.2 / 38.9; 48 rows 66 / 33, 45.5 / 41.5, 37.4 / 45.5; 64 rows on
+    // 564 keys 36 / 23, 29.7 / 25.6, 24.1 / 28.9; heads of 256, 32 rows, 17.5 / 27.5.
     p.chunk = rows > (dim <= 128u && bits == 16u ? 16u : bits == 4u ? 64u : 32u);
     const uint64_t per_tile = p.chunk ? 128u : 16u;
     p.row_tiles = (uint32_t)((rows + per_tile - 1u) / per_tile);
     const uint64_t blocks = (uint64_t)p.row_tiles * kv_heads * batch;
     // Enough workgroups for the chip, and two rounds of 32 keys for each wavefront of a split (four tiles of 64 for a workgroup).  More and
-    // smaller ones cost more in partial results than they gain (us by 512 / 1024 workgroups of 128 rows: 1024 tokens over 2048, heads of 128,
-    // 58 / 69, 512 over 9098 99 / 114; 1024 / 2048 of 16 rows: 8 tokens over 32768 129 / 136, in 8 bits 77 / 89), but with codes, where a tile
+    // smaller ones cost more in partial results than they gain (us by 512 / 1024 workgroups of 128 rows: 1024 tokens over 2048, heads of
+    // 128, 58 / 69, 512 over 9098 99 / 114; 1024 / 2048 of 16 rows: 8 tokens over 32768 129 / 136, in 8 bits 77 / 89), but with codes, where a tile
     // takes longer, and several sequences of lengths of their own (five of up to 333 tokens over 3000, 8 bits 99 / 88, 4 bits 106 / 94).
     const uint64_t wanted = !p.chunk || (bits < 16u && batch > 1u) ? 1024u : 512u;
     const uint64_t by_chip = blocks ? wanted / blocks : 1u, by_keys = (max_kv + 255u) / 256u;

@@ -157,6 +157,17 @@ def test_scores_far_apart(new, bits):
 
 
 @pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("new", [2, 100])
+@pytest.mark.parametrize("scale", [0.0, -0.25])
+def test_scales_of_zero_and_below(scale, new, bits):
+    """0: the mean of the values that a row sees, and of no other."""
+    import torch
+    from paper_2507_12205_amd import device as D
+    made = make(torch, D, [new, 1], [400, 1], 2, 2, 64, 16, bits, seed=13)
+    check(run(torch, D, *made, scale=scale), *made, scale=scale)
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4])
 def test_the_same_bits_every_time(bits):
     import torch
     from paper_2507_12205_amd import device as D
