@@ -1188,8 +1188,8 @@ __global__ __launch_bounds__(1024) void ecspmv_kernel(const uint32_t count, cons
 #endif
 }
 
-#if !ECS_EPILOGUE
 // ---- plain CSR, one wavefront per row (comparison only)
+#if !ECS_EPILOGUE
 __global__ __launch_bounds__(256) void csr_kernel(const int32_t *__restrict__ rowptr, const int32_t *__restrict__ col,
                                                   const uint16_t *__restrict__ val, const uint16_t *__restrict__ x,
                                                   uint16_t *__restrict__ y, uint32_t m)
