@@ -942,15 +942,19 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
     }
 }
 
-// ---- joining the splits: W wavefronts for each (token, head), on different splits -----------------------------------------------------
-template <int W>
-__global__ __launch_bounds__(256) void attention_join_kernel(const AttentionArgs a)
+// ---- joining the splits ----------------------------------------------------------------------------------------------------------------
+//
+// For each (token, head) the parts of its splits, each taken to the largest of their maxima:
+//   o = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s
+// What bounds it is the trip to memory, so that what a row needs is asked for at once and rows are many to a compute unit.
+//
+// Few rows: a workgroup for each, its wavefronts on different splits.
+__global__ __launch_bounds__(256) void attention_join_splits_kernel(const AttentionArgs a)
 {
     __shared__ float lds_o[4][256];
-    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = (tid >> 6) % W, dim = a.cache.dim;
-    const uint32_t r = blockIdx.x * (4u / W) + (tid >> 6) / W, token = r / a.q_heads, head = r - token * a.q_heads;
-    // of no sequence (q_start does not decrease: with one row to a workgroup all of it goes; with four nobody waits for the others)
-    if (r >= a.tokens * a.q_heads || (int32_t)token < a.q_start[0] || (int32_t)token >= a.q_start[a.batch]) return;
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6, dim = a.cache.dim;
+    const uint32_t r = blockIdx.x, token = r / a.q_heads, head = r - token * a.q_heads;
+    if ((int32_t)token < a.q_start[0] || (int32_t)token >= a.q_start[a.batch]) return;            // of no sequence (the whole workgroup)
     const uint64_t row = r, step = (uint64_t)a.tokens * a.q_heads;
     float l = 0.0f, o[4] = {0, 0, 0, 0}, top = kNone;
     // 64 splits at a time: a lane looks at one, its share goes to the others by readlane, so that all that is waited for is two trips
@@ -968,13 +972,13 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttentionArgs
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[i] *= before;
         const uint32_t count = min(a.splits - first, 64u);
-        for (uint32_t k = wave; k < count; k += 4u * W) {          // four splits of this wavefront on their way
+        for (uint32_t k = wave; k < count; k += 16u) {             // four splits of this wavefront on their way
             float x[4][4], f[4];
 #pragma unroll
             for (uint32_t u = 0; u < 4; ++u) {
-                const uint32_t at = min(k + W * u, count - 1u);
+                const uint32_t at = min(k + 4u * u, count - 1u);
                 f[u] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(share), (int)at));
-                if (k + W * u >= count) f[u] = 0.0f;
+                if (k + 4u * u >= count) f[u] = 0.0f;
 #pragma unroll
                 for (uint32_t i = 0; i < 4; ++i) x[u][i] = lane + 64u * i < dim ? a.part_o[(row + (first + at) * step) * dim + lane + 64u * i] : 0.0f;
             }
@@ -986,17 +990,60 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttentionArgs
     }
 #pragma unroll
     for (int x = 32; x > 0; x >>= 1) l += __shfl_xor(l, x, 64);    // (every wavefront has looked at all of them)
-    uint16_t *out = a.out.data + (int64_t)token * a.out.token_stride + (int64_t)head * a.out.head_stride;
-    auto put = [&](uint32_t d, float sum) { out[(int64_t)d * a.out.dim_stride] = __builtin_bit_cast(uint16_t, (_Float16)(l == 0.0f ? 0.0f : sum / l)); };
-    if constexpr (W == 1) {
 #pragma unroll
-        for (uint32_t i = 0; i < 4; ++i)
-            if (lane + 64u * i < dim) put(lane + 64u * i, o[i]);
+    for (int i = 0; i < 4; ++i) lds_o[wave][lane + 64u * i] = o[i];
+    __syncthreads();
+    if (tid >= dim) return;
+    const float sum = lds_o[0][tid] + lds_o[1][tid] + lds_o[2][tid] + lds_o[3][tid];
+    a.out.data[(int64_t)token * a.out.token_stride + (int64_t)head * a.out.head_stride + (int64_t)tid * a.out.dim_stride] =
+        __builtin_bit_cast(uint16_t, (_Float16)(l == 0.0f ? 0.0f : sum / l));
+}
+
+// Many rows, which have few splits: L lanes for each, four values a lane, four splits on their way.
+template <int L>
+__global__ __launch_bounds__(256) void attention_join_rows_kernel(const AttentionArgs a)
+{
+    const uint32_t r = blockIdx.x * (256u / L) + threadIdx.x / L, d = 4u * (threadIdx.x % L), dim = a.cache.dim;
+    const uint32_t token = r / a.q_heads, head = r - token * a.q_heads;
+    if (token >= a.tokens || d >= dim) return;
+    const int32_t first = a.q_start[0], last = a.q_start[a.batch];
+    const uint64_t row = r, step = (uint64_t)a.tokens * a.q_heads;
+    float l = 0.0f, top = kNone;
+    f32x4 o = {0, 0, 0, 0};
+    for (uint32_t s = 0; s < a.splits; s += 4u) {
+        float2 ml[4];
+        f32x4 x[4];
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u) {
+            const uint64_t at = row + min(s + u, a.splits - 1u) * step;
+            ml[u] = *reinterpret_cast<const float2 *>(a.part_ml + 2 * at);
+            x[u] = *reinterpret_cast<const f32x4 *>(a.part_o + at * dim + d);
+        }
+        float m = top;
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u) m = fmaxf(m, ml[u].x);    // (the last one, read again, changes nothing)
+        const float before = top == kNone ? 0.0f : __builtin_amdgcn_exp2f(top - m);
+        top = m;
+        l *= before;
+        o *= before;
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u) {
+            const float share = s + u >= a.splits || ml[u].x == kNone ? 0.0f : __builtin_amdgcn_exp2f(ml[u].x - m);
+            if (share == 0.0f) continue;
+            l = fmaf(share, ml[u].y, l);
+            o += share * x[u];
+        }
+    }
+    if ((int32_t)token < first || (int32_t)token >= last) return;  // of no sequence
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    uint16_t *p = a.out.data + (int64_t)token * a.out.token_stride + (int64_t)head * a.out.head_stride;
+    const uint32_t w0 = as_word(half2v{(_Float16)(o[0] * inv), (_Float16)(o[1] * inv)});
+    const uint32_t w1 = as_word(half2v{(_Float16)(o[2] * inv), (_Float16)(o[3] * inv)});
+    if (a.out_wide) {
+        *reinterpret_cast<uint2 *>(p + d) = make_uint2(w0, w1);
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) lds_o[wave][lane + 64u * i] = o[i];
-        __syncthreads();
-        if (tid < dim) put(tid, lds_o[0][tid] + lds_o[1][tid] + lds_o[2][tid] + lds_o[3][tid]);
+        for (int i = 0; i < 4; ++i) p[(int64_t)(d + i) * a.out.dim_stride] = (uint16_t)((i < 2 ? w0 : w1) >> (16 * (i & 1)));
     }
 }
 
@@ -1068,9 +1115,13 @@ int launch_attention(const AttentionArgs &a, void *stream)
 {
     const int e = a.cache.bits == 16 ? launch_bits<16>(a, stream) : a.cache.bits == 8 ? launch_bits<8>(a, stream) : launch_bits<4>(a, stream);
     if (e || a.splits == 1u) return e;
-    const uint32_t rows = a.tokens * a.q_heads;                    // four wavefronts for a row where there are few
-    return rows < 2048u ? launch_args<attention_join_kernel<4>>(a, rows, 1, 1, 256, stream)
-                        : launch_args<attention_join_kernel<1>>(a, (rows + 3u) / 4u, 1, 1, 256, stream);
+    // (us by a workgroup / by some lanes for each row: 320 rows of 25 splits 129 / 134, 1024 of 8 46.2 / 46.0; four bits, 1000 tokens of 32
+    // heads, two splits, by a wavefront 95, by 32 lanes 86)
+    const uint32_t rows = a.tokens * a.q_heads;
+    if (rows < 2048u) return launch_args<attention_join_splits_kernel>(a, rows, 1, 1, 256, stream);
+    if (a.cache.dim <= 64u) return launch_args<attention_join_rows_kernel<16>>(a, (rows + 15u) / 16u, 1, 1, 256, stream);
+    if (a.cache.dim <= 128u) return launch_args<attention_join_rows_kernel<32>>(a, (rows + 7u) / 8u, 1, 1, 256, stream);
+    return launch_args<attention_join_rows_kernel<64>>(a, (rows + 3u) / 4u, 1, 1, 256, stream);
 }
 
 }  // namespace ecs
