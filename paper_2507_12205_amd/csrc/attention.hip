@@ -1102,10 +1102,13 @@ AttentionPlan plan_attention(uint32_t batch, uint32_t kv_heads, uint32_t group, 
     const uint64_t blocks = (uint64_t)p.row_tiles * kv_heads * batch;
     // Enough workgroups for the chip, and two rounds of 32 keys for each wavefront of a split (four tiles of 64 for a workgroup).  More and
     // smaller ones cost more in partial results than they gain (us by 512 / 1024 workgroups of 128 rows: 1024 tokens over 2048, heads of
-    // 128, 58 / 69, 512 over 9098 99 / 114; 1024 / 2048 of 16 rows: 8 tokens over 32768 129 / 136, in 8 bits 77 / 89), but with codes, where a tile
-    // takes longer, and several sequences of lengths of their own (five of up to 333 tokens over 3000, 8 bits 99 / 88, 4 bits 106 / 94).
-    const uint64_t wanted = !p.chunk || (bits < 16u && batch > 1u) ? 1024u : 512u;
-    const uint64_t by_chip = blocks ? wanted / blocks : 1u, by_keys = (max_kv + 255u) / 256u;
+    // 128, 54 / 69, 512 over 9098 111 / 131, 200 over 2000 of three sequences, 4 bits, 52 / 61; 1024 / 2048 of 16 rows: 8 tokens over 32768
+    // 129 / 136, in 8 bits 77 / 89).  Several sequences whose chunks just fill the chip are split in two all the same: otherwise the
+    // longest one's workgroups are what the others wait for (five of up to 333 tokens over up to 3000 keys, FP16, 8 and 4 bits, whole 80, 103, 109,
+    // in two 74, 84, 87; lengths that are all the same 117, 135, 145 and 129, 149, 159).
+    const uint64_t wanted = p.chunk ? 512u : 1024u, by_keys = (max_kv + 255u) / 256u;
+    uint64_t by_chip = blocks ? wanted / blocks : 1u;
+    if (p.chunk && batch > 1u && by_chip == 1u) by_chip = 2u;
     p.splits = (uint32_t)std::max<uint64_t>(1u, std::min(by_chip, by_keys));
     if (p.splits > 1u) p.work_bytes = (uint64_t)p.splits * tokens * kv_heads * group * (dim + 2u) * sizeof(float);
     return p;

@@ -3,8 +3,9 @@
 // A row is what one token has in one head: dim values.  Eight of them go through a lane (one 128-bit access where the rows of k
 // and v allow it, else value by value), a row takes the next power of two of dim / 8 lanes, and its largest (and smallest) value
 // is found by exchanges between these lanes, so that every value is read once and every code written once: a row is one trip to
-// memory, and what bounds it is how many rows are under way (8191 tokens, 8 heads of 128: 16 bits 14.4 us, 67 MB at 4.6 TB/s; 8 bits 15.8, 4 bits 15.1; read back 11.9, 10.8, 10.5.  One lane
-// for k's and v's row together: 14.4, 15.3, 14.9 and 11.9, 10.8, 9.4, but 8 tokens of 40 heads 3.7 -> 5.1).
+// memory, and what bounds it is how many rows are under way (8191 tokens, 8 heads of 128: 16 bits 14.4 us, 67 MB at 4.6 TB/s; 8 bits
+// 15.8, 4 bits 15.1; read back 11.9, 10.8, 10.5.  One lane for k's and v's row together: 14.4, 15.3, 14.9 and 11.9, 10.8, 9.4, but 8
+// tokens of 40 heads 3.7 -> 5.1).
 //   8 bits: s = max|x| / 127 (FP32),                      code = rint(x / s),        x ~ s * code
 //   4 bits: z = min x, s = (max x - z) / 15 (both FP16),  code = rint((x - z) / s),  x ~ z + s * code
 // The steps are computed and applied in FP32; 4-bit codes are taken with the step as it is kept, in 16 bits, so that nothing but the

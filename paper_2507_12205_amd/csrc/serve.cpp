@@ -91,7 +91,8 @@ int check_attention(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *fr
     a.max_pages = (uint32_t)t.max_pages;
     a.max_new = (uint32_t)t.max_new < a.tokens ? (uint32_t)t.max_new : a.tokens;
     if ((uint64_t)a.max_pages << a.cache.page_shift > 0x7fffffffu) return ECSPMV_ERR_UNSUPPORTED;
-    plan = ecs::plan_attention(a.batch, a.cache.heads, a.group, a.cache.dim, a.cache.bits, a.tokens, a.max_new, (uint64_t)a.max_pages << a.cache.page_shift);
+    plan = ecs::plan_attention(a.batch, a.cache.heads, a.group, a.cache.dim, a.cache.bits, a.tokens, a.max_new,
+                               (uint64_t)a.max_pages << a.cache.page_shift);
     a.chunk = plan.chunk;
     a.row_tiles = plan.row_tiles;
     if ((uint64_t)plan.row_tiles * plan.splits > 65535u) return ECSPMV_ERR_UNSUPPORTED;          // (8 million rows: a grid's second dimension)
