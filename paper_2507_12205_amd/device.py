@@ -160,17 +160,18 @@ def attention_workspace(cache: KvCache, q: torch.Tensor, batch: int, max_new: in
 def attention(cache: KvCache, q: torch.Tensor, out: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, page_table: torch.Tensor,
               max_new: int, scale: float = None, workspace: torch.Tensor = None, stream=None) -> torch.Tensor:
     """out = causal attention of the new tokens q, (tokens, q_heads, head_dim) FP16 with any strides, over the cache that holds their
-    keys and values: sequence b has q[q_start[b]:q_start[b + 1]] and kv_len[b] keys in all, in the pages page_table[b] (all int32).
+    keys and values: sequence b has q[q_start[b]:q_start[b + 1]] and kv_len[b] keys in all, in the pages page_table[b] (all int32; rows of
+    the table that do not overlap).
     max_new: the most new tokens of a sequence; scale: 1 / sqrt(head_dim) if not given."""
     assert q.dtype is out.dtype is torch.float16 and q.shape == out.shape and q.shape[2] == cache.head_dim
     assert q.get_device() == out.get_device() == q_start.get_device() == kv_len.get_device() == page_table.get_device() == cache.device
     assert q_start.dtype is kv_len.dtype is page_table.dtype is torch.int32
     batch, pages = page_table.shape
     assert kv_len.shape == (batch,) and q_start.shape == (batch + 1,) and q_start.is_contiguous() and kv_len.is_contiguous()
-    assert pages <= 1 or page_table.stride(1) == 1
+    assert (pages <= 1 or page_table.stride(1) == 1) and (batch <= 1 or page_table.stride(0) >= pages)          # no expand()ed rows
     tokens, heads, _ = q.shape
     a = B.AttentionDesc(_ATTENTION, heads, tokens, batch, pages, max_new, cache.head_dim ** -0.5 if scale is None else scale,
-                        max(page_table.stride(0), pages), q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), _view(q), _view(out))
+                        page_table.stride(0) if batch > 1 else pages, q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), _view(q), _view(out))
     if workspace is None:
         workspace = torch.empty(B.ecspmv_attention_workspace(cache.desc, a), dtype=torch.uint8, device=q.device)
         if stream is not None:

@@ -1,0 +1,54 @@
+"""The Python calls around the products without a GPU: what they hand to the C ABI and what they refuse, on tensors of the CPU whose
+addresses nothing looks at."""
+import pytest
+import torch
+
+from paper_2507_12205_amd import binding as B
+from paper_2507_12205_amd import device as D
+
+
+class Stream:
+    cuda_stream = 0x55
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """The descriptions and workspaces that reach the C ABI, in order."""
+    seen = []
+    monkeypatch.setattr(D.B, "ecspmv_attention", lambda cache, a, work, size, stream: seen.append((a, work, size, stream)))
+    monkeypatch.setattr(D.B, "ecspmv_verify", lambda a, work, size, stream: seen.append((a, work, size, stream)))
+    monkeypatch.setattr(D, "_stream_handle", lambda stream=None: 0 if stream is None else stream.cuda_stream)
+    return seen
+
+
+def cache(pages=8, heads=2, page=16, dim=64):
+    """A cache of 16 bits as KvCache holds it, in host memory."""
+    c = object.__new__(D.KvCache)
+    c.bits, c.pages, c.heads, c.page_size, c.head_dim, c.device = 16, pages, heads, page, dim, -1
+    c.k, c.v = (torch.zeros((pages, heads, page, dim), dtype=torch.float16) for _ in range(2))
+    c.desc = B.KvCacheDesc(D._KV_CACHE, 16, pages, heads, page, dim, 0x100000, 0x200000, None, None)
+    return c
+
+
+def attention(c, table, q_heads=4, workspace=None, stream=None):
+    batch = table.shape[0]
+    q = torch.zeros((batch, q_heads, c.head_dim), dtype=torch.float16)
+    return D.attention(c, q, torch.empty_like(q), torch.arange(batch + 1, dtype=torch.int32), torch.full((batch,), 3, dtype=torch.int32), table, 1,
+                       workspace=workspace, stream=stream)
+
+
+def test_rows_of_the_page_table_lie_apart(calls):
+    """Rows that start less than their length apart (a table shared by expand(), overlapping rows) are refused: the C ABI has no such
+    stride, and another in its place would have the later sequences' pages read from behind the table."""
+    c, one = cache(), torch.arange(4, dtype=torch.int32)
+    for table in (one[None].expand(3, -1), torch.arange(8, dtype=torch.int32).as_strided((3, 4), (2, 1))):
+        with pytest.raises(AssertionError):
+            attention(c, table)
+    assert not calls
+    wide = torch.arange(30, dtype=torch.int32).view(3, 10)
+    for table, stride in ((wide, 10), (wide[:, :4], 10), (one[None], 4), (one[None].as_strided((1, 4), (0, 1)), 4), (wide[:1, :4], None),
+                          (wide[:0], None), (wide[:, :1], 10), (wide[:, :0], None)):
+        attention(c, table)
+        a = calls.pop()[0]
+        assert a.page_table == table.data_ptr() or table.numel() == 0
+        assert a.table_stride >= a.max_pages == table.shape[1] and (stride is None or a.table_stride == stride)
