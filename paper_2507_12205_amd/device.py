@@ -131,6 +131,15 @@ def _view(t: torch.Tensor) -> B.View:
     return B.View(t.data_ptr(), *t.stride())
 
 
+def _workspace(nbytes: int, beside: torch.Tensor, stream) -> torch.Tensor:
+    """Memory for one call, from the pool of the stream that it runs on: what is freed there is used again behind the call, and what is handed
+    out there was freed before it.  (A block of the current stream's pool may still be in use by that stream's kernels.)"""
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=beside.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device=beside.device)
+
+
 def _rows_of(cache: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
     assert k.dtype is v.dtype is torch.float16 and k.get_device() == v.get_device() == slots.get_device() == cache.device
     assert k.shape == v.shape == (*slots.shape, cache.heads, cache.head_dim)
@@ -173,9 +182,7 @@ def attention(cache: KvCache, q: torch.Tensor, out: torch.Tensor, q_start: torch
     a = B.AttentionDesc(_ATTENTION, heads, tokens, batch, pages, max_new, cache.head_dim ** -0.5 if scale is None else scale,
                         page_table.stride(0) if batch > 1 else pages, q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), _view(q), _view(out))
     if workspace is None:
-        workspace = torch.empty(B.ecspmv_attention_workspace(cache.desc, a), dtype=torch.uint8, device=q.device)
-        if stream is not None:
-            workspace.record_stream(stream)
+        workspace = _workspace(B.ecspmv_attention_workspace(cache.desc, a), q, stream)
     B.ecspmv_attention(cache.desc, a, workspace.data_ptr(), workspace.numel(), _stream_handle(stream))
     return out
 
@@ -209,8 +216,6 @@ def verify(target: torch.Tensor, draft, drafted: torch.Tensor, uniform: torch.Te
         assert count.dtype is torch.int32 and count.shape == (batch,) and count.is_contiguous() and count.get_device() == device
         a.count = count.data_ptr()
     if workspace is None:
-        workspace = torch.empty(verify_workspace(batch, vocab), dtype=torch.uint8, device=target.device)
-        if stream is not None:
-            workspace.record_stream(stream)
+        workspace = _workspace(verify_workspace(batch, vocab), target, stream)
     B.ecspmv_verify(a, workspace.data_ptr(), workspace.numel(), _stream_handle(stream))
     return tokens, accepted

@@ -52,3 +52,30 @@ def test_rows_of_the_page_table_lie_apart(calls):
         a = calls.pop()[0]
         assert a.page_table == table.data_ptr() or table.numel() == 0
         assert a.table_stride >= a.max_pages == table.shape[1] and (stride is None or a.table_stride == stride)
+
+
+@pytest.mark.parametrize("call", ["attention", "verify"])
+def test_workspace_of_the_launch_s_stream(calls, monkeypatch, call):
+    """A workspace that the call makes itself comes from the pool of the stream that the kernels run on: a block of another stream's pool may
+    still be in use by that stream's kernels."""
+    current, made = [None], []
+
+    class On:
+        def __init__(self, stream): self.stream = stream
+        def __enter__(self): current.append(self.stream)
+        def __exit__(self, *_): current.pop()
+    monkeypatch.setattr(torch.cuda, "stream", On)
+    empty = torch.empty
+    monkeypatch.setattr(torch, "empty", lambda *a, **k: (made.append(current[-1]), empty(*a, **k))[1])
+    for stream in (None, Stream()):
+        if call == "attention":
+            c, table = cache(), torch.arange(4, dtype=torch.int32)[None]
+            q, out = (torch.zeros((1, 4, 64), dtype=torch.float16) for _ in range(2))
+            ints = [torch.tensor(v, dtype=torch.int32) for v in ([0, 1], [3])]
+            D.attention(c, q, out, *ints, table, 1, stream=stream)
+        else:
+            p, q, x, u = torch.zeros(2, 4, 50), torch.zeros(2, 3, 50), torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, 4)
+            monkeypatch.setattr(torch.Tensor, "get_device", lambda self: 0)
+            D.verify(p, q, x, u, torch.zeros(2, 4, dtype=torch.int32), torch.zeros(2, dtype=torch.int32), stream=stream)
+        assert made == [stream] and calls.pop()[3] == (0x55 if stream else 0)
+        made.clear()
