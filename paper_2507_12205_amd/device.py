@@ -183,7 +183,8 @@ def attention(cache: KvCache, q: torch.Tensor, out: torch.Tensor, q_start: torch
                         page_table.stride(0) if batch > 1 else pages, q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), _view(q), _view(out))
     if workspace is None:
         workspace = _workspace(B.ecspmv_attention_workspace(cache.desc, a), q, stream)
-    B.ecspmv_attention(cache.desc, a, workspace.data_ptr(), workspace.numel(), _stream_handle(stream))
+    assert workspace.get_device() == cache.device and workspace.is_contiguous()
+    B.ecspmv_attention(cache.desc, a, workspace.data_ptr(), workspace.nbytes, _stream_handle(stream))
     return out
 
 
@@ -217,5 +218,6 @@ def verify(target: torch.Tensor, draft, drafted: torch.Tensor, uniform: torch.Te
         a.count = count.data_ptr()
     if workspace is None:
         workspace = _workspace(verify_workspace(batch, vocab), target, stream)
-    B.ecspmv_verify(a, workspace.data_ptr(), workspace.numel(), _stream_handle(stream))
+    assert workspace.get_device() == device and workspace.is_contiguous()
+    B.ecspmv_verify(a, workspace.data_ptr(), workspace.nbytes, _stream_handle(stream))
     return tokens, accepted

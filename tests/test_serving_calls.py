@@ -79,3 +79,25 @@ def test_workspace_of_the_launch_s_stream(calls, monkeypatch, call):
             D.verify(p, q, x, u, torch.zeros(2, 4, dtype=torch.int32), torch.zeros(2, dtype=torch.int32), stream=stream)
         assert made == [stream] and calls.pop()[3] == (0x55 if stream else 0)
         made.clear()
+
+
+def test_a_given_workspace_is_looked_at(calls, monkeypatch):
+    """Its device and whether it is one piece; its size in bytes, whatever its type."""
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda self: getattr(self, "place", 0))
+    c, table = cache(), torch.arange(4, dtype=torch.int32)[None]
+    c.device = 0
+    p, q, x, u = torch.zeros(2, 4, 50), torch.zeros(2, 3, 50), torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, 4)
+    tokens, accepted = torch.zeros(2, 4, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    elsewhere = torch.zeros(64, dtype=torch.uint8)
+    elsewhere.place = -1
+    for work in (elsewhere, torch.zeros(128, dtype=torch.uint8)[::2], torch.zeros(1, dtype=torch.uint8).expand(64)):
+        with pytest.raises(AssertionError):
+            attention(c, table, workspace=work)
+        with pytest.raises(AssertionError):
+            D.verify(p, q, x, u, tokens, accepted, workspace=work)
+    assert not calls
+    for work in (torch.zeros(64, dtype=torch.uint8), torch.zeros(8, dtype=torch.float64), torch.zeros((2, 8), dtype=torch.int32)):
+        attention(c, table, workspace=work)
+        D.verify(p, q, x, u, tokens, accepted, workspace=work)
+        assert [k[1:3] for k in calls] == [(work.data_ptr(), 64)] * 2
+        calls.clear()
