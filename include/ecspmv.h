@@ -297,7 +297,10 @@ typedef struct ecspmv_attention_t {
     ecspmv_view_t q, out;
 } ecspmv_attention_t;
 
+/* For this call: smaller calls may ask for more (fewer rows are split more often).  _most: enough for this one and for every one on
+ * this cache with the same q_heads and no more sequences, tokens, max_new and max_pages whose q has no rows beyond batch * max_new. */
 int ecspmv_attention_workspace(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *a, size_t *bytes);
+int ecspmv_attention_workspace_most(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *a, size_t *bytes);
 int ecspmv_attention(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *a, void *d_work, size_t work_bytes, void *stream);
 
 /* The check of drafted tokens.  Sequence b has drafted[b][0 ... count[b] - 1] (device int32, `drafts` to a row; count: device

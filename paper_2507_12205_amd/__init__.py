@@ -9,6 +9,6 @@ from .binding import (  # noqa: F401
     ecspmv_build_dense_f32, ecspmv_build_csr_f32,
     ecspmv_csr_build_dense, ecspmv_stream_read, ecspmv_stream_read_sliced, ecspmv_empty_launch,
     ecspmv_run_batch, Batch,
-    ecspmv_kv_write, ecspmv_kv_read, ecspmv_attention_workspace, ecspmv_attention, ecspmv_verify_workspace,
-    ecspmv_verify,
+    ecspmv_kv_write, ecspmv_kv_read, ecspmv_attention_workspace, ecspmv_attention_workspace_most, ecspmv_attention,
+    ecspmv_verify_workspace, ecspmv_verify,
 )

@@ -26,7 +26,8 @@ EXPORTS = (
     "ecspmv_stats", "ecspmv_decode", "ecspmv_decode_f32",
     "ecspmv_block_sets", "ecspmv_device_bytes", "ecspmv_export_image", "ecspmv_upload", "ecspmv_run", "ecspmv_run_batch", "ecspmv_run_multi", "ecspmv_run_epilogue",
     "ecspmv_csr_build_dense", "ecspmv_csr_destroy", "ecspmv_csr_device_bytes", "ecspmv_csr_upload",
-    "ecspmv_kv_write", "ecspmv_kv_read", "ecspmv_attention_workspace", "ecspmv_attention",
+    "ecspmv_kv_write", "ecspmv_kv_read", "ecspmv_attention_workspace", "ecspmv_attention_workspace_most",
+    "ecspmv_attention",
     "ecspmv_verify_workspace", "ecspmv_verify",
     "ecspmv_csr_run", "ecspmv_stream_read", "ecspmv_stream_read_sliced", "ecspmv_empty_launch", "ecspmv_strerror", "ecspmv_last_hip_error",
 )
@@ -132,6 +133,7 @@ def lib() -> ctypes.CDLL:
     L.ecspmv_kv_write.argtypes = [POINTER(KvCacheDesc), POINTER(View), POINTER(View), c_void_p, c_int64, c_void_p]
     L.ecspmv_kv_read.argtypes = [POINTER(KvCacheDesc), c_void_p, c_int64, POINTER(View), POINTER(View), c_void_p]
     L.ecspmv_attention_workspace.argtypes = [POINTER(KvCacheDesc), POINTER(AttentionDesc), POINTER(c_size_t)]
+    L.ecspmv_attention_workspace_most.argtypes = [POINTER(KvCacheDesc), POINTER(AttentionDesc), POINTER(c_size_t)]
     L.ecspmv_attention.argtypes = [POINTER(KvCacheDesc), POINTER(AttentionDesc), c_void_p, c_size_t, c_void_p]
     L.ecspmv_verify_workspace.argtypes = [POINTER(VerifyDesc), POINTER(c_size_t)]
     L.ecspmv_verify.argtypes = [POINTER(VerifyDesc), c_void_p, c_size_t, c_void_p]
@@ -419,6 +421,12 @@ def ecspmv_kv_read(cache: KvCacheDesc, d_slots: int, tokens: int, k: View, v: Vi
 def ecspmv_attention_workspace(cache: KvCacheDesc, a: AttentionDesc) -> int:
     n = c_size_t(0)
     _check(lib().ecspmv_attention_workspace(cache, a, byref(n)), "ecspmv_attention_workspace")
+    return int(n.value)
+
+
+def ecspmv_attention_workspace_most(cache: KvCacheDesc, a: AttentionDesc) -> int:
+    n = c_size_t(0)
+    _check(lib().ecspmv_attention_workspace_most(cache, a, byref(n)), "ecspmv_attention_workspace_most")
     return int(n.value)
 
 

@@ -1088,6 +1088,12 @@ int launch_bits(const AttentionArgs &a, void *stream)
 
 namespace ecs {
 
+// Rows of a workgroup, and how many workgroups are wanted, in the kernel for few rows and in the one whose rows share keys in LDS
+constexpr uint32_t kFewRows = 16, kFewWanted = 1024, kChunkRows = 128, kChunkWanted = 512;
+// (token, head) rows per head of the cache up to which the kernel for few rows takes a call (figures at plan_attention)
+static uint64_t rows_of_16(uint32_t dim, uint32_t bits) { return dim <= 128u && bits == 16u ? 16u : bits == 4u ? 64u : 32u; }
+static uint64_t splits_of_keys(uint64_t max_kv) { return (max_kv + 255u) / 256u; }
+
 AttentionPlan plan_attention(uint32_t batch, uint32_t kv_heads, uint32_t group, uint32_t dim, uint32_t bits, uint64_t tokens, uint32_t max_new,
                              uint64_t max_kv)
 {
@@ -1096,8 +1102,8 @@ AttentionPlan plan_attention(uint32_t batch, uint32_t kv_heads, uint32_t group, 
     // 128 rows that share their keys in LDS, or 16 a workgroup that each bring them: us by 16 / by 128, 24 rows on 8003 keys of four
     // sequences, heads of 128, 32.3 / 29.0, in 8 bits 32.8 / 35.7, in 4 28.2 / 38.9; 48 rows 66 / 33, 45.5 / 41.5, 37.4 / 45.5; 64 rows on
     // 564 keys 36 / 23, 29.7 / 25.6, 24.1 / 28.9; heads of 256, 32 rows, 17.5 / 27.5.
-    p.chunk = rows > (dim <= 128u && bits == 16u ? 16u : bits == 4u ? 64u : 32u);
-    const uint64_t per_tile = p.chunk ? 128u : 16u;
+    p.chunk = rows > rows_of_16(dim, bits);
+    const uint64_t per_tile = p.chunk ? kChunkRows : kFewRows;
     p.row_tiles = (uint32_t)((rows + per_tile - 1u) / per_tile);
     const uint64_t blocks = (uint64_t)p.row_tiles * kv_heads * batch;
     // Enough workgroups for the chip, and two rounds of 32 keys for each wavefront of a split (four tiles of 64 for a workgroup).  More and
@@ -1106,12 +1112,26 @@ AttentionPlan plan_attention(uint32_t batch, uint32_t kv_heads, uint32_t group, 
     // 129 / 136, in 8 bits 77 / 89).  Several sequences whose chunks just fill the chip are split in two all the same: otherwise the
     // longest one's workgroups are what the others wait for (five of up to 333 tokens over up to 3000 keys, FP16, 8 and 4 bits, whole 80, 103, 109,
     // in two 74, 84, 87; lengths that are all the same 117, 135, 145 and 129, 149, 159).
-    const uint64_t wanted = p.chunk ? 512u : 1024u, by_keys = (max_kv + 255u) / 256u;
+    const uint64_t wanted = p.chunk ? kChunkWanted : kFewWanted, by_keys = splits_of_keys(max_kv);
     uint64_t by_chip = blocks ? wanted / blocks : 1u;
     if (p.chunk && batch > 1u && by_chip == 1u) by_chip = 2u;
     p.splits = (uint32_t)std::max<uint64_t>(1u, std::min(by_chip, by_keys));
     if (p.splits > 1u) p.work_bytes = (uint64_t)p.splits * tokens * kv_heads * group * (dim + 2u) * sizeof(float);
     return p;
+}
+
+uint64_t most_attention_work(uint32_t batch, uint32_t kv_heads, uint32_t group, uint32_t dim, uint32_t bits, uint64_t tokens, uint32_t max_new,
+                             uint64_t max_kv)
+{
+    // A workgroup takes up to per_tile rows, and there are splits only while they are no more than `wanted` (twice that where two splits are the
+    // least): so many rows of partial results at most, whatever the call; and no more splits than the keys allow.
+    const uint64_t few = rows_of_16(dim, bits), by_keys = splits_of_keys(max_kv);
+    uint64_t most = 0;
+    if (group <= few) most = (uint64_t)kFewWanted * kFewRows;
+    if ((uint64_t)max_new * group > few) most = std::max<uint64_t>(most, (uint64_t)kChunkWanted * kChunkRows * (batch > 1u ? 2u : 1u));
+    if (by_keys <= 1u) return 0;
+    const uint64_t rows = std::min<uint64_t>(tokens, (uint64_t)batch * max_new) * kv_heads * group;
+    return std::min(most, by_keys * rows) * (dim + 2u) * sizeof(float);
 }
 
 int launch_attention(const AttentionArgs &a, void *stream)

@@ -137,6 +137,20 @@ int ecspmv_attention_workspace(const ecspmv_kv_cache_t *cache, const ecspmv_atte
     return ECSPMV_OK;
 }
 
+int ecspmv_attention_workspace_most(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *a, size_t *bytes)
+{
+    if (!bytes) return ECSPMV_ERR_INVALID;
+    ecs::AttentionArgs args;
+    ecs::AttentionPlan plan;
+    ecspmv_attention_t t;
+    const int s = check_attention(cache, a, args, plan, t);
+    if (s) return s;
+    const uint64_t most = ecs::most_attention_work(args.batch, args.cache.heads, args.group, args.cache.dim, args.cache.bits, args.tokens,
+                                                   args.max_new, (uint64_t)args.max_pages << args.cache.page_shift);
+    *bytes = (size_t)(most > plan.work_bytes ? most : plan.work_bytes);
+    return ECSPMV_OK;
+}
+
 int ecspmv_attention(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *a, void *d_work, size_t work_bytes, void *stream)
 {
     ecs::AttentionArgs args;

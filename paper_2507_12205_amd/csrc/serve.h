@@ -50,6 +50,9 @@ struct AttentionPlan {
 };
 AttentionPlan plan_attention(uint32_t batch, uint32_t kv_heads, uint32_t group, uint32_t dim, uint32_t bits, uint64_t tokens, uint32_t max_new,
                              uint64_t max_kv);
+// the most that a call of no more sequences, tokens, new tokens of one and places asks for, if q has no rows beyond batch * max_new
+uint64_t most_attention_work(uint32_t batch, uint32_t kv_heads, uint32_t group, uint32_t dim, uint32_t bits, uint64_t tokens, uint32_t max_new,
+                             uint64_t max_kv);
 int launch_attention(const AttentionArgs &a, void *stream);
 
 struct VerifyArgs {

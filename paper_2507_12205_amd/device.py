@@ -161,9 +161,10 @@ def kv_read(cache: KvCache, slots: torch.Tensor, k: torch.Tensor, v: torch.Tenso
 
 
 def attention_workspace(cache: KvCache, q: torch.Tensor, batch: int, max_new: int, max_kv: int) -> torch.Tensor:
-    """The workspace of attention() calls of up to these sizes: q's shape, sequences, new tokens of one, places in their page tables."""
+    """A workspace for attention() calls of up to these sizes: q's heads and no more tokens than it has (no more than batch * max_new if they
+    are fewer), sequences, new tokens of one, places in their page tables."""
     a = B.AttentionDesc(_ATTENTION, q.shape[1], q.shape[0], batch, -(-max_kv // cache.page_size), max_new)
-    return torch.empty(B.ecspmv_attention_workspace(cache.desc, a), dtype=torch.uint8, device=q.device)
+    return torch.empty(B.ecspmv_attention_workspace_most(cache.desc, a), dtype=torch.uint8, device=q.device)
 
 
 def attention(cache: KvCache, q: torch.Tensor, out: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, page_table: torch.Tensor,

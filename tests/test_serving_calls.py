@@ -1,5 +1,7 @@
 """The Python calls around the products without a GPU: what they hand to the C ABI and what they refuse, on tensors of the CPU whose
 addresses nothing looks at."""
+import random
+
 import pytest
 import torch
 
@@ -101,3 +103,22 @@ def test_a_given_workspace_is_looked_at(calls, monkeypatch):
         D.verify(p, q, x, u, tokens, accepted, workspace=work)
         assert [k[1:3] for k in calls] == [(work.data_ptr(), 64)] * 2
         calls.clear()
+
+
+@pytest.mark.parametrize("bits,heads,q_heads,dim", [(16, 32, 32, 128), (8, 8, 64, 128), (4, 2, 16, 96), (16, 1, 8, 256), (8, 1, 200, 64), (4, 40, 40, 64)])
+@pytest.mark.parametrize("batch,max_new,max_kv", [(32, 1, 4096), (4, 8, 30000), (32, 2048, 4096), (5, 333, 3000), (1, 2048, 100000), (3, 40, 200)])
+def test_a_workspace_for_all_smaller_calls(bits, heads, q_heads, dim, batch, max_new, max_kv):
+    """Made once for the largest sizes, it holds for fewer sequences, tokens, new tokens of one and places too (which have more splits)."""
+    c = cache(heads=heads, dim=dim)
+    c.desc.bits, c.desc.k_step, c.desc.v_step = bits, 0x300000, 0x400000
+    most = min(batch * max_new, (1 << 31) // q_heads - 1)
+    have = D.attention_workspace(c, torch.empty((most, q_heads, dim), dtype=torch.float16, device="meta"), batch, max_new, max_kv).nbytes
+    rng, need = random.Random(batch * max_new), 0
+    sizes = [(b, n, kv) for b in range(1, batch + 1) for n in (1, (max_new + 1) // 2, max_new) for kv in (300, max_kv)]
+    sizes += [(rng.randint(1, batch), rng.randint(1, max_new), rng.randint(1, max_kv)) for _ in range(2000)]
+    for b, n, kv in sizes:
+        tokens = rng.choice([b * n, rng.randint(n, b * n)])
+        a = B.AttentionDesc(D._ATTENTION, q_heads, tokens, b, -(-min(kv, max_kv) // 16), n)
+        need = max(need, B.ecspmv_attention_workspace(c.desc, a))
+        assert need <= have, (b, n, kv, tokens)
+    assert have <= 150 << 20                                 # and is not out of proportion
