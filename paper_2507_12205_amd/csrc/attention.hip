@@ -1028,8 +1028,9 @@ __global__ __launch_bounds__(256) void attention_join_rows_kernel(const Attentio
         o *= before;
 #pragma unroll
         for (uint32_t u = 0; u < 4; ++u) {
-            const float share = s + u >= a.splits || ml[u].x == kNone ? 0.0f : __builtin_amdgcn_exp2f(ml[u].x - m);
-            if (share == 0.0f) continue;
+            if (s + u >= a.splits) continue;
+            // (a split without a maximum has added up nothing, or scores that are all NaN: its sums are then NaN, and have to stay)
+            const float share = ml[u].x == kNone ? 0.0f : __builtin_amdgcn_exp2f(ml[u].x - m);
             l = fmaf(share, ml[u].y, l);
             o += share * x[u];
         }
