@@ -254,7 +254,8 @@ typedef struct ecspmv_view_t {
  *   bits = 8:  signed codes in [-127, 127], value = step * code, step = max|x| / 127 of the token and head;
  *              k_step, v_step: [pages][heads][page_size] float;
  *   bits = 4:  codes in [0, 15], two to a byte, the earlier one in the low half, value = low + step * code, low = min x,
- *              step = (max x - min x) / 15; k_step, v_step: [pages][heads][page_size][2] FP16 (step, low).
+ *              step = (max x - min x) / 15, the next smaller FP16 value where low + 15 step would round to infinity; k_step, v_step:
+ *              [pages][heads][page_size][2] FP16 (step, low).
  * In 8 and 4 bits NaN counts as 0 and an infinity as the largest FP16 value of its sign. */
 typedef struct ecspmv_kv_cache_t {
     uint32_t struct_size;                   /* sizeof(ecspmv_kv_cache_t) as the caller compiled it */

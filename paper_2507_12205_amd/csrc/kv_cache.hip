@@ -8,6 +8,7 @@
 // tokens of 40 heads 3.7 -> 5.1).
 //   8 bits: s = max|x| / 127 (FP32),                      code = rint(x / s),        x ~ s * code
 //   4 bits: z = min x, s = (max x - z) / 15 (both FP16),  code = rint((x - z) / s),  x ~ z + s * code
+//           (s is the next smaller FP16 value where z + 15 s would not be one)
 // The steps are computed and applied in FP32; 4-bit codes are taken with the step as it is kept, in 16 bits, so that nothing but the
 // code itself is rounded.  NaN counts as 0 and infinities as the largest FP16 value: a code stands for a finite value.
 #include <hip/hip_runtime.h>
@@ -124,7 +125,8 @@ __global__ __launch_bounds__(256) void kv_write_kernel(const KvArgs a)
             if (r.lane == 0) *reinterpret_cast<float *>(steps) = step;
         }
     } else {
-        const uint32_t step_bits = to_half((high - low) / 15.0f);
+        uint32_t step_bits = to_half((high - low) / 15.0f);
+        if (fmaf(15.0f, to_float(step_bits), low) >= 65520.0f) --step_bits;  // (rounded up, and the last code would be infinity in FP16)
         const float step = to_float(step_bits), inv = step > 0.0f ? 1.0f / step : 0.0f;
         uint32_t w = 0;
 #pragma unroll
