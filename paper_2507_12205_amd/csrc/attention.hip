@@ -118,6 +118,14 @@ __device__ __forceinline__ uint32_t here(uint32_t x)
     return x;
 }
 
+// A result as FP16.  It is a mean of values, so that what is finite here and past FP16's largest value is so by rounding only.
+__device__ __forceinline__ _Float16 to_result(float x)
+{
+    const float most = 65504.0f;
+    const float y = __builtin_amdgcn_fmed3f(x, -most, most);
+    return (_Float16)(fabsf(x) < __builtin_inff() ? y : x);
+}
+
 // the larger of a lane's value and that of the lane 32 (16) away, without LDS
 __device__ __forceinline__ float max_over_32(float x)
 {
@@ -467,7 +475,7 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) :
         uint16_t *p = a.out.data + (int64_t)(s.first + out_token) * a.out.token_stride + (int64_t)out_head * a.out.head_stride;
 #pragma unroll
         for (int i = 0; i < VD; i += 2) {
-            const half2v h = {(_Float16)(o[i] * inv), (_Float16)(o[i + 1] * inv)};
+            const half2v h = {to_result(o[i] * inv), to_result(o[i + 1] * inv)};
             if (a.out_wide) {
                 *reinterpret_cast<uint32_t *>(p + d0 + i) = as_word(h);
             } else {
@@ -919,7 +927,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
                 uint32_t o[2];
 #pragma unroll
                 for (int r = 0; r < 2; ++r)
-                    o[r] = as_word(half2v{(_Float16)((acc[y][i + 2 * r] + z_acc) * inv), (_Float16)((acc[y][i + 2 * r + 1] + z_acc) * inv)});
+                    o[r] = as_word(half2v{to_result((acc[y][i + 2 * r] + z_acc) * inv), to_result((acc[y][i + 2 * r + 1] + z_acc) * inv)});
                 if (a.out_wide) {
                     *reinterpret_cast<uint2 *>(p + d) = make_uint2(o[0], o[1]);
                 } else {
@@ -996,7 +1004,7 @@ __global__ __launch_bounds__(256) void attention_join_splits_kernel(const Attent
     if (tid >= dim) return;
     const float sum = lds_o[0][tid] + lds_o[1][tid] + lds_o[2][tid] + lds_o[3][tid];
     a.out.data[(int64_t)token * a.out.token_stride + (int64_t)head * a.out.head_stride + (int64_t)tid * a.out.dim_stride] =
-        __builtin_bit_cast(uint16_t, (_Float16)(l == 0.0f ? 0.0f : sum / l));
+        __builtin_bit_cast(uint16_t, to_result(l == 0.0f ? 0.0f : sum / l));
 }
 
 // Many rows, which have few splits: L lanes for each, four values a lane, four splits on their way.
@@ -1038,8 +1046,8 @@ __global__ __launch_bounds__(256) void attention_join_rows_kernel(const Attentio
     if ((int32_t)token < first || (int32_t)token >= last) return;  // of no sequence
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     uint16_t *p = a.out.data + (int64_t)token * a.out.token_stride + (int64_t)head * a.out.head_stride;
-    const uint32_t w0 = as_word(half2v{(_Float16)(o[0] * inv), (_Float16)(o[1] * inv)});
-    const uint32_t w1 = as_word(half2v{(_Float16)(o[2] * inv), (_Float16)(o[3] * inv)});
+    const uint32_t w0 = as_word(half2v{to_result(o[0] * inv), to_result(o[1] * inv)});
+    const uint32_t w1 = as_word(half2v{to_result(o[2] * inv), to_result(o[3] * inv)});
     if (a.out_wide) {
         *reinterpret_cast<uint2 *>(p + d) = make_uint2(w0, w1);
     } else {

@@ -30,3 +30,24 @@ def test_rows_that_reach_the_ends(bits):
         reach = np.abs(want).max(1) / 127 if bits == 8 else (want.max(1) - want.min(1)) / 15
         bound = reach * (0.5 + (0 if bits == 8 else 15 * 2 ** -10)) + 16 * 2 ** -24 + 2 ** -11 * np.abs(got).max(1)
         assert (np.abs(got - want).max(1) <= bound).all()
+
+
+@pytest.mark.parametrize("new", [1, 100])
+@pytest.mark.parametrize("bits", [8, 4])
+def test_attention_over_them(bits, new):
+    """One key repeated: the result is its value."""
+    import torch
+    from paper_2507_12205_amd import device as D
+    for a, b in ENDS[:3]:
+        row = torch.linspace(a, b, 64, device="cuda").half()
+        cache = D.kv_cache(8, 1, 16, 64, bits)
+        k = row.expand(new, 1, 64)
+        D.kv_write(cache, torch.zeros_like(k), k, torch.arange(new, device="cuda"))
+        back, other = torch.empty((new, 1, 64), dtype=torch.float16, device="cuda"), torch.empty((new, 1, 64), dtype=torch.float16, device="cuda")
+        D.kv_read(cache, torch.arange(new, device="cuda"), other, back)
+        out = torch.empty_like(back)
+        ints = [torch.tensor(v, dtype=torch.int32, device="cuda") for v in ([0, new], [new], [list(range(8))])]
+        D.attention(cache, torch.ones_like(out), out, *ints, new)
+        assert torch.isfinite(out).all()
+        # FP16 of what was read back and of the result, weights as FP16 in one or two parts
+        assert ((out - back).double().abs() <= 2 ** -9 * back.double().abs().max()).all()
