@@ -142,6 +142,9 @@ __device__ __forceinline__ float max_over_16(float x)
 __device__ __forceinline__ float step_of(uint32_t w) { return half_to_float(w & 0xFFFFu); }
 __device__ __forceinline__ float low_of(uint32_t w) { return fmaf(8.0f, step_of(w), half_to_float(w >> 16)); }
 
+// The power of two above a step, as an exponent; no less than -32 (the smallest step is 2^-31, a row of equal values has none)
+__device__ __forceinline__ float reach_of(float step) { return fmaxf((float)((int)(__float_as_uint(step) >> 23) - 126), -32.0f); }
+
 // A sequence's part of the arguments
 struct Sequence {
     uint32_t first, new_tokens, len;      // first token in q, how many, keys in all
@@ -214,10 +217,10 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) :
     f32x4 acc[VD];
 #pragma unroll
     for (int i = 0; i < VD; ++i) acc[i] = f32x4{0, 0, 0, 0};
-    // m: the maximum that weights are taken against, of t plus `unit` (with steps: the power of two above the largest step of V, so that
-    // weights with their steps stay in FP16's range); it may lie up to 8 below the true one, weights then go to 2^8, and what was added up
-    // is seldom scaled
-    float m = kNone, m_true = kNone, l = 0.0f, z_acc = 0.0f, unit = BITS < 16 ? -32.0f : 0.0f;   // (the smallest step is 2^-31)
+    // m: the maximum that weights are taken against, of t, with steps of t plus the key's reach_of(step of V): weights times steps, which go to
+    // the products as FP16, then stay in its range, and the largest of what this row sees are the ones that keep their bits, whatever steps
+    // lie beside them.  m may lie up to 8 below the true maximum, weights then go to 2^8, and what was added up is seldom scaled
+    float m = kNone, m_true = kNone, l = 0.0f, z_acc = 0.0f;
 
     // The keys of the next round are asked for as soon as this round's have been multiplied, its values before that: both are on their way
     // while the softmax is worked out.
@@ -339,24 +342,18 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) :
                 if (key >= seen) w[r] = kNone;
             }
         }
-        float most = w[0];
+        float most = kNone, step[8];
 #pragma unroll
-        for (int r = 1; r < 8; ++r) most = fmaxf(most, w[r]);
-        most = max_over_32(max_over_16(most));
-        m_true = fmaxf(m_true, most);
-        float step[8];
-        if constexpr (BITS < 16) {
-            float top = 0.0f;
-#pragma unroll
-            for (int r = 0; r < 8; ++r) {
+        for (int r = 0; r < 8; ++r) {
+            if constexpr (BITS < 16) {
+                if (some_hidden && key0 + (r < 4 ? 0u : 16u) + 4u * g + (r & 3) >= end) vs[r] = 0u;
                 step[r] = BITS == 8 ? __uint_as_float(vs[r]) : step_of(vs[r]);
-                if (some_hidden && key0 + (r < 4 ? 0u : 16u) + 4u * g + (r & 3) >= end) step[r] = 0.0f, vs[r] = 0u;
-                top = fmaxf(top, step[r]);
+                most = fmaxf(most, w[r] + reach_of(step[r]));
+            } else {
+                most = fmaxf(most, w[r]);
             }
-            top = max_over_32(max_over_16(top));
-            if (top > 0.0f) unit = fmaxf(unit, (float)(ilogbf(top) + 1));
         }
-        const float m_new = m_true + unit;
+        const float m_new = m_true = fmaxf(m_true, max_over_32(max_over_16(most)));
         if (const bool far = m_new > m + 8.0f; __any((int)far)) {
             const float alpha = far ? __builtin_amdgcn_exp2f(m - m_new) : 1.0f;       // (0 where nothing was seen before)
             m = far ? m_new : m;                                   // a row goes by its own scores alone
@@ -541,7 +538,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
     // (four objects and not two of twice the size: a read of LDS then waits for what is on its way into the same object only)
     __shared__ uint4 lds_k0[KT * RC], lds_k1[KT * RC], lds_v0[KT * RC], lds_v1[KT * RC];
     __shared__ float lds_step[2][2][2][KT];                                            // [buffer][k, v][step, low][key]
-    __shared__ float lds_top[2][4];
+    __shared__ float lds_reach[2][BITS < 16 ? KT : 1];                                 // reach_of a key's step of V
     __shared__ uint32_t lds_odd[2];
 
     const uint32_t tid = threadIdx.x, lane = tid & 63u, n = lane & 31u, h = lane >> 5;
@@ -699,11 +696,8 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
                 const float f = lane < 16u ? scale : 1.0f;
                 lds_step[b][lane >> 4][0][16u * group16 + (lane & 15u)] = f * step;
                 if constexpr (BITS == 4) lds_step[b][lane >> 4][1][16u * group16 + (lane & 15u)] = f * low;
+                if (lane >= 16u) lds_reach[b][16u * group16 + (lane & 15u)] = reach_of(step);
             }
-            float top = step;                                      // the largest step of the 16 values
-#pragma unroll
-            for (int o = 1; o < 16; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-            if (lane == 16u) lds_top[b][wave] = top;
         }
     };
 
@@ -716,10 +710,8 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
     for (int i = 0; i < kTiles; ++i)
 #pragma unroll
         for (int x = 0; x < 16; ++x) acc[i][x] = 0.0f;
-    // m: the maximum that weights are taken against, of t plus `unit` (with steps: the power of two above the largest step of V, so that
-    // weights with their steps stay in FP16's range); it may lie up to 8 below the true one, weights then go to 2^8
-    float m = kNone, m_true = kNone, l = 0.0f, z_acc = 0.0f, unit = 0.0f;
-    if constexpr (BITS < 16) unit = -32.0f;           // (the smallest step is 2^-31; not so low that weights without a step overflow)
+    // m: the maximum that weights are taken against, as in the kernel for few rows; it may lie up to 8 below the true one
+    float m = kNone, m_true = kNone, l = 0.0f, z_acc = 0.0f;
 
     auto compute = [&](uint32_t t, auto buffer) {
         const int b = buffer;
@@ -791,17 +783,19 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
             for (int i = 0; i < 16 * kHalves; ++i)
                 if (8 * (i / 4) + (i & 3) >= left) w[i] = kNone;
         }
-        float most = w[0];
+        float most = kNone;
+        if constexpr (BITS == 16) {
 #pragma unroll
-        for (int i = 1; i < 16 * kHalves; ++i) most = fmaxf(most, w[i]);
-        most = max_over_32(most);
-        m_true = fmaxf(m_true, most * by);
-        if constexpr (BITS < 16) {
-            float top = fmaxf(lds_top[b][2], lds_top[b][3]);
-            if constexpr (kGroups == 4) top = fmaxf(top, fmaxf(lds_top[b][0], lds_top[b][1]));
-            if (top > 0.0f) unit = fmaxf(unit, (float)(ilogbf(top) + 1));
+            for (int i = 0; i < 16 * kHalves; ++i) most = fmaxf(most, w[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16 * kHalves; i += 4) {
+                const f32x4 reach = *reinterpret_cast<const f32x4 *>(&lds_reach[b][8u * (i / 4) + 4u * h]);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) most = fmaxf(most, w[i + r] + reach[r]);
+            }
         }
-        const float m_new = m_true + unit;
+        const float m_new = m_true = fmaxf(m_true, max_over_32(most) * by);
         if (const bool far = m_new > m + 8.0f; __any((int)far)) {
             const float alpha = far ? __builtin_amdgcn_exp2f(m - m_new) : 1.0f;       // (0 where nothing was seen before)
             m = far ? m_new : m;                                   // a row goes by its own scores alone
