@@ -393,12 +393,14 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) :
             }
         }
         // The weights as FP16 and what that leaves out, also as FP16: the matrix instructions have time for both, and the result is then as
-        // exact as sums in FP32 (rounded once its error is 1.4 times that).
+        // exact as sums in FP32 (rounded once its error is 1.4 times that).  What is left out is that of the very value in pw: converted a
+        // second time, a weight times its step may round the other way, with the product of both rounded first or not.
         uint32_t pw[4], pr[4];
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
-            const half2v o = {(_Float16)w[2 * p], (_Float16)w[2 * p + 1]};
-            pw[p] = as_word(o);
+            pw[p] = as_word(half2v{(_Float16)w[2 * p], (_Float16)w[2 * p + 1]});
+            asm("" : "+v"(pw[p]));
+            const half2v o = as_half2(pw[p]);
             pr[p] = as_word(half2v{(_Float16)(w[2 * p] - (float)o[0]), (_Float16)(w[2 * p + 1] - (float)o[1])});
         }
         const half8v weights = as_half8(pw[0], pw[1], pw[2], pw[3]), rest = as_half8(pr[0], pr[1], pr[2], pr[3]);

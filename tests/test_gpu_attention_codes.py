@@ -13,8 +13,8 @@ from test_gpu_attention import make, run, values
 pytestmark = pytest.mark.gpu
 
 
-def bound(cache, q, start, total, table, scale):
-    """(result in 64 bits, bound of the error)"""
+def bound(cache, q, start, total, table, scale, weights=2 ** -11):
+    """(result in 64 bits, bound of the error); weights: how far those of 16 bits are off"""
     k, v = values(cache)
     q = q.cpu().numpy().astype(np.float64)
     want, slack = np.zeros(q.shape), np.zeros(q.shape)
@@ -33,7 +33,7 @@ def bound(cache, q, start, total, table, scale):
                 size = p @ np.abs(vr) if cache.bits == 8 else np.full(x.shape, parts * (p @ top))
                 score = 2 ** -22 * scale * np.abs(x).sum() * parts * np.abs(kr).max()
                 want[start[b] + t, h] = o = p @ vr
-                slack[start[b] + t, h] = 2 ** -11 * np.abs(o) + (2 ** -11 + 2 ** -14 + 2 * score) * size + seen * 2 ** -24 * parts * (p * top).max() + 2 ** -25
+                slack[start[b] + t, h] = 2 ** -11 * np.abs(o) + (weights + 2 ** -14 + 2 * score) * size + seen * 2 ** -24 * parts * (p * top).max() + 2 ** -25
     return want, slack
 
 
@@ -112,5 +112,18 @@ def test_values_of_all_sizes(new, total, bits):
             put_value(cache, table, at, head, x.half(), torch)
     got = run(torch, D, cache, q, start, lens, table)
     want, slack = bound(cache, q, start, lens, table, 128 ** -0.5)
+    worst = np.max(np.abs(got - want) / slack)
+    assert worst <= 1, worst
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+def test_both_parts_of_a_weight(bits):
+    """50000 rows of three keys: the two FP16 parts of every weight times step (2^-21 of it together) belong to one another, also where the
+    weight lies between two FP16 values."""
+    import torch
+    from paper_2507_12205_amd import device as D
+    cache, q, start, lens, table = make(torch, D, [1] * 800, [3] * 800, 64, 8, 64, 16, bits, seed=9)
+    got = run(torch, D, cache, q, start, lens, table)
+    want, slack = bound(cache, q, start, lens, table, 0.125, 2 ** -21)
     worst = np.max(np.abs(got - want) / slack)
     assert worst <= 1, worst
