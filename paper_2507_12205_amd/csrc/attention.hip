@@ -67,22 +67,22 @@ __device__ __forceinline__ uint32_t from_bytes(uint32_t w) { return minus(w | 0x
 // rounded weights then cancel less
 __device__ __forceinline__ uint32_t from_nibbles(uint32_t w) { return minus((w & 0x000F000Fu) | 0x64006400u, (_Float16)1032.0f); }
 
-// 8 neighbouring codes of a key as eight FP16 values, without taking anything off: each is kKeyOffset too large, which is q's sum times
-// that in a score.  (For a score's few terms that costs FP32 nothing; the sums over many keys are another matter.)  With 4 bits they come
-// in the order 0 4 1 5 2 6 3 7 (slot_dim): the values of q are put in the same order, and the order of a sum's terms is free.
+// 8 neighbouring codes of a key as eight FP16 values, in 4 bits 16 too large: the code is the first four bits behind the leading one of a
+// value in [16, 32), and q's sum times 16 steps comes off a score.  (Of 1032, which q's sum would come off without the shift that this takes,
+// FP32 is left with too little: a score of 128 terms off by up to 1e-3 where q has a mean; taken off the codes instead, 8 tokens over 32768
+// keys in 4 bits take 59.8 us in the place of 58.3, 16 x 1 token of up to 8192 33.7 of 31.6.)  With 4 bits they come in the order
+// 0 4 1 5 2 6 3 7 (slot_dim): the values of q are put in the same order, and the order of a sum's terms is free.
 template <int BITS>
-constexpr float kKeyOffset = BITS == 8 ? 1152.0f : 1032.0f;
-template <int BITS>
-__device__ __forceinline__ half8v key_values_offset(const uint32_t *w)
+__device__ __forceinline__ half8v key_values(const uint32_t *w)
 {
     if constexpr (BITS == 16) {
         return as_half8(w[0], w[1], w[2], w[3]);
     } else if constexpr (BITS == 8) {
-        auto two = [](uint32_t x, uint32_t select) { return __builtin_amdgcn_perm(0, x, select) ^ 0x64806480u; };
+        auto two = [](uint32_t x, uint32_t select) { return minus(__builtin_amdgcn_perm(0, x, select) ^ 0x64806480u, (_Float16)1152.0f); };
         return as_half8(two(w[0], 0x0C010C00u), two(w[0], 0x0C030C02u), two(w[1], 0x0C010C00u), two(w[1], 0x0C030C02u));
     } else {
-        auto two = [](uint32_t x) { return (x & 0x000F000Fu) | 0x64006400u; };
-        return as_half8(two(w[0]), two(w[0] >> 4), two(w[0] >> 8), two(w[0] >> 12));
+        auto two = [](uint32_t x) { return (x & 0x03C003C0u) | 0x4C004C00u; };
+        return as_half8(two(w[0] << 6), two(w[0] << 2), two(w[0] >> 2), two(w[0] >> 6));
     }
 }
 template <int BITS>
@@ -281,11 +281,11 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) :
                 const int d = slot_dim<BITS>(i);
                 const uint32_t h = (d & 1) ? w[d >> 1] >> 16 : w[d >> 1] & 0xFFFFu;
                 o[i >> 1] |= h << (16 * (i & 1));
-                if constexpr (BITS < 16) q_sum += half_to_float(h);
+                if constexpr (BITS == 4) q_sum += half_to_float(h);
             }
             q[t] = as_half8(o[0], o[1], o[2], o[3]);
         }
-        if constexpr (BITS < 16) {
+        if constexpr (BITS == 4) {
             q_sum += __shfl_xor(q_sum, 16, 64);
             q_sum += __shfl_xor(q_sum, 32, 64);
         }
@@ -320,14 +320,13 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) :
 #pragma unroll
             for (int t = 0; t < kSteps; ++t) {
                 constexpr int kPer = KB / 8;                       // steps that a load feeds
-                c = __builtin_amdgcn_mfma_f32_16x16x32_f16(key_values_offset<BITS>(&k[h][t / kPer].w[(t % kPer) * (BITS / 4)]), q[t], c, 0, 0, 0);
+                c = __builtin_amdgcn_mfma_f32_16x16x32_f16(key_values<BITS>(&k[h][t / kPer].w[(t % kPer) * (BITS / 4)]), q[t], c, 0, 0, 0);
             }
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 float d = c[r];
-                if constexpr (BITS < 16) d = fmaf(-kKeyOffset<BITS>, q_sum, d);
                 if constexpr (BITS == 8) d *= __uint_as_float(ks[4 * h + r]);
-                if constexpr (BITS == 4) d = fmaf(d, step_of(ks[4 * h + r]), q_sum * low_of(ks[4 * h + r]));
+                if constexpr (BITS == 4) d = fmaf(fmaf(-24.0f, q_sum, d), step_of(ks[4 * h + r]), q_sum * low_of(ks[4 * h + r]));
                 w[4 * h + r] = d * a.scale_log2;
             }
         }

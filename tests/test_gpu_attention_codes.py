@@ -13,6 +13,12 @@ from test_gpu_attention import make, run, values
 pytestmark = pytest.mark.gpu
 
 
+@pytest.fixture(autouse=True)
+def seed():
+    import torch
+    torch.manual_seed(1)
+
+
 def bound(cache, q, start, total, table, scale, weights=2 ** -11):
     """(result in 64 bits, bound of the error); weights: how far those of 16 bits are off"""
     k, v = values(cache)
@@ -125,5 +131,24 @@ def test_both_parts_of_a_weight(bits):
     cache, q, start, lens, table = make(torch, D, [1] * 800, [3] * 800, 64, 8, 64, 16, bits, seed=9)
     got = run(torch, D, cache, q, start, lens, table)
     want, slack = bound(cache, q, start, lens, table, 0.125, 2 ** -21)
+    worst = np.max(np.abs(got - want) / slack)
+    assert worst <= 1, worst
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("queries", ["of mean 6", "of a few large channels"])
+@pytest.mark.parametrize("new,total,heads,dim", [(1, 2, 64, 128), (2, 3, 32, 64), (1, 12, 64, 128), (2, 4, 16, 256), (3, 5, 8, 96), (150, 150, 2, 128)])
+def test_queries_that_do_not_cancel(new, total, heads, dim, queries, bits):
+    """Scores are as exact as sums of FP32 over the codes: nothing much larger than those is added up and taken off again.  (The weights of the
+    kernel for few rows are FP16 in two parts: 2^-21.)"""
+    import torch
+    from paper_2507_12205_amd import device as D
+    cache, q, start, lens, table = make(torch, D, [new] * 40, [total] * 40, heads, heads // 2, dim, 16, bits, seed=8)
+    if queries == "of mean 6":
+        q = (0.5 * q + 6).half()
+    else:
+        q = (q * torch.where(torch.rand(dim, device="cuda") < 0.04, 20.0, 1.0)).half()
+    got = run(torch, D, cache, q, start, lens, table)
+    want, slack = bound(cache, q, start, lens, table, dim ** -0.5, 2 ** -11 if new > 100 else 2 ** -21)
     worst = np.max(np.abs(got - want) / slack)
     assert worst <= 1, worst
