@@ -283,7 +283,8 @@ int ecspmv_kv_read(const ecspmv_kv_cache_t *cache, const int64_t *d_slots, int64
  * with sums and softmax in FP32; a token that sees no key gets zeros.  Head h of q reads head h / (q_heads / heads) of the
  * cache.  max_new is at least every sequence's number of new tokens (it shapes the launch).  Lengths beyond max_pages *
  * page_size count as that, page numbers outside the cache as a page of it.  What lies in the cache beyond kv_len has no
- * effect, nor have infinities and NaN in V on tokens that do not see them.  out must not overlap q.
+ * effect, nor have infinities and NaN in V on tokens that do not see them; for those that do, what is not finite adds up to the
+ * result (weights are above zero, however small).  out must not overlap q.
  * One launch, or two where long sequences are split for want of rows: then d_work (device, 16-byte aligned, at least
  * ecspmv_attention_workspace bytes, contents of no matter before and after) is used; it may be NULL where 0 bytes are
  * asked for.  The result has the same bits every time. */

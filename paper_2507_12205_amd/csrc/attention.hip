@@ -118,12 +118,22 @@ __device__ __forceinline__ uint32_t here(uint32_t x)
     return x;
 }
 
+// The share of a part of the softmax's sums whose maximum is m, where the largest of all is `top`: above zero, as weights are, so that an infinity
+// which the part has met stays one; 0 where it has met no key
+__device__ __forceinline__ float share_of(float m, float top)
+{
+    return m == kNone ? 0.0f : fmaxf(__builtin_amdgcn_exp2f(m - top), 1.17549435e-38f);
+}
+
+__device__ __forceinline__ bool finite(float x) { return fabsf(x) < __builtin_inff(); }
+__device__ __forceinline__ bool half_finite(uint32_t h) { return (h & 0x7C00u) != 0x7C00u; }
+
 // A result as FP16.  It is a mean of values, so that what is finite here and past FP16's largest value is so by rounding only.
 __device__ __forceinline__ _Float16 to_result(float x)
 {
     const float most = 65504.0f;
     const float y = __builtin_amdgcn_fmed3f(x, -most, most);
-    return (_Float16)(fabsf(x) < __builtin_inff() ? y : x);
+    return (_Float16)(finite(x) ? y : x);
 }
 
 // the larger of a lane's value and that of the lane 32 (16) away, without LDS
@@ -221,6 +231,7 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) :
     // the products as FP16, then stay in its range, and the largest of what this row sees are the ones that keep their bits, whatever steps
     // lie beside them.  m may lie up to 8 below the true maximum, weights then go to 2^8, and what was added up is seldom scaled
     float m = kNone, m_true = kNone, l = 0.0f, z_acc = 0.0f;
+    bool odd = false;                                              // values that are not finite were left out
 
     // The keys of the next round are asked for as soon as this round's have been multiplied, its values before that: both are on their way
     // while the softmax is worked out.
@@ -372,7 +383,6 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) :
         }
         l += sum;
 
-        bool odd = false;
         if constexpr (BITS == 16) {
             if (some_hidden) {
                 // Keys that no row of the tile sees may hold anything; and where V is not finite, a weight of 0 has to stay without
@@ -383,12 +393,11 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) :
 #pragma unroll
                     for (uint32_t &x : v[r].w) {
                         x = key < end ? x : 0u;
-                        const uint32_t keep = ((x & 0x7C00u) != 0x7C00u ? 0xFFFFu : 0u) | ((x & 0x7C000000u) != 0x7C000000u ? 0xFFFF0000u : 0u);
+                        const uint32_t keep = (half_finite(x) ? 0xFFFFu : 0u) | (half_finite(x >> 16) ? 0xFFFF0000u : 0u);
                         odd |= keep != 0xFFFFFFFFu;
                         x &= keep;
                     }
                 }
-                odd = __any((int)odd);
             }
         }
         // The weights as FP16 and what that leaves out, also as FP16: the matrix instructions have time for both, and the result is then as
@@ -409,25 +418,37 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) :
             acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(column, weights, acc[i], 0, 0, 0);
             acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(column, rest, acc[i], 0, 0, 0);
         }
-        if (odd) {
-            // what was left out, one key after the other, in the rows that see it
-            for (uint32_t k = 0; k < 32u && key0 + k < end; ++k) {
-                const uint32_t r = (k & 3u) + 4u * (k >> 4), from = j + 16u * ((k >> 2) & 3u);
-                float x = w[0];
+    }
+
+    if constexpr (BITS == 16) {
+        // Where V was not finite, the sum of what was not is the result: weights are above zero, but in FP16, or the second part of one, they
+        // may be zero or less.  Rare, and not fast.  (With a weight of NaN, l is NaN too.)
 #pragma unroll
-                for (uint32_t i = 1; i < 8; ++i) x = r == i ? w[i] : x;
-                x = __shfl(x, (int)from, 64);
-                if ((int32_t)(key0 + k) >= seen) continue;
-                const uint16_t *p = reinterpret_cast<const uint16_t *>(a.cache.v + (at[k >> 4] + (k & 15u)) * a.cache.row_bytes);
+        for (int i = 0; i < VD; ++i)
 #pragma unroll
-                for (int r2 = 0; r2 < 4; ++r2)
-#pragma unroll
-                    for (int i = 0; i < VD; ++i) {
-                        const uint32_t d = VD * (4u * g + r2) + i;
-                        if (PAD && d >= dim) continue;
-                        if ((p[d] & 0x7C00u) == 0x7C00u) acc[i][r2] = fmaf(x, half_to_float(p[d]), acc[i][r2]);
-                    }
+            for (int r = 0; r < 4; ++r) {
+                odd |= !finite(acc[i][r]);
+                acc[i][r] = finite(acc[i][r]) ? acc[i][r] : 0.0f;
             }
+        if (__any((int)odd)) {
+            for (uint32_t t = t0 + wave; t < t1; t += 4u)
+#pragma unroll 1
+                for (uint32_t key = 32u * t; key < min(32u * t + 32u, end); ++key) {
+                    if ((int32_t)key >= seen) continue;
+                    const uint64_t at = (uint64_t)page_of(a, s.table, key) * page_rows + head_rows + (key & page_mask);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const uint32_t d = VD * (4u * g + r);
+                        if (PAD && d >= dim) continue;
+                        ValueRaw x;
+                        x.load(a.cache.v + at * a.cache.row_bytes + 2u * d);
+#pragma unroll
+                        for (int i = 0; i < VD; ++i) {
+                            const uint32_t v = (i & 1) ? x.w[i >> 1] >> 16 : x.w[i >> 1] & 0xFFFFu;
+                            acc[i][r] += half_finite(v) ? 0.0f : half_to_float(v);
+                        }
+                    }
+                }
         }
     }
 
@@ -456,8 +477,7 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) :
     for (int x = 0; x < 4; ++x) most = fmaxf(most, lds_ml[x][n][0]);
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
-        share[x] = most == kNone ? 0.0f : __builtin_amdgcn_exp2f(lds_ml[x][n][0] - most);
-        if (lds_ml[x][n][0] == kNone) share[x] = 0.0f;             // (what it has added up is nothing)
+        share[x] = share_of(lds_ml[x][n][0], most);
         total += share[x] * lds_ml[x][n][1];
     }
     float o[VD];
@@ -673,7 +693,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
 #pragma unroll
                     for (uint32_t &y : w) {
                         y = key0 + x / RC < end ? y : 0u;
-                        const uint32_t keep = ((y & 0x7C00u) != 0x7C00u ? 0xFFFFu : 0u) | ((y & 0x7C000000u) != 0x7C000000u ? 0xFFFF0000u : 0u);
+                        const uint32_t keep = (half_finite(y) ? 0xFFFFu : 0u) | (half_finite(y >> 16) ? 0xFFFF0000u : 0u);
                         odd |= keep != 0xFFFFFFFFu;
                         y &= keep;
                     }
@@ -877,29 +897,28 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
     }
 
     if constexpr (BITS == 16) {
-        if (lds_odd[0] | lds_odd[1]) {
-            // Values that are not finite and were left out: with the weights worked out once more, one key after the other, in the rows
-            // that see them.  Rare, and not fast.
+        // Where V was not finite, as in the kernel for few rows
+        bool odd = (lds_odd[0] | lds_odd[1]) != 0u;
+#pragma unroll
+        for (int y = 0; y < kTiles; ++y)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                odd |= !finite(acc[y][i]);
+                acc[y][i] = finite(acc[y][i]) ? acc[y][i] : 0.0f;
+            }
+        if (__any((int)odd)) {
             const uint32_t last = min(t1 * KT, end);
-            for (uint32_t key = max(t0, all_see / KT) * KT; key < last; ++key) {
+#pragma unroll 1
+            for (uint32_t key = t0 * KT; key < last; ++key) {
                 if ((int32_t)key >= seen) continue;
                 const uint64_t at = (uint64_t)page_of(a, s.table, key) * page_rows + head_rows + (key & page_mask);
                 const uint16_t *vp = reinterpret_cast<const uint16_t *>(a.cache.v + at * a.cache.row_bytes);
-                const uint16_t *kp = reinterpret_cast<const uint16_t *>(a.cache.k + at * a.cache.row_bytes);
-                const uint16_t *qp = a.q.data + (int64_t)(s.first + token) * a.q.token_stride +
-                                     (int64_t)(head * a.group + (row - token * a.group)) * a.q.head_stride;
-                bool odd = false;
-                for (uint32_t d = 0; d < dim; ++d) odd |= (vp[d] & 0x7C00u) == 0x7C00u;
-                if (!odd) continue;
-                float x = 0.0f;
-                for (uint32_t d = 0; d < dim; ++d) x = fmaf(half_to_float(kp[d]), half_to_float(qp[(int64_t)d * a.q.dim_stride]), x);
-                x = __builtin_amdgcn_exp2f(x * a.scale_log2 - m);
 #pragma unroll
                 for (int y = 0; y < kTiles; ++y)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const uint32_t d = 32u * y + 8u * (i / 4) + 4u * h + (i & 3);
-                        if (d < dim && (vp[d] & 0x7C00u) == 0x7C00u) acc[y][i] = fmaf(x, half_to_float(vp[d]), acc[y][i]);
+                        if (d < dim && !half_finite(vp[d])) acc[y][i] += half_to_float(vp[d]);
                     }
             }
         }
@@ -968,9 +987,9 @@ __global__ __launch_bounds__(256) void attention_join_splits_kernel(const Attent
 #pragma unroll
         for (int x = 32; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor(m, x, 64));
         m = fmaxf(m, top);
-        const float before = top == kNone ? 0.0f : __builtin_amdgcn_exp2f(top - m);
+        const float before = share_of(top, m);
         top = m;
-        const float share = ml.x == kNone ? 0.0f : __builtin_amdgcn_exp2f(ml.x - m);
+        const float share = share_of(ml.x, m);
         l = l * before + share * ml.y;
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[i] *= before;
@@ -1025,7 +1044,7 @@ __global__ __launch_bounds__(256) void attention_join_rows_kernel(const Attentio
         float m = top;
 #pragma unroll
         for (uint32_t u = 0; u < 4; ++u) m = fmaxf(m, ml[u].x);    // (the last one, read again, changes nothing)
-        const float before = top == kNone ? 0.0f : __builtin_amdgcn_exp2f(top - m);
+        const float before = share_of(top, m);
         top = m;
         l *= before;
         o *= before;
@@ -1033,7 +1052,7 @@ __global__ __launch_bounds__(256) void attention_join_rows_kernel(const Attentio
         for (uint32_t u = 0; u < 4; ++u) {
             if (s + u >= a.splits) continue;
             // (a split without a maximum has added up nothing, or scores that are all NaN: its sums are then NaN, and have to stay)
-            const float share = ml[u].x == kNone ? 0.0f : __builtin_amdgcn_exp2f(ml[u].x - m);
+            const float share = share_of(ml[u].x, m);
             l = fmaf(share, ml[u].y, l);
             o += share * x[u];
         }

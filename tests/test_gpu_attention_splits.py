@@ -74,3 +74,27 @@ def test_nan_in_all_keys_of_a_split(name):
     assert np.isnan(got[:end, :group]).all()
     got[:end, :group] = clean[:end, :group]
     assert np.array_equal(got, clean)
+
+
+@pytest.mark.parametrize("scale", [None, 4.0])
+@pytest.mark.parametrize("name", WAYS)
+def test_values_that_are_not_finite(name, scale):
+    """Softmax's weights are above zero, however small they come out (the scale of 4: most of them below what FP16 or FP32 hold): an infinity in a
+    value that a row sees is its result, two of different sign or a NaN make NaN; other rows, heads and columns keep their bits."""
+    import torch
+    from paper_2507_12205_amd import device as D
+    cache, q, start, total, table = way(name, 16, 24, torch)
+    clean = run(torch, D, cache, q, start, total, table, scale=scale)
+    inf = float("inf")
+    odd = [(0, 5, inf), (2, 5, inf), (7, 6, -inf), (9, 8, inf), (11, 8, -inf), (12, 9, float("nan")), (30, 11, -inf), (int(total[0]) - 1, 12, inf)]
+    for key, d, x in odd:
+        cache.v[int(table[0, key // cache.page_size]), 0, key % cache.page_size, d] = x
+    want, group = clean.copy(), q.shape[1] // cache.heads
+    for t in range(int(start[1])):
+        seen = int(total[0] - start[1]) + t + 1
+        for d in {d for _, d, _ in odd}:
+            met = [x for key, e, x in odd if e == d and key < seen]
+            if met:
+                want[t, :group, d] = sum(met)
+    got = run(torch, D, cache, q, start, total, table, scale=scale)
+    assert np.array_equal(got, want, equal_nan=True)
