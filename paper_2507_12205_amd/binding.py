@@ -187,7 +187,8 @@ class Matrix:
     def __init__(self, handle: int):
         self._h = c_void_p(handle)
         self.d_image = None          # whatever object owns the device buffer (kept alive here)
-        self.value_bits = self.ecspmv_stats().value_bits     # 16 or 32: a handle's values never change
+        st = self.ecspmv_stats()                             # a handle's size and values never change
+        self.m, self.n, self.value_bits = st.m, st.n, st.value_bits          # (16 or 32 bits)
 
     def __del__(self):
         try:

@@ -58,17 +58,17 @@ def run_epilogue(mat: B.Matrix, x: torch.Tensor, y: torch.Tensor, bias: torch.Te
     (n, nb) and (m, nb) with nb in {1, 2, 4, 8}; bias (m,); gate and residual shaped as y, which either may be itself; all FP16, or FP32 for
     a matrix built from FP32 values.  activation: "none", "relu", "gelu" (with the error function) or "silu"."""
     want = torch.float32 if mat.value_bits == 32 else torch.float16
-    assert x.dtype is want and y.dtype is want and x.is_cuda and y.is_cuda and x.is_contiguous() and y.is_contiguous()
-    shape, e = y.shape, B.Epilogue(_EPILOGUE, _ACTIVATIONS[activation])
-    assert x.dim() == y.dim() and x.shape[1:] == shape[1:] and len(shape) in (1, 2)
+    device, shape, e = x.get_device(), y.shape, B.Epilogue(_EPILOGUE, _ACTIVATIONS[activation])
+    assert x.dtype is want and y.dtype is want and device >= 0 and y.get_device() == device and x.is_contiguous() and y.is_contiguous()
+    assert x.dim() == y.dim() and x.shape[1:] == shape[1:] and len(shape) in (1, 2) and x.shape[0] == mat.n and shape[0] == mat.m
     if bias is not None:
-        assert bias.dtype is want and bias.is_cuda and bias.shape == shape[:1] and bias.is_contiguous()
+        assert bias.dtype is want and bias.get_device() == device and bias.shape == shape[:1] and bias.is_contiguous()
         e.bias = bias.data_ptr()
     if gate is not None:
-        assert gate.dtype is want and gate.is_cuda and gate.shape == shape and gate.is_contiguous()
+        assert gate.dtype is want and gate.get_device() == device and gate.shape == shape and gate.is_contiguous()
         e.gate = gate.data_ptr()
     if residual is not None:
-        assert residual.dtype is want and residual.is_cuda and residual.shape == shape and residual.is_contiguous()
+        assert residual.dtype is want and residual.get_device() == device and residual.shape == shape and residual.is_contiguous()
         e.residual = residual.data_ptr()
     mat.ecspmv_run_epilogue(x.data_ptr(), y.data_ptr(), shape[1] if len(shape) == 2 else 1, e, _stream_handle(stream))
     return y

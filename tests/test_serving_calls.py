@@ -122,3 +122,29 @@ def test_a_workspace_for_all_smaller_calls(bits, heads, q_heads, dim, batch, max
         need = max(need, B.ecspmv_attention_workspace(c.desc, a))
         assert need <= have, (b, n, kv, tokens)
     assert have <= 150 << 20                                 # and is not out of proportion
+
+
+def test_products_with_an_epilogue_of_the_matrix_s_size(monkeypatch):
+    """x, y and what the epilogue reads are looked at for their size and device: the kernel goes by the matrix."""
+    import numpy as np
+    mat = B.ecspmv_build_dense(np.eye(16, 128, dtype=np.float16), B.make_opts())
+    seen = []
+    monkeypatch.setattr(B.Matrix, "ecspmv_run_epilogue", lambda self, *a: seen.append(a))
+    monkeypatch.setattr(torch.Tensor, "is_cuda", True)
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda self: getattr(self, "place", 0))
+    monkeypatch.setattr(D, "_stream_handle", lambda stream=None: 0)
+
+    def half(*shape, place=0):
+        t = torch.zeros(shape, dtype=torch.float16)
+        t.place = place
+        return t
+    right = dict(x=half(128, 4), y=half(16, 4), bias=half(16), gate=half(16, 4), residual=half(16, 4))
+    D.run_epilogue(mat, **right)
+    D.run_epilogue(mat, half(128), half(16))
+    assert len(seen) == 2
+    for wrong in (dict(x=half(127, 4)), dict(x=half(129, 4)), dict(y=half(15, 4), bias=None, gate=None, residual=None),
+                  dict(y=half(17, 4), bias=half(17), gate=half(17, 4), residual=half(17, 4)), dict(x=half(128, 4, place=1)),
+                  dict(bias=half(16, place=1)), dict(gate=half(16, 4, place=1)), dict(residual=half(16, 4, place=1))):
+        with pytest.raises(AssertionError):
+            D.run_epilogue(mat, **{**right, **wrong})
+    assert len(seen) == 2
