@@ -1094,9 +1094,7 @@ __global__ __launch_bounds__(1024) void ecspmv_kernel(const uint32_t count, cons
     const uint32_t j = tid & 15;
     if constexpr (NB == 1) {
         for (uint32_t r = tid >> 4; r < nrows; r += nt >> 4) {
-            if constexpr (EPILOGUE && !AHEAD) request_epilogue(r);
-            const EpilogueValues<VW> mine = ahead;
-            if constexpr (AHEAD) request_epilogue(r + (nt >> 4));
+            if constexpr (EPILOGUE) request_epilogue(r);
             float sum = 0.0f;
             if constexpr (TM != 0) {
                 const uint32_t s0 = rowslot[r], s1 = rowslot[r + 1];
@@ -1105,7 +1103,7 @@ __global__ __launch_bounds__(1024) void ecspmv_kernel(const uint32_t count, cons
             const uint32_t l0 = rowlu[r], l1 = rowlu[r + 1];
             for (uint32_t q = l0 + j; q < l1; q += 16) sum += part[q];
             float t = row16_allreduce(sum);
-            if constexpr (EPILOGUE) t = mine.apply(batch, t);
+            if constexpr (EPILOGUE) t = ahead.apply(batch, t);
             if constexpr (VW == 2) {
                 if (j == 0) y[rowidx[r]] = __half_as_ushort(__float2half_rn(t));
             } else {
@@ -1126,7 +1124,6 @@ __global__ __launch_bounds__(1024) void ecspmv_kernel(const uint32_t count, cons
         };
         if constexpr (!PHASES) {
             for (uint32_t r = tid >> 4; r < nrows; r += nt >> 4) {
-                if constexpr (EPILOGUE && !AHEAD) request_epilogue(r);
                 const EpilogueValues<VW> mine = ahead;
                 if constexpr (AHEAD) request_epilogue(r + (nt >> 4));
                 float sum[NB] = {};
