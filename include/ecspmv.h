@@ -280,7 +280,8 @@ int ecspmv_kv_read(const ecspmv_kv_cache_t *cache, const int64_t *d_slots, int64
  * and kv_len[b] keys in all (device int32), the new tokens' own last; its key i is in page page_table[b * table_stride +
  * i / page_size] (device int32), place i % page_size.  Token t of its n new tokens sees the keys up to kv_len - n + t and
  *   out = sum_i softmax_i(scale * q . k_i) v_i
- * with sums and softmax in FP32; a token that sees no key gets zeros.  Head h of q reads head h / (q_heads / heads) of the
+ * with sums and softmax in FP32.  Its weights meet V in 22 bits, where more than 16 to 64 (token, head) rows share a head of the cache in
+ * the 11 of FP16.  A token that sees no key, or whose scores are all minus infinity, gets zeros.  Head h of q reads head h / (q_heads / heads) of the
  * cache.  max_new is at least every sequence's number of new tokens (it shapes the launch).  Lengths beyond max_pages *
  * page_size count as that, page numbers outside the cache as a page of it.  What lies in the cache beyond kv_len has no
  * effect, nor have infinities and NaN in V on tokens that do not see them; for those that do, what is not finite adds up to the
@@ -309,7 +310,7 @@ int ecspmv_attention(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *a
  * int32, NULL for `drafts` each), target probabilities target[b][i][token] (device FP32, drafts + 1 rows of `vocab`), the
  * drafts' own draft[b][i][token] (device FP32, `drafts` rows; NULL where a draft was certain, probability 1) and random
  * numbers uniform[b][0 ... drafts] in [0, 1) (device FP32).  Draft i is accepted while
- *   uniform[i] * draft[i][x_i] < target[i][x_i]
+ *   uniform[i] * draft[i][x_i] < target[i][x_i]                 (the product in FP32)
  * and with n accepted the next token is the first v at which the running sum of w passes uniform[drafts] * sum(w), where
  * w = max(target[n] - draft[n], 0) after a refusal (target[n] where that leaves nothing) and w = target[n] without one.
  * Differences and sums are in 64 bits.  accepted[b] = n; tokens[b][0 ... drafts] (device int32) = the accepted drafts, the next token,

@@ -519,6 +519,12 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) :
 // Pieces of 16 bytes are swapped within a row by the key's number, so that a wavefront's reads spread over all banks: of K, 16 lanes
 // read the same piece of 16 rows; of V, 64 bytes of 8 rows.
 //
+// The weights go to the second product as one FP16 value, 2^-11 of each, where the kernel above has a second one for what that leaves out: the
+// error against 64 bits is 2.9e-4 of the result in place of the 2.1e-4 that its own rounding to FP16 makes.  Here the matrix instructions are
+// half of the time, and a second part costs what it takes (us by one / by two: 2048 tokens over 4096 keys, heads of 128, FP16 132 / 171, 8 bits 164 /
+// 194, 4 bits 168 / 202; 512 over 9098 108 / 133; five of up to 333 over 3000, heads of 80, 68 / 80, 4 bits 78 / 86).  With FP16 the sum of the weights is
+// that of the rounded ones.
+//
 // 2048 tokens over 4096 keys, 32 heads of 128, FP16: 132 us, 780 TFLOP/s of the products that the mask leaves (a large matrix product
 // alone reaches 1229 here).  A wavefront's products and its softmax follow one another, and those of the two wavefronts of a SIMD overlap only in
 // part; without the loads it would take 98 - 107.  32 rows to a wavefront: with 64 the accumulators moved between the two halves
@@ -1133,8 +1139,10 @@ AttentionPlan plan_attention(uint32_t batch, uint32_t kv_heads, uint32_t group, 
     // smaller ones cost more in partial results than they gain (us by 512 / 1024 workgroups of 128 rows: 1024 tokens over 2048, heads of
     // 128, 54 / 69, 512 over 9098 111 / 131, 200 over 2000 of three sequences, 4 bits, 52 / 61; 1024 / 2048 of 16 rows: 8 tokens over 32768
     // 129 / 136, in 8 bits 77 / 89).  Several sequences whose chunks just fill the chip are split in two all the same: otherwise the
-    // longest one's workgroups are what the others wait for (five of up to 333 tokens over up to 3000 keys, FP16, 8 and 4 bits, whole 80, 103, 109,
-    // in two 74, 84, 87; lengths that are all the same 117, 135, 145 and 129, 149, 159).
+    // longest one's workgroups are what the others wait for.  That is a bet on lengths that differ, which the host does not see (heads of 128, whole / in
+    // two, FP16, 8 and 4 bits: five of up to 333 tokens over up to 3000 keys 91 / 83, 108 / 115, 112 / 88, other lengths 80 / 74, 103 / 84, 109 / 87;
+    // five of one length 128 / 147, 150 / 166, 151 / 169).  With more workgroups than the chip holds at once the next one starts where one ends, and two
+    // splits cost in both cases (eight sequences 97 / 100, 149 / 155, 136 / 151, of one length 208 / 226; twelve 147 / 167, 189 / 190, 157 / 160).
     const uint64_t wanted = p.chunk ? kChunkWanted : kFewWanted, by_keys = splits_of_keys(max_kv);
     uint64_t by_chip = blocks ? wanted / blocks : 1u;
     if (p.chunk && batch > 1u && by_chip == 1u) by_chip = 2u;
