@@ -280,13 +280,13 @@ int ecspmv_kv_read(const ecspmv_kv_cache_t *cache, const int64_t *d_slots, int64
  * and kv_len[b] keys in all (device int32), the new tokens' own last; its key i is in page page_table[b * table_stride +
  * i / page_size] (device int32), place i % page_size.  Token t of its n new tokens sees the keys up to kv_len - n + t and
  *   out = sum_i softmax_i(scale * q . k_i) v_i
- * with sums and softmax in FP32.  Its weights meet V in 22 bits, where more than 16 to 64 (token, head) rows share a head of the cache in
- * the 11 of FP16.  A token that sees no key, or whose scores are all minus infinity, gets zeros.  Head h of q reads head h / (q_heads / heads) of the
- * cache.  max_new is at least every sequence's number of new tokens (it shapes the launch; what out holds for tokens beyond it is
- * anything).  Lengths beyond max_pages *
- * page_size count as that, page numbers outside the cache as a page of it.  What lies in the cache beyond kv_len has no
- * effect, nor have infinities and NaN in V on tokens that do not see them; for those that do, what is not finite adds up to the
- * result (weights are above zero, however small).  out must not overlap q.
+ * with sums and softmax in FP32.  Its weights meet V in 22 bits, where more than 16 to 64 (token, head) rows share
+ * a head of the cache in the 11 of FP16.  A token that sees no key, or whose scores are all minus infinity, gets
+ * zeros.  Head h of q reads head h / (q_heads / heads) of the cache.  max_new is at least every sequence's number
+ * of new tokens (it shapes the launch; what out holds for tokens beyond it is anything).  Lengths beyond the
+ * max_pages * page_size places of a table count as that, page numbers outside the cache as a page of it.  What
+ * lies in the cache beyond kv_len has no effect, nor have infinities and NaN in V on tokens that do not see them; for those that do, what is not
+ * finite adds up to the result (weights are above zero, however small).  out must not overlap q.
  * One launch, or two where long sequences are split for want of rows: then d_work (device, 16-byte aligned, at least
  * ecspmv_attention_workspace bytes, contents of no matter before and after) is used; it may be NULL where 0 bytes are
  * asked for.  The result has the same bits every time. */
