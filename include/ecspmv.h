@@ -275,6 +275,37 @@ int ecspmv_kv_write(const ecspmv_kv_cache_t *cache, const ecspmv_view_t *k, cons
 int ecspmv_kv_read(const ecspmv_kv_cache_t *cache, const int64_t *d_slots, int64_t tokens, const ecspmv_view_t *k,
                    const ecspmv_view_t *v, void *stream);
 
+/* The same writing with the tokens' positions in it: of each head's first rotary_dim values of k (and of q) the pairs (a, b) become
+ *   (a cos t - b sin t, a sin t + b cos t),   t = position[token] * frequency[pair],
+ * pair i being values i and i + rotary_dim / 2, or with `neighbours` values 2 i and 2 i + 1.  The angle is worked out in 64 bits, the
+ * rotation in 32; what comes of it is rounded once, to FP16 or to a code (in 8 and 4 bits what is beyond FP16's largest value counts as
+ * that).  Values go as they are; queries go to q_out, which may be q itself and overlaps nothing otherwise, also those of tokens that
+ * d_slots leaves out.  rotary_dim: even, at most head_dim, 0 for no rotation; q_heads: 0 for no queries.  One launch (none for no tokens). */
+typedef struct ecspmv_rotary_t {
+    uint32_t struct_size;                   /* sizeof(ecspmv_rotary_t) as the caller compiled it */
+    int32_t  rotary_dim, neighbours;        /* neighbours: 0 or 1 */
+    int32_t  q_heads;
+    const double  *frequency;               /* device, rotary_dim / 2, radians a position */
+    const int32_t *position;                /* device, one per token */
+    ecspmv_view_t q, q_out;
+} ecspmv_rotary_t;
+int ecspmv_kv_append(const ecspmv_kv_cache_t *cache, const ecspmv_view_t *k, const ecspmv_view_t *v, const int64_t *d_slots, int64_t tokens,
+                     const ecspmv_rotary_t *rotary, void *stream);
+
+/* The rows of accepted nodes (ecspmv_verify_tree) to where they follow one another: key first[b] + path[b][i] of sequence b becomes its key
+ * first[b] + i, for i < accepted[b], in `count` caches (host array of pointers; the layers of a model, alike but for their memory) of the same
+ * page table.  All device int32: first (batch; the key of node 0), path (`nodes` to a row, rows path_stride apart), accepted (batch; counts
+ * beyond 0 ... nodes as these), page_table (max_pages to a row, rows table_stride apart).  path[b][i] >= i, as it is on a path whose nodes
+ * come after their parents; a row with a smaller one, or whose place or new place is in no page of the cache, stays where it is.
+ * One launch per 64 caches (none for no sequences, nodes, pages or caches). */
+typedef struct ecspmv_keep_t {
+    uint32_t struct_size;                   /* sizeof(ecspmv_keep_t) as the caller compiled it */
+    int32_t  batch, nodes, max_pages;
+    int64_t  path_stride, table_stride;     /* >= nodes, >= max_pages */
+    const int32_t *first, *path, *accepted, *page_table;
+} ecspmv_keep_t;
+int ecspmv_kv_keep(const ecspmv_kv_cache_t *const *caches, int32_t count, const ecspmv_keep_t *a, void *stream);
+
 /* Attention of the new tokens of `batch` sequences over a cache that already holds their keys and values (ecspmv_kv_write).
  * Sequence b has the tokens q_start[b] ... q_start[b + 1] - 1 of q and out (device int32, batch + 1 entries, not decreasing)
  * and kv_len[b] keys in all (device int32), the new tokens' own last; its key i is in page page_table[b * table_stride +
@@ -307,6 +338,13 @@ int ecspmv_attention_workspace(const ecspmv_kv_cache_t *cache, const ecspmv_atte
 int ecspmv_attention_workspace_most(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *a, size_t *bytes);
 int ecspmv_attention(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *a, void *d_work, size_t work_bytes, void *stream);
 
+/* The same for new tokens that are the nodes of a tree, or see one another in any other way: token t sees every key before the first new one,
+ * and the i-th new token of its sequence, itself among them, where bit i % 32 of word i / 32 of its row of d_seen is set (device uint32, a row
+ * for each token of q, rows seen_stride >= ceil(min(max_new, tokens) / 32) apart; bits of new tokens that there are none of count for
+ * nothing).  Where kv_len is less than the number of new tokens, the first ones have no keys.  Workspaces are the same. */
+int ecspmv_attention_tree(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *a, const uint32_t *d_seen, int64_t seen_stride, void *d_work,
+                          size_t work_bytes, void *stream);
+
 /* The check of drafted tokens.  Sequence b has drafted[b][0 ... count[b] - 1] (device int32, `drafts` to a row; count: device
  * int32, NULL for `drafts` each), target probabilities target[b][i][token] (device FP32, drafts + 1 rows of `vocab`), the
  * drafts' own draft[b][i][token] (device FP32, `drafts` rows; NULL where a draft was certain, probability 1) and random
@@ -328,6 +366,30 @@ typedef struct ecspmv_verify_t {
 /* Two launches.  d_work: device, 8-byte aligned, at least ecspmv_verify_workspace bytes, contents of no matter before and after. */
 int ecspmv_verify_workspace(const ecspmv_verify_t *a, size_t *bytes);
 int ecspmv_verify(const ecspmv_verify_t *a, void *d_work, size_t work_bytes, void *stream);
+
+/* The check of a tree of drafted tokens.  Sequence b has the nodes 0 ... count[b] - 1 (device int32; NULL for `nodes` each), tokens drafted[b][i],
+ * below parent[b][i] < i, or below the token before the tree with -1 (both device int32, `nodes` to a row), target probabilities
+ * target[b][0][token] after the token before the tree and target[b][i + 1][token] after node i (device FP32, nodes + 1 rows of `vocab`), and
+ * random numbers uniform[b][0 ... nodes] in [0, 1) (device FP32).  From the token before the tree on, the children of where the walk stands
+ * are asked in the order of their numbers: child i is accepted, and the walk goes on there, where
+ *   uniform[i] * S < p(x_i),   S = 1 - (p of the children refused before it),   p = target after where the walk stands
+ * and where none is left, the next token is the first v at which the running sum of w passes uniform[nodes] * sum(w), where w is p
+ * without the refused tokens (p itself where that leaves nothing).  All of it in 64 bits.  So every token has the target's probability,
+ * however the tree was made; a tree without branches gives what ecspmv_verify gives without draft probabilities.  accepted[b] = n;
+ * path[b][0 ... nodes - 1] (device int32) = the accepted nodes, then -1; tokens[b][0 ... nodes] = their tokens, the next token, then -1 (also in the
+ * next token's place if p has nothing above 0).  A node whose token was refused at the same place already is not asked.  A drafted token
+ * outside [0, vocab) is refused and takes nothing from S; a node whose parent is none before it is not reached. */
+typedef struct ecspmv_verify_tree_t {
+    uint32_t struct_size;                   /* sizeof(ecspmv_verify_tree_t) as the caller compiled it */
+    int32_t  batch, nodes, vocab;           /* nodes in [0, 1024]; vocab in [1, 2^20] */
+    const float *target, *uniform;
+    int64_t  target_seq, target_row;        /* strides in elements from one sequence, resp. row, to the next */
+    const int32_t *drafted, *parent, *count;
+    int32_t *tokens, *path, *accepted;
+} ecspmv_verify_tree_t;
+/* Two launches.  d_work: device, 8-byte aligned, at least ecspmv_verify_tree_workspace bytes, contents of no matter before and after. */
+int ecspmv_verify_tree_workspace(const ecspmv_verify_tree_t *a, size_t *bytes);
+int ecspmv_verify_tree(const ecspmv_verify_tree_t *a, void *d_work, size_t work_bytes, void *stream);
 
 /* ---- comparison: plain CSR (int32 column index + FP16 value per entry, one wavefront per row) ------- */
 /* The CSR-32 format the paper's Section 8.2 measures storage against, with a kernel of its own (not one of the

@@ -29,6 +29,7 @@ EXPORTS = (
     "ecspmv_kv_write", "ecspmv_kv_read", "ecspmv_attention_workspace", "ecspmv_attention_workspace_most",
     "ecspmv_attention",
     "ecspmv_verify_workspace", "ecspmv_verify",
+    "ecspmv_kv_append", "ecspmv_kv_keep", "ecspmv_attention_tree", "ecspmv_verify_tree_workspace", "ecspmv_verify_tree",
     "ecspmv_csr_run", "ecspmv_stream_read", "ecspmv_stream_read_sliced", "ecspmv_empty_launch", "ecspmv_strerror", "ecspmv_last_hip_error",
 )
 
@@ -87,6 +88,22 @@ class VerifyDesc(Structure):
                 ("draft_row", c_int64), ("drafted", c_void_p), ("count", c_void_p), ("tokens", c_void_p), ("accepted", c_void_p)]
 
 
+class RotaryDesc(Structure):
+    _fields_ = [("struct_size", c_uint32), ("rotary_dim", c_int32), ("neighbours", c_int32), ("q_heads", c_int32), ("frequency", c_void_p),
+                ("position", c_void_p), ("q", View), ("q_out", View)]
+
+
+class KeepDesc(Structure):
+    _fields_ = [("struct_size", c_uint32), ("batch", c_int32), ("nodes", c_int32), ("max_pages", c_int32), ("path_stride", c_int64),
+                ("table_stride", c_int64), ("first", c_void_p), ("path", c_void_p), ("accepted", c_void_p), ("page_table", c_void_p)]
+
+
+class VerifyTreeDesc(Structure):
+    _fields_ = [("struct_size", c_uint32), ("batch", c_int32), ("nodes", c_int32), ("vocab", c_int32), ("target", c_void_p),
+                ("uniform", c_void_p), ("target_seq", c_int64), ("target_row", c_int64), ("drafted", c_void_p), ("parent", c_void_p),
+                ("count", c_void_p), ("tokens", c_void_p), ("path", c_void_p), ("accepted", c_void_p)]
+
+
 class EcspmvError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -137,6 +154,11 @@ def lib() -> ctypes.CDLL:
     L.ecspmv_attention.argtypes = [POINTER(KvCacheDesc), POINTER(AttentionDesc), c_void_p, c_size_t, c_void_p]
     L.ecspmv_verify_workspace.argtypes = [POINTER(VerifyDesc), POINTER(c_size_t)]
     L.ecspmv_verify.argtypes = [POINTER(VerifyDesc), c_void_p, c_size_t, c_void_p]
+    L.ecspmv_kv_append.argtypes = [POINTER(KvCacheDesc), POINTER(View), POINTER(View), c_void_p, c_int64, POINTER(RotaryDesc), c_void_p]
+    L.ecspmv_kv_keep.argtypes = [POINTER(POINTER(KvCacheDesc)), c_int32, POINTER(KeepDesc), c_void_p]
+    L.ecspmv_attention_tree.argtypes = [POINTER(KvCacheDesc), POINTER(AttentionDesc), c_void_p, c_int64, c_void_p, c_size_t, c_void_p]
+    L.ecspmv_verify_tree_workspace.argtypes = [POINTER(VerifyTreeDesc), POINTER(c_size_t)]
+    L.ecspmv_verify_tree.argtypes = [POINTER(VerifyTreeDesc), c_void_p, c_size_t, c_void_p]
     L.ecspmv_csr_build_dense.argtypes = [c_void_p, c_int64, c_int64, c_int64, POINTER(c_void_p)]
     L.ecspmv_csr_destroy.argtypes = [c_void_p]
     L.ecspmv_csr_destroy.restype = None
@@ -447,3 +469,40 @@ def ecspmv_verify(a: VerifyDesc, d_work: int, work_bytes: int, stream: int = 0) 
     status = (_lib or lib()).ecspmv_verify(a, _plain(d_work), work_bytes, _plain(stream))
     if status:
         raise EcspmvError(status, "ecspmv_verify")
+
+
+def ecspmv_kv_append(cache: KvCacheDesc, k: View, v: View, d_slots: int, tokens: int, rotary: RotaryDesc, stream: int = 0) -> None:
+    status = (_lib or lib()).ecspmv_kv_append(cache, k, v, _plain(d_slots), tokens, rotary, _plain(stream))
+    if status:
+        raise EcspmvError(status, "ecspmv_kv_append")
+
+
+def cache_array(caches):
+    """The caches of ecspmv_kv_keep: an array of pointers to their descriptions (which it keeps alive)."""
+    return (POINTER(KvCacheDesc) * len(caches))(*[ctypes.pointer(c) for c in caches])
+
+
+def ecspmv_kv_keep(caches, a: KeepDesc, stream: int = 0) -> None:
+    """caches: a cache_array."""
+    status = (_lib or lib()).ecspmv_kv_keep(caches, len(caches), a, _plain(stream))
+    if status:
+        raise EcspmvError(status, "ecspmv_kv_keep")
+
+
+def ecspmv_attention_tree(cache: KvCacheDesc, a: AttentionDesc, d_seen: int, seen_stride: int, d_work: int = 0, work_bytes: int = 0,
+                          stream: int = 0) -> None:
+    status = (_lib or lib()).ecspmv_attention_tree(cache, a, _plain(d_seen), seen_stride, _plain(d_work), work_bytes, _plain(stream))
+    if status:
+        raise EcspmvError(status, "ecspmv_attention_tree")
+
+
+def ecspmv_verify_tree_workspace(a: VerifyTreeDesc) -> int:
+    n = c_size_t(0)
+    _check(lib().ecspmv_verify_tree_workspace(a, byref(n)), "ecspmv_verify_tree_workspace")
+    return int(n.value)
+
+
+def ecspmv_verify_tree(a: VerifyTreeDesc, d_work: int, work_bytes: int, stream: int = 0) -> None:
+    status = (_lib or lib()).ecspmv_verify_tree(a, _plain(d_work), work_bytes, _plain(stream))
+    if status:
+        raise EcspmvError(status, "ecspmv_verify_tree")

@@ -10,8 +10,10 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libecspmv.so")
 TRACE_LIB = os.path.join(PKG, "libecspmv_trace.so")     # the same sources with clock stamps compiled in (timeline.py)
-SOURCES = ["api.cpp", "encoder.cpp", "kernels.hip", "epilogue.hip", "serve.cpp", "kv_cache.hip", "attention.hip", "verify.hip"]
-HEADERS = ["encoder.h", "launch.h", "ecspmv_format.h", "kernel_handle.h", "serve.h", "status.h", os.path.join("..", "..", "include", "ecspmv.h")]
+SOURCES = ["api.cpp", "encoder.cpp", "kernels.hip", "epilogue.hip", "serve.cpp", "kv_cache.hip", "kv_append.hip",
+           "kv_keep.hip", "attention.hip", "attention_tree.hip", "verify.hip", "verify_tree.hip"]
+HEADERS = ["encoder.h", "launch.h", "ecspmv_format.h", "kernel_handle.h", "serve.h", "status.h", "kv_rows.h", "verify_tiles.h",
+           os.path.join("..", "..", "include", "ecspmv.h")]
 
 
 def lib_path() -> str:

@@ -4,6 +4,10 @@
 // head r % group of the group.  A row sees the keys up to its own place, p = kv_len - new + token:
 //   o_r = sum_{j <= p} exp(t_j - m) v_j / sum_{j <= p} exp(t_j - m),   t_j = scale * q_r . k_j,   m = max t_j
 // in one pass over the keys: m and both sums are carried along, and what was added up under an older m is scaled by exp(m_old - m_new).
+//
+// With ECS_TREE the new tokens are the nodes of a tree: a row sees every key before the first of them, and of the new ones those whose bits
+// are set in its token's words (from there on the sum is over j that are seen).  The kernels are the same but for what is hidden in tiles that
+// new tokens reach into.
 #include <hip/hip_runtime.h>
 #include <hip/hip_fp16.h>
 #include <stdint.h>
@@ -16,6 +20,14 @@
 namespace {
 
 using ecs::AttentionArgs;
+
+#ifdef ECS_TREE
+constexpr bool kTree = true;
+#else
+constexpr bool kTree = false;
+#endif
+template <bool TREE>
+using ArgsOf = std::conditional_t<TREE, ecs::AttentionTreeArgs, AttentionArgs>;
 
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef _Float16 half8v __attribute__((ext_vector_type(8)));
@@ -173,6 +185,18 @@ struct Sequence {
     int32_t behind;                       // keys before the first new token (negative: the first tokens see nothing)
 };
 
+// Which of 32 keys a token of a tree sees: bit i is key `key0` + i, of `end` keys in all, the first new one of them `behind`
+__device__ __forceinline__ uint32_t seen_bits(const uint32_t *words, uint32_t count, uint32_t key0, int32_t behind, uint32_t end)
+{
+    const int32_t first = (int32_t)key0 - behind;                  // the new token that is key0 (negative: keys before the tree)
+    const uint32_t at = (uint32_t)max(first, 0) >> 5;
+    const uint64_t pair = (uint64_t)(at + 1u < count ? words[at + 1u] : 0u) << 32 | (at < count ? words[at] : 0u);
+    const uint32_t before = (uint32_t)min(max(-first, 0), 32);
+    const uint32_t bits = first >= 0 ? (uint32_t)(pair >> (first & 31)) : (uint32_t)(pair << before | ((1ull << before) - 1u));
+    const uint32_t left = end > key0 ? end - key0 : 0u;
+    return left < 32u ? bits & ((1u << left) - 1u) : bits;
+}
+
 // The page of a key, a number that is one whatever the table holds
 __device__ __forceinline__ uint32_t page_of(const AttentionArgs &a, const int32_t *table, uint32_t key)
 {
@@ -191,8 +215,8 @@ __device__ __forceinline__ uint32_t page_of(const AttentionArgs &a, const int32_
 // the join after the last, some 15 us together: one token over 200 keys, 12 heads of 64, 4.8 us; 16 sequences of up to 8192 keys, 8 heads
 // of 128 in 8 bits, 144 MB, 40 us; 8 tokens over 32768 keys, 40 heads of 128 in FP16, 671 MB, 126 us, 5.3 TB/s.  16 rows because that is
 // the least that a matrix instruction takes; four wavefronts on keys of their own need no barrier before the end.
-template <int BITS, int DP, bool PAD>
-__global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) : DP > 128 ? 1 : 2) void attention_rows_kernel(const AttentionArgs a)
+template <int BITS, int DP, bool PAD, bool TREE>
+__global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) : DP > 128 ? 1 : 2) void attention_rows_kernel(const ArgsOf<TREE> a)
 {
     constexpr int kSteps = DP / 32, VD = DP / 16;
     constexpr int KB = BITS == 16 ? 8 : BITS == 8 || PAD || DP == 64 ? 16 : 32;       // neighbouring values of a key in a lane
@@ -215,9 +239,11 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) :
     const uint32_t row = min(row0 + j, rows - 1u), token = row / a.group;
     const int32_t seen = min(s.behind + (int32_t)token + 1, (int32_t)s.len);             // keys that this row sees
     const uint32_t last_row = min(row0 + 15u, rows - 1u);
-    const int32_t end_i = min(s.behind + (int32_t)(last_row / a.group) + 1, (int32_t)s.len);
+    const int32_t end_i = TREE ? (int32_t)s.len : min(s.behind + (int32_t)(last_row / a.group) + 1, (int32_t)s.len);
     const uint32_t end = end_i > 0 ? (uint32_t)end_i : 0u;
-    const int32_t all_see = s.behind + (int32_t)(row0 / a.group) + 1;                    // keys that every row sees
+    const int32_t all_see = TREE ? s.behind : s.behind + (int32_t)(row0 / a.group) + 1;  // keys that every row sees
+    const uint32_t *words = nullptr;
+    if constexpr (TREE) words = a.seen + (int64_t)(s.first + token) * a.seen_stride;
 
     const uint32_t tiles = (end + 31u) >> 5, per = (tiles + a.splits - 1u) / a.splits;
     const uint32_t t0 = min(split * per, tiles), t1 = min(t0 + per, tiles);
@@ -346,10 +372,20 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) :
         __builtin_amdgcn_sched_barrier(0);
         const bool some_hidden = (int32_t)(key0 + 32u) > all_see || key0 + 32u > end;
         if (some_hidden) {
+            if constexpr (TREE) {
+                const uint32_t bits = seen_bits(words, a.seen_words, key0, s.behind, end) >> (4u * g);
 #pragma unroll
-            for (int r = 0; r < 8; ++r) {
-                const int32_t key = (int32_t)(key0 + (r < 4 ? 0u : 16u) + 4u * g + (r & 3));
-                if (key >= seen) w[r] = kNone;
+                for (int r = 0; r < 8; ++r)
+                    if (!(bits >> ((r < 4 ? 0 : 16) + (r & 3)) & 1u)) {
+                        w[r] = kNone;
+                        if constexpr (BITS < 16) vs[r] = 0u;       // (a node that was left out may have a step that is none)
+                    }
+            } else {
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    const int32_t key = (int32_t)(key0 + (r < 4 ? 0u : 16u) + 4u * g + (r & 3));
+                    if (key >= seen) w[r] = kNone;
+                }
             }
         }
         float most = kNone, step[8];
@@ -434,7 +470,11 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) :
             for (uint32_t t = t0 + wave; t < t1; t += 4u)
 #pragma unroll 1
                 for (uint32_t key = 32u * t; key < min(32u * t + 32u, end); ++key) {
-                    if ((int32_t)key >= seen) continue;
+                    if constexpr (TREE) {
+                        if (!(seen_bits(words, a.seen_words, key, s.behind, end) & 1u)) continue;
+                    } else {
+                        if ((int32_t)key >= seen) continue;
+                    }
                     const uint64_t at = (uint64_t)page_of(a, s.table, key) * page_rows + head_rows + (key & page_mask);
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
@@ -555,8 +595,8 @@ __device__ __forceinline__ uint4 code_values(const Raw<BITS> &r)
     }
 }
 
-template <int BITS, int DP>
-__global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(const AttentionArgs a)
+template <int BITS, int DP, bool TREE>
+__global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(const ArgsOf<TREE> a)
 {
     constexpr int RC = DP <= 32 ? 4 : DP <= 64 ? 8 : DP <= 128 ? 16 : 32;              // 16-byte pieces of a row in LDS
     constexpr int KT = RC == 32 ? 32 : 64, kHalves = KT / 32, kSteps = DP / 16, kTiles = DP / 32;
@@ -585,11 +625,14 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
 
     const uint32_t row = min(row0 + 32u * wave + n, rows - 1u), token = row / a.group;
     const int32_t seen = min(s.behind + (int32_t)token + 1, (int32_t)s.len);
-    auto sees = [&](uint32_t r) -> int32_t {                                           // keys that row r sees
-        return max(min(s.behind + (int32_t)(min(r, rows - 1u) / a.group) + 1, (int32_t)s.len), 0);
+    auto sees = [&](uint32_t r) -> int32_t {                                           // keys up to the last one that row r sees
+        return TREE ? (int32_t)s.len : max(min(s.behind + (int32_t)(min(r, rows - 1u) / a.group) + 1, (int32_t)s.len), 0);
     };
-    const uint32_t end = (uint32_t)sees(row0 + 127u), all_see = (uint32_t)sees(row0);  // of the workgroup
+    const uint32_t end = (uint32_t)sees(row0 + 127u);                                  // of the workgroup
+    const uint32_t all_see = TREE ? (uint32_t)max(s.behind, 0) : (uint32_t)sees(row0);
     const uint32_t wave_end = row0 + 32u * wave < rows ? (uint32_t)sees(row0 + 32u * wave + 31u) : 0u;
+    const uint32_t *words = nullptr;
+    if constexpr (TREE) words = a.seen + (int64_t)(s.first + token) * a.seen_stride;
 
     half8v q[kSteps];
     float q_sum = 0.0f;
@@ -717,6 +760,8 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
                 }
             }
             const bool in = key0 + (lane & 15u) < end;
+            if constexpr (TREE)                                    // (a node that was left out may have a step that is none)
+                if (!(BITS == 8 ? finite(__uint_as_float(raw_step)) : half_finite(raw_step) && half_finite(raw_step >> 16))) raw_step = 0u;
             const float step = !in ? 0.0f : BITS == 8 ? __uint_as_float(raw_step) : step_of(raw_step);
             const float low = !in || BITS == 8 ? 0.0f : low_of(raw_step);
             if (lane < 32u) {
@@ -803,7 +848,16 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
                 }
             }
         }
-        if (masked) {
+        if (TREE && masked) {
+            if constexpr (TREE)
+#pragma unroll
+                for (int x = 0; x < kHalves; ++x) {
+                    const uint32_t bits = seen_bits(words, a.seen_words, key0 + 32u * x, s.behind, end) >> (4u * h);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (!(bits >> (8 * (i / 4) + (i & 3)) & 1u)) w[16 * x + i] = kNone;
+                }
+        } else if (masked) {
             int32_t left = seen - (int32_t)(key0 + 4u * h);
             asm volatile("" : "+v"(left));                         // (kept a branch: few tiles take it)
 #pragma unroll
@@ -916,7 +970,11 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
             const uint32_t last = min(t1 * KT, end);
 #pragma unroll 1
             for (uint32_t key = t0 * KT; key < last; ++key) {
-                if ((int32_t)key >= seen) continue;
+                if constexpr (TREE) {
+                    if (!(seen_bits(words, a.seen_words, key, s.behind, end) & 1u)) continue;
+                } else {
+                    if ((int32_t)key >= seen) continue;
+                }
                 const uint64_t at = (uint64_t)page_of(a, s.table, key) * page_rows + head_rows + (key & page_mask);
                 const uint16_t *vp = reinterpret_cast<const uint16_t *>(a.cache.v + at * a.cache.row_bytes);
 #pragma unroll
@@ -970,6 +1028,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
     }
 }
 
+#ifndef ECS_TREE
 // ---- joining the splits ----------------------------------------------------------------------------------------------------------------
 //
 // For each (token, head) the parts of its splits, each taken to the largest of their maxima:
@@ -1076,39 +1135,41 @@ __global__ __launch_bounds__(256) void attention_join_rows_kernel(const Attentio
     }
 }
 
+#endif  // ECS_TREE
+
 template <int BITS>
-int launch_rows(const AttentionArgs &a, void *stream)
+int launch_rows(const ArgsOf<kTree> &a, void *stream)
 {
     const uint32_t gx = a.row_tiles * a.splits, gy = a.cache.heads, gz = a.batch;
     switch (a.cache.dim) {
-    case 64: return ecs::launch_args<attention_rows_kernel<BITS, 64, false>>(a, gx, gy, gz, 256, stream);
-    case 128: return ecs::launch_args<attention_rows_kernel<BITS, 128, false>>(a, gx, gy, gz, 256, stream);
-    case 256: return ecs::launch_args<attention_rows_kernel<BITS, 256, false>>(a, gx, gy, gz, 256, stream);
+    case 64: return ecs::launch_args<attention_rows_kernel<BITS, 64, false, kTree>>(a, gx, gy, gz, 256, stream);
+    case 128: return ecs::launch_args<attention_rows_kernel<BITS, 128, false, kTree>>(a, gx, gy, gz, 256, stream);
+    case 256: return ecs::launch_args<attention_rows_kernel<BITS, 256, false, kTree>>(a, gx, gy, gz, 256, stream);
     default: break;
     }
-    if (a.cache.dim < 64) return ecs::launch_args<attention_rows_kernel<BITS, 64, true>>(a, gx, gy, gz, 256, stream);
-    if (a.cache.dim < 128) return ecs::launch_args<attention_rows_kernel<BITS, 128, true>>(a, gx, gy, gz, 256, stream);
-    return ecs::launch_args<attention_rows_kernel<BITS, 256, true>>(a, gx, gy, gz, 256, stream);
+    if (a.cache.dim < 64) return ecs::launch_args<attention_rows_kernel<BITS, 64, true, kTree>>(a, gx, gy, gz, 256, stream);
+    if (a.cache.dim < 128) return ecs::launch_args<attention_rows_kernel<BITS, 128, true, kTree>>(a, gx, gy, gz, 256, stream);
+    return ecs::launch_args<attention_rows_kernel<BITS, 256, true, kTree>>(a, gx, gy, gz, 256, stream);
 }
 
 template <int BITS>
-int launch_chunk(const AttentionArgs &a, void *stream)
+int launch_chunk(const ArgsOf<kTree> &a, void *stream)
 {
     const uint32_t gx = a.cache.heads, gy = a.row_tiles * a.splits, gz = a.batch;
     switch ((a.cache.dim + 31u) / 32u) {
-    case 1: return ecs::launch_args<attention_chunk_kernel<BITS, 32>>(a, gx, gy, gz, 256, stream);
-    case 2: return ecs::launch_args<attention_chunk_kernel<BITS, 64>>(a, gx, gy, gz, 256, stream);
-    case 3: return ecs::launch_args<attention_chunk_kernel<BITS, 96>>(a, gx, gy, gz, 256, stream);
-    case 4: return ecs::launch_args<attention_chunk_kernel<BITS, 128>>(a, gx, gy, gz, 256, stream);
-    case 5: return ecs::launch_args<attention_chunk_kernel<BITS, 160>>(a, gx, gy, gz, 256, stream);
-    case 6: return ecs::launch_args<attention_chunk_kernel<BITS, 192>>(a, gx, gy, gz, 256, stream);
-    case 7: return ecs::launch_args<attention_chunk_kernel<BITS, 224>>(a, gx, gy, gz, 256, stream);
-    default: return ecs::launch_args<attention_chunk_kernel<BITS, 256>>(a, gx, gy, gz, 256, stream);
+    case 1: return ecs::launch_args<attention_chunk_kernel<BITS, 32, kTree>>(a, gx, gy, gz, 256, stream);
+    case 2: return ecs::launch_args<attention_chunk_kernel<BITS, 64, kTree>>(a, gx, gy, gz, 256, stream);
+    case 3: return ecs::launch_args<attention_chunk_kernel<BITS, 96, kTree>>(a, gx, gy, gz, 256, stream);
+    case 4: return ecs::launch_args<attention_chunk_kernel<BITS, 128, kTree>>(a, gx, gy, gz, 256, stream);
+    case 5: return ecs::launch_args<attention_chunk_kernel<BITS, 160, kTree>>(a, gx, gy, gz, 256, stream);
+    case 6: return ecs::launch_args<attention_chunk_kernel<BITS, 192, kTree>>(a, gx, gy, gz, 256, stream);
+    case 7: return ecs::launch_args<attention_chunk_kernel<BITS, 224, kTree>>(a, gx, gy, gz, 256, stream);
+    default: return ecs::launch_args<attention_chunk_kernel<BITS, 256, kTree>>(a, gx, gy, gz, 256, stream);
     }
 }
 
 template <int BITS>
-int launch_bits(const AttentionArgs &a, void *stream)
+int launch_bits(const ArgsOf<kTree> &a, void *stream)
 {
     return a.chunk ? launch_chunk<BITS>(a, stream) : launch_rows<BITS>(a, stream);
 }
@@ -1117,6 +1178,7 @@ int launch_bits(const AttentionArgs &a, void *stream)
 
 namespace ecs {
 
+#ifndef ECS_TREE
 // Rows of a workgroup, and how many workgroups are wanted, in the kernel for few rows and in the one whose rows share keys in LDS
 constexpr uint32_t kFewRows = 16, kFewWanted = 1024, kChunkRows = 128, kChunkWanted = 512;
 // (token, head) rows per head of the cache up to which the kernel for few rows takes a call (figures at plan_attention)
@@ -1165,10 +1227,8 @@ uint64_t most_attention_work(uint32_t batch, uint32_t kv_heads, uint32_t group, 
     return std::min(most, by_keys * rows) * (dim + 2u) * sizeof(float);
 }
 
-int launch_attention(const AttentionArgs &a, void *stream)
+int launch_attention_join(const AttentionArgs &a, void *stream)
 {
-    const int e = a.cache.bits == 16 ? launch_bits<16>(a, stream) : a.cache.bits == 8 ? launch_bits<8>(a, stream) : launch_bits<4>(a, stream);
-    if (e || a.splits == 1u) return e;
     // (us by a workgroup / by some lanes for each row: 320 rows of 25 splits 129 / 134, 1024 of 8 46.2 / 46.0; four bits, 1000 tokens of 32
     // heads, two splits, by a wavefront 95, by 32 lanes 86)
     const uint32_t rows = a.tokens * a.q_heads;
@@ -1176,6 +1236,15 @@ int launch_attention(const AttentionArgs &a, void *stream)
     if (a.cache.dim <= 64u) return launch_args<attention_join_rows_kernel<16>>(a, (rows + 15u) / 16u, 1, 1, 256, stream);
     if (a.cache.dim <= 128u) return launch_args<attention_join_rows_kernel<32>>(a, (rows + 7u) / 8u, 1, 1, 256, stream);
     return launch_args<attention_join_rows_kernel<64>>(a, (rows + 3u) / 4u, 1, 1, 256, stream);
+}
+
+int launch_attention(const AttentionArgs &a, void *stream)
+#else
+int launch_attention_tree(const AttentionTreeArgs &a, void *stream)
+#endif
+{
+    const int e = a.cache.bits == 16 ? launch_bits<16>(a, stream) : a.cache.bits == 8 ? launch_bits<8>(a, stream) : launch_bits<4>(a, stream);
+    return e || a.splits == 1u ? e : launch_attention_join(a, stream);
 }
 
 }  // namespace ecs

@@ -37,9 +37,9 @@ static int kernel_handle(void *stream, hipFunction_t *f)
     return 0;
 }
 
-// one launch of a kernel whose only parameter is an Args, handed over as it lies in memory; LDS is the kernel's own
+// one launch of a kernel whose only parameter is an Args, handed over as it lies in memory; lds: beside what the kernel has of its own
 template <auto KERNEL, class Args>
-static int launch_args(const Args &args, uint32_t gx, uint32_t gy, uint32_t gz, uint32_t threads, void *stream)
+static int launch_args(const Args &args, uint32_t gx, uint32_t gy, uint32_t gz, uint32_t threads, void *stream, uint32_t lds = 0)
 {
     hipFunction_t f = nullptr;
     const int e = kernel_handle<KERNEL>(stream, &f);
@@ -49,7 +49,7 @@ static int launch_args(const Args &args, uint32_t gx, uint32_t gy, uint32_t gz, 
     }
     size_t bytes = sizeof(Args);
     void *extra[] = {HIP_LAUNCH_PARAM_BUFFER_POINTER, const_cast<Args *>(&args), HIP_LAUNCH_PARAM_BUFFER_SIZE, &bytes, HIP_LAUNCH_PARAM_END};
-    const hipError_t s = hipModuleLaunchKernel(f, gx, gy, gz, threads, 1, 1, 0, (hipStream_t)stream, nullptr, extra);
+    const hipError_t s = hipModuleLaunchKernel(f, gx, gy, gz, threads, 1, 1, lds, (hipStream_t)stream, nullptr, extra);
     if (s != hipSuccess) (void)hipGetLastError();
     return (int)s;
 }

@@ -1,5 +1,5 @@
 // C ABI around the products (see include/ecspmv.h): argument checks of the cache, the attention over it and the check of drafted
-// tokens.  Nothing here allocates or can throw.
+// tokens, in a row and in trees.  Nothing here allocates or can throw.
 #include <cstdint>
 #include <cstring>
 
@@ -56,6 +56,13 @@ int check_view(const ecspmv_view_t *from, ecs::View &v, uint32_t &wide)
     return ECSPMV_OK;
 }
 
+// The lanes that share a row, and the neighbouring tokens of a head that follow one another
+void spread_rows(uint32_t dim, uint32_t tokens, uint32_t &lanes_shift, uint32_t &run_shift)
+{
+    while ((8u << lanes_shift) < dim) ++lanes_shift;
+    while ((1u << run_shift) < tokens && run_shift < 4u) ++run_shift;
+}
+
 int kv_call(const ecspmv_kv_cache_t *cache, const ecspmv_view_t *k, const ecspmv_view_t *v, const int64_t *d_slots, int64_t tokens,
             void *stream, int (*launch)(const ecs::KvArgs &, void *))
 {
@@ -70,8 +77,7 @@ int kv_call(const ecspmv_kv_cache_t *cache, const ecspmv_view_t *k, const ecspmv
     if (tokens > 0x7fffffff || ((uint64_t)tokens + 16u) * a.cache.heads > 0x7fffffffu) return ECSPMV_ERR_UNSUPPORTED;
     a.slots = d_slots;
     a.tokens = (uint32_t)tokens;
-    while ((8u << a.lanes_shift) < a.cache.dim) ++a.lanes_shift;
-    while ((1u << a.run_shift) < a.tokens && a.run_shift < 4u) ++a.run_shift;
+    spread_rows(a.cache.dim, a.tokens, a.lanes_shift, a.run_shift);
     return ecs::hip_status(launch(a, stream));
 }
 
@@ -100,12 +106,46 @@ int check_attention(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *fr
     return ECSPMV_OK;
 }
 
+// What both attentions look at before they launch; `nothing`: there is nothing to compute
+int prepare_attention(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *a, void *d_work, size_t work_bytes, ecs::AttentionArgs &args,
+                      bool &nothing)
+{
+    ecs::AttentionPlan plan;
+    ecspmv_attention_t t;
+    int s = check_attention(cache, a, args, plan, t);
+    if (s) return s;
+    nothing = args.tokens == 0 || args.batch == 0 || args.max_new == 0;
+    if (nothing) return ECSPMV_OK;
+    if ((s = check_view(&t.q, args.q, args.q_wide)) || (s = check_view(&t.out, args.out, args.out_wide))) return s;
+    if (!t.q_start || !t.kv_len || !aligned(t.q_start, 4) || !aligned(t.kv_len, 4)) return ECSPMV_ERR_INVALID;
+    if (args.max_pages && (!t.page_table || !aligned(t.page_table, 4) || t.table_stride < t.max_pages)) return ECSPMV_ERR_INVALID;
+    if (plan.work_bytes && (!d_work || !aligned(d_work, 16))) return ECSPMV_ERR_INVALID;
+    if (work_bytes < plan.work_bytes) return ECSPMV_ERR_TOO_SMALL;
+    args.q_start = t.q_start;
+    args.kv_len = t.kv_len;
+    args.table = t.page_table;
+    args.table_stride = t.table_stride;
+    args.part_o = static_cast<float *>(d_work);
+    args.part_ml = args.part_o + (uint64_t)plan.splits * args.tokens * args.q_heads * args.cache.dim;
+    args.scale_log2 = t.scale * 1.44269504088896340736f;
+    return ECSPMV_OK;
+}
+
 int check_verify(const ecspmv_verify_t *from, ecspmv_verify_t &t)
 {
     const int s = copy_struct(from, t);
     if (s) return s;
     if (t.batch < 0 || t.drafts < 0 || t.vocab < 1) return ECSPMV_ERR_INVALID;
     if (t.batch > 65535 || t.vocab > 1 << 20 || t.drafts > 1 << 20) return ECSPMV_ERR_UNSUPPORTED;
+    return ECSPMV_OK;
+}
+
+int check_verify_tree(const ecspmv_verify_tree_t *from, ecspmv_verify_tree_t &t)
+{
+    const int s = copy_struct(from, t);
+    if (s) return s;
+    if (t.batch < 0 || t.nodes < 0 || t.vocab < 1) return ECSPMV_ERR_INVALID;
+    if (t.batch > 65535 || t.vocab > 1 << 20 || t.nodes > (int32_t)ecs::kMostNodes) return ECSPMV_ERR_UNSUPPORTED;
     return ECSPMV_OK;
 }
 
@@ -123,6 +163,80 @@ int ecspmv_kv_read(const ecspmv_kv_cache_t *cache, const int64_t *d_slots, int64
                    const ecspmv_view_t *v, void *stream)
 {
     return kv_call(cache, k, v, d_slots, tokens, stream, ecs::launch_kv_read);
+}
+
+int ecspmv_kv_append(const ecspmv_kv_cache_t *cache, const ecspmv_view_t *k, const ecspmv_view_t *v, const int64_t *d_slots, int64_t tokens,
+                     const ecspmv_rotary_t *rotary, void *stream)
+{
+    ecs::AppendArgs a;
+    std::memset(&a, 0, sizeof(a));
+    ecspmv_rotary_t t;
+    int s = check_cache(cache, a.cache);
+    if (s || (s = copy_struct(rotary, t))) return s;
+    if (t.rotary_dim < 0 || t.rotary_dim % 2 || t.rotary_dim > (int32_t)a.cache.dim || t.q_heads < 0 || tokens < 0) return ECSPMV_ERR_INVALID;
+    if (t.neighbours != 0 && t.neighbours != 1) return ECSPMV_ERR_UNSUPPORTED;
+    if (tokens == 0) return ECSPMV_OK;
+    if ((s = check_view(k, a.k, a.k_wide)) || (s = check_view(v, a.v, a.v_wide))) return s;
+    if (t.q_heads && ((s = check_view(&t.q, a.q, a.q_wide)) || (s = check_view(&t.q_out, a.q_out, a.q_out_wide)))) return s;
+    if (!d_slots || !aligned(d_slots, 8)) return ECSPMV_ERR_INVALID;
+    if (t.rotary_dim && (!t.frequency || !aligned(t.frequency, 8) || !t.position || !aligned(t.position, 4))) return ECSPMV_ERR_INVALID;
+    if (tokens > 1 << 27 || t.q_heads > 65535 || ((uint64_t)tokens + 16u) * (2u * a.cache.heads + (uint32_t)t.q_heads) > 0x7fffffffu)
+        return ECSPMV_ERR_UNSUPPORTED;
+    a.slots = d_slots;
+    a.position = t.position;
+    a.frequency = t.frequency;
+    a.tokens = (uint32_t)tokens;
+    a.q_heads = (uint32_t)t.q_heads;
+    a.pairs = (uint32_t)t.rotary_dim / 2u;
+    a.neighbours = (uint32_t)t.neighbours;
+    spread_rows(a.cache.dim, a.tokens, a.lanes_shift, a.run_shift);
+    return ecs::hip_status(ecs::launch_kv_append(a, stream));
+}
+
+int ecspmv_kv_keep(const ecspmv_kv_cache_t *const *caches, int32_t count, const ecspmv_keep_t *from, void *stream)
+{
+    ecspmv_keep_t t;
+    int s = copy_struct(from, t);
+    if (s) return s;
+    if (count < 0 || t.batch < 0 || t.nodes < 0 || t.max_pages < 0 || (count && !caches)) return ECSPMV_ERR_INVALID;
+    if (t.batch > 65535) return ECSPMV_ERR_UNSUPPORTED;
+    ecs::KeepArgs a;
+    std::memset(&a, 0, sizeof(a));
+    ecs::Cache all, one;
+    for (int32_t i = 0; i < count; ++i) {                                  // every one of them before anything is launched
+        if ((s = check_cache(caches[i], one))) return s;
+        if (i == 0) all = one;
+        if (one.pages != all.pages || one.heads != all.heads || one.page_shift != all.page_shift || one.dim != all.dim || one.bits != all.bits)
+            return ECSPMV_ERR_INVALID;
+    }
+    if (count == 0 || t.batch == 0 || t.nodes == 0 || t.max_pages == 0) return ECSPMV_OK;
+    if ((uint64_t)t.max_pages << all.page_shift > 0x7fffffffu) return ECSPMV_ERR_UNSUPPORTED;
+    const void *needed[] = {t.first, t.path, t.accepted, t.page_table};
+    for (const void *p : needed)
+        if (!p || !aligned(p, 4)) return ECSPMV_ERR_INVALID;
+    if (t.table_stride < t.max_pages || t.path_stride < t.nodes) return ECSPMV_ERR_INVALID;
+    a.first = t.first;
+    a.path = t.path;
+    a.accepted = t.accepted;
+    a.table = t.page_table;
+    a.path_stride = t.path_stride;
+    a.table_stride = t.table_stride;
+    a.nodes = (uint32_t)t.nodes;
+    a.max_pages = (uint32_t)t.max_pages;
+    a.pages = all.pages;
+    a.heads = all.heads;
+    a.page_shift = all.page_shift;
+    a.row_bytes = all.row_bytes;
+    a.steps = all.bits != 16u;
+    for (int32_t i = 0; i < count;) {
+        uint32_t layers = 0;
+        for (; i < count && layers < ecs::kKeepLayers; ++i, ++layers) {
+            if ((s = check_cache(caches[i], one))) return s;
+            a.layer[layers] = {one.k, one.v, one.k_step, one.v_step};
+        }
+        if ((s = ecs::hip_status(ecs::launch_kv_keep(a, layers, (uint32_t)t.batch, stream)))) return s;
+    }
+    return ECSPMV_OK;
 }
 
 int ecspmv_attention_workspace(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *a, size_t *bytes)
@@ -154,24 +268,24 @@ int ecspmv_attention_workspace_most(const ecspmv_kv_cache_t *cache, const ecspmv
 int ecspmv_attention(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *a, void *d_work, size_t work_bytes, void *stream)
 {
     ecs::AttentionArgs args;
-    ecs::AttentionPlan plan;
-    ecspmv_attention_t t;
-    int s = check_attention(cache, a, args, plan, t);
-    if (s) return s;
-    if (args.tokens == 0 || args.batch == 0 || args.max_new == 0) return ECSPMV_OK;          // nothing to compute
-    if ((s = check_view(&t.q, args.q, args.q_wide)) || (s = check_view(&t.out, args.out, args.out_wide))) return s;
-    if (!t.q_start || !t.kv_len || !aligned(t.q_start, 4) || !aligned(t.kv_len, 4)) return ECSPMV_ERR_INVALID;
-    if (args.max_pages && (!t.page_table || !aligned(t.page_table, 4) || t.table_stride < t.max_pages)) return ECSPMV_ERR_INVALID;
-    if (plan.work_bytes && (!d_work || !aligned(d_work, 16))) return ECSPMV_ERR_INVALID;
-    if (work_bytes < plan.work_bytes) return ECSPMV_ERR_TOO_SMALL;
-    args.q_start = t.q_start;
-    args.kv_len = t.kv_len;
-    args.table = t.page_table;
-    args.table_stride = t.table_stride;
-    args.part_o = static_cast<float *>(d_work);
-    args.part_ml = args.part_o + (uint64_t)plan.splits * args.tokens * args.q_heads * args.cache.dim;
-    args.scale_log2 = t.scale * 1.44269504088896340736f;
-    return ecs::hip_status(ecs::launch_attention(args, stream));
+    bool nothing;
+    const int s = prepare_attention(cache, a, d_work, work_bytes, args, nothing);
+    return s || nothing ? s : ecs::hip_status(ecs::launch_attention(args, stream));
+}
+
+int ecspmv_attention_tree(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *a, const uint32_t *d_seen, int64_t seen_stride, void *d_work,
+                          size_t work_bytes, void *stream)
+{
+    ecs::AttentionTreeArgs args;
+    std::memset(&args, 0, sizeof(args));
+    bool nothing;
+    const int s = prepare_attention(cache, a, d_work, work_bytes, args, nothing);
+    if (s || nothing) return s;
+    args.seen = d_seen;
+    args.seen_stride = seen_stride;
+    args.seen_words = (args.max_new + 31u) / 32u;
+    if (!d_seen || !aligned(d_seen, 4) || seen_stride < (int64_t)args.seen_words) return ECSPMV_ERR_INVALID;
+    return ecs::hip_status(ecs::launch_attention_tree(args, stream));
 }
 
 int ecspmv_verify_workspace(const ecspmv_verify_t *from, size_t *bytes)
@@ -213,6 +327,46 @@ int ecspmv_verify(const ecspmv_verify_t *from, void *d_work, size_t work_bytes, 
     a.vocab = (uint32_t)t.vocab;
     a.sums = static_cast<double *>(d_work);
     return ecs::hip_status(ecs::launch_verify(a, (uint32_t)t.batch, stream));
+}
+
+int ecspmv_verify_tree_workspace(const ecspmv_verify_tree_t *from, size_t *bytes)
+{
+    ecspmv_verify_tree_t t;
+    const int s = check_verify_tree(from, t);
+    if (s) return s;
+    if (!bytes) return ECSPMV_ERR_INVALID;
+    *bytes = (size_t)ecs::verify_tree_work_bytes((uint32_t)t.batch, (uint32_t)t.vocab);
+    return ECSPMV_OK;
+}
+
+int ecspmv_verify_tree(const ecspmv_verify_tree_t *from, void *d_work, size_t work_bytes, void *stream)
+{
+    ecspmv_verify_tree_t t;
+    const int s = check_verify_tree(from, t);
+    if (s) return s;
+    if (t.batch == 0) return ECSPMV_OK;
+    if (!d_work || !aligned(d_work, 8)) return ECSPMV_ERR_INVALID;
+    if (work_bytes < ecs::verify_tree_work_bytes((uint32_t)t.batch, (uint32_t)t.vocab)) return ECSPMV_ERR_TOO_SMALL;
+    if (!t.target || !t.uniform || !t.tokens || !t.accepted || (t.nodes && (!t.drafted || !t.parent || !t.path))) return ECSPMV_ERR_INVALID;
+    const void *all[] = {t.target, t.uniform, t.drafted, t.parent, t.count, t.tokens, t.path, t.accepted};
+    for (const void *p : all)
+        if (!aligned(p, 4)) return ECSPMV_ERR_INVALID;
+    ecs::VerifyTreeArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.target = t.target;
+    a.uniform = t.uniform;
+    a.drafted = t.drafted;
+    a.parent = t.parent;
+    a.count = t.count;
+    a.tokens = t.tokens;
+    a.path = t.path;
+    a.accepted = t.accepted;
+    a.target_seq = t.target_seq;
+    a.target_row = t.target_row;
+    a.nodes = (uint32_t)t.nodes;
+    a.vocab = (uint32_t)t.vocab;
+    a.sums = static_cast<double *>(d_work);
+    return ecs::hip_status(ecs::launch_verify_tree(a, (uint32_t)t.batch, stream));
 }
 
 }  // extern "C"

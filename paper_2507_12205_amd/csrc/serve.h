@@ -32,6 +32,32 @@ struct KvArgs {
 int launch_kv_write(const KvArgs &a, void *stream);
 int launch_kv_read(const KvArgs &a, void *stream);
 
+struct AppendArgs {
+    Cache cache;
+    View q, q_out, k, v;
+    const int64_t *slots;
+    const int32_t *position;
+    const double *frequency;              // of each pair
+    uint32_t tokens, q_heads, pairs, neighbours;
+    uint32_t lanes_shift, run_shift;      // as in KvArgs
+    uint32_t heads_per_block;             // heads of q, k and v, one after the other, that a workgroup takes
+    uint32_t q_wide, q_out_wide, k_wide, v_wide;
+};
+int launch_kv_append(AppendArgs &a, void *stream);                         // (chooses heads_per_block)
+
+constexpr uint32_t kKeepLayers = 64;      // of a launch
+struct KeepArgs {
+    struct Tensors {
+        uint8_t *k, *v, *k_step, *v_step;
+    } layer[kKeepLayers];
+    const int32_t *first, *path, *accepted, *table;
+    int64_t path_stride, table_stride;
+    uint32_t nodes, max_pages;
+    uint32_t pages, heads, page_shift, row_bytes;
+    uint32_t steps, blocks;               // whether rows have steps; workgroups to the keys or values of a layer
+};
+int launch_kv_keep(KeepArgs &a, uint32_t layers, uint32_t batch, void *stream);
+
 struct AttentionArgs {
     Cache cache;
     View q, out;
@@ -54,6 +80,14 @@ AttentionPlan plan_attention(uint32_t batch, uint32_t kv_heads, uint32_t group, 
 uint64_t most_attention_work(uint32_t batch, uint32_t kv_heads, uint32_t group, uint32_t dim, uint32_t bits, uint64_t tokens, uint32_t max_new,
                              uint64_t max_kv);
 int launch_attention(const AttentionArgs &a, void *stream);
+int launch_attention_join(const AttentionArgs &a, void *stream);          // of the splits' results
+
+struct AttentionTreeArgs : AttentionArgs {
+    const uint32_t *seen;                 // bit i of a token's words: it sees its sequence's i-th new token
+    int64_t seen_stride;                  // words from one token to the next
+    uint32_t seen_words, pad_;            // words that count
+};
+int launch_attention_tree(const AttentionTreeArgs &a, void *stream);
 
 struct VerifyArgs {
     const float *target, *draft, *uniform;
@@ -65,6 +99,18 @@ struct VerifyArgs {
 };
 uint64_t verify_work_bytes(uint32_t batch, uint32_t vocab);
 int launch_verify(const VerifyArgs &a, uint32_t batch, void *stream);
+
+constexpr uint32_t kMostNodes = 1024;
+struct VerifyTreeArgs {
+    const float *target, *uniform;
+    const int32_t *drafted, *parent, *count;
+    int32_t *tokens, *path, *accepted;
+    int64_t target_seq, target_row;       // strides in elements
+    uint32_t nodes, vocab;
+    double *sums;                         // verify_tree_work_bytes
+};
+uint64_t verify_tree_work_bytes(uint32_t batch, uint32_t vocab);
+int launch_verify_tree(const VerifyTreeArgs &a, uint32_t batch, void *stream);
 
 }  // namespace ecs
 #endif

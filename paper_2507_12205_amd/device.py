@@ -3,6 +3,7 @@ from __future__ import annotations
 
 from ctypes import sizeof
 
+import numpy as np
 import torch
 from torch import _C
 
@@ -90,6 +91,7 @@ def csr_run(csr: B.CsrMatrix, x: torch.Tensor, y: torch.Tensor, stream=None) -> 
 # ---- around the products ---------------------------------------------------------------------------------
 
 _VIEW, _KV_CACHE, _ATTENTION, _VERIFY = (sizeof(t) for t in (B.View, B.KvCacheDesc, B.AttentionDesc, B.VerifyDesc))
+_ROTARY, _KEEP, _VERIFY_TREE = (sizeof(t) for t in (B.RotaryDesc, B.KeepDesc, B.VerifyTreeDesc))
 
 
 class KvCache:
@@ -160,11 +162,80 @@ def kv_read(cache: KvCache, slots: torch.Tensor, k: torch.Tensor, v: torch.Tenso
     return k, v
 
 
+def kv_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, position: torch.Tensor, frequency: torch.Tensor,
+              q: torch.Tensor = None, q_out: torch.Tensor = None, neighbours: bool = False, stream=None):
+    """kv_write() of keys that are rotated by their tokens' positions, (tokens,) int32, on the way; queries q, (tokens, q_heads, head_dim) FP16 with
+    any strides, are rotated into q_out (q itself if not given), which is returned.  frequency: (pairs,) FP64 radians a position (rotary_frequency());
+    pair i of a head is its values i and i + pairs, or with `neighbours` values 2 i and 2 i + 1; the values beyond 2 * pairs stay as they are."""
+    _rows_of(cache, k, v, slots)
+    pairs, = frequency.shape
+    assert position.dtype is torch.int32 and position.shape == slots.shape and position.is_contiguous() and position.get_device() == cache.device
+    assert frequency.dtype is torch.float64 and frequency.is_contiguous() and frequency.get_device() == cache.device
+    r = B.RotaryDesc(_ROTARY, 2 * pairs, 1 if neighbours else 0, 0, frequency.data_ptr() or None, position.data_ptr() or None)
+    if q is None:
+        assert q_out is None
+    else:
+        if q_out is None:
+            q_out = q
+        assert q.dtype is q_out.dtype is torch.float16 and q.get_device() == q_out.get_device() == cache.device
+        assert q.dim() == 3 and q.shape == q_out.shape and q.shape[0] == slots.shape[0] and q.shape[2] == cache.head_dim
+        r.q_heads, r.q, r.q_out = q.shape[1], _view(q), _view(q_out)
+    B.ecspmv_kv_append(cache.desc, _view(k), _view(v), slots.data_ptr(), slots.shape[0], r, _stream_handle(stream))
+    return q_out
+
+
+def rotary_frequency(pairs: int, base: float = 10000.0, device="cuda:0") -> torch.Tensor:
+    """base ** (-i / pairs), for kv_append()."""
+    return base ** (-torch.arange(pairs, dtype=torch.float64, device=device) / pairs)
+
+
+class KvCaches:
+    """The caches of a model's layers, alike but for their memory, for kv_keep()."""
+
+    def __init__(self, caches):
+        self.caches = list(caches)
+        assert self.caches and all((c.bits, c.pages, c.heads, c.page_size, c.head_dim, c.device) == self._shape() for c in self.caches)
+        self.device, self.descs = self.caches[0].device, B.cache_array([c.desc for c in self.caches])
+
+    def _shape(self):
+        c = self.caches[0]
+        return c.bits, c.pages, c.heads, c.page_size, c.head_dim, c.device
+
+
+def kv_keep(caches: KvCaches, first: torch.Tensor, path: torch.Tensor, accepted: torch.Tensor, page_table: torch.Tensor, stream=None) -> None:
+    """The rows of accepted nodes to where they follow one another, in all caches: key first[b] + path[b, i] of sequence b becomes its key
+    first[b] + i for i < accepted[b].  first: (batch,), the key of node 0; path: (batch, nodes) and accepted: (batch,) as verify_tree() leaves
+    them; page_table as in attention(); all int32."""
+    batch, nodes = path.shape
+    pages = page_table.shape[1]
+    assert first.dtype is path.dtype is accepted.dtype is page_table.dtype is torch.int32
+    assert first.get_device() == path.get_device() == accepted.get_device() == page_table.get_device() == caches.device
+    assert first.shape == accepted.shape == (batch,) and page_table.shape[0] == batch and first.is_contiguous() and accepted.is_contiguous()
+    assert (nodes <= 1 or path.stride(1) == 1) and (batch <= 1 or path.stride(0) >= nodes)
+    assert (pages <= 1 or page_table.stride(1) == 1) and (batch <= 1 or page_table.stride(0) >= pages)
+    a = B.KeepDesc(_KEEP, batch, nodes, pages, path.stride(0) if batch > 1 else nodes, page_table.stride(0) if batch > 1 else pages,
+                   first.data_ptr(), path.data_ptr(), accepted.data_ptr(), page_table.data_ptr())
+    B.ecspmv_kv_keep(caches.descs, a, _stream_handle(stream))
+
+
 def attention_workspace(cache: KvCache, q: torch.Tensor, batch: int, max_new: int, max_kv: int) -> torch.Tensor:
     """A workspace for attention() calls of up to these sizes: q's heads and no more tokens than it has (no more than batch * max_new if they
     are fewer), sequences, new tokens of one, places in their page tables."""
     a = B.AttentionDesc(_ATTENTION, q.shape[1], q.shape[0], batch, -(-max_kv // cache.page_size), max_new)
     return torch.empty(B.ecspmv_attention_workspace_most(cache.desc, a), dtype=torch.uint8, device=q.device)
+
+
+def _attention_of(cache: KvCache, q: torch.Tensor, out: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, page_table: torch.Tensor,
+                  max_new: int, scale) -> B.AttentionDesc:
+    assert q.dtype is out.dtype is torch.float16 and q.shape == out.shape and q.shape[2] == cache.head_dim
+    assert q.get_device() == out.get_device() == q_start.get_device() == kv_len.get_device() == page_table.get_device() == cache.device
+    assert q_start.dtype is kv_len.dtype is page_table.dtype is torch.int32
+    batch, pages = page_table.shape
+    assert kv_len.shape == (batch,) and q_start.shape == (batch + 1,) and q_start.is_contiguous() and kv_len.is_contiguous()
+    assert (pages <= 1 or page_table.stride(1) == 1) and (batch <= 1 or page_table.stride(0) >= pages)          # no expand()ed rows
+    tokens, heads, _ = q.shape
+    return B.AttentionDesc(_ATTENTION, heads, tokens, batch, pages, max_new, cache.head_dim ** -0.5 if scale is None else scale,
+                           page_table.stride(0) if batch > 1 else pages, q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), _view(q), _view(out))
 
 
 def attention(cache: KvCache, q: torch.Tensor, out: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, page_table: torch.Tensor,
@@ -173,20 +244,46 @@ def attention(cache: KvCache, q: torch.Tensor, out: torch.Tensor, q_start: torch
     keys and values: sequence b has q[q_start[b]:q_start[b + 1]] and kv_len[b] keys in all, in the pages page_table[b] (all int32; rows of
     the table that do not overlap).
     max_new: the most new tokens of a sequence; scale: 1 / sqrt(head_dim) if not given."""
-    assert q.dtype is out.dtype is torch.float16 and q.shape == out.shape and q.shape[2] == cache.head_dim
-    assert q.get_device() == out.get_device() == q_start.get_device() == kv_len.get_device() == page_table.get_device() == cache.device
-    assert q_start.dtype is kv_len.dtype is page_table.dtype is torch.int32
-    batch, pages = page_table.shape
-    assert kv_len.shape == (batch,) and q_start.shape == (batch + 1,) and q_start.is_contiguous() and kv_len.is_contiguous()
-    assert (pages <= 1 or page_table.stride(1) == 1) and (batch <= 1 or page_table.stride(0) >= pages)          # no expand()ed rows
-    tokens, heads, _ = q.shape
-    a = B.AttentionDesc(_ATTENTION, heads, tokens, batch, pages, max_new, cache.head_dim ** -0.5 if scale is None else scale,
-                        page_table.stride(0) if batch > 1 else pages, q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), _view(q), _view(out))
+    a = _attention_of(cache, q, out, q_start, kv_len, page_table, max_new, scale)
     if workspace is None:
         workspace = _workspace(B.ecspmv_attention_workspace(cache.desc, a), q, stream)
     assert workspace.get_device() == cache.device and workspace.is_contiguous()
     B.ecspmv_attention(cache.desc, a, workspace.data_ptr(), workspace.nbytes, _stream_handle(stream))
     return out
+
+
+def attention_tree(cache: KvCache, q: torch.Tensor, out: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, page_table: torch.Tensor,
+                   seen: torch.Tensor, max_new: int, scale: float = None, workspace: torch.Tensor = None, stream=None) -> torch.Tensor:
+    """attention() of new tokens that are the nodes of a tree: each sees every key before the first new token of its sequence, and of the new tokens
+    those whose bits are set in its row of seen, (tokens, words) int32 with 32 of them to a word, the first in the lowest bit (tree_seen()).
+    words: no fewer than max_new / 32 (or, if there are fewer tokens than max_new, than those)."""
+    a = _attention_of(cache, q, out, q_start, kv_len, page_table, max_new, scale)
+    tokens, words = seen.shape
+    assert seen.dtype is torch.int32 and seen.get_device() == cache.device and tokens == q.shape[0] and 32 * words >= min(max_new, tokens)
+    assert (words <= 1 or seen.stride(1) == 1) and (tokens <= 1 or seen.stride(0) >= words)
+    if workspace is None:
+        workspace = _workspace(B.ecspmv_attention_workspace(cache.desc, a), q, stream)
+    assert workspace.get_device() == cache.device and workspace.is_contiguous()
+    B.ecspmv_attention_tree(cache.desc, a, seen.data_ptr(), seen.stride(0) if tokens > 1 else words, workspace.data_ptr(), workspace.nbytes,
+                            _stream_handle(stream))
+    return out
+
+
+def tree_seen(parents, device="cuda:0") -> torch.Tensor:
+    """The bits of attention_tree() of new tokens each of which sees itself and what its parent sees.  parents: a list for each sequence, of the number
+    of each token's parent among the sequence's new tokens (less than its own; -1: none).  Worked out on the host."""
+    count = sum(len(p) for p in parents)
+    words = max([1] + [-(-len(p) // 32) for p in parents])
+    seen, at = np.zeros((count, words), np.uint32), 0
+    for of in parents:
+        for i, p in enumerate(of):
+            if not -1 <= p < i:
+                raise ValueError(f"token {i} has the parent {p}")
+            if p >= 0:
+                seen[at + i] = seen[at + p]
+            seen[at + i, i // 32] |= np.uint32(1 << i % 32)
+        at += len(of)
+    return torch.from_numpy(seen.view(np.int32)).to(device)
 
 
 def verify_workspace(batch: int, vocab: int) -> int:
@@ -222,3 +319,36 @@ def verify(target: torch.Tensor, draft, drafted: torch.Tensor, uniform: torch.Te
     assert workspace.get_device() == device and workspace.is_contiguous()
     B.ecspmv_verify(a, workspace.data_ptr(), workspace.nbytes, _stream_handle(stream))
     return tokens, accepted
+
+
+def verify_tree_workspace(batch: int, vocab: int) -> int:
+    """Bytes of a workspace for verify_tree() calls of this size."""
+    return B.ecspmv_verify_tree_workspace(B.VerifyTreeDesc(_VERIFY_TREE, batch, 0, vocab))
+
+
+def verify_tree(target: torch.Tensor, drafted: torch.Tensor, parent: torch.Tensor, uniform: torch.Tensor, tokens: torch.Tensor, path: torch.Tensor,
+                accepted: torch.Tensor, count: torch.Tensor = None, workspace: torch.Tensor = None, stream=None):
+    """Which path of a tree of drafted tokens stands, and the token after it.  target: (batch, nodes + 1, vocab) probabilities, after the token before
+    the tree and after each node, uniform: (batch, nodes + 1) random numbers in [0, 1), all FP32; drafted: (batch, nodes) and parent: (batch, nodes)
+    int32, -1 for the token before the tree; count: (batch,) int32, how many nodes there are (None: all).  tokens: (batch, nodes + 1), path: (batch,
+    nodes), accepted: (batch,) int32.  workspace: of verify_tree_workspace(), or allocated here."""
+    batch, rows, vocab = target.shape
+    nodes = rows - 1
+    assert target.dtype is uniform.dtype is torch.float32
+    assert drafted.dtype is parent.dtype is tokens.dtype is path.dtype is accepted.dtype is torch.int32
+    device = target.get_device()
+    assert device >= 0 and device == uniform.get_device() == drafted.get_device() == parent.get_device()
+    assert device == tokens.get_device() == path.get_device() == accepted.get_device()
+    assert uniform.shape == tokens.shape == (batch, rows) and drafted.shape == parent.shape == path.shape == (batch, nodes) and accepted.shape == (batch,)
+    assert uniform.is_contiguous() and tokens.is_contiguous() and drafted.is_contiguous() and parent.is_contiguous()
+    assert path.is_contiguous() and accepted.is_contiguous() and (target.numel() == 0 or vocab == 1 or target.stride(2) == 1)
+    a = B.VerifyTreeDesc(_VERIFY_TREE, batch, nodes, vocab, target.data_ptr(), uniform.data_ptr(), target.stride(0), target.stride(1),
+                         drafted.data_ptr() or None, parent.data_ptr() or None, None, tokens.data_ptr(), path.data_ptr() or None, accepted.data_ptr())
+    if count is not None:
+        assert count.dtype is torch.int32 and count.shape == (batch,) and count.is_contiguous() and count.get_device() == device
+        a.count = count.data_ptr()
+    if workspace is None:
+        workspace = _workspace(verify_tree_workspace(batch, vocab), target, stream)
+    assert workspace.get_device() == device and workspace.is_contiguous()
+    B.ecspmv_verify_tree(a, workspace.data_ptr(), workspace.nbytes, _stream_handle(stream))
+    return tokens, path, accepted

@@ -1,0 +1,255 @@
+"""Attention of the nodes of trees over the paged cache against 64 bits: trees and other masks of what new tokens see of one another, what lies in
+places that a token does not see, rows that see nothing.  The bound is that of test_gpu_attention."""
+import numpy as np
+import pytest
+import tree_reference as tree
+import serve_reference as ref
+from test_gpu_attention import make, place, values
+
+pytestmark = pytest.mark.gpu
+
+
+def trees(rng, new):
+    return [tree.tree_seen(tree.parents(rng, n)) for n in new]
+
+
+def words_of(seen, extra=0, rng=None):
+    """The rows of all sequences, `extra` words beyond the widest (and bits of new tokens that there are none of) of any content."""
+    words = max([1] + [-(-s.shape[0] // 32) for s in seen]) + extra
+    out = np.zeros((sum(s.shape[0] for s in seen), words), np.uint32)
+    at = 0
+    for s in seen:
+        n = s.shape[0]
+        if rng is not None:
+            wild = rng.random((n, 32 * words)) < 0.5
+            wild[:, :n] = s
+            s = wild
+        out[at:at + n, :max(1, -(-s.shape[1] // 32))] = tree.pack(s).view(np.uint32)[:n] if n else 0
+        at += n
+    return out.view(np.int32)
+
+
+def run(torch, D, cache, q, start, total, table, words, layout="tokens", scale=None, workspace="own", max_new=None):
+    out = place(torch.full_like(q, float("nan")), layout, torch)
+    args = [torch.from_numpy(np.ascontiguousarray(x)).cuda() for x in (start, total, table, words)]
+    most = int(np.diff(start).max()) if max_new is None else max_new
+    ws = D.attention_workspace(cache, q, len(total), most, table.shape[1] * cache.page_size) if workspace == "own" else workspace
+    if ws is not None and ws.numel():
+        ws.fill_(255)
+    D.attention_tree(cache, place(q, layout, torch), out, *args, most, scale, ws)
+    torch.cuda.synchronize()
+    return out.cpu().numpy().astype(np.float64)
+
+
+def check(got, made, seen, scale=None):
+    cache, q, start, total, table = made
+    k, v = values(cache)
+    want, size = tree.attention(q.cpu().numpy().astype(np.float64), k, v, start, total, table, seen, cache.head_dim ** -0.5 if scale is None else scale)
+    assert np.isfinite(got).all()
+    top = max((np.abs(ref.gather(v, table[b], n)).max() for b, n in enumerate(total) if n), default=0.0)
+    bound = 2 ** -11 * np.abs(want) + (2 ** -11 + 2 ** -14) * (size + (top if cache.bits == 4 else 0.0)) + max(total) * 2 ** -24 * top + 2 ** -25
+    worst = np.max(np.abs(got - want) / bound) if got.size else 0.0
+    assert worst <= 1.0, worst
+
+
+CASES = [
+    # new tokens and keys of each sequence, heads, heads of the cache, dim, page
+    ([1], [1], 1, 1, 16, 16), ([2], [2], 4, 2, 64, 16), ([8], [8], 4, 4, 64, 16), ([16], [300], 12, 12, 64, 16), ([33], [2049], 8, 1, 128, 64),
+    ([8], [1000], 4, 4, 128, 32), ([3, 1, 7, 2], [3, 17, 260, 513], 8, 2, 128, 16), ([17, 40], [17, 333], 6, 2, 80, 32),
+    ([130], [130], 2, 1, 96, 16), ([65, 1, 33], [700, 1, 33], 4, 4, 64, 128), ([5], [4100], 2, 2, 256, 256), ([200], [456], 3, 3, 128, 64),
+    ([31, 32], [100, 63], 16, 1, 240, 16), ([70], [71], 5, 5, 48, 1024), ([64], [1025], 2, 2, 128, 16), ([300], [999], 4, 1, 64, 32),
+]
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("case", CASES)
+def test_trees(case, bits):
+    import torch
+    from paper_2507_12205_amd import device as D
+    rng = np.random.default_rng(CASES.index(case))
+    made = make(torch, D, *case, bits, seed=CASES.index(case), stale=float("nan"))
+    seen = trees(rng, case[0])
+    check(run(torch, D, *made, words_of(seen)), made, seen)
+    check(run(torch, D, *made, words_of(seen, 2, rng)), made, seen)          # words and bits beyond the new tokens: anything
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("new,total", [([7, 40], [300, 45]), ([150, 3], [1150, 3])])
+def test_any_mask(new, total, bits):
+    """Later tokens too, not itself, everything, nothing."""
+    import torch
+    from paper_2507_12205_amd import device as D
+    rng = np.random.default_rng(new[0])
+    made = make(torch, D, new, total, 8, 4, 128, 32, bits, seed=3, stale=float("nan"))
+    for share in (0.0, 0.1, 0.7, 1.0):
+        seen = [rng.random((n, n)) < share for n in new]
+        got = run(torch, D, *made, words_of(seen))
+        check(got, made, seen)
+        if share == 0.0 and total[1] == new[1]:
+            assert not got[new[0]:].any()
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("layout", ["columns", "odd", "heads"])
+@pytest.mark.parametrize("new,total", [([8], [300]), ([150, 3], [150, 90])])
+def test_layouts(layout, bits, new, total):
+    import torch
+    from paper_2507_12205_amd import device as D
+    made = make(torch, D, new, total, 8, 4, 128, 32, bits, seed=3, stale=float("inf"))
+    words = words_of(trees(np.random.default_rng(1), new))
+    assert np.array_equal(run(torch, D, *made, words, layout=layout), run(torch, D, *made, words))
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4])
+def test_rows_that_see_nothing(bits):
+    """More new tokens than keys (the first ones have none); sequences without tokens, and without keys; rows without a bit and without a past."""
+    import torch
+    from paper_2507_12205_amd import device as D
+    rng, new = np.random.default_rng(5), [5, 0, 2, 40, 20, 150]
+    made = make(torch, D, new, [3, 20, 0, 30, 20, 150], 4, 2, 64, 16, bits, seed=9, stale=float("nan"))
+    seen = trees(rng, new)
+    seen[4][3], seen[5][149] = False, False
+    got = run(torch, D, *made, words_of(seen))
+    assert not got[5:7].any() and not got[50].any() and not got[-1].any()
+    check(got, made, seen)
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("new,total", [(6, 70), (40, 200), (200, 330), (7, 3000)])
+def test_a_row_of_the_whole_past_only(new, total, bits):
+    """No new token seen: what attention gives of one new token before them."""
+    import torch
+    from paper_2507_12205_amd import device as D
+    made = make(torch, D, [new], [total], 4, 2, 128, 16, bits, seed=4, stale=float("nan"))
+    seen = [np.zeros((new, new), bool)]
+    check(run(torch, D, *made, words_of(seen)), made, seen)
+
+
+@pytest.mark.parametrize("new,total", [(6, 70), (40, 200), (200, 330), (6, 3000)])
+@pytest.mark.parametrize("odd", [float("nan"), float("inf")])
+def test_values_that_other_branches_see(new, total, odd):
+    """An infinity or NaN in a node's key or value stays with the nodes that see it."""
+    import torch
+    from paper_2507_12205_amd import device as D
+    cache, q, start, lens, table = made = make(torch, D, [new], [total], 4, 2, 128, 16, 16, seed=4)
+    seen = trees(np.random.default_rng(new), [new])
+    words = words_of(seen)
+    clean = run(torch, D, *made, words)
+    node = new // 2
+    at = total - new + node
+    page, off = int(table[0, at // 16]), at % 16
+    sees = seen[0][:, node]
+    assert sees.any() and not sees.all()
+    for tensor in (cache.v, cache.k):
+        keep = tensor[page, 1, off, 5].clone()
+        tensor[page, 1, off, 5] = odd
+        got = run(torch, D, *made, words)
+        assert np.array_equal(got[~sees], clean[~sees]) and np.array_equal(got[:, :2], clean[:, :2])
+        if tensor is cache.v:
+            rest = [d for d in range(128) if d != 5]
+            assert np.allclose(got[:, :, rest], clean[:, :, rest], rtol=2 ** -9, atol=2 ** -12)
+            assert not np.isfinite(got[sees][:, 2:, 5]).any()
+        else:
+            assert odd == float("inf") or not np.isfinite(got[sees][:, 2:]).any()
+        tensor[page, 1, off, 5] = keep
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("new,total", [(6, 70), (40, 200), (200, 330)])
+def test_nodes_that_were_left_out(new, total, bits):
+    """A node that nobody sees may have a row that was never written: steps of NaN, any codes."""
+    import torch
+    from paper_2507_12205_amd import device as D
+    cache, q, start, lens, table = made = make(torch, D, [new], [total], 4, 2, 128, 16, bits, seed=4)
+    seen = trees(np.random.default_rng(new), [new])
+    node = new // 2
+    seen[0][:, node] = False
+    words = words_of(seen)
+    clean = run(torch, D, *made, words)
+    check(clean, made, seen)
+    at = total - new + node
+    page, off = int(table[0, at // 16]), at % 16
+    for odd in (float("nan"), float("inf"), -60000.0):
+        for code, step in ((cache.k, cache.k_step), (cache.v, cache.v_step)):
+            code[page, :, off], step[page, :, off] = 77, odd
+        assert np.array_equal(run(torch, D, *made, words), clean)
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("new", [2, 100])
+@pytest.mark.parametrize("scale", [0.0, -0.25])
+def test_scales_of_zero_and_below(scale, new, bits):
+    import torch
+    from paper_2507_12205_amd import device as D
+    made = make(torch, D, [new, 1], [400, 1], 2, 2, 64, 16, bits, seed=13)
+    seen = trees(np.random.default_rng(2), [new, 1])
+    check(run(torch, D, *made, words_of(seen), scale=scale), made, seen, scale)
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("new,total", [([4, 1], [2500, 900]), ([50, 70], [2500, 900])])
+def test_the_same_bits_every_time(new, total, bits):
+    import torch
+    from paper_2507_12205_amd import device as D
+    made = make(torch, D, new, total, 8, 2, 128, 16, bits, seed=5)
+    words = words_of(trees(np.random.default_rng(2), new))
+    first = run(torch, D, *made, words)
+    for _ in range(3):
+        assert np.array_equal(run(torch, D, *made, words), first)
+    assert np.array_equal(run(torch, D, *made, words, workspace=None), first)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_tokens_beyond_max_new(bits):
+    """More tokens of a sequence than max_new: the first max_new are as they are, where they see none of the others (whose words there are none of)."""
+    import torch
+    from paper_2507_12205_amd import device as D
+    cache, q, start, total, table = made = make(torch, D, [40, 90], [200, 300], 4, 2, 64, 16, bits, seed=5)
+    seen = trees(np.random.default_rng(2), [40, 90])
+    full = run(torch, D, *made, words_of(seen))
+    short = run(torch, D, *made, np.ascontiguousarray(words_of(seen)[:, :2]), max_new=64)
+    k, v = values(cache)
+    assert np.isfinite(short[:40]).all() and np.abs(short[:104] - full[:104]).max() <= 2 ** -9 * np.abs(v).max()
+
+
+def test_tree_seen():
+    import torch
+    from paper_2507_12205_amd import device as D
+    rng = np.random.default_rng(3)
+    parents = [tree.parents(rng, n) for n in (1, 70, 33)]
+    assert np.array_equal(D.tree_seen(parents).cpu().numpy(), words_of([tree.tree_seen(p) for p in parents]))
+    assert D.tree_seen([]).shape == (0, 1)
+    with pytest.raises(ValueError):
+        D.tree_seen([[-1, 1]])
+    torch.cuda.synchronize()
+
+
+def test_in_a_graph_and_on_another_stream():
+    """Lengths and masks are read when the kernels run: a captured step goes on with what the tensors hold then."""
+    import torch
+    from paper_2507_12205_amd import device as D
+    for new, total in (([5], [600]), ([70], [600])):
+        made = cache, q, start, lens, table = make(torch, D, new, total, 4, 2, 64, 16, 8, seed=6)
+        s, n, t = (torch.from_numpy(x).cuda() for x in (start, lens, table))
+        words = torch.zeros((new[0], 3), dtype=torch.int32, device="cuda")
+        out, eager = torch.empty_like(q), torch.empty_like(q)
+        ws = D.attention_workspace(cache, q, 1, new[0], table.shape[1] * 16)
+        side = torch.cuda.Stream()
+        D.attention_tree(cache, q, out, s, n, t, words, new[0], None, ws)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            D.attention_tree(cache, q, out, s, n, t, words, new[0], None, ws)
+        for turn, length in enumerate((600, 599, 90, 70, 3, 0, 600)):
+            seen = trees(np.random.default_rng(turn), new)
+            w = words_of(seen)
+            words.zero_()
+            words[:, :w.shape[1]] = torch.from_numpy(w).cuda()
+            n.fill_(length)
+            out.fill_(float("nan"))
+            graph.replay()
+            torch.cuda.synchronize()
+            check(out.cpu().numpy().astype(np.float64), (cache, q, start, np.array([length], np.int32), table), seen)
+            D.attention_tree(cache, q, eager, s, n, t, words, new[0], None, None, stream=side)
+            side.synchronize()
+            assert torch.equal(eager, out)
