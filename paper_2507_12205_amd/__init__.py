@@ -11,5 +11,5 @@ from .binding import (  # noqa: F401
     ecspmv_run_batch, Batch,
     ecspmv_kv_write, ecspmv_kv_read, ecspmv_attention_workspace, ecspmv_attention_workspace_most, ecspmv_attention,
     ecspmv_verify_workspace, ecspmv_verify,
-    ecspmv_kv_append, ecspmv_kv_keep, ecspmv_attention_tree, ecspmv_verify_tree_workspace, ecspmv_verify_tree,
+    ecspmv_kv_append, ecspmv_kv_keep, ecspmv_attention_tree_workspace, ecspmv_attention_tree, ecspmv_verify_tree_workspace, ecspmv_verify_tree,
 )

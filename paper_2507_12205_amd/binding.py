@@ -29,7 +29,7 @@ EXPORTS = (
     "ecspmv_kv_write", "ecspmv_kv_read", "ecspmv_attention_workspace", "ecspmv_attention_workspace_most",
     "ecspmv_attention",
     "ecspmv_verify_workspace", "ecspmv_verify",
-    "ecspmv_kv_append", "ecspmv_kv_keep", "ecspmv_attention_tree", "ecspmv_verify_tree_workspace", "ecspmv_verify_tree",
+    "ecspmv_kv_append", "ecspmv_kv_keep", "ecspmv_attention_tree_workspace", "ecspmv_attention_tree", "ecspmv_verify_tree_workspace", "ecspmv_verify_tree",
     "ecspmv_csr_run", "ecspmv_stream_read", "ecspmv_stream_read_sliced", "ecspmv_empty_launch", "ecspmv_strerror", "ecspmv_last_hip_error",
 )
 
@@ -156,6 +156,7 @@ def lib() -> ctypes.CDLL:
     L.ecspmv_verify.argtypes = [POINTER(VerifyDesc), c_void_p, c_size_t, c_void_p]
     L.ecspmv_kv_append.argtypes = [POINTER(KvCacheDesc), POINTER(View), POINTER(View), c_void_p, c_int64, POINTER(RotaryDesc), c_void_p]
     L.ecspmv_kv_keep.argtypes = [POINTER(POINTER(KvCacheDesc)), c_int32, POINTER(KeepDesc), c_void_p]
+    L.ecspmv_attention_tree_workspace.argtypes = [POINTER(KvCacheDesc), POINTER(AttentionDesc), POINTER(c_size_t)]
     L.ecspmv_attention_tree.argtypes = [POINTER(KvCacheDesc), POINTER(AttentionDesc), c_void_p, c_int64, c_void_p, c_size_t, c_void_p]
     L.ecspmv_verify_tree_workspace.argtypes = [POINTER(VerifyTreeDesc), POINTER(c_size_t)]
     L.ecspmv_verify_tree.argtypes = [POINTER(VerifyTreeDesc), c_void_p, c_size_t, c_void_p]
@@ -487,6 +488,12 @@ def ecspmv_kv_keep(caches, a: KeepDesc, stream: int = 0) -> None:
     status = (_lib or lib()).ecspmv_kv_keep(caches, len(caches), a, _plain(stream))
     if status:
         raise EcspmvError(status, "ecspmv_kv_keep")
+
+
+def ecspmv_attention_tree_workspace(cache: KvCacheDesc, a: AttentionDesc) -> int:
+    n = c_size_t(0)
+    _check(lib().ecspmv_attention_tree_workspace(cache, a, byref(n)), "ecspmv_attention_tree_workspace")
+    return int(n.value)
 
 
 def ecspmv_attention_tree(cache: KvCacheDesc, a: AttentionDesc, d_seen: int, seen_stride: int, d_work: int = 0, work_bytes: int = 0,

@@ -197,6 +197,88 @@ __device__ __forceinline__ uint32_t seen_bits(const uint32_t *words, uint32_t co
     return left < 32u ? bits & ((1u << left) - 1u) : bits;
 }
 
+// ---- what a workgroup takes of several sequences' rows and keys -----------------------------------------------------------------------------
+//
+// For rows that all see all keys, the work of a sequence is (tiles of its rows) x (tiles of its keys).  Sequences differ in both, and the host
+// sees neither, so that the workgroups of a launch are dealt out here, by every one of them for itself: with each sequence's keys cut into
+// pieces of L tiles at most, L is the least length (but for a few steps of halving) at which all pieces find a workgroup.
+// (us by equal numbers of splits for all / by this: 16 trees of up to 16 nodes over up to 8192 keys, 64/8 heads of 128, 8 bits, 98.7 / @B; eight of up to
+// 49 over up to 2000, 32 heads of 80, 4 bits, 61 / @C.)
+// inclusive results over the lanes of an operation whose neutral element is all zeros
+template <class T, class F>
+__device__ __forceinline__ T lanes_scan(T v, F with)
+{
+    auto step = [&](auto from, auto rows) {
+        const int t = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(from)::value, decltype(rows)::value, 0xF, false);
+        v = with(v, __builtin_bit_cast(T, t));
+    };
+    typedef std::integral_constant<int, 0xF> all;
+    step(std::integral_constant<int, 0x111>(), all());             // from 1, 2, 4, 8 lanes before, of 16
+    step(std::integral_constant<int, 0x112>(), all());
+    step(std::integral_constant<int, 0x114>(), all());
+    step(std::integral_constant<int, 0x118>(), all());
+    step(std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xA>());      // from the last lane of the 16, the 32 before
+    step(std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xC>());
+    return v;
+}
+__device__ __forceinline__ uint32_t sums_to(uint32_t v)
+{
+    return lanes_scan(v, [](uint32_t x, uint32_t y) { return x + y; });
+}
+template <class T>
+__device__ __forceinline__ T last_lane(T v)
+{
+    return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
+
+struct Share {
+    uint32_t seq, tile, split, splits;    // splits == 0: nothing
+    uint32_t base;                        // balanced: where the sequence's partial results start, in rows of all heads of the cache
+};
+
+template <uint32_t ROWS, uint32_t KEYS>
+__device__ __forceinline__ Share share_of_work(const ecs::AttentionTreeArgs &a, bool first_wave)
+{
+    const uint32_t slot = blockIdx.y + gridDim.y * blockIdx.z;     // (blockIdx.x: the head)
+    if (slot >= a.slots) return {0, 0, 0, 0, 0};
+    if (!a.balanced) {
+        const uint32_t item = slot / a.splits;
+        return {item / a.row_tiles, item % a.row_tiles, slot % a.splits, a.splits, 0};
+    }
+    const uint32_t lane = threadIdx.x & 63u, b = min(lane, a.batch - 1u);
+    const Sequence s(a, b);
+    const uint32_t rows = lane < a.batch ? s.new_tokens * a.group : 0u, items = (rows + ROWS - 1u) / ROWS;
+    const uint32_t keys = lane < a.batch ? max((s.len + KEYS - 1u) / KEYS, 1u) : 1u;
+    const uint32_t all = last_lane(sums_to(items));
+    const uint32_t longest = last_lane(lanes_scan(keys, [](uint32_t x, uint32_t y) { return max(x, y); }));
+    const float work = last_lane(lanes_scan((float)items * (float)keys, [](float x, float y) { return x + y; }));
+    auto pieces = [&](uint32_t length) { return (keys + length - 1u) / length; };
+    // the least length there could be, and one at which it works out: work / length + all <= slots (in case FP32 says otherwise: no pieces)
+    uint32_t low = max((uint32_t)(work / (float)a.slots), 256u / KEYS), length = longest;
+    if (a.slots > all) {
+        const uint32_t enough = max((uint32_t)(work / (float)(a.slots - all)) + 1u, low);
+        if (last_lane(sums_to(items * pieces(enough))) <= a.slots) length = min(length, enough);
+    }
+    for (int step = 0; step < 5 && low < length; ++step) {
+        const uint32_t middle = (low + length) / 2u;
+        if (last_lane(sums_to(items * pieces(middle))) <= a.slots)
+            length = middle;
+        else
+            low = middle + 1u;
+    }
+    const uint32_t mine = pieces(length), to = sums_to(items * mine), rows_to = sums_to(rows * mine);
+    const uint32_t before = to - items * mine, rows_before = rows_to - rows * mine;
+    // (rows that would lie behind the workspace: starts that are not in order)
+    const uint32_t splits = mine > 1u && rows_to > a.part_rows ? 0u : mine;
+    if (first_wave && slot == 0 && blockIdx.x == 0) a.plan[lane] = {splits, rows_before, lane < a.batch ? s.first : 0xFFFFFFFFu, s.new_tokens};
+    const uint32_t seq = (uint32_t)__popcll(__ballot(to <= slot));
+    if (seq >= a.batch) return {0, 0, 0, 0, 0};
+    const uint32_t in = slot - (uint32_t)__builtin_amdgcn_readlane((int)before, (int)seq);
+    const uint32_t tiles = (uint32_t)__builtin_amdgcn_readlane((int)items, (int)seq), split = in / tiles;
+    return {seq, in - split * tiles, split, (uint32_t)__builtin_amdgcn_readlane((int)splits, (int)seq),
+            (uint32_t)__builtin_amdgcn_readlane((int)rows_before, (int)seq)};
+}
+
 // The page of a key, a number that is one whatever the table holds
 __device__ __forceinline__ uint32_t page_of(const AttentionArgs &a, const int32_t *table, uint32_t key)
 {
@@ -229,8 +311,14 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) :
 
     const uint32_t tid = threadIdx.x, lane = tid & 63u, j = lane & 15u, g = lane >> 4;
     const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid >> 6));
-    const uint32_t tile = blockIdx.x / a.splits, split = blockIdx.x - tile * a.splits, head = blockIdx.y;
-    const Sequence s(a, blockIdx.z);
+    uint32_t tile = blockIdx.x / a.splits, split = blockIdx.x - tile * a.splits, head = blockIdx.y, seq = blockIdx.z, splits = a.splits, base = 0;
+    if constexpr (TREE) {
+        head = blockIdx.x;
+        const Share mine = share_of_work<16, 32>(a, tid < 64u);
+        tile = mine.tile, split = mine.split, seq = mine.seq, splits = mine.splits, base = mine.base;
+        if (splits == 0) return;
+    }
+    const Sequence s(a, seq);
     const uint32_t rows = s.new_tokens * a.group, row0 = 16u * tile;
     if (row0 >= rows) return;
     const uint32_t dim = PAD ? a.cache.dim : DP;
@@ -245,7 +333,7 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) :
     const uint32_t *words = nullptr;
     if constexpr (TREE) words = a.seen + (int64_t)(s.first + token) * a.seen_stride;
 
-    const uint32_t tiles = (end + 31u) >> 5, per = (tiles + a.splits - 1u) / a.splits;
+    const uint32_t tiles = (end + 31u) >> 5, per = (tiles + splits - 1u) / splits;
     const uint32_t t0 = min(split * per, tiles), t1 = min(t0 + per, tiles);
     const uint32_t page_mask = (1u << a.cache.page_shift) - 1u;
     const uint64_t page_rows = (uint64_t)a.cache.heads << a.cache.page_shift, head_rows = (uint64_t)head << a.cache.page_shift;
@@ -528,7 +616,7 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) :
         for (int x = 0; x < 4; ++x) o[i] += share[x] * lds_o[x][n][d0 + i];
     }
     const uint32_t out_row = row0 + n, out_token = out_row / a.group, out_head = head * a.group + (out_row - out_token * a.group);
-    if (a.splits == 1u) {
+    if (splits == 1u) {
         const float inv = total == 0.0f ? 0.0f : 1.0f / total;
         uint16_t *p = a.out.data + (int64_t)(s.first + out_token) * a.out.token_stride + (int64_t)out_head * a.out.head_stride;
 #pragma unroll
@@ -542,7 +630,9 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) :
             }
         }
     } else {
-        const uint64_t at = ((uint64_t)split * a.tokens + s.first + out_token) * a.q_heads + out_head;
+        uint64_t at = ((uint64_t)split * a.tokens + s.first + out_token) * a.q_heads + out_head;
+        if constexpr (TREE)
+            if (a.balanced) at = ((uint64_t)base + split * rows + out_row) * a.cache.heads + head;
 #pragma unroll
         for (int i = 0; i < VD; i += 4) *reinterpret_cast<f32x4 *>(a.part_o + at * dim + d0 + i) = f32x4{o[i], o[i + 1], o[i + 2], o[i + 3]};
         if ((tid & 15u) == 0) a.part_ml[2 * at] = most, a.part_ml[2 * at + 1] = total;
@@ -612,13 +702,19 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
     const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid >> 6));
     // the last rows see the most keys: their workgroups start first.  Where all workgroups run at once (two on a compute unit, one that
     // starts early beside one that starts late), the second half goes the other way, so that each pair has the same to do.
-    uint32_t tile = blockIdx.y / a.splits;
-    if (tile < (a.row_tiles + 1u) / 2u || gridDim.x * gridDim.y * gridDim.z > 512u)
+    uint32_t tile = blockIdx.y / a.splits, head = blockIdx.x, split = blockIdx.y % a.splits, seq = blockIdx.z, splits = a.splits, base = 0;
+    if (TREE)
+        ;
+    else if (tile < (a.row_tiles + 1u) / 2u || gridDim.x * gridDim.y * gridDim.z > 512u)
         tile = a.row_tiles - 1u - tile;
     else
         tile -= (a.row_tiles + 1u) / 2u;
-    const uint32_t head = blockIdx.x, split = blockIdx.y % a.splits;
-    const Sequence s(a, blockIdx.z);
+    if constexpr (TREE) {
+        const Share mine = share_of_work<128, KT>(a, tid < 64u);
+        tile = mine.tile, split = mine.split, seq = mine.seq, splits = mine.splits, base = mine.base;
+        if (splits == 0) return;
+    }
+    const Sequence s(a, seq);
     const uint32_t rows = s.new_tokens * a.group, row0 = 128u * tile;
     if (row0 >= rows) return;
     const uint32_t dim = a.cache.dim, pieces = dim / 8u;
@@ -665,7 +761,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
     // (a scale of 0 as the least there is: a hidden key's score, minus infinity, stays that)
     const float scale = a.scale_log2 == 0.0f ? 1.17549435e-38f : fabsf(a.scale_log2), by = BITS == 16 ? scale : 1.0f;
 
-    const uint32_t tiles = (end + KT - 1u) / KT, per = (tiles + a.splits - 1u) / a.splits;
+    const uint32_t tiles = (end + KT - 1u) / KT, per = (tiles + splits - 1u) / splits;
     const uint32_t t0 = min(split * per, tiles), t1 = min(t0 + per, tiles);
     const uint32_t page_mask = (1u << a.cache.page_shift) - 1u;
     const uint64_t page_rows = (uint64_t)a.cache.heads << a.cache.page_shift, head_rows = (uint64_t)head << a.cache.page_shift;
@@ -993,7 +1089,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
     const uint32_t out_row = row0 + 32u * wave + n;
     if (out_row >= rows) return;
     const uint32_t out_head = head * a.group + (row - token * a.group);
-    if (a.splits == 1u) {
+    if (splits == 1u) {
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;
         uint16_t *p = a.out.data + (int64_t)(s.first + token) * a.out.token_stride + (int64_t)out_head * a.out.head_stride;
 #pragma unroll
@@ -1014,7 +1110,9 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
                 }
             }
     } else {
-        const uint64_t at = ((uint64_t)split * a.tokens + s.first + token) * a.q_heads + out_head;
+        uint64_t at = ((uint64_t)split * a.tokens + s.first + token) * a.q_heads + out_head;
+        if constexpr (TREE)
+            if (a.balanced) at = ((uint64_t)base + split * rows + out_row) * a.cache.heads + head;
 #pragma unroll
         for (int y = 0; y < kTiles; ++y)
 #pragma unroll
@@ -1028,26 +1126,62 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
     }
 }
 
-#ifndef ECS_TREE
 // ---- joining the splits ----------------------------------------------------------------------------------------------------------------
 //
 // For each (token, head) the parts of its splits, each taken to the largest of their maxima:
 //   o = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s
 // What bounds it is the trip to memory, so that what a row needs is asked for at once and rows are many to a compute unit.
 //
+// Where a row's parts are: the s-th is row first + s * step of the partial results.  With shares of several sequences by their lengths
+// a row belongs to one of them, whose splits and place the first launch has written down.
+struct Parts {
+    uint64_t first, step;
+    uint32_t splits;                      // 0: nothing to join
+};
+
+template <bool TREE, uint32_t LANES>
+__device__ __forceinline__ Parts parts_of(const ArgsOf<TREE> &a, uint32_t token, uint32_t head)
+{
+    if constexpr (TREE) {
+        if (a.balanced) {
+            // the last sequence that starts at this token or before it, for each of the wavefront's rows
+            const uint32_t lane = threadIdx.x & 63u;
+            const ecs::AttentionTreeArgs::Words mine = a.plan[lane];
+            uint32_t b = 0;
+#pragma unroll
+            for (uint32_t r = 0; r < 64u; r += LANES) {
+                const uint32_t of = (uint32_t)__builtin_amdgcn_readlane((int)token, (int)r);
+                const uint32_t count = (uint32_t)__popcll(__ballot(mine.z <= of));
+                if (lane >= r) b = max(count, 1u) - 1u;
+            }
+            const uint32_t splits = (uint32_t)__shfl((int)mine.x, (int)b, 64), base = (uint32_t)__shfl((int)mine.y, (int)b, 64);
+            const uint32_t first = (uint32_t)__shfl((int)mine.z, (int)b, 64), news = (uint32_t)__shfl((int)mine.w, (int)b, 64);
+            const uint32_t in = token - first, rows = news * a.group;
+            if (token < first || in >= news || splits < 2u) return {0, 0, 0};
+            const uint32_t of_cache = head / a.group, row = in * a.group + (head - of_cache * a.group);
+            return {((uint64_t)base + row) * a.cache.heads + of_cache, (uint64_t)rows * a.cache.heads, splits};
+        }
+    }
+    return {(uint64_t)token * a.q_heads + head, (uint64_t)a.tokens * a.q_heads, a.splits};
+}
+
 // Few rows: a workgroup for each, its wavefronts on different splits.
-__global__ __launch_bounds__(256) void attention_join_splits_kernel(const AttentionArgs a)
+template <bool TREE>
+__global__ __launch_bounds__(256) void attention_join_splits_kernel(const ArgsOf<TREE> a)
 {
     __shared__ float lds_o[4][256];
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6, dim = a.cache.dim;
     const uint32_t r = blockIdx.x, token = r / a.q_heads, head = r - token * a.q_heads;
     if ((int32_t)token < a.q_start[0] || (int32_t)token >= a.q_start[a.batch]) return;            // of no sequence (the whole workgroup)
-    const uint64_t row = r, step = (uint64_t)a.tokens * a.q_heads;
+    const Parts parts = parts_of<TREE, 64>(a, token, head);
+    if (TREE && parts.splits == 0) return;
+    const uint64_t row = parts.first, step = parts.step;
+    const uint32_t splits = TREE ? parts.splits : a.splits;
     float l = 0.0f, o[4] = {0, 0, 0, 0}, top = kNone;
     // 64 splits at a time: a lane looks at one, its share goes to the others by readlane, so that all that is waited for is two trips
-    for (uint32_t first = 0; first < a.splits; first += 64u) {
+    for (uint32_t first = 0; first < splits; first += 64u) {
         const uint32_t s = first + lane;
-        const float2 ml = s < a.splits ? *reinterpret_cast<const float2 *>(a.part_ml + 2 * (row + s * step)) : make_float2(kNone, 0.0f);
+        const float2 ml = s < splits ? *reinterpret_cast<const float2 *>(a.part_ml + 2 * (row + s * step)) : make_float2(kNone, 0.0f);
         float m = ml.x;
 #pragma unroll
         for (int x = 32; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor(m, x, 64));
@@ -1058,7 +1192,7 @@ __global__ __launch_bounds__(256) void attention_join_splits_kernel(const Attent
         l = l * before + share * ml.y;
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[i] *= before;
-        const uint32_t count = min(a.splits - first, 64u);
+        const uint32_t count = min(splits - first, 64u);
         for (uint32_t k = wave; k < count; k += 16u) {             // four splits of this wavefront on their way
             float x[4][4], f[4];
 #pragma unroll
@@ -1087,22 +1221,25 @@ __global__ __launch_bounds__(256) void attention_join_splits_kernel(const Attent
 }
 
 // Many rows, which have few splits: L lanes for each, four values a lane, four splits on their way.
-template <int L>
-__global__ __launch_bounds__(256) void attention_join_rows_kernel(const AttentionArgs a)
+template <int L, bool TREE>
+__global__ __launch_bounds__(256) void attention_join_rows_kernel(const ArgsOf<TREE> a)
 {
     const uint32_t r = blockIdx.x * (256u / L) + threadIdx.x / L, d = 4u * (threadIdx.x % L), dim = a.cache.dim;
     const uint32_t token = r / a.q_heads, head = r - token * a.q_heads;
+    const Parts parts = parts_of<TREE, L>(a, token, head);         // (by the whole wavefront)
     if (token >= a.tokens || d >= dim) return;
     const int32_t first = a.q_start[0], last = a.q_start[a.batch];
-    const uint64_t row = r, step = (uint64_t)a.tokens * a.q_heads;
+    const uint64_t row = parts.first, step = parts.step;
+    const uint32_t splits = TREE ? parts.splits : a.splits;
+    if (TREE && splits == 0) return;
     float l = 0.0f, top = kNone;
     f32x4 o = {0, 0, 0, 0};
-    for (uint32_t s = 0; s < a.splits; s += 4u) {
+    for (uint32_t s = 0; s < splits; s += 4u) {
         float2 ml[4];
         f32x4 x[4];
 #pragma unroll
         for (uint32_t u = 0; u < 4; ++u) {
-            const uint64_t at = row + min(s + u, a.splits - 1u) * step;
+            const uint64_t at = row + min(s + u, splits - 1u) * step;
             ml[u] = *reinterpret_cast<const float2 *>(a.part_ml + 2 * at);
             x[u] = *reinterpret_cast<const f32x4 *>(a.part_o + at * dim + d);
         }
@@ -1115,7 +1252,7 @@ __global__ __launch_bounds__(256) void attention_join_rows_kernel(const Attentio
         o *= before;
 #pragma unroll
         for (uint32_t u = 0; u < 4; ++u) {
-            if (s + u >= a.splits) continue;
+            if (s + u >= splits) continue;
             // (a split without a maximum has added up nothing, or scores that are all NaN: its sums are then NaN, and have to stay)
             const float share = share_of(ml[u].x, m);
             l = fmaf(share, ml[u].y, l);
@@ -1135,12 +1272,14 @@ __global__ __launch_bounds__(256) void attention_join_rows_kernel(const Attentio
     }
 }
 
-#endif  // ECS_TREE
-
 template <int BITS>
 int launch_rows(const ArgsOf<kTree> &a, void *stream)
 {
+#ifdef ECS_TREE
+    const uint32_t gx = a.cache.heads, gy = std::min(a.slots, 32768u), gz = (a.slots + gy - 1u) / gy;
+#else
     const uint32_t gx = a.row_tiles * a.splits, gy = a.cache.heads, gz = a.batch;
+#endif
     switch (a.cache.dim) {
     case 64: return ecs::launch_args<attention_rows_kernel<BITS, 64, false, kTree>>(a, gx, gy, gz, 256, stream);
     case 128: return ecs::launch_args<attention_rows_kernel<BITS, 128, false, kTree>>(a, gx, gy, gz, 256, stream);
@@ -1155,7 +1294,11 @@ int launch_rows(const ArgsOf<kTree> &a, void *stream)
 template <int BITS>
 int launch_chunk(const ArgsOf<kTree> &a, void *stream)
 {
+#ifdef ECS_TREE
+    const uint32_t gx = a.cache.heads, gy = std::min(a.slots, 32768u), gz = (a.slots + gy - 1u) / gy;
+#else
     const uint32_t gx = a.cache.heads, gy = a.row_tiles * a.splits, gz = a.batch;
+#endif
     switch ((a.cache.dim + 31u) / 32u) {
     case 1: return ecs::launch_args<attention_chunk_kernel<BITS, 32, kTree>>(a, gx, gy, gz, 256, stream);
     case 2: return ecs::launch_args<attention_chunk_kernel<BITS, 64, kTree>>(a, gx, gy, gz, 256, stream);
@@ -1172,6 +1315,17 @@ template <int BITS>
 int launch_bits(const ArgsOf<kTree> &a, void *stream)
 {
     return a.chunk ? launch_chunk<BITS>(a, stream) : launch_rows<BITS>(a, stream);
+}
+
+int launch_join(const ArgsOf<kTree> &a, void *stream)
+{
+    // (us by a workgroup / by some lanes for each row: 320 rows of 25 splits 129 / 134, 1024 of 8 46.2 / 46.0; four bits, 1000 tokens of 32
+    // heads, two splits, by a wavefront 95, by 32 lanes 86)
+    const uint32_t rows = a.tokens * a.q_heads;
+    if (rows < 2048u) return ecs::launch_args<attention_join_splits_kernel<kTree>>(a, rows, 1, 1, 256, stream);
+    if (a.cache.dim <= 64u) return ecs::launch_args<attention_join_rows_kernel<16, kTree>>(a, (rows + 15u) / 16u, 1, 1, 256, stream);
+    if (a.cache.dim <= 128u) return ecs::launch_args<attention_join_rows_kernel<32, kTree>>(a, (rows + 7u) / 8u, 1, 1, 256, stream);
+    return ecs::launch_args<attention_join_rows_kernel<64, kTree>>(a, (rows + 3u) / 4u, 1, 1, 256, stream);
 }
 
 }  // namespace
@@ -1213,29 +1367,39 @@ AttentionPlan plan_attention(uint32_t batch, uint32_t kv_heads, uint32_t group, 
     return p;
 }
 
+// Of trees: how the launch's workgroups are dealt out, and whether by the sequences' lengths (share_of_work)
+TreePlan plan_attention_tree(uint32_t batch, uint32_t kv_heads, uint32_t group, uint32_t dim, uint32_t bits, uint64_t tokens, uint32_t max_new,
+                             uint64_t max_kv)
+{
+    TreePlan t = {};
+    static_cast<AttentionPlan &>(t) = plan_attention(batch, kv_heads, group, dim, bits, tokens, max_new, max_kv);
+    const uint64_t wanted = (t.chunk ? kChunkWanted : kFewWanted) / kv_heads, items = (uint64_t)batch * t.row_tiles;
+    // One sequence with a tile of rows for every workgroup, and sequences that fill the chip twice over, are left whole
+    t.balanced = batch <= 64u && splits_of_keys(max_kv) > 1u && (batch > 1u ? items < 2u * wanted : items < wanted);
+    if (t.balanced) {
+        t.slots = std::max(items, wanted);
+        t.splits = 1;
+        t.part_rows = (uint32_t)std::min<uint64_t>(t.slots * (t.chunk ? kChunkRows : kFewRows), splits_of_keys(max_kv) * std::min<uint64_t>(tokens, (uint64_t)batch * max_new) * group);
+        t.work_bytes = kTreePlanBytes + (uint64_t)t.part_rows * kv_heads * (dim + 2u) * sizeof(float);
+    } else {
+        if (batch <= 64u) t.splits = 1, t.work_bytes = 0;
+        t.slots = items * t.splits;
+    }
+    return t;
+}
+
 uint64_t most_attention_work(uint32_t batch, uint32_t kv_heads, uint32_t group, uint32_t dim, uint32_t bits, uint64_t tokens, uint32_t max_new,
                              uint64_t max_kv)
 {
     // A workgroup takes up to per_tile rows, and there are splits only while they are no more than `wanted` (twice that where two splits are the
-    // least): so many rows of partial results at most, whatever the call; and no more splits than the keys allow.
+    // least, and for trees of several sequences): so many rows of partial results at most, whatever the call; and no more splits than the keys allow.
     const uint64_t few = rows_of_16(dim, bits), by_keys = splits_of_keys(max_kv);
     uint64_t most = 0;
-    if (group <= few) most = (uint64_t)kFewWanted * kFewRows;
+    if (group <= few) most = (uint64_t)kFewWanted * kFewRows * (batch > 1u ? 2u : 1u);
     if ((uint64_t)max_new * group > few) most = std::max<uint64_t>(most, (uint64_t)kChunkWanted * kChunkRows * (batch > 1u ? 2u : 1u));
     if (by_keys <= 1u) return 0;
     const uint64_t rows = std::min<uint64_t>(tokens, (uint64_t)batch * max_new) * kv_heads * group;
-    return std::min(most, by_keys * rows) * (dim + 2u) * sizeof(float);
-}
-
-int launch_attention_join(const AttentionArgs &a, void *stream)
-{
-    // (us by a workgroup / by some lanes for each row: 320 rows of 25 splits 129 / 134, 1024 of 8 46.2 / 46.0; four bits, 1000 tokens of 32
-    // heads, two splits, by a wavefront 95, by 32 lanes 86)
-    const uint32_t rows = a.tokens * a.q_heads;
-    if (rows < 2048u) return launch_args<attention_join_splits_kernel>(a, rows, 1, 1, 256, stream);
-    if (a.cache.dim <= 64u) return launch_args<attention_join_rows_kernel<16>>(a, (rows + 15u) / 16u, 1, 1, 256, stream);
-    if (a.cache.dim <= 128u) return launch_args<attention_join_rows_kernel<32>>(a, (rows + 7u) / 8u, 1, 1, 256, stream);
-    return launch_args<attention_join_rows_kernel<64>>(a, (rows + 3u) / 4u, 1, 1, 256, stream);
+    return kTreePlanBytes + std::min(most, by_keys * rows) * (dim + 2u) * sizeof(float);
 }
 
 int launch_attention(const AttentionArgs &a, void *stream)
@@ -1244,7 +1408,7 @@ int launch_attention_tree(const AttentionTreeArgs &a, void *stream)
 #endif
 {
     const int e = a.cache.bits == 16 ? launch_bits<16>(a, stream) : a.cache.bits == 8 ? launch_bits<8>(a, stream) : launch_bits<4>(a, stream);
-    return e || a.splits == 1u ? e : launch_attention_join(a, stream);
+    return e || !a.joins() ? e : launch_join(a, stream);
 }
 
 }  // namespace ecs

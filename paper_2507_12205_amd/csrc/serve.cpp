@@ -106,30 +106,44 @@ int check_attention(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *fr
     return ECSPMV_OK;
 }
 
-// What both attentions look at before they launch; `nothing`: there is nothing to compute
-int prepare_attention(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *a, void *d_work, size_t work_bytes, ecs::AttentionArgs &args,
-                      bool &nothing)
+// What both attentions look at before they launch; `need`: bytes of the workspace
+int check_tensors(const ecspmv_attention_t &t, uint64_t need, void *d_work, size_t work_bytes, ecs::AttentionArgs &args)
 {
-    ecs::AttentionPlan plan;
-    ecspmv_attention_t t;
-    int s = check_attention(cache, a, args, plan, t);
-    if (s) return s;
-    nothing = args.tokens == 0 || args.batch == 0 || args.max_new == 0;
-    if (nothing) return ECSPMV_OK;
+    int s;
     if ((s = check_view(&t.q, args.q, args.q_wide)) || (s = check_view(&t.out, args.out, args.out_wide))) return s;
     if (!t.q_start || !t.kv_len || !aligned(t.q_start, 4) || !aligned(t.kv_len, 4)) return ECSPMV_ERR_INVALID;
     if (args.max_pages && (!t.page_table || !aligned(t.page_table, 4) || t.table_stride < t.max_pages)) return ECSPMV_ERR_INVALID;
-    if (plan.work_bytes && (!d_work || !aligned(d_work, 16))) return ECSPMV_ERR_INVALID;
-    if (work_bytes < plan.work_bytes) return ECSPMV_ERR_TOO_SMALL;
+    if (need && (!d_work || !aligned(d_work, 16))) return ECSPMV_ERR_INVALID;
+    if (work_bytes < need) return ECSPMV_ERR_TOO_SMALL;
     args.q_start = t.q_start;
     args.kv_len = t.kv_len;
     args.table = t.page_table;
     args.table_stride = t.table_stride;
-    args.part_o = static_cast<float *>(d_work);
-    args.part_ml = args.part_o + (uint64_t)plan.splits * args.tokens * args.q_heads * args.cache.dim;
     args.scale_log2 = t.scale * 1.44269504088896340736f;
     return ECSPMV_OK;
 }
+
+int check_attention_tree(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *from, ecs::AttentionTreeArgs &a, ecs::TreePlan &plan,
+                         ecspmv_attention_t &t)
+{
+    std::memset(&a, 0, sizeof(a));
+    ecs::AttentionPlan rows;
+    const int s = check_attention(cache, from, a, rows, t);
+    if (s) return s;
+    plan = ecs::plan_attention_tree(a.batch, a.cache.heads, a.group, a.cache.dim, a.cache.bits, a.tokens, a.max_new,
+                                    (uint64_t)a.max_pages << a.cache.page_shift);
+    if (plan.slots > 0x7fffffffu) return ECSPMV_ERR_UNSUPPORTED;
+    a.chunk = plan.chunk;
+    a.row_tiles = plan.row_tiles;
+    a.splits = plan.splits;
+    a.slots = (uint32_t)plan.slots;
+    a.balanced = plan.balanced;
+    a.part_rows = plan.part_rows;
+    a.seen_words = (a.max_new + 31u) / 32u;
+    return ECSPMV_OK;
+}
+
+bool nothing_to_compute(const ecs::AttentionArgs &a) { return a.tokens == 0 || a.batch == 0 || a.max_new == 0; }
 
 int check_verify(const ecspmv_verify_t *from, ecspmv_verify_t &t)
 {
@@ -268,23 +282,47 @@ int ecspmv_attention_workspace_most(const ecspmv_kv_cache_t *cache, const ecspmv
 int ecspmv_attention(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *a, void *d_work, size_t work_bytes, void *stream)
 {
     ecs::AttentionArgs args;
-    bool nothing;
-    const int s = prepare_attention(cache, a, d_work, work_bytes, args, nothing);
-    return s || nothing ? s : ecs::hip_status(ecs::launch_attention(args, stream));
+    ecs::AttentionPlan plan;
+    ecspmv_attention_t t;
+    int s = check_attention(cache, a, args, plan, t);
+    if (s) return s;
+    if (nothing_to_compute(args)) return ECSPMV_OK;
+    if ((s = check_tensors(t, plan.work_bytes, d_work, work_bytes, args))) return s;
+    args.part_o = static_cast<float *>(d_work);
+    args.part_ml = args.part_o + (uint64_t)plan.splits * args.tokens * args.q_heads * args.cache.dim;
+    return ecs::hip_status(ecs::launch_attention(args, stream));
+}
+
+int ecspmv_attention_tree_workspace(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *a, size_t *bytes)
+{
+    if (!bytes) return ECSPMV_ERR_INVALID;
+    ecs::AttentionTreeArgs args;
+    ecs::TreePlan plan;
+    ecspmv_attention_t t;
+    const int s = check_attention_tree(cache, a, args, plan, t);
+    if (s) return s;
+    *bytes = (size_t)plan.work_bytes;
+    return ECSPMV_OK;
 }
 
 int ecspmv_attention_tree(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *a, const uint32_t *d_seen, int64_t seen_stride, void *d_work,
                           size_t work_bytes, void *stream)
 {
     ecs::AttentionTreeArgs args;
-    std::memset(&args, 0, sizeof(args));
-    bool nothing;
-    const int s = prepare_attention(cache, a, d_work, work_bytes, args, nothing);
-    if (s || nothing) return s;
+    ecs::TreePlan plan;
+    ecspmv_attention_t t;
+    int s = check_attention_tree(cache, a, args, plan, t);
+    if (s) return s;
+    if (nothing_to_compute(args)) return ECSPMV_OK;
+    if ((s = check_tensors(t, plan.work_bytes, d_work, work_bytes, args))) return s;
+    if (!d_seen || !aligned(d_seen, 4) || seen_stride < (int64_t)args.seen_words) return ECSPMV_ERR_INVALID;
     args.seen = d_seen;
     args.seen_stride = seen_stride;
-    args.seen_words = (args.max_new + 31u) / 32u;
-    if (!d_seen || !aligned(d_seen, 4) || seen_stride < (int64_t)args.seen_words) return ECSPMV_ERR_INVALID;
+    uint8_t *work = static_cast<uint8_t *>(d_work);
+    args.plan = reinterpret_cast<ecs::AttentionTreeArgs::Words *>(work);
+    args.part_o = reinterpret_cast<float *>(work + (plan.balanced ? ecs::kTreePlanBytes : 0u));
+    args.part_ml = args.part_o + (plan.balanced ? (uint64_t)plan.part_rows * args.cache.heads : (uint64_t)plan.splits * args.tokens * args.q_heads) *
+                                     args.cache.dim;
     return ecs::hip_status(ecs::launch_attention_tree(args, stream));
 }
 

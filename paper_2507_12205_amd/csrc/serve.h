@@ -69,6 +69,7 @@ struct AttentionArgs {
     uint32_t chunk, row_tiles, splits;    // chunk: 128 rows per workgroup instead of 16
     uint32_t q_wide, out_wide;
     float scale_log2;                     // scale * log2(e)
+    bool joins() const { return splits > 1u; }
 };
 struct AttentionPlan {
     uint32_t chunk, row_tiles, splits;
@@ -80,12 +81,23 @@ AttentionPlan plan_attention(uint32_t batch, uint32_t kv_heads, uint32_t group, 
 uint64_t most_attention_work(uint32_t batch, uint32_t kv_heads, uint32_t group, uint32_t dim, uint32_t bits, uint64_t tokens, uint32_t max_new,
                              uint64_t max_kv);
 int launch_attention(const AttentionArgs &a, void *stream);
-int launch_attention_join(const AttentionArgs &a, void *stream);          // of the splits' results
 
+constexpr uint32_t kTreePlanBytes = 1024; // of the workspace: four words for each of 64 sequences
+struct TreePlan : AttentionPlan {
+    uint64_t slots;                       // workgroups to a head
+    uint32_t balanced, part_rows;         // shares by the sequences' lengths; rows of partial results that there is room for
+};
+TreePlan plan_attention_tree(uint32_t batch, uint32_t kv_heads, uint32_t group, uint32_t dim, uint32_t bits, uint64_t tokens, uint32_t max_new,
+                             uint64_t max_kv);
 struct AttentionTreeArgs : AttentionArgs {
     const uint32_t *seen;                 // bit i of a token's words: it sees its sequence's i-th new token
     int64_t seen_stride;                  // words from one token to the next
-    uint32_t seen_words, pad_;            // words that count
+    uint32_t seen_words;                  // words that count
+    uint32_t slots, balanced, part_rows;  // as planned
+    struct alignas(16) Words {
+        uint32_t x, y, z, w;
+    } *plan;                              // where shares are balanced, of each sequence: splits, first row of its partial results, first token, tokens
+    bool joins() const { return balanced || splits > 1u; }
 };
 int launch_attention_tree(const AttentionTreeArgs &a, void *stream);
 

@@ -219,7 +219,7 @@ def kv_keep(caches: KvCaches, first: torch.Tensor, path: torch.Tensor, accepted:
 
 
 def attention_workspace(cache: KvCache, q: torch.Tensor, batch: int, max_new: int, max_kv: int) -> torch.Tensor:
-    """A workspace for attention() calls of up to these sizes: q's heads and no more tokens than it has (no more than batch * max_new if they
+    """A workspace for attention() and attention_tree() calls of up to these sizes: q's heads and no more tokens than it has (no more than batch * max_new if they
     are fewer), sequences, new tokens of one, places in their page tables."""
     a = B.AttentionDesc(_ATTENTION, q.shape[1], q.shape[0], batch, -(-max_kv // cache.page_size), max_new)
     return torch.empty(B.ecspmv_attention_workspace_most(cache.desc, a), dtype=torch.uint8, device=q.device)
@@ -262,7 +262,7 @@ def attention_tree(cache: KvCache, q: torch.Tensor, out: torch.Tensor, q_start: 
     assert seen.dtype is torch.int32 and seen.get_device() == cache.device and tokens == q.shape[0] and 32 * words >= min(max_new, tokens)
     assert (words <= 1 or seen.stride(1) == 1) and (tokens <= 1 or seen.stride(0) >= words)
     if workspace is None:
-        workspace = _workspace(B.ecspmv_attention_workspace(cache.desc, a), q, stream)
+        workspace = _workspace(B.ecspmv_attention_tree_workspace(cache.desc, a), q, stream)
     assert workspace.get_device() == cache.device and workspace.is_contiguous()
     B.ecspmv_attention_tree(cache.desc, a, seen.data_ptr(), seen.stride(0) if tokens > 1 else words, workspace.data_ptr(), workspace.nbytes,
                             _stream_handle(stream))

@@ -72,7 +72,7 @@ out["short"] = [L.ecspmv_kv_append(cache(), view(), view(), 0x800000, 5, short, 
                 L.ecspmv_attention_tree(cache(), None, 0xC00000, 1, 0, 0, 0), L.ecspmv_verify_tree(None, 0x900000, 1 << 20, 0),
                 L.ecspmv_verify_tree_workspace(verify(), None)]
 long = attention(max_pages=100, table_stride=100)
-work = B.ecspmv_attention_workspace(cache(), long)
+work = B.ecspmv_attention_tree_workspace(cache(), long)
 out["enough"] = [outcome(lambda: B.ecspmv_attention_tree(cache(), long, 0xC00000, 1, 0x900000, work - d, stream[0])) for d in (0, 1)]
 out["none"] = outcome(lambda: B.ecspmv_attention_tree(cache(), long, 0xC00000, 1, 0, work, stream[0]))
 need = B.ecspmv_verify_tree_workspace(verify())

@@ -1,5 +1,7 @@
 """The Python calls of decoding with trees without a GPU: what they hand to the C ABI and what they refuse, on tensors of the CPU whose addresses
 nothing looks at; the bits of a tree; and the registers of the kernels."""
+import random
+
 import numpy as np
 import pytest
 import torch
@@ -96,7 +98,7 @@ def test_keep(calls, devices):
 
 
 def test_attention(calls, devices, monkeypatch):
-    monkeypatch.setattr(D.B, "ecspmv_attention_workspace", lambda *a: 256)
+    monkeypatch.setattr(D.B, "ecspmv_attention_tree_workspace", lambda *a: 256)
     monkeypatch.setattr(D, "_workspace", lambda n, beside, stream: torch.zeros(n, dtype=torch.uint8))
     c = cache()
     c.device = 0
@@ -161,3 +163,18 @@ def test_frequencies():
 def test_no_scratch_memory():
     found = {n: v for n, v in kernels().items() if any(x in n for x in ("kv_append", "kv_keep", "verify_tree", "attention_rows_kernel", "attention_chunk_kernel"))}
     assert len(found) > 40 and not {n: v for n, v in found.items() if v[1]}
+
+
+@pytest.mark.parametrize("bits,heads,q_heads,dim", [(16, 32, 32, 128), (8, 8, 64, 128), (4, 2, 16, 96), (16, 1, 8, 256), (8, 1, 200, 64), (4, 40, 40, 64)])
+@pytest.mark.parametrize("batch,max_new,max_kv", [(32, 1, 4096), (4, 8, 30000), (32, 64, 4096), (5, 333, 3000), (1, 257, 100000), (100, 40, 5000), (3, 40, 200)])
+def test_a_workspace_for_all_smaller_calls(bits, heads, q_heads, dim, batch, max_new, max_kv):
+    """Made once for the largest sizes, it holds for fewer sequences, tokens, new tokens of one and places too."""
+    c, rng = cache(heads=heads, dim=dim), random.Random(batch * max_new)
+    c.desc.bits, c.desc.k_step, c.desc.v_step = bits, 0x300000, 0x400000
+    have = D.attention_workspace(c, torch.empty((batch * max_new, q_heads, dim), dtype=F16, device="meta"), batch, max_new, max_kv).nbytes
+    sizes = [(b, n, kv) for b in range(1, batch + 1) for n in (1, (max_new + 1) // 2, max_new) for kv in (300, max_kv)]
+    sizes += [(rng.randint(1, batch), rng.randint(1, max_new), rng.randint(1, max_kv)) for _ in range(2000)]
+    for b, n, kv in sizes:
+        tokens = rng.choice([b * n, rng.randint(n, b * n)])
+        a = B.AttentionDesc(D._ATTENTION, q_heads, tokens, b, -(-min(kv, max_kv) // 16), n)
+        assert B.ecspmv_attention_tree_workspace(c.desc, a) <= have, (b, n, kv, tokens)
