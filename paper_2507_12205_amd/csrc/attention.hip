@@ -73,11 +73,24 @@ struct Raw {
 
 // Codes as FP16 values, exactly: the code goes into the last bits of 1024, which is then taken off.
 __device__ __forceinline__ uint32_t minus(uint32_t w, _Float16 c) { return as_word(as_half2(w) - half2v{c, c}); }
+// a constant in a register, where an instruction that has two would need two: the mask and what it is joined with
+__device__ __forceinline__ uint32_t held(uint32_t x)
+{
+    asm("" : "+v"(x));
+    return x;
+}
+// (w & mask) | bits in one instruction
+__device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t mask, uint32_t bits) { return (w & held(mask)) | held(bits); }
 // two bytes (in the low halves of 16 bits each, the sign bit flipped) of 8-bit codes
 __device__ __forceinline__ uint32_t from_bytes(uint32_t w) { return minus(w | 0x64006400u, (_Float16)1152.0f); }
+// bytes `first` and `first` + 1 of a word, the sign bits flipped
+__device__ __forceinline__ uint32_t from_bytes_of(uint32_t w, int first)
+{
+    return minus(__builtin_amdgcn_perm(held(0x64646464u), w, first ? 0x04030402u : 0x04010400u), (_Float16)1152.0f);
+}
 // two nibbles, in bits 0-3 and 16-19; less 8, and the lowest value of a row is taken 8 steps higher (low_of): sums of products with
 // rounded weights then cancel less
-__device__ __forceinline__ uint32_t from_nibbles(uint32_t w) { return minus((w & 0x000F000Fu) | 0x64006400u, (_Float16)1032.0f); }
+__device__ __forceinline__ uint32_t from_nibbles(uint32_t w) { return minus(and_or(w, 0x000F000Fu, 0x64006400u), (_Float16)1032.0f); }
 
 // 8 neighbouring codes of a key as eight FP16 values, in 4 bits 16 too large: the code is the first four bits behind the leading one of a
 // value in [16, 32), and q's sum times 16 steps comes off a score.  (Of 1032, which q's sum would come off without the shift that this takes,
@@ -90,10 +103,10 @@ __device__ __forceinline__ half8v key_values(const uint32_t *w)
     if constexpr (BITS == 16) {
         return as_half8(w[0], w[1], w[2], w[3]);
     } else if constexpr (BITS == 8) {
-        auto two = [](uint32_t x, uint32_t select) { return minus(__builtin_amdgcn_perm(0, x, select) ^ 0x64806480u, (_Float16)1152.0f); };
-        return as_half8(two(w[0], 0x0C010C00u), two(w[0], 0x0C030C02u), two(w[1], 0x0C010C00u), two(w[1], 0x0C030C02u));
+        const uint32_t a = w[0] ^ 0x80808080u, b = w[1] ^ 0x80808080u;
+        return as_half8(from_bytes_of(a, 0), from_bytes_of(a, 2), from_bytes_of(b, 0), from_bytes_of(b, 2));
     } else {
-        auto two = [](uint32_t x) { return (x & 0x03C003C0u) | 0x4C004C00u; };
+        auto two = [](uint32_t x) { return and_or(x, 0x03C003C0u, 0x4C004C00u); };
         return as_half8(two(w[0] << 6), two(w[0] << 2), two(w[0] >> 2), two(w[0] >> 6));
     }
 }
@@ -186,8 +199,9 @@ struct Sequence {
 };
 
 // Which of 32 keys a token of a tree sees: bit i is key `key0` + i, of `end` keys in all, the first new one of them `behind`
-__device__ __forceinline__ uint32_t seen_bits(const uint32_t *words, uint32_t count, uint32_t key0, int32_t behind, uint32_t end)
+__device__ __forceinline__ uint32_t seen_bits(const ecs::AttentionTreeArgs &a, uint32_t token, uint32_t key0, int32_t behind, uint32_t end)
 {
+    const uint32_t *words = a.seen + (int64_t)token * a.seen_stride, count = a.seen_words;
     const int32_t first = (int32_t)key0 - behind;                  // the new token that is key0 (negative: keys before the tree)
     const uint32_t at = (uint32_t)max(first, 0) >> 5;
     const uint64_t pair = (uint64_t)(at + 1u < count ? words[at + 1u] : 0u) << 32 | (at < count ? words[at] : 0u);
@@ -202,8 +216,8 @@ __device__ __forceinline__ uint32_t seen_bits(const uint32_t *words, uint32_t co
 // For rows that all see all keys, the work of a sequence is (tiles of its rows) x (tiles of its keys).  Sequences differ in both, and the host
 // sees neither, so that the workgroups of a launch are dealt out here, by every one of them for itself: with each sequence's keys cut into
 // pieces of L tiles at most, L is the least length (but for a few steps of halving) at which all pieces find a workgroup.
-// (us by equal numbers of splits for all / by this: 16 trees of up to 16 nodes over up to 8192 keys, 64/8 heads of 128, 8 bits, 98.7 / @B; eight of up to
-// 49 over up to 2000, 32 heads of 80, 4 bits, 61 / @C.)
+// (us by equal numbers of splits for all / by this: 16 trees of up to 16 nodes over up to 8192 keys, 64/8 heads of 128, 8 bits, 98.7 / 85.8; eight of up to
+// 49 over up to 2000, 32 heads of 80, 4 bits, 61.2 / 41.8.)
 // inclusive results over the lanes of an operation whose neutral element is all zeros
 template <class T, class F>
 __device__ __forceinline__ T lanes_scan(T v, F with)
@@ -253,15 +267,17 @@ __device__ __forceinline__ Share share_of_work(const ecs::AttentionTreeArgs &a, 
     const uint32_t longest = last_lane(lanes_scan(keys, [](uint32_t x, uint32_t y) { return max(x, y); }));
     const float work = last_lane(lanes_scan((float)items * (float)keys, [](float x, float y) { return x + y; }));
     auto pieces = [&](uint32_t length) { return (keys + length - 1u) / length; };
-    // the least length there could be, and one at which it works out: work / length + all <= slots (in case FP32 says otherwise: no pieces)
-    uint32_t low = max((uint32_t)(work / (float)a.slots), 256u / KEYS), length = longest;
-    if (a.slots > all) {
-        const uint32_t enough = max((uint32_t)(work / (float)(a.slots - all)) + 1u, low);
-        if (last_lane(sums_to(items * pieces(enough))) <= a.slots) length = min(length, enough);
+    // as many pieces as the chip has workgroups at once, or, with more tiles of rows than that, as it has in whole rounds
+    const uint32_t goal = min(a.slots, max((all + a.at_once - 1u) / a.at_once, 1u) * a.at_once);
+    // the least length there could be, and one at which it works out: work / length + all <= goal (in case FP32 says otherwise: no pieces)
+    uint32_t low = max((uint32_t)(work / (float)goal), 256u / KEYS), length = longest;
+    if (goal > all) {
+        const uint32_t enough = max((uint32_t)(work / (float)(goal - all)) + 1u, low);
+        if (last_lane(sums_to(items * pieces(enough))) <= goal) length = min(length, enough);
     }
     for (int step = 0; step < 5 && low < length; ++step) {
         const uint32_t middle = (low + length) / 2u;
-        if (last_lane(sums_to(items * pieces(middle))) <= a.slots)
+        if (last_lane(sums_to(items * pieces(middle))) <= goal)
             length = middle;
         else
             low = middle + 1u;
@@ -330,8 +346,6 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) :
     const int32_t end_i = TREE ? (int32_t)s.len : min(s.behind + (int32_t)(last_row / a.group) + 1, (int32_t)s.len);
     const uint32_t end = end_i > 0 ? (uint32_t)end_i : 0u;
     const int32_t all_see = TREE ? s.behind : s.behind + (int32_t)(row0 / a.group) + 1;  // keys that every row sees
-    const uint32_t *words = nullptr;
-    if constexpr (TREE) words = a.seen + (int64_t)(s.first + token) * a.seen_stride;
 
     const uint32_t tiles = (end + 31u) >> 5, per = (tiles + splits - 1u) / splits;
     const uint32_t t0 = min(split * per, tiles), t1 = min(t0 + per, tiles);
@@ -461,7 +475,7 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) :
         const bool some_hidden = (int32_t)(key0 + 32u) > all_see || key0 + 32u > end;
         if (some_hidden) {
             if constexpr (TREE) {
-                const uint32_t bits = seen_bits(words, a.seen_words, key0, s.behind, end) >> (4u * g);
+                const uint32_t bits = seen_bits(a, s.first + token, key0, s.behind, end) >> (4u * g);
 #pragma unroll
                 for (int r = 0; r < 8; ++r)
                     if (!(bits >> ((r < 4 ? 0 : 16) + (r & 3)) & 1u)) {
@@ -559,7 +573,7 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) :
 #pragma unroll 1
                 for (uint32_t key = 32u * t; key < min(32u * t + 32u, end); ++key) {
                     if constexpr (TREE) {
-                        if (!(seen_bits(words, a.seen_words, key, s.behind, end) & 1u)) continue;
+                        if (!(seen_bits(a, s.first + token, key, s.behind, end) & 1u)) continue;
                     } else {
                         if ((int32_t)key >= seen) continue;
                     }
@@ -678,18 +692,21 @@ __device__ __forceinline__ uint4 code_values(const Raw<BITS> &r)
 {
     if constexpr (BITS == 8) {
         const uint32_t a = r.w[0] ^ 0x80808080u, b = r.w[1] ^ 0x80808080u;
-        return make_uint4(from_bytes(__builtin_amdgcn_perm(0, a, 0x0C010C00u)), from_bytes(__builtin_amdgcn_perm(0, a, 0x0C030C02u)),
-                          from_bytes(__builtin_amdgcn_perm(0, b, 0x0C010C00u)), from_bytes(__builtin_amdgcn_perm(0, b, 0x0C030C02u)));
+        return make_uint4(from_bytes_of(a, 0), from_bytes_of(a, 2), from_bytes_of(b, 0), from_bytes_of(b, 2));
     } else {
         return nibble_values(r.w[0]);
     }
 }
 
-template <int BITS, int DP, bool TREE>
+//
+// With ON_KEYS == 2 a workgroup has 64 rows, and two wavefronts share 32 of them: each works on half of a tile's keys, and their results meet
+// in LDS at the end.
+template <int BITS, int DP, bool TREE, int ON_KEYS>
 __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(const ArgsOf<TREE> a)
 {
     constexpr int RC = DP <= 32 ? 4 : DP <= 64 ? 8 : DP <= 128 ? 16 : 32;              // 16-byte pieces of a row in LDS
-    constexpr int KT = RC == 32 ? 32 : 64, kHalves = KT / 32, kSteps = DP / 16, kTiles = DP / 32;
+    constexpr int KT = RC == 32 && ON_KEYS == 1 ? 32 : 64, kHalves = KT / 32 / ON_KEYS, kSteps = DP / 16, kTiles = DP / 32;       // halves: of a wavefront
+    constexpr uint32_t kRows = 128 / ON_KEYS;
     constexpr int kGroups = KT / 16;                                                   // a wavefront brings 16 keys; with 32, of K or of V
     constexpr int kIssues = RC / 4;                                                    // accesses per lane for 16 rows
     // (four objects and not two of twice the size: a read of LDS then waits for what is on its way into the same object only)
@@ -710,25 +727,24 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
     else
         tile -= (a.row_tiles + 1u) / 2u;
     if constexpr (TREE) {
-        const Share mine = share_of_work<128, KT>(a, tid < 64u);
+        const Share mine = share_of_work<kRows, KT>(a, tid < 64u);
         tile = mine.tile, split = mine.split, seq = mine.seq, splits = mine.splits, base = mine.base;
         if (splits == 0) return;
     }
     const Sequence s(a, seq);
-    const uint32_t rows = s.new_tokens * a.group, row0 = 128u * tile;
+    const uint32_t rows = s.new_tokens * a.group, row0 = kRows * tile;
     if (row0 >= rows) return;
     const uint32_t dim = a.cache.dim, pieces = dim / 8u;
 
-    const uint32_t row = min(row0 + 32u * wave + n, rows - 1u), token = row / a.group;
+    const uint32_t wave_row = row0 + 32u * (wave % (4u / ON_KEYS)), half0 = kHalves * (wave / (4u / ON_KEYS));     // first row, first half of a tile
+    const uint32_t row = min(wave_row + n, rows - 1u), token = row / a.group;
     const int32_t seen = min(s.behind + (int32_t)token + 1, (int32_t)s.len);
     auto sees = [&](uint32_t r) -> int32_t {                                           // keys up to the last one that row r sees
         return TREE ? (int32_t)s.len : max(min(s.behind + (int32_t)(min(r, rows - 1u) / a.group) + 1, (int32_t)s.len), 0);
     };
-    const uint32_t end = (uint32_t)sees(row0 + 127u);                                  // of the workgroup
+    const uint32_t end = (uint32_t)sees(row0 + kRows - 1u);                                  // of the workgroup
     const uint32_t all_see = TREE ? (uint32_t)max(s.behind, 0) : (uint32_t)sees(row0);
-    const uint32_t wave_end = row0 + 32u * wave < rows ? (uint32_t)sees(row0 + 32u * wave + 31u) : 0u;
-    const uint32_t *words = nullptr;
-    if constexpr (TREE) words = a.seen + (int64_t)(s.first + token) * a.seen_stride;
+    const uint32_t wave_end = wave_row < rows ? (uint32_t)sees(wave_row + 31u) : 0u;
 
     half8v q[kSteps];
     float q_sum = 0.0f;
@@ -768,7 +784,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
     const uint32_t group16 = kGroups == 4 ? wave : wave & 1u;
     const bool brings_k = kGroups == 4 || wave < 2u, brings_v = kGroups == 4 || wave >= 2u;
 
-    if (dim < (uint32_t)DP)
+    if (pieces < (uint32_t)RC)
         for (uint32_t i = tid; i < KT * RC; i += 256u)             // what is beyond dim stays zero
             lds_k0[i] = lds_k1[i] = lds_v0[i] = lds_v1[i] = make_uint4(0, 0, 0, 0);
     if (tid < 2u) lds_odd[tid] = 0;
@@ -895,7 +911,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
         auto read_k = [&](int y) {
 #pragma unroll
             for (int x = 0; x < kHalves; ++x) {
-                const uint32_t key = 32u * x + key_n;
+                const uint32_t key = 32u * (half0 + x) + key_n;
                 kf[x][y] = __builtin_bit_cast(half8v, lds_k[key * RC + ((2u * y + h) ^ k_swap<RC>(key))]);
             }
         };
@@ -909,7 +925,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
         s16x4 vf[kReads];
         auto read_v = [&](int i) {
             const int x = i / (2 * kTiles), y = i % (2 * kTiles) / 2, e = i % 2;
-            const uint32_t key = 16u * x + 8u * e + 4u * h + i16 / 4u;
+            const uint32_t key = 32u * half0 + 16u * x + 8u * e + 4u * h + i16 / 4u;
             const uint32_t c = 4u * y + 2u * sub + ((i16 >> 1) & 1u);
             const uint4 *p = &lds_v[key * RC + (c ^ v_swap<RC>(key))];
             vf[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(reinterpret_cast<const uint2 *>(p) + (i16 & 1u)));
@@ -932,7 +948,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
         if constexpr (BITS < 16) {
 #pragma unroll
             for (int i = 0; i < 16 * kHalves; i += 4) {            // (the steps of the keys have the scale in them)
-                const uint32_t key = 8u * (i / 4) + 4u * h;
+                const uint32_t key = 32u * half0 + 8u * (i / 4) + 4u * h;
                 const f32x4 step = *reinterpret_cast<const f32x4 *>(&lds_step[b][0][0][key]);
                 if constexpr (BITS == 4) {
                     const f32x4 low = *reinterpret_cast<const f32x4 *>(&lds_step[b][0][1][key]) * q_sum;
@@ -948,13 +964,13 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
             if constexpr (TREE)
 #pragma unroll
                 for (int x = 0; x < kHalves; ++x) {
-                    const uint32_t bits = seen_bits(words, a.seen_words, key0 + 32u * x, s.behind, end) >> (4u * h);
+                    const uint32_t bits = seen_bits(a, here(s.first + token), key0 + 32u * (half0 + x), s.behind, end) >> (4u * h);
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
                         if (!(bits >> (8 * (i / 4) + (i & 3)) & 1u)) w[16 * x + i] = kNone;
                 }
         } else if (masked) {
-            int32_t left = seen - (int32_t)(key0 + 4u * h);
+            int32_t left = seen - (int32_t)(key0 + 32u * half0 + 4u * h);
             asm volatile("" : "+v"(left));                         // (kept a branch: few tiles take it)
 #pragma unroll
             for (int i = 0; i < 16 * kHalves; ++i)
@@ -967,7 +983,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
         } else {
 #pragma unroll
             for (int i = 0; i < 16 * kHalves; i += 4) {
-                const f32x4 reach = *reinterpret_cast<const f32x4 *>(&lds_reach[b][8u * (i / 4) + 4u * h]);
+                const f32x4 reach = *reinterpret_cast<const f32x4 *>(&lds_reach[b][32u * half0 + 8u * (i / 4) + 4u * h]);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) most = fmaxf(most, w[i + r] + reach[r]);
             }
@@ -991,7 +1007,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
         if constexpr (BITS < 16) {
 #pragma unroll
             for (int i = 0; i < 16 * kHalves; i += 4) {
-                const uint32_t key = 8u * (i / 4) + 4u * h;
+                const uint32_t key = 32u * half0 + 8u * (i / 4) + 4u * h;
                 const f32x4 step = *reinterpret_cast<const f32x4 *>(&lds_step[b][1][0][key]);
                 if constexpr (BITS == 4) {
                     const f32x4 low = *reinterpret_cast<const f32x4 *>(&lds_step[b][1][1][key]);
@@ -1067,7 +1083,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
 #pragma unroll 1
             for (uint32_t key = t0 * KT; key < last; ++key) {
                 if constexpr (TREE) {
-                    if (!(seen_bits(words, a.seen_words, key, s.behind, end) & 1u)) continue;
+                    if (!(seen_bits(a, s.first + token, key, s.behind, end) & 1u)) continue;
                 } else {
                     if ((int32_t)key >= seen) continue;
                 }
@@ -1086,7 +1102,35 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
 
     l += __shfl_xor(l, 32, 64);
     if constexpr (BITS == 4) z_acc += __shfl_xor(z_acc, 32, 64);
-    const uint32_t out_row = row0 + 32u * wave + n;
+    if constexpr (ON_KEYS == 2) {
+        // the second half's results to the wavefront that has the first (the last tile has been waited for by all)
+        __shared__ float lds_mlz[2][3][32];
+        const uint32_t pair = wave & 1u;
+        uint4 *to = pair ? lds_v0 : lds_k0;
+        if (wave >= 2u) {
+#pragma unroll
+            for (int y = 0; y < kTiles; ++y)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    to[64u * (4 * y + i) + lane] = __builtin_bit_cast(uint4, f32x4{acc[y][4 * i], acc[y][4 * i + 1], acc[y][4 * i + 2], acc[y][4 * i + 3]});
+            if (h == 0) lds_mlz[pair][0][n] = m, lds_mlz[pair][1][n] = l, lds_mlz[pair][2][n] = z_acc;
+        }
+        __syncthreads();
+        if (wave >= 2u) return;
+        const float other = lds_mlz[pair][0][n], top = fmaxf(m, other), f0 = share_of(m, top), f1 = share_of(other, top);
+        m = top;
+        l = f0 * l + f1 * lds_mlz[pair][1][n];
+        z_acc = f0 * z_acc + f1 * lds_mlz[pair][2][n];
+#pragma unroll
+        for (int y = 0; y < kTiles; ++y)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const f32x4 o = __builtin_bit_cast(f32x4, to[64u * (4 * y + i) + lane]);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[y][4 * i + r] = f0 * acc[y][4 * i + r] + f1 * o[r];
+            }
+    }
+    const uint32_t out_row = wave_row + n;
     if (out_row >= rows) return;
     const uint32_t out_head = head * a.group + (row - token * a.group);
     if (splits == 1u) {
@@ -1291,7 +1335,7 @@ int launch_rows(const ArgsOf<kTree> &a, void *stream)
     return ecs::launch_args<attention_rows_kernel<BITS, 256, true, kTree>>(a, gx, gy, gz, 256, stream);
 }
 
-template <int BITS>
+template <int BITS, int ON_KEYS>
 int launch_chunk(const ArgsOf<kTree> &a, void *stream)
 {
 #ifdef ECS_TREE
@@ -1300,21 +1344,24 @@ int launch_chunk(const ArgsOf<kTree> &a, void *stream)
     const uint32_t gx = a.cache.heads, gy = a.row_tiles * a.splits, gz = a.batch;
 #endif
     switch ((a.cache.dim + 31u) / 32u) {
-    case 1: return ecs::launch_args<attention_chunk_kernel<BITS, 32, kTree>>(a, gx, gy, gz, 256, stream);
-    case 2: return ecs::launch_args<attention_chunk_kernel<BITS, 64, kTree>>(a, gx, gy, gz, 256, stream);
-    case 3: return ecs::launch_args<attention_chunk_kernel<BITS, 96, kTree>>(a, gx, gy, gz, 256, stream);
-    case 4: return ecs::launch_args<attention_chunk_kernel<BITS, 128, kTree>>(a, gx, gy, gz, 256, stream);
-    case 5: return ecs::launch_args<attention_chunk_kernel<BITS, 160, kTree>>(a, gx, gy, gz, 256, stream);
-    case 6: return ecs::launch_args<attention_chunk_kernel<BITS, 192, kTree>>(a, gx, gy, gz, 256, stream);
-    case 7: return ecs::launch_args<attention_chunk_kernel<BITS, 224, kTree>>(a, gx, gy, gz, 256, stream);
-    default: return ecs::launch_args<attention_chunk_kernel<BITS, 256, kTree>>(a, gx, gy, gz, 256, stream);
+    case 1: return ecs::launch_args<attention_chunk_kernel<BITS, 32, kTree, ON_KEYS>>(a, gx, gy, gz, 256, stream);
+    case 2: return ecs::launch_args<attention_chunk_kernel<BITS, 64, kTree, ON_KEYS>>(a, gx, gy, gz, 256, stream);
+    case 3: return ecs::launch_args<attention_chunk_kernel<BITS, 96, kTree, ON_KEYS>>(a, gx, gy, gz, 256, stream);
+    case 4: return ecs::launch_args<attention_chunk_kernel<BITS, 128, kTree, ON_KEYS>>(a, gx, gy, gz, 256, stream);
+    case 5: return ecs::launch_args<attention_chunk_kernel<BITS, 160, kTree, ON_KEYS>>(a, gx, gy, gz, 256, stream);
+    case 6: return ecs::launch_args<attention_chunk_kernel<BITS, 192, kTree, ON_KEYS>>(a, gx, gy, gz, 256, stream);
+    case 7: return ecs::launch_args<attention_chunk_kernel<BITS, 224, kTree, ON_KEYS>>(a, gx, gy, gz, 256, stream);
+    default: return ecs::launch_args<attention_chunk_kernel<BITS, 256, kTree, ON_KEYS>>(a, gx, gy, gz, 256, stream);
     }
 }
 
 template <int BITS>
 int launch_bits(const ArgsOf<kTree> &a, void *stream)
 {
-    return a.chunk ? launch_chunk<BITS>(a, stream) : launch_rows<BITS>(a, stream);
+#ifdef ECS_TREE
+    if (a.chunk == 2u) return launch_chunk<BITS, 2>(a, stream);
+#endif
+    return a.chunk ? launch_chunk<BITS, 1>(a, stream) : launch_rows<BITS>(a, stream);
 }
 
 int launch_join(const ArgsOf<kTree> &a, void *stream)
@@ -1367,23 +1414,38 @@ AttentionPlan plan_attention(uint32_t batch, uint32_t kv_heads, uint32_t group, 
     return p;
 }
 
-// Of trees: how the launch's workgroups are dealt out, and whether by the sequences' lengths (share_of_work)
-TreePlan plan_attention_tree(uint32_t batch, uint32_t kv_heads, uint32_t group, uint32_t dim, uint32_t bits, uint64_t tokens, uint32_t max_new,
+// Of trees.  Rows per workgroup: 16 that bring their keys themselves, or 64 or 128 that share them in LDS; us by 16 / 64 / 128 (heads of 128 where not
+// said): 32 rows on up to 8000 keys of four sequences FP16 - / 75 / 80, 8 bits 45.6 / 54.0 / -, 4 bits 48 / 69 / -; 40 on 3000, 4 bits, 72.9 / 68.5 / -; 64 on
+// 8000, 8 bits, - / 77 / 87, 4 bits 72 / 64 / -; 100 on 4000, FP16, - / 34.5 / 37.5; 128 on 8192 of sixteen, 8 bits, - / 156 / 125, FP16 equal; heads of 256,
+// 128 rows on 8000, FP16, - / 39.5 / 46.8, 192 of four, 8 bits, - / 27.5 / 36.6.
+constexpr uint32_t kHalfRows = 64;
+static uint32_t tree_rows_of_16(uint32_t dim, uint32_t bits) { return dim <= 128u && bits == 16u ? kFewRows : 2u * kFewRows; }
+
+TreePlan plan_attention_tree(uint32_t batch, uint32_t kv_heads, uint32_t group, uint32_t dim, uint32_t bits, uint32_t max_new, uint64_t tokens,
                              uint64_t max_kv)
 {
     TreePlan t = {};
-    static_cast<AttentionPlan &>(t) = plan_attention(batch, kv_heads, group, dim, bits, tokens, max_new, max_kv);
-    const uint64_t wanted = (t.chunk ? kChunkWanted : kFewWanted) / kv_heads, items = (uint64_t)batch * t.row_tiles;
-    // One sequence with a tile of rows for every workgroup, and sequences that fill the chip twice over, are left whole
-    t.balanced = batch <= 64u && splits_of_keys(max_kv) > 1u && (batch > 1u ? items < 2u * wanted : items < wanted);
-    if (t.balanced) {
-        t.slots = std::max(items, wanted);
-        t.splits = 1;
-        t.part_rows = (uint32_t)std::min<uint64_t>(t.slots * (t.chunk ? kChunkRows : kFewRows), splits_of_keys(max_kv) * std::min<uint64_t>(tokens, (uint64_t)batch * max_new) * group);
-        t.work_bytes = kTreePlanBytes + (uint64_t)t.part_rows * kv_heads * (dim + 2u) * sizeof(float);
-    } else {
-        if (batch <= 64u) t.splits = 1, t.work_bytes = 0;
+    const uint64_t rows = (uint64_t)max_new * group, keys = splits_of_keys(max_kv);
+    t.chunk = rows <= tree_rows_of_16(dim, bits) ? 0u : dim > 128u || rows <= kHalfRows ? 2u : 1u;
+    const uint32_t per_tile = t.chunk == 0u ? kFewRows : t.chunk == 1u ? kChunkRows : kHalfRows;
+    t.row_tiles = (uint32_t)((rows + per_tile - 1u) / per_tile);
+    // Pieces for the workgroups that the chip holds at once, by the kernels' registers and LDS (heads of 256, 8 tokens over 8000 keys in FP16: by 1024
+    // workgroups 22.3 us, by 256 20.1; two of up to 8000 in 8 bits, heads of 128, 1024 41.5, 768 37.9)
+    const uint64_t resident = t.chunk ? (dim > 128u ? 256u : 512u) : dim <= 64u ? 1024u : dim <= 128u ? 768u : bits == 4u ? 512u : 256u;
+    const uint64_t at_once = resident / kv_heads, items = (uint64_t)batch * t.row_tiles;
+    t.splits = 1;
+    t.slots = items;
+    if (batch > kTreeSequences) {                                  // (more sequences than the lanes of a wavefront: equal splits for all)
+        t.splits = (uint32_t)std::max<uint64_t>(1u, std::min(at_once / std::max<uint64_t>(items, 1u), keys));
         t.slots = items * t.splits;
+        if (t.splits > 1u) t.work_bytes = (uint64_t)t.splits * tokens * kv_heads * group * (dim + 2u) * sizeof(float);
+    } else if (keys > 1u && (batch > 1u ? items < 2u * at_once : items < at_once)) {
+        // (one sequence with a tile of rows for every workgroup, and several that fill the chip twice over, are left whole)
+        t.balanced = 1;
+        t.at_once = (uint32_t)at_once;
+        t.slots = std::max(items, at_once);
+        t.part_rows = (uint32_t)std::min<uint64_t>(t.slots * per_tile, keys * std::min<uint64_t>(tokens, (uint64_t)batch * max_new) * group);
+        t.work_bytes = kTreePlanBytes + (uint64_t)t.part_rows * kv_heads * (dim + 2u) * sizeof(float);
     }
     return t;
 }
@@ -1396,7 +1458,7 @@ uint64_t most_attention_work(uint32_t batch, uint32_t kv_heads, uint32_t group, 
     const uint64_t few = rows_of_16(dim, bits), by_keys = splits_of_keys(max_kv);
     uint64_t most = 0;
     if (group <= few) most = (uint64_t)kFewWanted * kFewRows * (batch > 1u ? 2u : 1u);
-    if ((uint64_t)max_new * group > few) most = std::max<uint64_t>(most, (uint64_t)kChunkWanted * kChunkRows * (batch > 1u ? 2u : 1u));
+    if ((uint64_t)max_new * group > tree_rows_of_16(dim, bits)) most = std::max<uint64_t>(most, (uint64_t)kChunkWanted * kChunkRows * (batch > 1u ? 2u : 1u));
     if (by_keys <= 1u) return 0;
     const uint64_t rows = std::min<uint64_t>(tokens, (uint64_t)batch * max_new) * kv_heads * group;
     return kTreePlanBytes + std::min(most, by_keys * rows) * (dim + 2u) * sizeof(float);

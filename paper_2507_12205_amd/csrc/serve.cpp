@@ -130,7 +130,7 @@ int check_attention_tree(const ecspmv_kv_cache_t *cache, const ecspmv_attention_
     ecs::AttentionPlan rows;
     const int s = check_attention(cache, from, a, rows, t);
     if (s) return s;
-    plan = ecs::plan_attention_tree(a.batch, a.cache.heads, a.group, a.cache.dim, a.cache.bits, a.tokens, a.max_new,
+    plan = ecs::plan_attention_tree(a.batch, a.cache.heads, a.group, a.cache.dim, a.cache.bits, a.max_new, a.tokens,
                                     (uint64_t)a.max_pages << a.cache.page_shift);
     if (plan.slots > 0x7fffffffu) return ECSPMV_ERR_UNSUPPORTED;
     a.chunk = plan.chunk;
@@ -139,6 +139,7 @@ int check_attention_tree(const ecspmv_kv_cache_t *cache, const ecspmv_attention_
     a.slots = (uint32_t)plan.slots;
     a.balanced = plan.balanced;
     a.part_rows = plan.part_rows;
+    a.at_once = plan.at_once;
     a.seen_words = (a.max_new + 31u) / 32u;
     return ECSPMV_OK;
 }

@@ -66,7 +66,7 @@ struct AttentionArgs {
     float *part_o, *part_ml;              // partial results of the splits (splits > 1)
     uint32_t tokens, q_heads, group;      // group: heads of q per head of the cache
     uint32_t batch, max_pages, max_new;
-    uint32_t chunk, row_tiles, splits;    // chunk: 128 rows per workgroup instead of 16
+    uint32_t chunk, row_tiles, splits;    // chunk: 128 rows per workgroup instead of 16 (2, with trees: 64)
     uint32_t q_wide, out_wide;
     float scale_log2;                     // scale * log2(e)
     bool joins() const { return splits > 1u; }
@@ -82,18 +82,20 @@ uint64_t most_attention_work(uint32_t batch, uint32_t kv_heads, uint32_t group, 
                              uint64_t max_kv);
 int launch_attention(const AttentionArgs &a, void *stream);
 
-constexpr uint32_t kTreePlanBytes = 1024; // of the workspace: four words for each of 64 sequences
+constexpr uint32_t kTreeSequences = 64;   // that are dealt out by their lengths
+constexpr uint32_t kTreePlanBytes = 16 * kTreeSequences;                  // of the workspace: four words for each
 struct TreePlan : AttentionPlan {
     uint64_t slots;                       // workgroups to a head
     uint32_t balanced, part_rows;         // shares by the sequences' lengths; rows of partial results that there is room for
+    uint32_t at_once;                     // balanced: workgroups to a head that the chip has at once
 };
-TreePlan plan_attention_tree(uint32_t batch, uint32_t kv_heads, uint32_t group, uint32_t dim, uint32_t bits, uint64_t tokens, uint32_t max_new,
+TreePlan plan_attention_tree(uint32_t batch, uint32_t kv_heads, uint32_t group, uint32_t dim, uint32_t bits, uint32_t max_new, uint64_t tokens,
                              uint64_t max_kv);
 struct AttentionTreeArgs : AttentionArgs {
     const uint32_t *seen;                 // bit i of a token's words: it sees its sequence's i-th new token
     int64_t seen_stride;                  // words from one token to the next
     uint32_t seen_words;                  // words that count
-    uint32_t slots, balanced, part_rows;  // as planned
+    uint32_t slots, balanced, part_rows, at_once;               // as planned
     struct alignas(16) Words {
         uint32_t x, y, z, w;
     } *plan;                              // where shares are balanced, of each sequence: splits, first row of its partial results, first token, tokens

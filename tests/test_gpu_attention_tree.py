@@ -58,6 +58,9 @@ CASES = [
     ([8], [1000], 4, 4, 128, 32), ([3, 1, 7, 2], [3, 17, 260, 513], 8, 2, 128, 16), ([17, 40], [17, 333], 6, 2, 80, 32),
     ([130], [130], 2, 1, 96, 16), ([65, 1, 33], [700, 1, 33], 4, 4, 64, 128), ([5], [4100], 2, 2, 256, 256), ([200], [456], 3, 3, 128, 64),
     ([31, 32], [100, 63], 16, 1, 240, 16), ([70], [71], 5, 5, 48, 1024), ([64], [1025], 2, 2, 128, 16), ([300], [999], 4, 1, 64, 32),
+    ([40], [500], 4, 4, 160, 16), ([20, 50], [300, 800], 2, 2, 192, 16), ([100], [400], 2, 1, 224, 32), ([60], [1200], 8, 8, 32, 16),
+    ([9, 30, 2, 0, 1], [3000, 700, 5, 40, 2100], 4, 4, 128, 16), ([3, 5, 1] * 30, [900, 5, 300] * 30, 4, 2, 64, 16),
+    ([50, 1] * 32, [60, 600] * 32, 2, 2, 64, 16), ([130, 260], [2000, 900], 2, 2, 128, 64),
 ]
 
 
