@@ -69,7 +69,7 @@ __global__ __launch_bounds__(256) void kv_write_kernel(const KvArgs a)
         float x[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = to_float(e.get(i));
-        ecs::store_codes<BITS, false>(x, codes, steps, r.at, a.cache.dim, a.lanes_shift, r.valid);
+        ecs::store_codes<BITS, false>(x, codes, steps, {r.at}, a.cache.dim, a.lanes_shift, r.valid);
     }
 }
 

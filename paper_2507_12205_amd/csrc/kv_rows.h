@@ -49,36 +49,39 @@ __device__ __forceinline__ void store_eight(const View &v, uint32_t wide, uint32
     }
 }
 
-// The codes and the step of a row of 2^lanes_shift neighbouring lanes, eight values x of it in each (none in a lane with at >= dim), to where they lie;
-// `valid`: whether the row has a place.  All lanes of the row come here.  FIFTEENTH: a 4-bit step is the range times 1/15 in FP32, which may be its
-// last place away from the range divided by 15, and saves the division.
-template <int BITS, bool FIFTEENTH>
-__device__ __forceinline__ void store_codes(float (&x)[8], uint8_t *codes, uint8_t *steps, uint32_t at, uint32_t dim, uint32_t lanes_shift, bool valid)
+// The codes and the step of a row that 2^lanes_shift neighbouring lanes have, N values each in pieces of eight that start at at[...] of the row (a piece
+// that starts beyond it is none), to where they lie; `valid`: whether the row has a place.  All lanes of the row come here.  FIFTEENTH: a 4-bit
+// step is the range times 1/15 in FP32, which may be its last place away from the range divided by 15, and saves the division.
+template <int BITS, bool FIFTEENTH, int N>
+__device__ __forceinline__ void store_codes(float (&x)[N], uint8_t *codes, uint8_t *steps, const uint32_t (&at)[N / 8], uint32_t dim, uint32_t lanes_shift,
+                                            bool valid)
 {
     float low = 65504.0f, high = -65504.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < N; ++i) {
         x[i] = x[i] != x[i] ? 0.0f : fminf(fmaxf(x[i], -65504.0f), 65504.0f);
-        low = fminf(low, x[i]);
-        high = fmaxf(high, x[i]);
+        if (at[i / 8] < dim) {
+            low = fminf(low, x[i]);
+            high = fmaxf(high, x[i]);
+        }
     }
-    if (at >= dim) low = 65504.0f, high = -65504.0f;                      // a lane without values
     for (uint32_t o = 1u; o < 1u << lanes_shift; o <<= 1) {
         low = fminf(low, __shfl_xor(low, (int)o, 64));
         high = fmaxf(high, __shfl_xor(high, (int)o, 64));
     }
     if constexpr (BITS == 8) {
         const float most = fmaxf(-low, high), step = most / 127.0f, inv = most > 0.0f ? 1.0f / most * 127.0f : 0.0f;
-        uint32_t w[2] = {0, 0};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int c = (int)fminf(fmaxf(rintf(x[i] * inv), -127.0f), 127.0f);
-            w[i >> 2] |= ((uint32_t)c & 0xFFu) << (8 * (i & 3));
+        for (int k = 0; k < N / 8; ++k) {
+            uint32_t w[2] = {0, 0};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int c = (int)fminf(fmaxf(rintf(x[8 * k + i] * inv), -127.0f), 127.0f);
+                w[i >> 2] |= ((uint32_t)c & 0xFFu) << (8 * (i & 3));
+            }
+            if (valid && at[k] < dim) *reinterpret_cast<uint2 *>(codes + at[k]) = make_uint2(w[0], w[1]);
         }
-        if (valid) {
-            *reinterpret_cast<uint2 *>(codes + at) = make_uint2(w[0], w[1]);
-            if (at == 0) *reinterpret_cast<float *>(steps) = step;
-        }
+        if (valid && at[0] == 0) *reinterpret_cast<float *>(steps) = step;
     } else {
         const uint32_t low_bits = to_half(low);
         low = to_float(low_bits);
@@ -88,13 +91,14 @@ __device__ __forceinline__ void store_codes(float (&x)[8], uint8_t *codes, uint8
         uint32_t step_bits = to_half(wide_step);
         if (fmaf(15.0f, to_float(step_bits), low) >= 65520.0f) --step_bits;  // (rounded up, and the last code would be infinity in FP16)
         const float step = to_float(step_bits), inv = step > 0.0f ? 1.0f / step : 0.0f;
-        uint32_t w = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w |= (uint32_t)fminf(fmaxf(rintf((x[i] - low) * inv), 0.0f), 15.0f) << (4 * i);
-        if (valid) {
-            *reinterpret_cast<uint32_t *>(codes + (at >> 1)) = w;
-            if (at == 0) *reinterpret_cast<uint32_t *>(steps) = step_bits | low_bits << 16;
+        for (int k = 0; k < N / 8; ++k) {
+            uint32_t w = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w |= (uint32_t)fminf(fmaxf(rintf((x[8 * k + i] - low) * inv), 0.0f), 15.0f) << (4 * i);
+            if (valid && at[k] < dim) *reinterpret_cast<uint32_t *>(codes + (at[k] >> 1)) = w;
         }
+        if (valid && at[0] == 0) *reinterpret_cast<uint32_t *>(steps) = step_bits | low_bits << 16;
     }
 }
 

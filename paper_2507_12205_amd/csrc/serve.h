@@ -39,11 +39,11 @@ struct AppendArgs {
     const int32_t *position;
     const double *frequency;              // of each pair
     uint32_t tokens, q_heads, pairs, neighbours;
-    uint32_t lanes_shift, run_shift;      // as in KvArgs
-    uint32_t heads_per_block;             // heads of q, k and v, one after the other, that a workgroup takes
+    uint32_t lanes_shift, run_shift;      // as in KvArgs, but a lane has 16 values
+    uint32_t heads_per_block, q_blocks;   // heads of q, or of k and v, that a workgroup takes; workgroups for q
     uint32_t q_wide, q_out_wide, k_wide, v_wide;
 };
-int launch_kv_append(AppendArgs &a, void *stream);                         // (chooses heads_per_block)
+int launch_kv_append(AppendArgs &a, void *stream);                         // (chooses lanes_shift, heads_per_block, q_blocks)
 
 constexpr uint32_t kKeepLayers = 64;      // of a launch
 struct KeepArgs {
