@@ -89,8 +89,10 @@ class VerifyDesc(Structure):
 
 
 class RotaryDesc(Structure):
+    """The views of q and q_out field by field: an object less for each."""
     _fields_ = [("struct_size", c_uint32), ("rotary_dim", c_int32), ("neighbours", c_int32), ("q_heads", c_int32), ("frequency", c_void_p),
-                ("position", c_void_p), ("q", View), ("q_out", View)]
+                ("position", c_void_p), ("q", c_void_p), ("q_token_stride", c_int64), ("q_head_stride", c_int64), ("q_dim_stride", c_int64),
+                ("q_out", c_void_p), ("q_out_token_stride", c_int64), ("q_out_head_stride", c_int64), ("q_out_dim_stride", c_int64)]
 
 
 class KeepDesc(Structure):

@@ -374,7 +374,7 @@ int ecspmv_verify_tree_workspace(const ecspmv_verify_tree_t *from, size_t *bytes
     const int s = check_verify_tree(from, t);
     if (s) return s;
     if (!bytes) return ECSPMV_ERR_INVALID;
-    *bytes = (size_t)ecs::verify_tree_work_bytes((uint32_t)t.batch, (uint32_t)t.vocab);
+    *bytes = (size_t)ecs::verify_tree_work_bytes((uint32_t)t.batch, (uint32_t)t.nodes, (uint32_t)t.vocab);
     return ECSPMV_OK;
 }
 
@@ -385,7 +385,7 @@ int ecspmv_verify_tree(const ecspmv_verify_tree_t *from, void *d_work, size_t wo
     if (s) return s;
     if (t.batch == 0) return ECSPMV_OK;
     if (!d_work || !aligned(d_work, 8)) return ECSPMV_ERR_INVALID;
-    if (work_bytes < ecs::verify_tree_work_bytes((uint32_t)t.batch, (uint32_t)t.vocab)) return ECSPMV_ERR_TOO_SMALL;
+    if (work_bytes < ecs::verify_tree_work_bytes((uint32_t)t.batch, (uint32_t)t.nodes, (uint32_t)t.vocab)) return ECSPMV_ERR_TOO_SMALL;
     if (!t.target || !t.uniform || !t.tokens || !t.accepted || (t.nodes && (!t.drafted || !t.parent || !t.path))) return ECSPMV_ERR_INVALID;
     const void *all[] = {t.target, t.uniform, t.drafted, t.parent, t.count, t.tokens, t.path, t.accepted};
     for (const void *p : all)
@@ -404,7 +404,7 @@ int ecspmv_verify_tree(const ecspmv_verify_tree_t *from, void *d_work, size_t wo
     a.target_row = t.target_row;
     a.nodes = (uint32_t)t.nodes;
     a.vocab = (uint32_t)t.vocab;
-    a.sums = static_cast<double *>(d_work);
+    a.work = static_cast<uint8_t *>(d_work);
     return ecs::hip_status(ecs::launch_verify_tree(a, (uint32_t)t.batch, stream));
 }
 

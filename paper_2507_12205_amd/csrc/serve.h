@@ -121,9 +121,9 @@ struct VerifyTreeArgs {
     int32_t *tokens, *path, *accepted;
     int64_t target_seq, target_row;       // strides in elements
     uint32_t nodes, vocab;
-    double *sums;                         // verify_tree_work_bytes
+    uint8_t *work;                        // verify_tree_work_bytes
 };
-uint64_t verify_tree_work_bytes(uint32_t batch, uint32_t vocab);
+uint64_t verify_tree_work_bytes(uint32_t batch, uint32_t nodes, uint32_t vocab);
 int launch_verify_tree(const VerifyTreeArgs &a, uint32_t batch, void *stream);
 
 }  // namespace ecs

@@ -9,7 +9,9 @@
 // for the children of the node that it is at.  Everything that the walk needs of p is asked for at once, before it starts.
 //
 // Two launches, as for drafts in a row (verify.hip): the first adds up tiles of the row that counts, each workgroup after a walk of its
-// own, the second draws the token.
+// own, one of which writes down what came of it; the second draws the token.  What bounds it are the trips to memory, one after the other: the
+// tree, its p, the row; the sums, the tile.  26 nodes over 32000 tokens @A us, 32 sequences of up to 63 over 128256 @B (with a second walk in the
+// second launch instead of the first one's result 12.3 and 18.3).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -91,8 +93,9 @@ __device__ __forceinline__ void walk_tree(const VerifyTreeArgs &a, uint32_t seq,
                 const uint64_t children = __ballot(parent == at && !dead);
                 if (!children) break;
                 const int j = __ffsll((unsigned long long)children) - 1;
-                const float pj = __shfl(p, j, 64), uj = __shfl(u, j, 64);
-                const int32_t x = __shfl(token, j, 64);
+                const float pj = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(p), j));
+                const float uj = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(u), j));
+                const int32_t x = __builtin_amdgcn_readlane(token, j);
                 if (x >= 0 && (double)uj * left < (double)pj) {
                     at = (int32_t)(i0 + j);
                     if (lane == 0) s.path[n] = at;
@@ -117,20 +120,25 @@ __device__ __forceinline__ void walk_tree(const VerifyTreeArgs &a, uint32_t seq,
     __syncthreads();
 }
 
-__device__ __forceinline__ Weights weights_of(const VerifyTreeArgs &a, uint32_t seq, const Walk &s)
+// What a walk leaves for the second launch, behind a sequence's sums: accepted, refused, the row of p that counts; the refused tokens
+struct Left {
+    int32_t accepted, refused, row, pad;
+    int32_t gone[];
+};
+__device__ __forceinline__ uint32_t sequence_bytes(uint32_t nodes, uint32_t vocab)
 {
-    const int32_t row = s.accepted ? s.path[s.accepted - 1u] + 1 : 0;
-    return {a.target + seq * a.target_seq + row * a.target_row, s.gone, s.refused, a.vocab};
+    return (vocab + kTile - 1u) / kTile * 8u + (uint32_t)sizeof(Left) + (nodes + 1u) / 2u * 8u;
 }
 
 __global__ __launch_bounds__(kThreads) void verify_tree_sums_kernel(const VerifyTreeArgs a)
 {
     __shared__ Walk s;
-    const uint32_t seq = blockIdx.y, lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    const uint32_t seq = blockIdx.y, tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
     walk_tree(a, seq, s);
-    const Weights w = weights_of(a, seq, s);
-    const uint32_t tiles = (a.vocab + kTile - 1u) / kTile;
-    double *sums = a.sums + (size_t)seq * tiles;
+    const uint32_t n = s.accepted, refused = s.refused, tiles = (a.vocab + kTile - 1u) / kTile;
+    const int32_t row = n ? s.path[n - 1u] + 1 : 0;
+    double *sums = reinterpret_cast<double *>(a.work + (size_t)seq * sequence_bytes(a.nodes, a.vocab));
+    const Weights w = {a.target + seq * a.target_seq + row * a.target_row, s.gone, refused, a.vocab};
 #pragma unroll
     for (uint32_t k = 0; k < kTilesPerBlock / (kThreads / 64u); ++k) {
         const uint32_t t = blockIdx.x * kTilesPerBlock + k * (kThreads / 64u) + wave;
@@ -138,32 +146,44 @@ __global__ __launch_bounds__(kThreads) void verify_tree_sums_kernel(const Verify
         const double sum = ecs::tile_sum(w, t, lane);
         if (lane == 0) sums[t] = sum;
     }
+    if (blockIdx.x) return;
+    Left *left = reinterpret_cast<Left *>(sums + tiles);
+    if (tid == 0) {
+        left->accepted = (int32_t)n, left->refused = (int32_t)refused, left->row = row;
+        a.accepted[seq] = (int32_t)n;
+    }
+    for (uint32_t i = tid; i < refused; i += kThreads) left->gone[i] = s.gone[i];
+    int32_t *tokens = a.tokens + (size_t)seq * (a.nodes + 1u), *path = a.path + (size_t)seq * a.nodes;
+    for (uint32_t i = tid; i <= a.nodes; i += kThreads) {
+        const int32_t node = i < n ? s.path[i] : -1;
+        if (i != n) tokens[i] = i < n ? s.token[node] : -1;
+        if (i < a.nodes) path[i] = node;
+    }
 }
 
 __global__ __launch_bounds__(kThreads) void verify_tree_token_kernel(const VerifyTreeArgs a)
 {
-    __shared__ Walk s;
+    __shared__ int32_t gone[kMostNodes];
     __shared__ ecs::Drawing shared;
-    const uint32_t seq = blockIdx.x, tid = threadIdx.x;
-    walk_tree(a, seq, s);
-    Weights w = weights_of(a, seq, s);
-    const uint32_t tiles = (a.vocab + kTile - 1u) / kTile, n = s.accepted;
+    const uint32_t seq = blockIdx.x, tid = threadIdx.x, tiles = (a.vocab + kTile - 1u) / kTile;
+    const double *sums = reinterpret_cast<const double *>(a.work + (size_t)seq * sequence_bytes(a.nodes, a.vocab));
+    const Left *left = reinterpret_cast<const Left *>(sums + tiles);
     const double u = (double)a.uniform[(size_t)seq * (a.nodes + 1u) + a.nodes];
-    const int32_t token = ecs::draw_token(w, a.sums + (size_t)seq * tiles, u, a.vocab, shared);
-    int32_t *tokens = a.tokens + (size_t)seq * (a.nodes + 1u), *path = a.path + (size_t)seq * a.nodes;
-    for (uint32_t i = tid; i <= a.nodes; i += kThreads) {
-        const int32_t node = i < n ? s.path[i] : -1;
-        tokens[i] = i < n ? s.token[node] : i == n ? token : -1;
-        if (i < a.nodes) path[i] = node;
-    }
-    if (tid == 0) a.accepted[seq] = (int32_t)n;
+    const uint32_t n = (uint32_t)left->accepted, refused = (uint32_t)left->refused;
+    for (uint32_t i = tid; i < a.nodes; i += kThreads) gone[i] = left->gone[i];          // (all that there is room for: not waiting for how many)
+    Weights w = {a.target + seq * a.target_seq + left->row * a.target_row, gone, refused, a.vocab};
+    const int32_t token = ecs::draw_token(w, sums, u, a.vocab, shared);    // (a barrier before `gone` is read)
+    if (tid == 0) a.tokens[(size_t)seq * (a.nodes + 1u) + n] = token;
 }
 
 }  // namespace
 
 namespace ecs {
 
-uint64_t verify_tree_work_bytes(uint32_t batch, uint32_t vocab) { return (uint64_t)batch * ((vocab + kTile - 1u) / kTile) * sizeof(double); }
+uint64_t verify_tree_work_bytes(uint32_t batch, uint32_t nodes, uint32_t vocab)
+{
+    return (uint64_t)batch * ((uint64_t)((vocab + kTile - 1u) / kTile) * 8u + 16u + (nodes + 1u) / 2u * 8u);
+}
 
 int launch_verify_tree(const VerifyTreeArgs &a, uint32_t batch, void *stream)
 {

@@ -167,20 +167,24 @@ def kv_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Ten
     """kv_write() of keys that are rotated by their tokens' positions, (tokens,) int32, on the way; queries q, (tokens, q_heads, head_dim) FP16 with
     any strides, are rotated into q_out (q itself if not given), which is returned.  frequency: (pairs,) FP64 radians a position (rotary_frequency());
     pair i of a head is its values i and i + pairs, or with `neighbours` values 2 i and 2 i + 1; the values beyond 2 * pairs stay as they are."""
-    _rows_of(cache, k, v, slots)
-    pairs, = frequency.shape
-    assert position.dtype is torch.int32 and position.shape == slots.shape and position.is_contiguous() and position.get_device() == cache.device
-    assert frequency.dtype is torch.float64 and frequency.is_contiguous() and frequency.get_device() == cache.device
-    r = B.RotaryDesc(_ROTARY, 2 * pairs, 1 if neighbours else 0, 0, frequency.data_ptr() or None, position.data_ptr() or None)
+    device, shape = cache.device, k.shape
+    assert k.dtype is v.dtype is torch.float16 and slots.dtype is torch.int64 and position.dtype is torch.int32 and frequency.dtype is torch.float64
+    assert device == k.get_device() == v.get_device() == slots.get_device() == position.get_device() == frequency.get_device()
+    tokens, pairs = slots.numel(), frequency.numel()
+    assert shape == v.shape == (tokens, cache.heads, cache.head_dim) and slots.dim() == position.dim() == frequency.dim() == 1
+    assert position.numel() == tokens and slots.is_contiguous() and position.is_contiguous() and frequency.is_contiguous()
     if q is None:
         assert q_out is None
+        r = B.RotaryDesc(_ROTARY, 2 * pairs, neighbours, 0, frequency.data_ptr(), position.data_ptr())
     else:
         if q_out is None:
             q_out = q
-        assert q.dtype is q_out.dtype is torch.float16 and q.get_device() == q_out.get_device() == cache.device
-        assert q.dim() == 3 and q.shape == q_out.shape and q.shape[0] == slots.shape[0] and q.shape[2] == cache.head_dim
-        r.q_heads, r.q, r.q_out = q.shape[1], _view(q), _view(q_out)
-    B.ecspmv_kv_append(cache.desc, _view(k), _view(v), slots.data_ptr(), slots.shape[0], r, _stream_handle(stream))
+        q_tokens, q_heads, dim = q.shape
+        assert q.dtype is q_out.dtype is torch.float16 and device == q.get_device() == q_out.get_device()
+        assert q_tokens == tokens and dim == cache.head_dim and q_out.shape == q.shape
+        r = B.RotaryDesc(_ROTARY, 2 * pairs, neighbours, q_heads, frequency.data_ptr(), position.data_ptr(), q.data_ptr(), *q.stride(),
+                         q_out.data_ptr(), *q_out.stride())
+    B.ecspmv_kv_append(cache.desc, B.View(k.data_ptr(), *k.stride()), B.View(v.data_ptr(), *v.stride()), slots.data_ptr(), tokens, r, _stream_handle(stream))
     return q_out
 
 
@@ -321,9 +325,9 @@ def verify(target: torch.Tensor, draft, drafted: torch.Tensor, uniform: torch.Te
     return tokens, accepted
 
 
-def verify_tree_workspace(batch: int, vocab: int) -> int:
+def verify_tree_workspace(batch: int, nodes: int, vocab: int) -> int:
     """Bytes of a workspace for verify_tree() calls of this size."""
-    return B.ecspmv_verify_tree_workspace(B.VerifyTreeDesc(_VERIFY_TREE, batch, 0, vocab))
+    return B.ecspmv_verify_tree_workspace(B.VerifyTreeDesc(_VERIFY_TREE, batch, nodes, vocab))
 
 
 def verify_tree(target: torch.Tensor, drafted: torch.Tensor, parent: torch.Tensor, uniform: torch.Tensor, tokens: torch.Tensor, path: torch.Tensor,
@@ -348,7 +352,7 @@ def verify_tree(target: torch.Tensor, drafted: torch.Tensor, parent: torch.Tenso
         assert count.dtype is torch.int32 and count.shape == (batch,) and count.is_contiguous() and count.get_device() == device
         a.count = count.data_ptr()
     if workspace is None:
-        workspace = _workspace(verify_tree_workspace(batch, vocab), target, stream)
+        workspace = _workspace(B.ecspmv_verify_tree_workspace(a), target, stream)
     assert workspace.get_device() == device and workspace.is_contiguous()
     B.ecspmv_verify_tree(a, workspace.data_ptr(), workspace.nbytes, _stream_handle(stream))
     return tokens, path, accepted

@@ -119,7 +119,7 @@ def test_in_a_graph_and_on_another_stream(batch, nodes, vocab):
     made = [torch.from_numpy(x).cuda() for x in make(batch, nodes, vocab, 5)]
     out, eager = ([torch.empty(s, dtype=torch.int32, device="cuda") for s in ((batch, nodes + 1), (batch, nodes), (batch,))] for _ in range(2))
     count = torch.full((batch,), nodes, dtype=torch.int32, device="cuda")
-    work = torch.empty(D.verify_tree_workspace(batch, vocab), dtype=torch.uint8, device="cuda")
+    work = torch.empty(D.verify_tree_workspace(batch, nodes, vocab), dtype=torch.uint8, device="cuda")
     side = torch.cuda.Stream()
     D.verify_tree(*made, *out, count, work)
     torch.cuda.synchronize()

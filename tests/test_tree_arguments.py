@@ -10,8 +10,10 @@ def cache(**o):
 def view(data=0x500000, t=128, h=64, d=1):
     return B.View(data, t, h, d)
 def rotary(**o):
-    d = dict(rotary_dim=64, neighbours=0, q_heads=4, frequency=0xA00000, position=0xB00000, q=view(0x700000, 256), q_out=view(0x710000, 256))
-    d.update({k: view(v, 256) if k in ("q", "q_out") else v for k, v in o.items()})
+    d = dict(rotary_dim=64, neighbours=0, q_heads=4, frequency=0xA00000, position=0xB00000, q=0x700000, q_out=0x710000)
+    for name in ("q", "q_out"):
+        d.update({name + "_token_stride": 256, name + "_head_stride": 64, name + "_dim_stride": 1})
+    d.update(o)
     return B.RotaryDesc(ctypes.sizeof(B.RotaryDesc), **d)
 def attention(**o):
     d = dict(q_heads=4, tokens=3, batch=2, max_pages=4, max_new=2, scale=0.125, table_stride=4, q_start=0x600000, kv_len=0x600100,
@@ -144,6 +146,6 @@ def test_refusals(tmp_path):
     assert got["layers"] == 2 * 6                            # 64 caches in the first launch, 6 in the second
     assert got["short"] == [INVALID] * 11
     assert got["enough"] == [1, [SMALL, 0]] and got["none"] == [INVALID, 0]
-    assert got["verify work"] == [2 * 8, 1, [SMALL, 0], [INVALID, 0], [INVALID, 0]]
+    assert got["verify work"] == [2 * (8 + 16 + 16), 1, [SMALL, 0], [INVALID, 0], [INVALID, 0]]
     assert got["stream"] == [[0x1000, 0x100], [0x2000, 0x200], [0, 0x100], HIP] * 4
     assert all(g < 1 << 32 for g in got["grid"])

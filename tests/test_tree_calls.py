@@ -53,11 +53,12 @@ def test_append(calls, devices):
     assert D.kv_append(**right) is right["q_out"]
     (_, (desc, k, v, slots, tokens, r, stream)), = calls
     assert tokens == 5 and (r.rotary_dim, r.neighbours, r.q_heads) == (40, 1, 6) and r.frequency == right["frequency"].data_ptr()
-    assert r.position == right["position"].data_ptr() and r.q.data == right["q"].data_ptr() and r.q_out.data == right["q_out"].data_ptr()
+    assert (r.q_token_stride, r.q_head_stride, r.q_dim_stride) == right["q"].stride() == (r.q_out_token_stride, r.q_out_head_stride, r.q_out_dim_stride)
+    assert r.position == right["position"].data_ptr() and r.q == right["q"].data_ptr() and r.q_out == right["q_out"].data_ptr()
     calls.clear()
     assert D.kv_append(**{**right, "q_out": None, "neighbours": False}, stream=Stream()) is right["q"]
     (_, a), = calls
-    assert a[5].q_out.data == right["q"].data_ptr() and a[5].neighbours == 0 and a[6] == 0x55
+    assert a[5].q_out == right["q"].data_ptr() and a[5].neighbours == 0 and a[6] == 0x55
     calls.clear()
     assert D.kv_append(**{**right, "q": None, "q_out": None}) is None and calls.pop()[1][5].q_heads == 0
     wide = torch.zeros((5, 2), dtype=I32)
@@ -124,9 +125,9 @@ def test_verify(calls, devices, monkeypatch):
     i32 = lambda *s: torch.zeros(s, dtype=I32)                                # noqa: E731
     right = dict(target=torch.zeros(2, 4, 50), drafted=i32(2, 3), parent=i32(2, 3), uniform=torch.zeros(2, 4), tokens=i32(2, 4), path=i32(2, 3),
                  accepted=i32(2), count=i32(2))
-    assert D.verify_tree(**right) == (right["tokens"], right["path"], right["accepted"]) and D.verify_tree_workspace(3, 2049) == 3 * 3 * 8
+    assert D.verify_tree(**right) == (right["tokens"], right["path"], right["accepted"]) and D.verify_tree_workspace(3, 5, 2049) == 3 * (3 * 8 + 16 + 24)
     (_, (a, work, size, stream)), = calls
-    assert (a.batch, a.nodes, a.vocab, a.target_seq, a.target_row, size) == (2, 3, 50, 200, 50, 16)
+    assert (a.batch, a.nodes, a.vocab, a.target_seq, a.target_row, size) == (2, 3, 50, 200, 50, 2 * (8 + 16 + 16))
     assert a.parent == right["parent"].data_ptr() and a.path == right["path"].data_ptr() and a.count == right["count"].data_ptr()
     calls.clear()
     D.verify_tree(**{**right, "count": None, "target": torch.zeros(2, 5, 60)[:, :4, :50]}, stream=Stream())
