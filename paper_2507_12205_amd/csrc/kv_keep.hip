@@ -1,8 +1,13 @@
 // The rows of an accepted path, which lie where their nodes were written, moved to follow one another: key first + path[i] of a sequence
 // becomes its key first + i, in the caches of many layers at once.
 //
-// path[i] >= i (a path grows): a row lies behind every place that rows before it go to, and rows that are copied in order stay whole.  A thread copies one piece of a row, the same one of every row of its sequence, head and layer: nobody else reads or writes
-// these places, so there is nothing to wait for between rows, and eight of them are under way at once.  Bits are copied as they are.
+// path[i] >= i (a path grows): a row lies behind every place that rows before it go to, so that rows which are copied in order stay whole.  A
+// thread copies one piece of a row, the same one of every row of its sequence, head and layer, eight of them under way at once: nobody else
+// reads or writes these places, and there is nothing to wait for.  Bits are copied as they are.
+//
+// What bounds it are four trips to memory, one after the other (how many and where, pages, rows, their new places), and rows that lie apart: five
+// rows of 40 heads of 128 in 40 layers, 16 bits, 4.5 us (16 MB moved); four of 8 heads of 128 of 32 sequences in 32 layers, 4 bits, 7.9 (131072
+// pieces of 64 and 4 bytes each way; several rows at once in a workgroup, all read before any is written: 8.3).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
