@@ -50,9 +50,10 @@ __device__ __forceinline__ void store_eight(const View &v, uint32_t wide, uint32
 }
 
 // The codes and the step of a row that 2^lanes_shift neighbouring lanes have, N values each in pieces of eight that start at at[...] of the row (a piece
-// that starts beyond it is none), to where they lie; `valid`: whether the row has a place.  All lanes of the row come here.  FIFTEENTH: a 4-bit
-// step is the range times 1/15 in FP32, which may be its last place away from the range divided by 15, and saves the division.
-template <int BITS, bool FIFTEENTH, int N>
+// that starts beyond it is none), to where they lie; `valid`: whether the row has a place.  All lanes of the row come here.  WIDE: values are not FP16
+// values, so that the lowest one is rounded to what is kept of it; and a 4-bit step is the range times 1/15 in FP32, which may be its last
+// place away from the range divided by 15, and saves the division.
+template <int BITS, bool WIDE, int N>
 __device__ __forceinline__ void store_codes(float (&x)[N], uint8_t *codes, uint8_t *steps, const uint32_t (&at)[N / 8], uint32_t dim, uint32_t lanes_shift,
                                             bool valid)
 {
@@ -60,11 +61,12 @@ __device__ __forceinline__ void store_codes(float (&x)[N], uint8_t *codes, uint8
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         x[i] = x[i] != x[i] ? 0.0f : fminf(fmaxf(x[i], -65504.0f), 65504.0f);
-        if (at[i / 8] < dim) {
+        if (N == 8 || at[i / 8] < dim) {
             low = fminf(low, x[i]);
             high = fmaxf(high, x[i]);
         }
     }
+    if (N == 8 && at[0] >= dim) low = 65504.0f, high = -65504.0f;         // a lane without values
     for (uint32_t o = 1u; o < 1u << lanes_shift; o <<= 1) {
         low = fminf(low, __shfl_xor(low, (int)o, 64));
         high = fmaxf(high, __shfl_xor(high, (int)o, 64));
@@ -79,16 +81,20 @@ __device__ __forceinline__ void store_codes(float (&x)[N], uint8_t *codes, uint8
                 const int c = (int)fminf(fmaxf(rintf(x[8 * k + i] * inv), -127.0f), 127.0f);
                 w[i >> 2] |= ((uint32_t)c & 0xFFu) << (8 * (i & 3));
             }
-            if (valid && at[k] < dim) *reinterpret_cast<uint2 *>(codes + at[k]) = make_uint2(w[0], w[1]);
+            if (valid && (N == 8 || at[k] < dim)) *reinterpret_cast<uint2 *>(codes + at[k]) = make_uint2(w[0], w[1]);
         }
         if (valid && at[0] == 0) *reinterpret_cast<float *>(steps) = step;
     } else {
         const uint32_t low_bits = to_half(low);
-        low = to_float(low_bits);
-        const float range = fmaxf(high - low, 0.0f);                       // (rounded up, the lowest value may be above the largest)
-        float wide_step = FIFTEENTH ? range * (1.0f / 15.0f) : range / 15.0f;
-        asm("" : "+v"(wide_step));                                         // (a product in FP32: not one that is rounded to FP16 at once)
-        uint32_t step_bits = to_half(wide_step);
+        uint32_t step_bits;
+        if constexpr (WIDE) {
+            low = to_float(low_bits);
+            float step = fmaxf(high - low, 0.0f) * (1.0f / 15.0f);         // (rounded up, the lowest value may be above the largest)
+            asm("" : "+v"(step));                                          // (a product in FP32: not one that is rounded to FP16 at once)
+            step_bits = to_half(step);
+        } else {
+            step_bits = to_half((high - low) / 15.0f);
+        }
         if (fmaf(15.0f, to_float(step_bits), low) >= 65520.0f) --step_bits;  // (rounded up, and the last code would be infinity in FP16)
         const float step = to_float(step_bits), inv = step > 0.0f ? 1.0f / step : 0.0f;
 #pragma unroll
@@ -96,7 +102,7 @@ __device__ __forceinline__ void store_codes(float (&x)[N], uint8_t *codes, uint8
             uint32_t w = 0;
 #pragma unroll
             for (int i = 0; i < 8; ++i) w |= (uint32_t)fminf(fmaxf(rintf((x[8 * k + i] - low) * inv), 0.0f), 15.0f) << (4 * i);
-            if (valid && at[k] < dim) *reinterpret_cast<uint32_t *>(codes + (at[k] >> 1)) = w;
+            if (valid && (N == 8 || at[k] < dim)) *reinterpret_cast<uint32_t *>(codes + (at[k] >> 1)) = w;
         }
         if (valid && at[0] == 0) *reinterpret_cast<uint32_t *>(steps) = step_bits | low_bits << 16;
     }
