@@ -210,15 +210,14 @@ def kv_keep(caches: KvCaches, first: torch.Tensor, path: torch.Tensor, accepted:
     """The rows of accepted nodes to where they follow one another, in all caches: key first[b] + path[b, i] of sequence b becomes its key
     first[b] + i for i < accepted[b].  first: (batch,), the key of node 0; path: (batch, nodes) and accepted: (batch,) as verify_tree() leaves
     them; page_table as in attention(); all int32."""
-    batch, nodes = path.shape
-    pages = page_table.shape[1]
+    device, (batch, nodes), (sequences, pages), (row, node), (pages_row, place) = caches.device, path.shape, page_table.shape, path.stride(), page_table.stride()
     assert first.dtype is path.dtype is accepted.dtype is page_table.dtype is torch.int32
-    assert first.get_device() == path.get_device() == accepted.get_device() == page_table.get_device() == caches.device
-    assert first.shape == accepted.shape == (batch,) and page_table.shape[0] == batch and first.is_contiguous() and accepted.is_contiguous()
-    assert (nodes <= 1 or path.stride(1) == 1) and (batch <= 1 or path.stride(0) >= nodes)
-    assert (pages <= 1 or page_table.stride(1) == 1) and (batch <= 1 or page_table.stride(0) >= pages)
-    a = B.KeepDesc(_KEEP, batch, nodes, pages, path.stride(0) if batch > 1 else nodes, page_table.stride(0) if batch > 1 else pages,
-                   first.data_ptr(), path.data_ptr(), accepted.data_ptr(), page_table.data_ptr())
+    assert device == first.get_device() == path.get_device() == accepted.get_device() == page_table.get_device()
+    assert first.numel() == accepted.numel() == sequences == batch and first.dim() == accepted.dim() == 1
+    assert first.is_contiguous() and accepted.is_contiguous()
+    assert (nodes <= 1 or node == 1) and (batch <= 1 or row >= nodes) and (pages <= 1 or place == 1) and (batch <= 1 or pages_row >= pages)
+    a = B.KeepDesc(_KEEP, batch, nodes, pages, row if batch > 1 else nodes, pages_row if batch > 1 else pages, first.data_ptr(), path.data_ptr(),
+                   accepted.data_ptr(), page_table.data_ptr())
     B.ecspmv_kv_keep(caches.descs, a, _stream_handle(stream))
 
 
@@ -231,15 +230,17 @@ def attention_workspace(cache: KvCache, q: torch.Tensor, batch: int, max_new: in
 
 def _attention_of(cache: KvCache, q: torch.Tensor, out: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, page_table: torch.Tensor,
                   max_new: int, scale) -> B.AttentionDesc:
-    assert q.dtype is out.dtype is torch.float16 and q.shape == out.shape and q.shape[2] == cache.head_dim
-    assert q.get_device() == out.get_device() == q_start.get_device() == kv_len.get_device() == page_table.get_device() == cache.device
-    assert q_start.dtype is kv_len.dtype is page_table.dtype is torch.int32
-    batch, pages = page_table.shape
-    assert kv_len.shape == (batch,) and q_start.shape == (batch + 1,) and q_start.is_contiguous() and kv_len.is_contiguous()
-    assert (pages <= 1 or page_table.stride(1) == 1) and (batch <= 1 or page_table.stride(0) >= pages)          # no expand()ed rows
-    tokens, heads, _ = q.shape
-    return B.AttentionDesc(_ATTENTION, heads, tokens, batch, pages, max_new, cache.head_dim ** -0.5 if scale is None else scale,
-                           page_table.stride(0) if batch > 1 else pages, q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), _view(q), _view(out))
+    device, (tokens, heads, dim), (batch, pages) = cache.device, q.shape, page_table.shape
+    assert q.dtype is out.dtype is torch.float16 and q_start.dtype is kv_len.dtype is page_table.dtype is torch.int32
+    assert device == q.get_device() == out.get_device() == q_start.get_device() == kv_len.get_device() == page_table.get_device()
+    assert dim == cache.head_dim and out.shape == q.shape
+    assert kv_len.numel() == batch and q_start.numel() == batch + 1 and kv_len.dim() == q_start.dim() == 1
+    assert q_start.is_contiguous() and kv_len.is_contiguous()
+    row, place = page_table.stride()
+    assert (pages <= 1 or place == 1) and (batch <= 1 or row >= pages)          # no expand()ed rows
+    return B.AttentionDesc(_ATTENTION, heads, tokens, batch, pages, max_new, dim ** -0.5 if scale is None else scale, row if batch > 1 else pages,
+                           q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), B.View(q.data_ptr(), *q.stride()),
+                           B.View(out.data_ptr(), *out.stride()))
 
 
 def attention(cache: KvCache, q: torch.Tensor, out: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, page_table: torch.Tensor,
@@ -262,13 +263,13 @@ def attention_tree(cache: KvCache, q: torch.Tensor, out: torch.Tensor, q_start: 
     those whose bits are set in its row of seen, (tokens, words) int32 with 32 of them to a word, the first in the lowest bit (tree_seen()).
     words: no fewer than max_new / 32 (or, if there are fewer tokens than max_new, than those)."""
     a = _attention_of(cache, q, out, q_start, kv_len, page_table, max_new, scale)
-    tokens, words = seen.shape
-    assert seen.dtype is torch.int32 and seen.get_device() == cache.device and tokens == q.shape[0] and 32 * words >= min(max_new, tokens)
-    assert (words <= 1 or seen.stride(1) == 1) and (tokens <= 1 or seen.stride(0) >= words)
+    (tokens, words), (row, word) = seen.shape, seen.stride()
+    assert seen.dtype is torch.int32 and seen.get_device() == cache.device and tokens == a.tokens and 32 * words >= min(max_new, tokens)
+    assert (words <= 1 or word == 1) and (tokens <= 1 or row >= words)
     if workspace is None:
         workspace = _workspace(B.ecspmv_attention_tree_workspace(cache.desc, a), q, stream)
     assert workspace.get_device() == cache.device and workspace.is_contiguous()
-    B.ecspmv_attention_tree(cache.desc, a, seen.data_ptr(), seen.stride(0) if tokens > 1 else words, workspace.data_ptr(), workspace.nbytes,
+    B.ecspmv_attention_tree(cache.desc, a, seen.data_ptr(), row if tokens > 1 else words, workspace.data_ptr(), workspace.nbytes,
                             _stream_handle(stream))
     return out
 
@@ -336,18 +337,17 @@ def verify_tree(target: torch.Tensor, drafted: torch.Tensor, parent: torch.Tenso
     the tree and after each node, uniform: (batch, nodes + 1) random numbers in [0, 1), all FP32; drafted: (batch, nodes) and parent: (batch, nodes)
     int32, -1 for the token before the tree; count: (batch,) int32, how many nodes there are (None: all).  tokens: (batch, nodes + 1), path: (batch,
     nodes), accepted: (batch,) int32.  workspace: of verify_tree_workspace(), or allocated here."""
-    batch, rows, vocab = target.shape
+    device, (batch, rows, vocab), (seq, row, token) = target.get_device(), target.shape, target.stride()
     nodes = rows - 1
     assert target.dtype is uniform.dtype is torch.float32
     assert drafted.dtype is parent.dtype is tokens.dtype is path.dtype is accepted.dtype is torch.int32
-    device = target.get_device()
-    assert device >= 0 and device == uniform.get_device() == drafted.get_device() == parent.get_device()
+    assert 0 <= device == uniform.get_device() == drafted.get_device() == parent.get_device()
     assert device == tokens.get_device() == path.get_device() == accepted.get_device()
     assert uniform.shape == tokens.shape == (batch, rows) and drafted.shape == parent.shape == path.shape == (batch, nodes) and accepted.shape == (batch,)
     assert uniform.is_contiguous() and tokens.is_contiguous() and drafted.is_contiguous() and parent.is_contiguous()
-    assert path.is_contiguous() and accepted.is_contiguous() and (target.numel() == 0 or vocab == 1 or target.stride(2) == 1)
-    a = B.VerifyTreeDesc(_VERIFY_TREE, batch, nodes, vocab, target.data_ptr(), uniform.data_ptr(), target.stride(0), target.stride(1),
-                         drafted.data_ptr() or None, parent.data_ptr() or None, None, tokens.data_ptr(), path.data_ptr() or None, accepted.data_ptr())
+    assert path.is_contiguous() and accepted.is_contiguous() and (token == 1 or vocab == 1 or target.numel() == 0)
+    a = B.VerifyTreeDesc(_VERIFY_TREE, batch, nodes, vocab, target.data_ptr(), uniform.data_ptr(), seq, row, drafted.data_ptr(), parent.data_ptr(), None,
+                         tokens.data_ptr(), path.data_ptr(), accepted.data_ptr())
     if count is not None:
         assert count.dtype is torch.int32 and count.shape == (batch,) and count.is_contiguous() and count.get_device() == device
         a.count = count.data_ptr()
