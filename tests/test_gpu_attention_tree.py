@@ -61,6 +61,7 @@ CASES = [
     ([40], [500], 4, 4, 160, 16), ([20, 50], [300, 800], 2, 2, 192, 16), ([100], [400], 2, 1, 224, 32), ([60], [1200], 8, 8, 32, 16),
     ([9, 30, 2, 0, 1], [3000, 700, 5, 40, 2100], 4, 4, 128, 16), ([3, 5, 1] * 30, [900, 5, 300] * 30, 4, 2, 64, 16),
     ([50, 1] * 32, [60, 600] * 32, 2, 2, 64, 16), ([130, 260], [2000, 900], 2, 2, 128, 64),
+    ([40, 3], [300, 2000], 2, 2, 256, 16), ([64], [5000], 3, 3, 256, 64),
 ]
 
 
@@ -256,3 +257,38 @@ def test_in_a_graph_and_on_another_stream():
             D.attention_tree(cache, q, eager, s, n, t, words, new[0], None, None, stream=side)
             side.synchronize()
             assert torch.equal(eager, out)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("new,total", [([7, 0, 5], [1000, 30, 40]), ([40, 70], [900, 2000]), ([3, 2] * 40, [600, 20] * 40)])
+def test_rows_of_no_sequence_stay(new, total, bits):
+    """Tokens before the first sequence and behind the last one are left as they were, and change nothing."""
+    import torch
+    from paper_2507_12205_amd import device as D
+    cache, q, start, lens, table = made = make(torch, D, new, total, 4, 2, 64, 16, bits, seed=8)
+    words = words_of(trees(np.random.default_rng(1), new))
+    want = run(torch, D, *made, words)
+    wide = torch.randn((len(q) + 9, *q.shape[1:]), device="cuda").half()
+    wide[4:4 + len(q)] = q
+    out = torch.full_like(wide, 77.0)
+    seen = np.full((len(wide), words.shape[1]), -1, np.int32)
+    seen[4:4 + len(q)] = words
+    args = [torch.from_numpy(np.ascontiguousarray(x)).cuda() for x in (start + 4, lens, table, seen)]
+    D.attention_tree(cache, wide, out, *args, int(np.diff(start).max()))
+    got = out.cpu().numpy().astype(np.float64)
+    assert (got[:4] == 77).all() and (got[4 + len(q):] == 77).all()
+    v = values(cache)[1]
+    assert np.abs(got[4:4 + len(q)] - want).max() <= 2 ** -9 * np.abs(v).max()          # (splits may differ with the number of tokens)
+
+
+def test_very_many_sequences():
+    """More sequences than a grid's second dimension holds of workgroups at once: each has one key, which is the result."""
+    import torch
+    from paper_2507_12205_amd import device as D
+    n = 40000
+    cache = D.kv_cache(n, 1, 16, 16)
+    k, v, q = (torch.randn((n, 1, 16), device="cuda").half() for _ in range(3))
+    D.kv_write(cache, k, v, torch.arange(n, device="cuda") * 16)
+    out, i = torch.full_like(q, float("nan")), torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    D.attention_tree(cache, q, out, i, torch.ones(n, dtype=torch.int32, device="cuda"), i[:n, None], torch.ones((n, 1), dtype=torch.int32, device="cuda"), 1)
+    assert torch.equal(out, v)

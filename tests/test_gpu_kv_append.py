@@ -222,3 +222,17 @@ def test_no_tokens():
     D.kv_append(cache, x, x, torch.empty(0, dtype=torch.int64, device="cuda"), torch.empty(0, dtype=torch.int32, device="cuda"), D.rotary_frequency(8), x)
     torch.cuda.synchronize()
     assert not cache.k.any()
+
+
+@pytest.mark.parametrize("neighbours", [False, True])
+def test_one_tensor_of_queries_keys_and_values(neighbours):
+    """q, k and v as slices of one tensor, the queries rotated where they lie: nothing else of it changes."""
+    import torch
+    from paper_2507_12205_amd import device as D
+    a, b = (D.kv_cache(9, 2, 16, 64, 16) for _ in range(2))
+    both = values((50, 8, 64), 6, torch)
+    before = both.clone()
+    slots, position, freq = torch.arange(50, device="cuda"), torch.arange(7, 57, dtype=torch.int32, device="cuda"), D.rotary_frequency(32)
+    want = D.kv_append(a, *(before[:, i:j].contiguous() for i, j in ((4, 6), (6, 8))), slots, position, freq, before[:, :4].contiguous(), None, neighbours)
+    D.kv_append(b, both[:, 4:6], both[:, 6:], slots, position, freq, both[:, :4], None, neighbours)
+    assert torch.equal(both[:, :4], want) and torch.equal(both[:, 4:], before[:, 4:]) and torch.equal(a.k, b.k) and torch.equal(a.v, b.v)
