@@ -216,7 +216,7 @@ __device__ __forceinline__ uint32_t seen_bits(const ecs::AttentionTreeArgs &a, u
 // For rows that all see all keys, the work of a sequence is (tiles of its rows) x (tiles of its keys).  Sequences differ in both, and the host
 // sees neither, so that the workgroups of a launch are dealt out here, by every one of them for itself: with each sequence's keys cut into
 // pieces of L tiles at most, L is the least length (but for a few steps of halving) at which all pieces find a workgroup.
-// (us by equal numbers of splits for all / by this: 16 trees of up to 16 nodes over up to 8192 keys, 64/8 heads of 128, 8 bits, 98.7 / 85.8; eight of up to
+// (us by equal numbers of splits for all / by this: 16 trees of up to 16 nodes over up to 8192 keys, 64/8 heads of 128, 8 bits, 98.7 / 85.8 at that time; eight of up to
 // 49 over up to 2000, 32 heads of 80, 4 bits, 61.2 / 41.8.)
 // inclusive results over the lanes of an operation whose neutral element is all zeros
 template <class T, class F>
@@ -250,7 +250,7 @@ struct Share {
     uint32_t base;                        // balanced: where the sequence's partial results start, in rows of all heads of the cache
 };
 
-template <uint32_t ROWS, uint32_t KEYS>
+template <uint32_t ROWS, uint32_t KEYS, uint32_t HALF>
 __device__ __forceinline__ Share share_of_work(const ecs::AttentionTreeArgs &a, bool first_wave)
 {
     const uint32_t slot = blockIdx.y + gridDim.y * blockIdx.z;     // (blockIdx.x: the head)
@@ -262,7 +262,9 @@ __device__ __forceinline__ Share share_of_work(const ecs::AttentionTreeArgs &a, 
     const uint32_t lane = threadIdx.x & 63u, b = min(lane, a.batch - 1u);
     const Sequence s(a, b);
     const uint32_t rows = lane < a.batch ? s.new_tokens * a.group : 0u, items = (rows + ROWS - 1u) / ROWS;
-    const uint32_t keys = lane < a.batch ? max((s.len + KEYS - 1u) / KEYS, 1u) : 1u;
+    const uint32_t tiles_of_keys = lane < a.batch ? max((s.len + KEYS - 1u) / KEYS, 1u) : 1u;
+    // what a tile of keys costs: HALF sixteenths where rows are half of a tile's at most
+    const uint32_t keys = HALF == 16u || rows > ROWS / 2u ? tiles_of_keys : max(tiles_of_keys * HALF / 16u, 1u);
     const uint32_t all = last_lane(sums_to(items));
     const uint32_t longest = last_lane(lanes_scan(keys, [](uint32_t x, uint32_t y) { return max(x, y); }));
     const float work = last_lane(lanes_scan((float)items * (float)keys, [](float x, float y) { return x + y; }));
@@ -330,7 +332,7 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) :
     uint32_t tile = blockIdx.x / a.splits, split = blockIdx.x - tile * a.splits, head = blockIdx.y, seq = blockIdx.z, splits = a.splits, base = 0;
     if constexpr (TREE) {
         head = blockIdx.x;
-        const Share mine = share_of_work<16, 32>(a, tid < 64u);
+        const Share mine = share_of_work<16, 32, 16>(a, tid < 64u);
         tile = mine.tile, split = mine.split, seq = mine.seq, splits = mine.splits, base = mine.base;
         if (splits == 0) return;
     }
@@ -669,8 +671,8 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) :
 // 194, 4 bits 168 / 202; 512 over 9098 108 / 133; five of up to 333 over 3000, heads of 80, 68 / 80, 4 bits 78 / 86).  With FP16 the sum of the weights is
 // that of the rounded ones.
 //
-// 2048 tokens over 4096 keys, 32 heads of 128, FP16: 132 us, 780 TFLOP/s of the products that the mask leaves (a large matrix product
-// alone reaches 1229 here).  A wavefront's products and its softmax follow one another, and those of the two wavefronts of a SIMD overlap only in
+// 2048 tokens over 4096 keys, 32 heads of 128, FP16: 121 - 127 us, 810 - 850 TFLOP/s of the products that the mask leaves (a large matrix
+// product alone reaches 1140 - 1229 here).  A wavefront's products and its softmax follow one another, and those of the two wavefronts of a SIMD overlap only in
 // part; without the loads it would take 98 - 107.  32 rows to a wavefront: with 64 the accumulators moved between the two halves
 // of the register file (208 us).  Softmax and products of neighbouring halves interleaved in one wavefront took 123 us here, but 122 for
 // 110 where 512 tokens see 9098 keys, 105 for 71 with five sequences in FP16 and 402 for 158 in 4 bits.
@@ -700,13 +702,16 @@ __device__ __forceinline__ uint4 code_values(const Raw<BITS> &r)
 
 //
 // With ON_KEYS == 2 a workgroup has 64 rows, and two wavefronts share 32 of them: each works on half of a tile's keys, and their results meet
-// in LDS at the end.
+// in LDS at the end.  Where the rows of a tree's tile of 128 are 64 or fewer, its workgroup does the same if keys and values are codes (16 trees of up to 16
+// nodes over up to 8192 keys, 64/8 heads of 128, 8 bits: 83.8 us without, 78.9 with; FP16 has not the registers): a tile of keys then costs 0.72 of what it
+// costs otherwise (128 and 64 rows, sixteen sequences of one length, 127 and 91 us), and shares are dealt out by that (9/16 85.6, 13/16 81.2).
 template <int BITS, int DP, bool TREE, int ON_KEYS>
 __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(const ArgsOf<TREE> a)
 {
     constexpr int RC = DP <= 32 ? 4 : DP <= 64 ? 8 : DP <= 128 ? 16 : 32;              // 16-byte pieces of a row in LDS
-    constexpr int KT = RC == 32 && ON_KEYS == 1 ? 32 : 64, kHalves = KT / 32 / ON_KEYS, kSteps = DP / 16, kTiles = DP / 32;       // halves: of a wavefront
+    constexpr int KT = RC == 32 && ON_KEYS == 1 ? 32 : 64, kSteps = DP / 16, kTiles = DP / 32;
     constexpr uint32_t kRows = 128 / ON_KEYS;
+    constexpr bool kByRows = TREE && ON_KEYS == 1 && BITS < 16 && DP <= 128;           // a tile of 64 rows or fewer is worked on as with ON_KEYS == 2
     constexpr int kGroups = KT / 16;                                                   // a wavefront brings 16 keys; with 32, of K or of V
     constexpr int kIssues = RC / 4;                                                    // accesses per lane for 16 rows
     // (four objects and not two of twice the size: a read of LDS then waits for what is on its way into the same object only)
@@ -714,6 +719,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
     __shared__ float lds_step[2][2][2][KT];                                            // [buffer][k, v][step, low][key]
     __shared__ float lds_reach[2][BITS < 16 ? KT : 1];                                 // reach_of a key's step of V
     __shared__ uint32_t lds_odd[2];
+    __shared__ float lds_mlz[2][3][32];                                                // of the second of two wavefronts that share rows
 
     const uint32_t tid = threadIdx.x, lane = tid & 63u, n = lane & 31u, h = lane >> 5;
     const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid >> 6));
@@ -727,7 +733,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
     else
         tile -= (a.row_tiles + 1u) / 2u;
     if constexpr (TREE) {
-        const Share mine = share_of_work<kRows, KT>(a, tid < 64u);
+        const Share mine = share_of_work<kRows, KT, kByRows ? 11 : 16>(a, tid < 64u);
         tile = mine.tile, split = mine.split, seq = mine.seq, splits = mine.splits, base = mine.base;
         if (splits == 0) return;
     }
@@ -736,437 +742,447 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
     if (row0 >= rows) return;
     const uint32_t dim = a.cache.dim, pieces = dim / 8u;
 
-    const uint32_t wave_row = row0 + 32u * (wave % (4u / ON_KEYS)), half0 = kHalves * (wave / (4u / ON_KEYS));     // first row, first half of a tile
-    const uint32_t row = min(wave_row + n, rows - 1u), token = row / a.group;
-    const int32_t seen = min(s.behind + (int32_t)token + 1, (int32_t)s.len);
-    auto sees = [&](uint32_t r) -> int32_t {                                           // keys up to the last one that row r sees
-        return TREE ? (int32_t)s.len : max(min(s.behind + (int32_t)(min(r, rows - 1u) / a.group) + 1, (int32_t)s.len), 0);
-    };
-    const uint32_t end = (uint32_t)sees(row0 + kRows - 1u);                                  // of the workgroup
-    const uint32_t all_see = TREE ? (uint32_t)max(s.behind, 0) : (uint32_t)sees(row0);
-    const uint32_t wave_end = wave_row < rows ? (uint32_t)sees(wave_row + 31u) : 0u;
-
-    half8v q[kSteps];
-    float q_sum = 0.0f;
-    {
-        const uint16_t *p = a.q.data + (int64_t)(s.first + token) * a.q.token_stride +
-                            (int64_t)(head * a.group + (row - token * a.group)) * a.q.head_stride;
-#pragma unroll
-        for (int t = 0; t < kSteps; ++t) {
-            const uint32_t d0 = 16u * t + 8u * h;
-            uint32_t w[4] = {0, 0, 0, 0};
-            if (d0 < dim) {
-                if (a.q_wide) {
-                    const uint4 v = *reinterpret_cast<const uint4 *>(p + d0);
-                    w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) w[i >> 1] |= (uint32_t)p[(int64_t)(d0 + i) * a.q.dim_stride] << (16 * (i & 1));
-                }
-            }
-            if (a.scale_log2 < 0.0f)                               // the largest score is the one with the largest product
-#pragma unroll
-                for (uint32_t &x : w) x ^= 0x80008000u;
-            if constexpr (BITS == 4)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) q_sum += half_to_float(w[i] & 0xFFFFu) + half_to_float(w[i] >> 16);
-            q[t] = as_half8(w[0], w[1], w[2], w[3]);
-        }
-        if constexpr (BITS == 4) q_sum += __shfl_xor(q_sum, 32, 64);
-    }
-    // (a scale of 0 as the least there is: a hidden key's score, minus infinity, stays that)
-    const float scale = a.scale_log2 == 0.0f ? 1.17549435e-38f : fabsf(a.scale_log2), by = BITS == 16 ? scale : 1.0f;
-
-    const uint32_t tiles = (end + KT - 1u) / KT, per = (tiles + splits - 1u) / splits;
-    const uint32_t t0 = min(split * per, tiles), t1 = min(t0 + per, tiles);
-    const uint32_t page_mask = (1u << a.cache.page_shift) - 1u;
-    const uint64_t page_rows = (uint64_t)a.cache.heads << a.cache.page_shift, head_rows = (uint64_t)head << a.cache.page_shift;
-    const uint32_t group16 = kGroups == 4 ? wave : wave & 1u;
-    const bool brings_k = kGroups == 4 || wave < 2u, brings_v = kGroups == 4 || wave >= 2u;
-
-    if (pieces < (uint32_t)RC)
-        for (uint32_t i = tid; i < KT * RC; i += 256u)             // what is beyond dim stays zero
-            lds_k0[i] = lds_k1[i] = lds_v0[i] = lds_v1[i] = make_uint4(0, 0, 0, 0);
-    if (tid < 2u) lds_odd[tid] = 0;
-    __syncthreads();
-
-    // Bringing tile t into buffer b, this wavefront's 16 keys of it: request() sends the loads off, arrive() waits for them and writes what
-    // has come through registers.
-    Raw<BITS> raw_k[BITS < 16 ? kIssues : 1], raw_v[BITS < 16 ? kIssues : 1];
-    uint32_t raw_step = 0;
-    auto first_key = [&](uint32_t t) { return min(t * KT + 16u * group16, (end - 1u) & ~15u); };      // (beyond the end: the last 16 keys again)
-    uint32_t page_list = 0;                                        // lane i: the page of this wavefront's keys in the i-th tile of 64
-    auto request = [&](uint32_t t, auto buffer) {
-        const int b = buffer;
-        uint4 *lds_k = b ? lds_k1 : lds_k0, *lds_v = b ? lds_v1 : lds_v0;
-        if (((t - t0) & 63u) == 0) {
-            page_list = page_of(a, s.table, first_key(t + lane));
-            asm volatile("" : "+v"(page_list));                    // waited for here, where it happens, and not by every tile
-        }
-        const uint32_t key = first_key(t);
-        const uint32_t page = (uint32_t)__builtin_amdgcn_readlane((int)page_list, (int)((t - t0) & 63u));
-        const uint64_t at = (uint64_t)page * page_rows + head_rows + (key & page_mask);
-        const uint8_t *kp = a.cache.k + at * a.cache.row_bytes, *vp = a.cache.v + at * a.cache.row_bytes;
-        const uint32_t self = here(lane);
-        auto bring = [&](auto whole) {                             // whole: dim fills the rows of LDS
-#pragma unroll
-            for (int i = 0; i < kIssues; ++i) {
-                const uint32_t r = (64u * i + self) / RC, c = self % RC;             // row of the 16, piece
-                const uint32_t row = decltype(whole)::value ? r * (2u * DP) : r * a.cache.row_bytes;
-                if constexpr (BITS == 16) {
-                    const uint32_t to = (16u * group16) * RC + 64u * i;
-                    if (const uint32_t from = c ^ k_swap<RC>(16u * group16 + r); brings_k && (decltype(whole)::value || from < pieces))
-                        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(kp + (row + 16u * from)),
-                                                         (__attribute__((address_space(3))) void *)(&lds_k[to]), 16, 0, 0);
-                    if (const uint32_t from = c ^ v_swap<RC>(16u * group16 + r); brings_v && (decltype(whole)::value || from < pieces))
-                        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(vp + (row + 16u * from)),
-                                                         (__attribute__((address_space(3))) void *)(&lds_v[to]), 16, 0, 0);
-                } else {
-                    const uint32_t from = row + min(c, pieces - 1u) * BITS;
-                    if (brings_k) raw_k[i].load(kp + from);
-                    if (brings_v) raw_v[i].load(vp + from);
-                }
-            }
+    auto work = [&](auto shared_by) {                              // by how many wavefronts rows are shared
+        constexpr int kShared = decltype(shared_by)::value, kHalves = KT / 32 / kShared;                           // halves of a tile: of a wavefront
+        const uint32_t wave_row = row0 + 32u * (wave % (4u / kShared)), half0 = kHalves * (wave / (4u / kShared));     // first row, first half of a tile
+        const uint32_t row = min(wave_row + n, rows - 1u), token = row / a.group;
+        const int32_t seen = min(s.behind + (int32_t)token + 1, (int32_t)s.len);
+        auto sees = [&](uint32_t r) -> int32_t {                                           // keys up to the last one that row r sees
+            return TREE ? (int32_t)s.len : max(min(s.behind + (int32_t)(min(r, rows - 1u) / a.group) + 1, (int32_t)s.len), 0);
         };
-        if (BITS == 16 && DP == 8 * RC && pieces == RC)
-            bring(std::true_type{});
-        else
-            bring(std::false_type{});
-        if constexpr (BITS < 16)                                   // lanes 0 ... 15 the steps of the keys, 16 ... 31 those of the values
-            raw_step = *reinterpret_cast<const uint32_t *>(((self & 16u) ? a.cache.v_step : a.cache.k_step) + 4u * (at + (self & 15u)));
-    };
-    auto arrive = [&](uint32_t t, auto buffer) {
-        const int b = buffer;
-        uint4 *lds_k = b ? lds_k1 : lds_k0, *lds_v = b ? lds_v1 : lds_v0;
-        const uint32_t key0 = t * KT + 16u * group16, self = here(lane);
-        if constexpr (BITS == 16) {
-            __builtin_amdgcn_s_waitcnt(0x0F70);                    // vmcnt(0): what went straight to LDS is there
-            asm volatile("" ::: "memory");
-            if ((t + 1u) * KT > all_see && brings_v) {
-                // Some rows do not see all of this tile.  What no row sees may be anything: zeros; and values that are not finite are
-                // left out here, so that a weight of 0 makes nothing of them (they are added at the end in the rows that see them).
-                bool odd = false;
+        const uint32_t end = (uint32_t)sees(row0 + kRows - 1u);                                  // of the workgroup
+        const uint32_t all_see = TREE ? (uint32_t)max(s.behind, 0) : (uint32_t)sees(row0);
+        const uint32_t wave_end = wave_row < rows ? (uint32_t)sees(wave_row + 31u) : 0u;
+
+        half8v q[kSteps];
+        float q_sum = 0.0f;
+        {
+            const uint16_t *p = a.q.data + (int64_t)(s.first + token) * a.q.token_stride +
+                                (int64_t)(head * a.group + (row - token * a.group)) * a.q.head_stride;
+#pragma unroll
+            for (int t = 0; t < kSteps; ++t) {
+                const uint32_t d0 = 16u * t + 8u * h;
+                uint32_t w[4] = {0, 0, 0, 0};
+                if (d0 < dim) {
+                    if (a.q_wide) {
+                        const uint4 v = *reinterpret_cast<const uint4 *>(p + d0);
+                        w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) w[i >> 1] |= (uint32_t)p[(int64_t)(d0 + i) * a.q.dim_stride] << (16 * (i & 1));
+                    }
+                }
+                if (a.scale_log2 < 0.0f)                               // the largest score is the one with the largest product
+#pragma unroll
+                    for (uint32_t &x : w) x ^= 0x80008000u;
+                if constexpr (BITS == 4)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) q_sum += half_to_float(w[i] & 0xFFFFu) + half_to_float(w[i] >> 16);
+                q[t] = as_half8(w[0], w[1], w[2], w[3]);
+            }
+            if constexpr (BITS == 4) q_sum += __shfl_xor(q_sum, 32, 64);
+        }
+        // (a scale of 0 as the least there is: a hidden key's score, minus infinity, stays that)
+        const float scale = a.scale_log2 == 0.0f ? 1.17549435e-38f : fabsf(a.scale_log2), by = BITS == 16 ? scale : 1.0f;
+
+        const uint32_t tiles = (end + KT - 1u) / KT, per = (tiles + splits - 1u) / splits;
+        const uint32_t t0 = min(split * per, tiles), t1 = min(t0 + per, tiles);
+        const uint32_t page_mask = (1u << a.cache.page_shift) - 1u;
+        const uint64_t page_rows = (uint64_t)a.cache.heads << a.cache.page_shift, head_rows = (uint64_t)head << a.cache.page_shift;
+        const uint32_t group16 = kGroups == 4 ? wave : wave & 1u;
+        const bool brings_k = kGroups == 4 || wave < 2u, brings_v = kGroups == 4 || wave >= 2u;
+
+        if (pieces < (uint32_t)RC)
+            for (uint32_t i = tid; i < KT * RC; i += 256u)             // what is beyond dim stays zero
+                lds_k0[i] = lds_k1[i] = lds_v0[i] = lds_v1[i] = make_uint4(0, 0, 0, 0);
+        if (tid < 2u) lds_odd[tid] = 0;
+        __syncthreads();
+
+        // Bringing tile t into buffer b, this wavefront's 16 keys of it: request() sends the loads off, arrive() waits for them and writes what
+        // has come through registers.
+        Raw<BITS> raw_k[BITS < 16 ? kIssues : 1], raw_v[BITS < 16 ? kIssues : 1];
+        uint32_t raw_step = 0;
+        auto first_key = [&](uint32_t t) { return min(t * KT + 16u * group16, (end - 1u) & ~15u); };      // (beyond the end: the last 16 keys again)
+        uint32_t page_list = 0;                                        // lane i: the page of this wavefront's keys in the i-th tile of 64
+        auto request = [&](uint32_t t, auto buffer) {
+            const int b = buffer;
+            uint4 *lds_k = b ? lds_k1 : lds_k0, *lds_v = b ? lds_v1 : lds_v0;
+            if (((t - t0) & 63u) == 0) {
+                page_list = page_of(a, s.table, first_key(t + lane));
+                asm volatile("" : "+v"(page_list));                    // waited for here, where it happens, and not by every tile
+            }
+            const uint32_t key = first_key(t);
+            const uint32_t page = (uint32_t)__builtin_amdgcn_readlane((int)page_list, (int)((t - t0) & 63u));
+            const uint64_t at = (uint64_t)page * page_rows + head_rows + (key & page_mask);
+            const uint8_t *kp = a.cache.k + at * a.cache.row_bytes, *vp = a.cache.v + at * a.cache.row_bytes;
+            const uint32_t self = here(lane);
+            auto bring = [&](auto whole) {                             // whole: dim fills the rows of LDS
 #pragma unroll
                 for (int i = 0; i < kIssues; ++i) {
-                    const uint32_t x = 64u * i + self, at = (16u * group16) * RC + x;
-                    uint4 v = lds_v[at];
-                    uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                    for (uint32_t &y : w) {
-                        y = key0 + x / RC < end ? y : 0u;
-                        const uint32_t keep = (half_finite(y) ? 0xFFFFu : 0u) | (half_finite(y >> 16) ? 0xFFFF0000u : 0u);
-                        odd |= keep != 0xFFFFFFFFu;
-                        y &= keep;
+                    const uint32_t r = (64u * i + self) / RC, c = self % RC;             // row of the 16, piece
+                    const uint32_t row = decltype(whole)::value ? r * (2u * DP) : r * a.cache.row_bytes;
+                    if constexpr (BITS == 16) {
+                        const uint32_t to = (16u * group16) * RC + 64u * i;
+                        if (const uint32_t from = c ^ k_swap<RC>(16u * group16 + r); brings_k && (decltype(whole)::value || from < pieces))
+                            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(kp + (row + 16u * from)),
+                                                             (__attribute__((address_space(3))) void *)(&lds_k[to]), 16, 0, 0);
+                        if (const uint32_t from = c ^ v_swap<RC>(16u * group16 + r); brings_v && (decltype(whole)::value || from < pieces))
+                            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(vp + (row + 16u * from)),
+                                                             (__attribute__((address_space(3))) void *)(&lds_v[to]), 16, 0, 0);
+                    } else {
+                        const uint32_t from = row + min(c, pieces - 1u) * BITS;
+                        if (brings_k) raw_k[i].load(kp + from);
+                        if (brings_v) raw_v[i].load(vp + from);
                     }
-                    lds_v[at] = make_uint4(w[0], w[1], w[2], w[3]);
                 }
-                if (odd) lds_odd[b] = 1u;
-            }
-        } else {
+            };
+            if (BITS == 16 && DP == 8 * RC && pieces == RC)
+                bring(std::true_type{});
+            else
+                bring(std::false_type{});
+            if constexpr (BITS < 16)                                   // lanes 0 ... 15 the steps of the keys, 16 ... 31 those of the values
+                raw_step = *reinterpret_cast<const uint32_t *>(((self & 16u) ? a.cache.v_step : a.cache.k_step) + 4u * (at + (self & 15u)));
+        };
+        auto arrive = [&](uint32_t t, auto buffer) {
+            const int b = buffer;
+            uint4 *lds_k = b ? lds_k1 : lds_k0, *lds_v = b ? lds_v1 : lds_v0;
+            const uint32_t key0 = t * KT + 16u * group16, self = here(lane);
+            if constexpr (BITS == 16) {
+                __builtin_amdgcn_s_waitcnt(0x0F70);                    // vmcnt(0): what went straight to LDS is there
+                asm volatile("" ::: "memory");
+                if ((t + 1u) * KT > all_see && brings_v) {
+                    // Some rows do not see all of this tile.  What no row sees may be anything: zeros; and values that are not finite are
+                    // left out here, so that a weight of 0 makes nothing of them (they are added at the end in the rows that see them).
+                    bool odd = false;
 #pragma unroll
-            for (int i = 0; i < kIssues; ++i) {
-                const uint32_t x = 64u * i + self, r = x / RC, c = x % RC, kk = 16u * group16 + r;
-                if (c < pieces) {
-                    if (brings_k) lds_k[kk * RC + (c ^ k_swap<RC>(kk))] = code_values<BITS>(raw_k[i]);
-                    if (brings_v) lds_v[kk * RC + (c ^ v_swap<RC>(kk))] = code_values<BITS>(raw_v[i]);
+                    for (int i = 0; i < kIssues; ++i) {
+                        const uint32_t x = 64u * i + self, at = (16u * group16) * RC + x;
+                        uint4 v = lds_v[at];
+                        uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                        for (uint32_t &y : w) {
+                            y = key0 + x / RC < end ? y : 0u;
+                            const uint32_t keep = (half_finite(y) ? 0xFFFFu : 0u) | (half_finite(y >> 16) ? 0xFFFF0000u : 0u);
+                            odd |= keep != 0xFFFFFFFFu;
+                            y &= keep;
+                        }
+                        lds_v[at] = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                    if (odd) lds_odd[b] = 1u;
                 }
-            }
-            const bool in = key0 + (lane & 15u) < end;
-            if constexpr (TREE)                                    // (a node that was left out may have a step that is none)
-                if (!(BITS == 8 ? finite(__uint_as_float(raw_step)) : half_finite(raw_step) && half_finite(raw_step >> 16))) raw_step = 0u;
-            const float step = !in ? 0.0f : BITS == 8 ? __uint_as_float(raw_step) : step_of(raw_step);
-            const float low = !in || BITS == 8 ? 0.0f : low_of(raw_step);
-            if (lane < 32u) {
-                const float f = lane < 16u ? scale : 1.0f;
-                lds_step[b][lane >> 4][0][16u * group16 + (lane & 15u)] = f * step;
-                if constexpr (BITS == 4) lds_step[b][lane >> 4][1][16u * group16 + (lane & 15u)] = f * low;
-                if (lane >= 16u) lds_reach[b][16u * group16 + (lane & 15u)] = reach_of(step);
-            }
-        }
-    };
-
-    auto hold = []() {                                             // (with codes there are not the registers for it)
-        if constexpr (BITS == 16) __builtin_amdgcn_sched_barrier(0);
-    };
-    typedef float f32x16 __attribute__((ext_vector_type(16)));
-    f32x16 acc[kTiles];
+            } else {
 #pragma unroll
-    for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-        for (int x = 0; x < 16; ++x) acc[i][x] = 0.0f;
-    // m: the maximum that weights are taken against, as in the kernel for few rows; it may lie up to 8 below the true one
-    float m = kNone, m_true = kNone, l = 0.0f, z_acc = 0.0f;
-
-    auto compute = [&](uint32_t t, auto buffer) {
-        const int b = buffer;
-        const uint4 *lds_k = b ? lds_k1 : lds_k0, *lds_v = b ? lds_v1 : lds_v0;
-        const uint32_t key0 = t * KT;
-        const bool masked = key0 + KT > all_see;                   // not all rows see all of the tile
-        float w[16 * kHalves];
-        // What is read of K and V is asked for a few products ahead, V's first half before the weights are worked out.  (Left to the
-        // compiler, the reads come pair by pair right before their products, and a wavefront waits for each: 140 us
-        // in the place of 133 for 2048 tokens over 4096 keys.)
-        half8v kf[kHalves][kSteps];
-        const uint32_t key_n = here(n);
-        auto read_k = [&](int y) {
-#pragma unroll
-            for (int x = 0; x < kHalves; ++x) {
-                const uint32_t key = 32u * (half0 + x) + key_n;
-                kf[x][y] = __builtin_bit_cast(half8v, lds_k[key * RC + ((2u * y + h) ^ k_swap<RC>(key))]);
+                for (int i = 0; i < kIssues; ++i) {
+                    const uint32_t x = 64u * i + self, r = x / RC, c = x % RC, kk = 16u * group16 + r;
+                    if (c < pieces) {
+                        if (brings_k) lds_k[kk * RC + (c ^ k_swap<RC>(kk))] = code_values<BITS>(raw_k[i]);
+                        if (brings_v) lds_v[kk * RC + (c ^ v_swap<RC>(kk))] = code_values<BITS>(raw_v[i]);
+                    }
+                }
+                const bool in = key0 + (lane & 15u) < end;
+                if constexpr (TREE)                                    // (a node that was left out may have a step that is none)
+                    if (!(BITS == 8 ? finite(__uint_as_float(raw_step)) : half_finite(raw_step) && half_finite(raw_step >> 16))) raw_step = 0u;
+                const float step = !in ? 0.0f : BITS == 8 ? __uint_as_float(raw_step) : step_of(raw_step);
+                const float low = !in || BITS == 8 ? 0.0f : low_of(raw_step);
+                if (lane < 32u) {
+                    const float f = lane < 16u ? scale : 1.0f;
+                    lds_step[b][lane >> 4][0][16u * group16 + (lane & 15u)] = f * step;
+                    if constexpr (BITS == 4) lds_step[b][lane >> 4][1][16u * group16 + (lane & 15u)] = f * low;
+                    if (lane >= 16u) lds_reach[b][16u * group16 + (lane & 15u)] = reach_of(step);
+                }
             }
         };
-        constexpr int kAhead = kSteps < 4 ? kSteps : 4;
-#pragma unroll
-        for (int y = 0; y < kAhead; ++y) read_k(y);
-        hold();
-        typedef short s16x4 __attribute__((ext_vector_type(4)));
-        const uint32_t i16 = lane & 15u, sub = (lane >> 4) & 1u;   // a lane of 16: row i16 / 4 of four keys, values 4 (i16 % 4) ... + 3
-        constexpr int kReads = 4 * kHalves * kTiles;               // [16 keys][8 of them][32 values]
-        s16x4 vf[kReads];
-        auto read_v = [&](int i) {
-            const int x = i / (2 * kTiles), y = i % (2 * kTiles) / 2, e = i % 2;
-            const uint32_t key = 32u * half0 + 16u * x + 8u * e + 4u * h + i16 / 4u;
-            const uint32_t c = 4u * y + 2u * sub + ((i16 >> 1) & 1u);
-            const uint4 *p = &lds_v[key * RC + (c ^ v_swap<RC>(key))];
-            vf[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(reinterpret_cast<const uint2 *>(p) + (i16 & 1u)));
+
+        auto hold = []() {                                             // (with codes there are not the registers for it)
+            if constexpr (BITS == 16) __builtin_amdgcn_sched_barrier(0);
         };
-        f32x16 c[kHalves];
+        typedef float f32x16 __attribute__((ext_vector_type(16)));
+        f32x16 acc[kTiles];
 #pragma unroll
-        for (int x = 0; x < kHalves; ++x) c[x] = f32x16{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+        for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-        for (int y = 0; y < kSteps; ++y) {
+            for (int x = 0; x < 16; ++x) acc[i][x] = 0.0f;
+        // m: the maximum that weights are taken against, as in the kernel for few rows; it may lie up to 8 below the true one
+        float m = kNone, m_true = kNone, l = 0.0f, z_acc = 0.0f;
+
+        auto compute = [&](uint32_t t, auto buffer) {
+            const int b = buffer;
+            const uint4 *lds_k = b ? lds_k1 : lds_k0, *lds_v = b ? lds_v1 : lds_v0;
+            const uint32_t key0 = t * KT;
+            const bool masked = key0 + KT > all_see;                   // not all rows see all of the tile
+            float w[16 * kHalves];
+            // What is read of K and V is asked for a few products ahead, V's first half before the weights are worked out.  (Left to the
+            // compiler, the reads come pair by pair right before their products, and a wavefront waits for each: 140 us
+            // in the place of 133 for 2048 tokens over 4096 keys.)
+            half8v kf[kHalves][kSteps];
+            const uint32_t key_n = here(n);
+            auto read_k = [&](int y) {
 #pragma unroll
-            for (int x = 0; x < kHalves; ++x) c[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[x][y], q[y], c[x], 0, 0, 0);
-            if (y + kAhead < kSteps) read_k(y + kAhead);
-            if (y >= kSteps - kAhead)
+                for (int x = 0; x < kHalves; ++x) {
+                    const uint32_t key = 32u * (half0 + x) + key_n;
+                    kf[x][y] = __builtin_bit_cast(half8v, lds_k[key * RC + ((2u * y + h) ^ k_swap<RC>(key))]);
+                }
+            };
+            constexpr int kAhead = kSteps < 4 ? kSteps : 4;
 #pragma unroll
-                for (int i = (y + kAhead - kSteps) * (kReads / 2) / kAhead; i < (y + 1 + kAhead - kSteps) * (kReads / 2) / kAhead; ++i) read_v(i);
+            for (int y = 0; y < kAhead; ++y) read_k(y);
             hold();
-        }
+            typedef short s16x4 __attribute__((ext_vector_type(4)));
+            const uint32_t i16 = lane & 15u, sub = (lane >> 4) & 1u;   // a lane of 16: row i16 / 4 of four keys, values 4 (i16 % 4) ... + 3
+            constexpr int kReads = 4 * kHalves * kTiles;               // [16 keys][8 of them][32 values]
+            s16x4 vf[kReads];
+            auto read_v = [&](int i) {
+                const int x = i / (2 * kTiles), y = i % (2 * kTiles) / 2, e = i % 2;
+                const uint32_t key = 32u * half0 + 16u * x + 8u * e + 4u * h + i16 / 4u;
+                const uint32_t c = 4u * y + 2u * sub + ((i16 >> 1) & 1u);
+                const uint4 *p = &lds_v[key * RC + (c ^ v_swap<RC>(key))];
+                vf[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(reinterpret_cast<const uint2 *>(p) + (i16 & 1u)));
+            };
+            f32x16 c[kHalves];
 #pragma unroll
-        for (int i = 0; i < 16 * kHalves; ++i) w[i] = c[i / 16][i % 16];
-        if constexpr (BITS < 16) {
+            for (int x = 0; x < kHalves; ++x) c[x] = f32x16{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-            for (int i = 0; i < 16 * kHalves; i += 4) {            // (the steps of the keys have the scale in them)
-                const uint32_t key = 32u * half0 + 8u * (i / 4) + 4u * h;
-                const f32x4 step = *reinterpret_cast<const f32x4 *>(&lds_step[b][0][0][key]);
-                if constexpr (BITS == 4) {
-                    const f32x4 low = *reinterpret_cast<const f32x4 *>(&lds_step[b][0][1][key]) * q_sum;
+            for (int y = 0; y < kSteps; ++y) {
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) w[i + r] = fmaf(w[i + r], step[r], low[r]);
-                } else {
+                for (int x = 0; x < kHalves; ++x) c[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[x][y], q[y], c[x], 0, 0, 0);
+                if (y + kAhead < kSteps) read_k(y + kAhead);
+                if (y >= kSteps - kAhead)
+#pragma unroll
+                    for (int i = (y + kAhead - kSteps) * (kReads / 2) / kAhead; i < (y + 1 + kAhead - kSteps) * (kReads / 2) / kAhead; ++i) read_v(i);
+                hold();
+            }
+#pragma unroll
+            for (int i = 0; i < 16 * kHalves; ++i) w[i] = c[i / 16][i % 16];
+            if constexpr (BITS < 16) {
+#pragma unroll
+                for (int i = 0; i < 16 * kHalves; i += 4) {            // (the steps of the keys have the scale in them)
+                    const uint32_t key = 32u * half0 + 8u * (i / 4) + 4u * h;
+                    const f32x4 step = *reinterpret_cast<const f32x4 *>(&lds_step[b][0][0][key]);
+                    if constexpr (BITS == 4) {
+                        const f32x4 low = *reinterpret_cast<const f32x4 *>(&lds_step[b][0][1][key]) * q_sum;
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) w[i + r] = fmaf(w[i + r], step[r], low[r]);
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) w[i + r] *= step[r];
+                    }
+                }
+            }
+            if (TREE && masked) {
+                if constexpr (TREE)
+#pragma unroll
+                    for (int x = 0; x < kHalves; ++x) {
+                        const uint32_t bits = seen_bits(a, here(s.first + token), key0 + 32u * (half0 + x), s.behind, end) >> (4u * h);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (!(bits >> (8 * (i / 4) + (i & 3)) & 1u)) w[16 * x + i] = kNone;
+                    }
+            } else if (masked) {
+                int32_t left = seen - (int32_t)(key0 + 32u * half0 + 4u * h);
+                asm volatile("" : "+v"(left));                         // (kept a branch: few tiles take it)
+#pragma unroll
+                for (int i = 0; i < 16 * kHalves; ++i)
+                    if (8 * (i / 4) + (i & 3) >= left) w[i] = kNone;
+            }
+            float most = kNone;
+            if constexpr (BITS == 16) {
+#pragma unroll
+                for (int i = 0; i < 16 * kHalves; ++i) most = fmaxf(most, w[i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16 * kHalves; i += 4) {
+                    const f32x4 reach = *reinterpret_cast<const f32x4 *>(&lds_reach[b][32u * half0 + 8u * (i / 4) + 4u * h]);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) most = fmaxf(most, w[i + r] + reach[r]);
+                }
+            }
+            const float m_new = m_true = fmaxf(m_true, max_over_32(most) * by);
+            if (const bool far = m_new > m + 8.0f; __any((int)far)) {
+                const float alpha = far ? __builtin_amdgcn_exp2f(m - m_new) : 1.0f;       // (0 where nothing was seen before)
+                m = far ? m_new : m;                                   // a row goes by its own scores alone
+                l *= alpha;
+                z_acc *= alpha;
+#pragma unroll
+                for (int i = 0; i < kTiles; ++i) acc[i] *= alpha;
+            }
+            const float base = m == kNone ? 0.0f : m;
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 16 * kHalves; ++i) {
+                w[i] = __builtin_amdgcn_exp2f(BITS == 16 ? fmaf(w[i], by, -base) : w[i] - base);
+                if constexpr (BITS < 16) sum += w[i];                  // (with FP16 the rounded ones are added up, below)
+            }
+            if constexpr (BITS < 16) {
+#pragma unroll
+                for (int i = 0; i < 16 * kHalves; i += 4) {
+                    const uint32_t key = 32u * half0 + 8u * (i / 4) + 4u * h;
+                    const f32x4 step = *reinterpret_cast<const f32x4 *>(&lds_step[b][1][0][key]);
+                    if constexpr (BITS == 4) {
+                        const f32x4 low = *reinterpret_cast<const f32x4 *>(&lds_step[b][1][1][key]);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) z_acc = fmaf(w[i + r], low[r], z_acc);
+                    }
 #pragma unroll
                     for (int r = 0; r < 4; ++r) w[i + r] *= step[r];
                 }
             }
-        }
-        if (TREE && masked) {
-            if constexpr (TREE)
+            half8v weights[2 * kHalves];
 #pragma unroll
-                for (int x = 0; x < kHalves; ++x) {
-                    const uint32_t bits = seen_bits(a, here(s.first + token), key0 + 32u * (half0 + x), s.behind, end) >> (4u * h);
+            for (int x = 0; x < 2 * kHalves; ++x) {
+                uint32_t o[4];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (!(bits >> (8 * (i / 4) + (i & 3)) & 1u)) w[16 * x + i] = kNone;
+                for (int i = 0; i < 4; ++i) {
+                    const half2v p = {(_Float16)w[8 * x + 2 * i], (_Float16)w[8 * x + 2 * i + 1]};
+                    if constexpr (BITS == 16) sum = __builtin_amdgcn_fdot2(p, half2v{(_Float16)1.0f, (_Float16)1.0f}, sum, false);
+                    o[i] = as_word(p);
                 }
-        } else if (masked) {
-            int32_t left = seen - (int32_t)(key0 + 32u * half0 + 4u * h);
-            asm volatile("" : "+v"(left));                         // (kept a branch: few tiles take it)
-#pragma unroll
-            for (int i = 0; i < 16 * kHalves; ++i)
-                if (8 * (i / 4) + (i & 3) >= left) w[i] = kNone;
-        }
-        float most = kNone;
-        if constexpr (BITS == 16) {
-#pragma unroll
-            for (int i = 0; i < 16 * kHalves; ++i) most = fmaxf(most, w[i]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 16 * kHalves; i += 4) {
-                const f32x4 reach = *reinterpret_cast<const f32x4 *>(&lds_reach[b][32u * half0 + 8u * (i / 4) + 4u * h]);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) most = fmaxf(most, w[i + r] + reach[r]);
+                weights[x] = as_half8(o[0], o[1], o[2], o[3]);
             }
-        }
-        const float m_new = m_true = fmaxf(m_true, max_over_32(most) * by);
-        if (const bool far = m_new > m + 8.0f; __any((int)far)) {
-            const float alpha = far ? __builtin_amdgcn_exp2f(m - m_new) : 1.0f;       // (0 where nothing was seen before)
-            m = far ? m_new : m;                                   // a row goes by its own scores alone
-            l *= alpha;
-            z_acc *= alpha;
+            l += sum;
 #pragma unroll
-            for (int i = 0; i < kTiles; ++i) acc[i] *= alpha;
-        }
-        const float base = m == kNone ? 0.0f : m;
-        float sum = 0.0f;
+            for (int x = 0; x < 2 * kHalves; ++x)
 #pragma unroll
-        for (int i = 0; i < 16 * kHalves; ++i) {
-            w[i] = __builtin_amdgcn_exp2f(BITS == 16 ? fmaf(w[i], by, -base) : w[i] - base);
-            if constexpr (BITS < 16) sum += w[i];                  // (with FP16 the rounded ones are added up, below)
-        }
-        if constexpr (BITS < 16) {
-#pragma unroll
-            for (int i = 0; i < 16 * kHalves; i += 4) {
-                const uint32_t key = 32u * half0 + 8u * (i / 4) + 4u * h;
-                const f32x4 step = *reinterpret_cast<const f32x4 *>(&lds_step[b][1][0][key]);
-                if constexpr (BITS == 4) {
-                    const f32x4 low = *reinterpret_cast<const f32x4 *>(&lds_step[b][1][1][key]);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) z_acc = fmaf(w[i + r], low[r], z_acc);
-                }
-#pragma unroll
-                for (int r = 0; r < 4; ++r) w[i + r] *= step[r];
-            }
-        }
-        half8v weights[2 * kHalves];
-#pragma unroll
-        for (int x = 0; x < 2 * kHalves; ++x) {
-            uint32_t o[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const half2v p = {(_Float16)w[8 * x + 2 * i], (_Float16)w[8 * x + 2 * i + 1]};
-                if constexpr (BITS == 16) sum = __builtin_amdgcn_fdot2(p, half2v{(_Float16)1.0f, (_Float16)1.0f}, sum, false);
-                o[i] = as_word(p);
-            }
-            weights[x] = as_half8(o[0], o[1], o[2], o[3]);
-        }
-        l += sum;
-#pragma unroll
-        for (int x = 0; x < 2 * kHalves; ++x)
-#pragma unroll
-            for (int y = 0; y < kTiles; ++y) {
-                const int at = x * kTiles + y;
-                const uint2 lo = __builtin_bit_cast(uint2, vf[2 * at]), hi = __builtin_bit_cast(uint2, vf[2 * at + 1]);
-                acc[y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_half8(lo.x, lo.y, hi.x, hi.y), weights[x], acc[y], 0, 0, 0);
-                if (2 * at + 1 + kReads / 2 < kReads) {
-                    read_v(2 * at + kReads / 2);
-                    read_v(2 * at + 1 + kReads / 2);
-                    hold();
-                }
-            }
-    };
-
-    auto step = [&](uint32_t t, auto buffer, auto other) {
-        if (t + 1u < t1) request(t + 1u, other);
-        if (t * KT < wave_end) compute(t, buffer);
-        if (t + 1u < t1) arrive(t + 1u, other);
-        __syncthreads();
-    };
-    if (t0 < t1) {
-        const std::integral_constant<int, 0> first;
-        const std::integral_constant<int, 1> second;
-        request(t0, first);
-        arrive(t0, first);
-        __syncthreads();
-        if constexpr (BITS == 16) {
-            for (uint32_t t = t0; t < t1; t += 2u) {
-                step(t, first, second);
-                if (t + 1u < t1) step(t + 1u, second, first);
-            }
-        } else {                                                   // (nothing goes straight to LDS: one copy of the code, and fewer registers)
-            for (uint32_t t = t0, b = 0; t < t1; ++t, b ^= 1u) step(t, (int)b, (int)(b ^ 1u));
-        }
-    }
-
-    if constexpr (BITS == 16) {
-        // Where V was not finite, as in the kernel for few rows
-        bool odd = (lds_odd[0] | lds_odd[1]) != 0u;
-#pragma unroll
-        for (int y = 0; y < kTiles; ++y)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                odd |= !finite(acc[y][i]);
-                acc[y][i] = finite(acc[y][i]) ? acc[y][i] : 0.0f;
-            }
-        if (__any((int)odd)) {
-            const uint32_t last = min(t1 * KT, end);
-#pragma unroll 1
-            for (uint32_t key = t0 * KT; key < last; ++key) {
-                if constexpr (TREE) {
-                    if (!(seen_bits(a, s.first + token, key, s.behind, end) & 1u)) continue;
-                } else {
-                    if ((int32_t)key >= seen) continue;
-                }
-                const uint64_t at = (uint64_t)page_of(a, s.table, key) * page_rows + head_rows + (key & page_mask);
-                const uint16_t *vp = reinterpret_cast<const uint16_t *>(a.cache.v + at * a.cache.row_bytes);
-#pragma unroll
-                for (int y = 0; y < kTiles; ++y)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const uint32_t d = 32u * y + 8u * (i / 4) + 4u * h + (i & 3);
-                        if (d < dim && !half_finite(vp[d])) acc[y][i] += half_to_float(vp[d]);
+                for (int y = 0; y < kTiles; ++y) {
+                    const int at = x * kTiles + y;
+                    const uint2 lo = __builtin_bit_cast(uint2, vf[2 * at]), hi = __builtin_bit_cast(uint2, vf[2 * at + 1]);
+                    acc[y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_half8(lo.x, lo.y, hi.x, hi.y), weights[x], acc[y], 0, 0, 0);
+                    if (2 * at + 1 + kReads / 2 < kReads) {
+                        read_v(2 * at + kReads / 2);
+                        read_v(2 * at + 1 + kReads / 2);
+                        hold();
                     }
+                }
+        };
+
+        auto step = [&](uint32_t t, auto buffer, auto other) {
+            if (t + 1u < t1) request(t + 1u, other);
+            if (t * KT < wave_end) compute(t, buffer);
+            if (t + 1u < t1) arrive(t + 1u, other);
+            __syncthreads();
+        };
+        if (t0 < t1) {
+            const std::integral_constant<int, 0> first;
+            const std::integral_constant<int, 1> second;
+            request(t0, first);
+            arrive(t0, first);
+            __syncthreads();
+            if constexpr (BITS == 16) {
+                for (uint32_t t = t0; t < t1; t += 2u) {
+                    step(t, first, second);
+                    if (t + 1u < t1) step(t + 1u, second, first);
+                }
+            } else {                                                   // (nothing goes straight to LDS: one copy of the code, and fewer registers)
+                for (uint32_t t = t0, b = 0; t < t1; ++t, b ^= 1u) step(t, (int)b, (int)(b ^ 1u));
             }
         }
-    }
 
-    l += __shfl_xor(l, 32, 64);
-    if constexpr (BITS == 4) z_acc += __shfl_xor(z_acc, 32, 64);
-    if constexpr (ON_KEYS == 2) {
-        // the second half's results to the wavefront that has the first (the last tile has been waited for by all)
-        __shared__ float lds_mlz[2][3][32];
-        const uint32_t pair = wave & 1u;
-        uint4 *to = pair ? lds_v0 : lds_k0;
-        if (wave >= 2u) {
+        if constexpr (BITS == 16) {
+            // Where V was not finite, as in the kernel for few rows
+            bool odd = (lds_odd[0] | lds_odd[1]) != 0u;
 #pragma unroll
             for (int y = 0; y < kTiles; ++y)
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    to[64u * (4 * y + i) + lane] = __builtin_bit_cast(uint4, f32x4{acc[y][4 * i], acc[y][4 * i + 1], acc[y][4 * i + 2], acc[y][4 * i + 3]});
-            if (h == 0) lds_mlz[pair][0][n] = m, lds_mlz[pair][1][n] = l, lds_mlz[pair][2][n] = z_acc;
-        }
-        __syncthreads();
-        if (wave >= 2u) return;
-        const float other = lds_mlz[pair][0][n], top = fmaxf(m, other), f0 = share_of(m, top), f1 = share_of(other, top);
-        m = top;
-        l = f0 * l + f1 * lds_mlz[pair][1][n];
-        z_acc = f0 * z_acc + f1 * lds_mlz[pair][2][n];
+                for (int i = 0; i < 16; ++i) {
+                    odd |= !finite(acc[y][i]);
+                    acc[y][i] = finite(acc[y][i]) ? acc[y][i] : 0.0f;
+                }
+            if (__any((int)odd)) {
+                const uint32_t last = min(t1 * KT, end);
+#pragma unroll 1
+                for (uint32_t key = t0 * KT; key < last; ++key) {
+                    if constexpr (TREE) {
+                        if (!(seen_bits(a, s.first + token, key, s.behind, end) & 1u)) continue;
+                    } else {
+                        if ((int32_t)key >= seen) continue;
+                    }
+                    const uint64_t at = (uint64_t)page_of(a, s.table, key) * page_rows + head_rows + (key & page_mask);
+                    const uint16_t *vp = reinterpret_cast<const uint16_t *>(a.cache.v + at * a.cache.row_bytes);
 #pragma unroll
-        for (int y = 0; y < kTiles; ++y)
+                    for (int y = 0; y < kTiles; ++y)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const f32x4 o = __builtin_bit_cast(f32x4, to[64u * (4 * y + i) + lane]);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) acc[y][4 * i + r] = f0 * acc[y][4 * i + r] + f1 * o[r];
-            }
-    }
-    const uint32_t out_row = wave_row + n;
-    if (out_row >= rows) return;
-    const uint32_t out_head = head * a.group + (row - token * a.group);
-    if (splits == 1u) {
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-        uint16_t *p = a.out.data + (int64_t)(s.first + token) * a.out.token_stride + (int64_t)out_head * a.out.head_stride;
-#pragma unroll
-        for (int y = 0; y < kTiles; ++y)
-#pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-                const uint32_t d = 32u * y + 8u * (i / 4) + 4u * h;
-                if (d >= dim) continue;
-                uint32_t o[2];
-#pragma unroll
-                for (int r = 0; r < 2; ++r)
-                    o[r] = as_word(half2v{to_result((acc[y][i + 2 * r] + z_acc) * inv), to_result((acc[y][i + 2 * r + 1] + z_acc) * inv)});
-                if (a.out_wide) {
-                    *reinterpret_cast<uint2 *>(p + d) = make_uint2(o[0], o[1]);
-                } else {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) p[(int64_t)(d + r) * a.out.dim_stride] = (uint16_t)(o[r >> 1] >> (16 * (r & 1)));
+                        for (int i = 0; i < 16; ++i) {
+                            const uint32_t d = 32u * y + 8u * (i / 4) + 4u * h + (i & 3);
+                            if (d < dim && !half_finite(vp[d])) acc[y][i] += half_to_float(vp[d]);
+                        }
                 }
             }
-    } else {
-        uint64_t at = ((uint64_t)split * a.tokens + s.first + token) * a.q_heads + out_head;
-        if constexpr (TREE)
-            if (a.balanced) at = ((uint64_t)base + split * rows + out_row) * a.cache.heads + head;
+        }
+
+        l += __shfl_xor(l, 32, 64);
+        if constexpr (BITS == 4) z_acc += __shfl_xor(z_acc, 32, 64);
+        if constexpr (kShared == 2) {
+            // the second half's results to the wavefront that has the first (the last tile has been waited for by all)
+            const uint32_t pair = wave & 1u;
+            uint4 *to = pair ? lds_v0 : lds_k0;
+            if (wave >= 2u) {
 #pragma unroll
-        for (int y = 0; y < kTiles; ++y)
+                for (int y = 0; y < kTiles; ++y)
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-                const uint32_t d = 32u * y + 8u * (i / 4) + 4u * h;
-                if (d < dim)
-                    *reinterpret_cast<f32x4 *>(a.part_o + at * dim + d) =
-                        f32x4{acc[y][i] + z_acc, acc[y][i + 1] + z_acc, acc[y][i + 2] + z_acc, acc[y][i + 3] + z_acc};
+                    for (int i = 0; i < 4; ++i)
+                        to[64u * (4 * y + i) + lane] = __builtin_bit_cast(uint4, f32x4{acc[y][4 * i], acc[y][4 * i + 1], acc[y][4 * i + 2], acc[y][4 * i + 3]});
+                if (h == 0) lds_mlz[pair][0][n] = m, lds_mlz[pair][1][n] = l, lds_mlz[pair][2][n] = z_acc;
             }
-        if (h == 0) a.part_ml[2 * at] = m, a.part_ml[2 * at + 1] = l;
+            __syncthreads();
+            if (wave >= 2u) return;
+            const float other = lds_mlz[pair][0][n], top = fmaxf(m, other), f0 = share_of(m, top), f1 = share_of(other, top);
+            m = top;
+            l = f0 * l + f1 * lds_mlz[pair][1][n];
+            z_acc = f0 * z_acc + f1 * lds_mlz[pair][2][n];
+#pragma unroll
+            for (int y = 0; y < kTiles; ++y)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const f32x4 o = __builtin_bit_cast(f32x4, to[64u * (4 * y + i) + lane]);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[y][4 * i + r] = f0 * acc[y][4 * i + r] + f1 * o[r];
+                }
+        }
+        const uint32_t out_row = wave_row + n;
+        if (out_row >= rows) return;
+        const uint32_t out_head = head * a.group + (row - token * a.group);
+        if (splits == 1u) {
+            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+            uint16_t *p = a.out.data + (int64_t)(s.first + token) * a.out.token_stride + (int64_t)out_head * a.out.head_stride;
+#pragma unroll
+            for (int y = 0; y < kTiles; ++y)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    const uint32_t d = 32u * y + 8u * (i / 4) + 4u * h;
+                    if (d >= dim) continue;
+                    uint32_t o[2];
+#pragma unroll
+                    for (int r = 0; r < 2; ++r)
+                        o[r] = as_word(half2v{to_result((acc[y][i + 2 * r] + z_acc) * inv), to_result((acc[y][i + 2 * r + 1] + z_acc) * inv)});
+                    if (a.out_wide) {
+                        *reinterpret_cast<uint2 *>(p + d) = make_uint2(o[0], o[1]);
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) p[(int64_t)(d + r) * a.out.dim_stride] = (uint16_t)(o[r >> 1] >> (16 * (r & 1)));
+                    }
+                }
+        } else {
+            uint64_t at = ((uint64_t)split * a.tokens + s.first + token) * a.q_heads + out_head;
+            if constexpr (TREE)
+                if (a.balanced) at = ((uint64_t)base + split * rows + out_row) * a.cache.heads + head;
+#pragma unroll
+            for (int y = 0; y < kTiles; ++y)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    const uint32_t d = 32u * y + 8u * (i / 4) + 4u * h;
+                    if (d < dim)
+                        *reinterpret_cast<f32x4 *>(a.part_o + at * dim + d) =
+                            f32x4{acc[y][i] + z_acc, acc[y][i + 1] + z_acc, acc[y][i + 2] + z_acc, acc[y][i + 3] + z_acc};
+                }
+            if (h == 0) a.part_ml[2 * at] = m, a.part_ml[2 * at + 1] = l;
+        }
+    };
+    if constexpr (kByRows) {
+        if (rows - row0 <= 64u)
+            work(std::integral_constant<int, 2>());
+        else
+            work(std::integral_constant<int, 1>());
+    } else {
+        work(std::integral_constant<int, ON_KEYS>());
     }
 }
 
