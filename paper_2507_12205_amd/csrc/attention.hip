@@ -216,8 +216,9 @@ __device__ __forceinline__ uint32_t seen_bits(const ecs::AttentionTreeArgs &a, u
 // For rows that all see all keys, the work of a sequence is (tiles of its rows) x (tiles of its keys).  Sequences differ in both, and the host
 // sees neither, so that the workgroups of a launch are dealt out here, by every one of them for itself: with each sequence's keys cut into
 // pieces of L tiles at most, L is the least length (but for a few steps of halving) at which all pieces find a workgroup.
-// (us by equal numbers of splits for all / by this: 16 trees of up to 16 nodes over up to 8192 keys, 64/8 heads of 128, 8 bits, 98.7 / 85.8 at that time; eight of up to
-// 49 over up to 2000, 32 heads of 80, 4 bits, 61.2 / 41.8.)
+// (us by equal numbers of splits for all / by this, all else as it was then: 16 trees of up to 16 nodes over up to 8192 keys, 64/8 heads of 128, 8 bits,
+// 98.7 / 85.8; eight of up to 49 over up to 2000, 32 heads of 80, 4 bits, 61.2 / 41.8.)
+
 // inclusive results over the lanes of an operation whose neutral element is all zeros
 template <class T, class F>
 __device__ __forceinline__ T lanes_scan(T v, F with)

@@ -292,3 +292,39 @@ def test_very_many_sequences():
     out, i = torch.full_like(q, float("nan")), torch.arange(n + 1, dtype=torch.int32, device="cuda")
     D.attention_tree(cache, q, out, i, torch.ones(n, dtype=torch.int32, device="cuda"), i[:n, None], torch.ones((n, 1), dtype=torch.int32, device="cuda"), 1)
     assert torch.equal(out, v)
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+def test_two_graphs_that_share_a_workspace(bits):
+    """Attention of a row of new tokens and of trees, captured apart with one workspace for both: its contents do not matter before and after."""
+    import torch
+    from paper_2507_12205_amd import device as D
+    made = [make(torch, D, new, total, 4, 2, 64, 16, bits, seed=i) for i, (new, total) in enumerate((([5, 2], [1600, 700]), ([40, 9, 3], [900, 2000, 30])))]
+    seen = [trees(np.random.default_rng(i), list(np.diff(m[2]))) for i, m in enumerate(made)]
+    ws = torch.empty(max(D.attention_workspace(m[0], m[1], len(m[3]), 40, 2048).nbytes for m in made), dtype=torch.uint8, device="cuda")
+    graphs, outs, eager, kept = [], [], [], []
+    for m, s in zip(made, seen):
+        cache, q, *rest = m
+        args = [torch.from_numpy(np.ascontiguousarray(x)).cuda() for x in (*rest, words_of(s))]
+        tree_out, row_out, most = torch.empty_like(q), torch.empty_like(q), int(np.diff(m[2]).max())
+        kept.append(args)                                    # what the graphs read
+
+        def call(work):
+            D.attention_tree(cache, q, tree_out, *args, most, None, work)
+            D.attention(cache, q, row_out, *args[:3], most, None, work)
+        call(None)
+        eager.append((tree_out.clone(), row_out.clone()))
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call(ws)
+        graphs.append(graph)
+        outs.append((tree_out, row_out))
+    for turn in (0, 1, 1, 0, 1, 0, 0):
+        for t in outs[turn]:
+            t.fill_(float("nan"))
+        graphs[turn].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(outs[turn], eager[turn]))
+        if turn:
+            ws.fill_(255)
