@@ -251,7 +251,13 @@ struct Share {
     uint32_t base;                        // balanced: where the sequence's partial results start, in rows of all heads of the cache
 };
 
-template <uint32_t ROWS, uint32_t KEYS, uint32_t HALF>
+// Keys up to which sequences are left whole: what a split saves has to be more than the join and its launch take.  us in a graph, whole / split: 16 rows,
+// four sequences of 8 tokens, 32 heads of 128, 768 keys FP16 12.9 / 14.4, 8 bits 12.9 / 12.0, 4 bits 12.4 / 14.4, 908 keys 15.0 / 17.6, 15.9 / 14.7, 14.2 / 13.8; one
+// of 8, 508 keys 9.5 / 11.7, 908 14.9 / 12.6; rows that share keys in LDS, FP16, eight sequences of 30 tokens, 430 keys 16.8 / 19.9, four, 530 17.7 / 19.6, one
+// of 64, 704 19.0 / 15.9; 4 bits, one of 40, 540 keys 21.2 / 16.1.
+__host__ __device__ constexpr uint32_t whole_keys(bool few_rows, bool codes) { return few_rows ? 768u : codes ? 256u : 512u; }
+
+template <uint32_t ROWS, uint32_t KEYS, uint32_t HALF, uint32_t WHOLE>
 __device__ __forceinline__ Share share_of_work(const ecs::AttentionTreeArgs &a, bool first_wave)
 {
     const uint32_t slot = blockIdx.y + gridDim.y * blockIdx.z;     // (blockIdx.x: the head)
@@ -273,7 +279,7 @@ __device__ __forceinline__ Share share_of_work(const ecs::AttentionTreeArgs &a, 
     // as many pieces as the chip has workgroups at once, or, with more tiles of rows than that, as it has in whole rounds
     const uint32_t goal = min(a.slots, max((all + a.at_once - 1u) / a.at_once, 1u) * a.at_once);
     // the least length there could be, and one at which it works out: work / length + all <= goal (in case FP32 says otherwise: no pieces)
-    uint32_t low = max((uint32_t)(work / (float)goal), 256u / KEYS), length = longest;
+    uint32_t low = longest <= WHOLE / KEYS ? longest : max((uint32_t)(work / (float)goal), 256u / KEYS), length = longest;
     if (goal > all) {
         const uint32_t enough = max((uint32_t)(work / (float)(goal - all)) + 1u, low);
         if (last_lane(sums_to(items * pieces(enough))) <= goal) length = min(length, enough);
@@ -333,7 +339,7 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) :
     uint32_t tile = blockIdx.x / a.splits, split = blockIdx.x - tile * a.splits, head = blockIdx.y, seq = blockIdx.z, splits = a.splits, base = 0;
     if constexpr (TREE) {
         head = blockIdx.x;
-        const Share mine = share_of_work<16, 32, 16>(a, tid < 64u);
+        const Share mine = share_of_work<16, 32, 16, whole_keys(true, BITS < 16)>(a, tid < 64u);
         tile = mine.tile, split = mine.split, seq = mine.seq, splits = mine.splits, base = mine.base;
         if (splits == 0) return;
     }
@@ -734,7 +740,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
     else
         tile -= (a.row_tiles + 1u) / 2u;
     if constexpr (TREE) {
-        const Share mine = share_of_work<kRows, KT, kByRows ? 11 : 16>(a, tid < 64u);
+        const Share mine = share_of_work<kRows, KT, kByRows ? 11 : 16, whole_keys(false, BITS < 16)>(a, tid < 64u);
         tile = mine.tile, split = mine.split, seq = mine.seq, splits = mine.splits, base = mine.base;
         if (splits == 0) return;
     }
@@ -1442,7 +1448,7 @@ TreePlan plan_attention_tree(uint32_t batch, uint32_t kv_heads, uint32_t group, 
                              uint64_t max_kv)
 {
     TreePlan t = {};
-    const uint64_t rows = (uint64_t)max_new * group, keys = splits_of_keys(max_kv);
+    const uint64_t rows = (uint64_t)max_new * group;
     t.chunk = rows <= tree_rows_of_16(dim, bits) ? 0u : dim > 128u || rows <= kHalfRows ? 2u : 1u;
     const uint32_t per_tile = t.chunk == 0u ? kFewRows : t.chunk == 1u ? kChunkRows : kHalfRows;
     t.row_tiles = (uint32_t)((rows + per_tile - 1u) / per_tile);
@@ -1453,15 +1459,15 @@ TreePlan plan_attention_tree(uint32_t batch, uint32_t kv_heads, uint32_t group, 
     t.splits = 1;
     t.slots = items;
     if (batch > kTreeSequences) {                                  // (more sequences than the lanes of a wavefront: equal splits for all)
-        t.splits = (uint32_t)std::max<uint64_t>(1u, std::min(at_once / std::max<uint64_t>(items, 1u), keys));
+        t.splits = (uint32_t)std::max<uint64_t>(1u, std::min(at_once / std::max<uint64_t>(items, 1u), splits_of_keys(max_kv)));
         t.slots = items * t.splits;
         if (t.splits > 1u) t.work_bytes = (uint64_t)t.splits * tokens * kv_heads * group * (dim + 2u) * sizeof(float);
-    } else if (keys > 1u && (batch > 1u ? items < 2u * at_once : items < at_once)) {
+    } else if (max_kv > whole_keys(t.chunk == 0u, bits < 16u) && (batch > 1u ? items < 2u * at_once : items < at_once)) {
         // (one sequence with a tile of rows for every workgroup, and several that fill the chip twice over, are left whole)
         t.balanced = 1;
         t.at_once = (uint32_t)at_once;
         t.slots = std::max(items, at_once);
-        t.part_rows = (uint32_t)std::min<uint64_t>(t.slots * per_tile, keys * std::min<uint64_t>(tokens, (uint64_t)batch * max_new) * group);
+        t.part_rows = (uint32_t)std::min<uint64_t>(t.slots * per_tile, splits_of_keys(max_kv) * std::min<uint64_t>(tokens, (uint64_t)batch * max_new) * group);
         t.work_bytes = kTreePlanBytes + (uint64_t)t.part_rows * kv_heads * (dim + 2u) * sizeof(float);
     }
     return t;
