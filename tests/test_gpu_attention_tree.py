@@ -190,6 +190,43 @@ def test_scales_of_zero_and_below(scale, new, bits):
     check(run(torch, D, *made, words_of(seen), scale=scale), made, seen, scale)
 
 
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("new,total", [(6, 333), (40, 200), (200, 330), (100, 3000)])
+def test_values_of_very_different_sizes(new, total, bits):
+    """Rows of zeros and of equal values, which have no step, beside steps that are eight powers of ten apart.
+
+    The bound is that above with p times a key's own largest value in the place of the largest of all: weights go to the products with their step, below
+    the normal range by 2^-25 of the largest such product, and codes are 127 at most; in 4 bits a row's code 8 is at most 8/15 of its range
+    away from any of its values, 16/15 of its largest."""
+    import torch
+    from paper_2507_12205_amd import device as D
+    rng = np.random.default_rng(new)
+    made = make(torch, D, [new], [total], 4, 2, 128, 16, bits, seed=31, stale=float("nan"))
+    cache, q, start, lens, table = made
+    shape = (total, 2, 128)
+    k = rng.normal(size=shape)
+    v = rng.normal(size=shape) * rng.choice([0.0, 1e-6, 1e-3, 1.0, 1e4], size=(total, 2, 1))
+    v[rng.random((total, 2)) < 0.1] = 0.75
+    i = np.arange(total)
+    slots = torch.from_numpy(table[0, i // 16].astype(np.int64) * 16 + i % 16).cuda()
+    D.kv_write(cache, *(torch.from_numpy(x.astype(np.float16)).cuda() for x in (k, v)), slots)
+    seen = trees(rng, [new])
+    got = run(torch, D, *made, words_of(seen))
+    keys, vals = values(cache)
+    q64 = q.cpu().numpy().astype(np.float64)
+    want, size = tree.attention(q64, keys, vals, start, lens, table, seen, 128 ** -0.5)
+    reach = np.broadcast_to(np.abs(vals).max(-1, keepdims=True), vals.shape)
+    most, _ = tree.attention(q64, keys, reach, start, lens, table, seen, 128 ** -0.5)
+    bound = 2 ** -11 * np.abs(want) + (2 ** -11 + 2 ** -14) * (size + (16 / 15 * most if bits == 4 else 0.0)) + total * 2 ** -24 * most + 2 ** -25
+    assert np.isfinite(got).all() and (np.abs(got - want) <= bound).all()
+    zero = torch.zeros(shape, dtype=torch.float16, device="cuda")
+    D.kv_write(cache, torch.from_numpy(k.astype(np.float16)).cuda(), zero, slots)
+    assert not run(torch, D, *made, words_of(seen)).any()
+    D.kv_write(cache, torch.from_numpy(k.astype(np.float16)).cuda(), zero + 0.75, slots)
+    # of equal values the mean is that value: in 4 bits kept as it is, in 8 as 127 steps of it
+    assert (np.abs(run(torch, D, *made, words_of(seen)) - 0.75) <= 0.75 * (2 ** -11 + 2 ** -14 + (2 ** -11 if bits == 8 else 0))).all()
+
+
 @pytest.mark.parametrize("bits", [16, 8, 4])
 @pytest.mark.parametrize("new,total", [([4, 1], [2500, 900]), ([50, 70], [2500, 900])])
 def test_the_same_bits_every_time(new, total, bits):
