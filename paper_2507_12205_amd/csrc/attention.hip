@@ -91,6 +91,8 @@ __device__ __forceinline__ uint32_t from_bytes_of(uint32_t w, int first)
 // two nibbles, in bits 0-3 and 16-19; less 8, and the lowest value of a row is taken 8 steps higher (low_of): sums of products with
 // rounded weights then cancel less
 __device__ __forceinline__ uint32_t from_nibbles(uint32_t w) { return minus(and_or(w, 0x000F000Fu, 0x64006400u), (_Float16)1032.0f); }
+// those in bits 4-7 and 20-23, without a shift: whole numbers of the values from 64 to 80
+__device__ __forceinline__ uint32_t from_high_nibbles(uint32_t w) { return minus(and_or(w, 0x00F000F0u, 0x54005400u), (_Float16)72.0f); }
 
 // 8 neighbouring codes of a key as eight FP16 values, in 4 bits 16 too large: the code is the first four bits behind the leading one of a
 // value in [16, 32), and q's sum times 16 steps comes off a score.  (Of 1032, which q's sum would come off without the shift that this takes,
@@ -128,7 +130,7 @@ __device__ __forceinline__ half8v value_column(const R (&v)[8], int i)
         } else {
             const uint32_t s = 0x0C040C00u + 0x00010001u * (uint32_t)((i >> 1) & 3);
             const uint32_t t = __builtin_amdgcn_perm(v[2 * p + 1].w[i >> 3], v[2 * p].w[i >> 3], s);
-            o[p] = from_nibbles((i & 1) ? t >> 4 : t);
+            o[p] = (i & 1) ? from_high_nibbles(t) : from_nibbles(t);
         }
     }
     return as_half8(o[0], o[1], o[2], o[3]);
@@ -690,22 +692,24 @@ __device__ __forceinline__ uint32_t k_swap(uint32_t key) { return RC >= 16 ? key
 template <int RC>
 __device__ __forceinline__ uint32_t v_swap(uint32_t key) { return RC >= 16 ? (key & 3u) << 2 : RC == 8 ? (key & 2u) << 1 : 0u; }
 
-// eight 4-bit codes, less 8, in their own order
+// eight 4-bit codes, less 8, in their own order, or as they come
+template <bool SLOTS>
 __device__ __forceinline__ uint4 nibble_values(uint32_t w)
 {
-    const uint32_t a = from_nibbles(w), b = from_nibbles(w >> 4), c = from_nibbles(w >> 8), d = from_nibbles(w >> 12);    // 0 4, 1 5, 2 6, 3 7
+    const uint32_t a = from_nibbles(w), b = from_high_nibbles(w), c = from_nibbles(w >> 8), d = from_high_nibbles(w >> 8);    // 0 4, 1 5, 2 6, 3 7
+    if constexpr (SLOTS) return make_uint4(a, b, c, d);
     return make_uint4(__builtin_amdgcn_perm(b, a, 0x05040100u), __builtin_amdgcn_perm(d, c, 0x05040100u),
                       __builtin_amdgcn_perm(b, a, 0x07060302u), __builtin_amdgcn_perm(d, c, 0x07060302u));
 }
 // eight codes of 8 or 4 bits as FP16 values
-template <int BITS>
+template <int BITS, bool SLOTS>
 __device__ __forceinline__ uint4 code_values(const Raw<BITS> &r)
 {
     if constexpr (BITS == 8) {
         const uint32_t a = r.w[0] ^ 0x80808080u, b = r.w[1] ^ 0x80808080u;
         return make_uint4(from_bytes_of(a, 0), from_bytes_of(a, 2), from_bytes_of(b, 0), from_bytes_of(b, 2));
     } else {
-        return nibble_values(r.w[0]);
+        return nibble_values<SLOTS>(r.w[0]);
     }
 }
 
@@ -719,6 +723,8 @@ __device__ __forceinline__ uint4 code_values(const Raw<BITS> &r)
 // exponents, and the sum of the weights that of p step / step.  A multiplication and an addition fewer for each score (of some seven beside the
 // exponential): the same trees in 8 bits 81.1 -> 76.3 us, 8 x 49 of 2000 in 4 bits 40.0 -> 38.5.  The logarithm, of at most 32 in size, is off by some 2^-19 of it,
 // and a weight by 2^-19.5 of itself above and below the line alike.  A row of equal values has no step: 2^-32 stands for it, its codes are 0.
+// In 4 bits eight codes are left in the order in which two masks and a shift take them apart, in LDS and in the accumulators, and the lanes' results put in order
+// at the end: 8 x 49 of 2000 38.8 -> 36.9.
 template <int BITS, int DP, bool TREE, int ON_KEYS>
 __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(const ArgsOf<TREE> a)
 {
@@ -727,6 +733,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
     constexpr uint32_t kRows = 128 / ON_KEYS;
     constexpr bool kByRows = TREE && ON_KEYS == 1 && BITS < 16 && DP <= 128;           // a tile of 64 rows or fewer is worked on as with ON_KEYS == 2
     constexpr bool kStepInExponent = TREE && BITS < 16;            // (of V; lds_step has 1 / step and low / step of it)
+    constexpr bool kSlots = TREE && BITS == 4;                     // dims in LDS in the order 0 4 1 5 2 6 3 7 (slot_dim) of each eight
     constexpr int kGroups = KT / 16;                                                   // a wavefront brings 16 keys; with 32, of K or of V
     constexpr int kIssues = RC / 4;                                                    // accesses per lane for 16 rows
     // (four objects and not two of twice the size: a read of LDS then waits for what is on its way into the same object only)
@@ -793,7 +800,9 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
                 if constexpr (BITS == 4)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) q_sum += half_to_float(w[i] & 0xFFFFu) + half_to_float(w[i] >> 16);
-                q[t] = as_half8(w[0], w[1], w[2], w[3]);
+                q[t] = !kSlots ? as_half8(w[0], w[1], w[2], w[3])
+                               : as_half8(__builtin_amdgcn_perm(w[2], w[0], 0x05040100u), __builtin_amdgcn_perm(w[2], w[0], 0x07060302u),
+                                          __builtin_amdgcn_perm(w[3], w[1], 0x05040100u), __builtin_amdgcn_perm(w[3], w[1], 0x07060302u));
             }
             if constexpr (BITS == 4) q_sum += __shfl_xor(q_sum, 32, 64);
         }
@@ -890,8 +899,8 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
                 for (int i = 0; i < kIssues; ++i) {
                     const uint32_t x = 64u * i + self, r = x / RC, c = x % RC, kk = 16u * group16 + r;
                     if (c < pieces) {
-                        if (brings_k) lds_k[kk * RC + (c ^ k_swap<RC>(kk))] = code_values<BITS>(raw_k[i]);
-                        if (brings_v) lds_v[kk * RC + (c ^ v_swap<RC>(kk))] = code_values<BITS>(raw_v[i]);
+                        if (brings_k) lds_k[kk * RC + (c ^ k_swap<RC>(kk))] = code_values<BITS, kSlots>(raw_k[i]);
+                        if (brings_v) lds_v[kk * RC + (c ^ v_swap<RC>(kk))] = code_values<BITS, kSlots>(raw_v[i]);
                     }
                 }
                 const bool in = key0 + (lane & 15u) < end;
@@ -1172,6 +1181,16 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
                     for (int r = 0; r < 4; ++r) acc[y][4 * i + r] = f0 * acc[y][4 * i + r] + f1 * o[r];
                 }
         }
+        if constexpr (kSlots)                                          // a lane's 0 4 1 5 or 2 6 3 7 become 0 1 2 3 or 4 5 6 7
+#pragma unroll
+            for (int y = 0; y < kTiles; ++y)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    const auto even = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[y][i]), __float_as_uint(acc[y][i + 1]), false, false);
+                    const auto odd = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[y][i + 2]), __float_as_uint(acc[y][i + 3]), false, false);
+                    acc[y][i] = __uint_as_float(even[0]), acc[y][i + 1] = __uint_as_float(odd[0]);
+                    acc[y][i + 2] = __uint_as_float(even[1]), acc[y][i + 3] = __uint_as_float(odd[1]);
+                }
         const uint32_t out_row = wave_row + n;
         if (out_row >= rows) return;
         const uint32_t out_head = head * a.group + (row - token * a.group);
