@@ -279,8 +279,8 @@ int ecspmv_kv_read(const ecspmv_kv_cache_t *cache, const int64_t *d_slots, int64
  *   (a cos t - b sin t, a sin t + b cos t),   t = position[token] * frequency[pair],
  * pair i being values i and i + rotary_dim / 2, or with `neighbours` values 2 i and 2 i + 1.  The angle is worked out in 64 bits, the
  * rotation in 32; what comes of it is rounded once, to FP16 or to a code (in 8 and 4 bits what is beyond FP16's largest value counts as
- * that).  Values go as they are; queries go to q_out, which may be q itself and overlaps nothing otherwise, also those of tokens that
- * d_slots leaves out.  rotary_dim: even, at most head_dim, 0 for no rotation; q_heads: 0 for no queries.  One launch (none for no tokens). */
+ * that).  Values go as they are; queries go to q_out, which may be q itself and overlaps nothing otherwise (a stride of 0
+ * from one of its values to another is refused), also those of tokens that d_slots leaves out.  rotary_dim: even, at most head_dim, 0 for no rotation; q_heads: 0 for no queries.  One launch (none for no tokens). */
 typedef struct ecspmv_rotary_t {
     uint32_t struct_size;                   /* sizeof(ecspmv_rotary_t) as the caller compiled it */
     int32_t  rotary_dim, neighbours;        /* neighbours: 0 or 1 */
@@ -342,7 +342,8 @@ int ecspmv_attention(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *a
 /* The same for new tokens that are the nodes of a tree, or see one another in any other way: token t sees every key before the first new one,
  * and the i-th new token of its sequence, itself among them, where bit i % 32 of word i / 32 of its row of d_seen is set (device uint32, a row
  * for each token of q, rows seen_stride >= ceil(min(max_new, tokens) / 32) apart; bits of new tokens that there are none of count for
- * nothing).  Where kv_len is less than the number of new tokens, the first ones have no keys.  Long sequences of several are split by their
+ * nothing).  Where kv_len is less than the number of new tokens, the first ones have no keys.  A stride of 0 from one value of out to another is
+ * refused.  Long sequences of several are split by their
  * lengths, and the workspace is another: _tree_workspace for one call; what ecspmv_attention_workspace_most says holds here too. */
 int ecspmv_attention_tree_workspace(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *a, size_t *bytes);
 int ecspmv_attention_tree(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *a, const uint32_t *d_seen, int64_t seen_stride, void *d_work,

@@ -56,6 +56,12 @@ int check_view(const ecspmv_view_t *from, ecs::View &v, uint32_t &wide)
     return ECSPMV_OK;
 }
 
+// Whether an output's values all have a place of their own, as far as a stride of 0 tells
+bool spread_out(const ecspmv_view_t &v, int64_t tokens, int64_t heads)
+{
+    return (v.token_stride != 0 || tokens <= 1) && (v.head_stride != 0 || heads <= 1) && v.dim_stride != 0;
+}
+
 // The lanes that share a row, and the neighbouring tokens of a head that follow one another
 void spread_rows(uint32_t dim, uint32_t tokens, uint32_t &lanes_shift, uint32_t &run_shift)
 {
@@ -193,6 +199,7 @@ int ecspmv_kv_append(const ecspmv_kv_cache_t *cache, const ecspmv_view_t *k, con
     if (tokens == 0) return ECSPMV_OK;
     if ((s = check_view(k, a.k, a.k_wide)) || (s = check_view(v, a.v, a.v_wide))) return s;
     if (t.q_heads && ((s = check_view(&t.q, a.q, a.q_wide)) || (s = check_view(&t.q_out, a.q_out, a.q_out_wide)))) return s;
+    if (t.q_heads && !spread_out(t.q_out, tokens, t.q_heads)) return ECSPMV_ERR_INVALID;
     if (!d_slots || !aligned(d_slots, 8)) return ECSPMV_ERR_INVALID;
     if (t.rotary_dim && (!t.frequency || !aligned(t.frequency, 8) || !t.position || !aligned(t.position, 4))) return ECSPMV_ERR_INVALID;
     if (tokens > 1 << 27 || t.q_heads > 65535 || ((uint64_t)tokens + 16u) * (2u * a.cache.heads + (uint32_t)t.q_heads) > 0x7fffffffu)
@@ -316,6 +323,7 @@ int ecspmv_attention_tree(const ecspmv_kv_cache_t *cache, const ecspmv_attention
     if (s) return s;
     if (nothing_to_compute(args)) return ECSPMV_OK;
     if ((s = check_tensors(t, plan.work_bytes, d_work, work_bytes, args))) return s;
+    if (!spread_out(t.out, t.tokens, t.q_heads)) return ECSPMV_ERR_INVALID;
     if (!d_seen || !aligned(d_seen, 4) || seen_stride < (int64_t)args.seen_words) return ECSPMV_ERR_INVALID;
     args.seen = d_seen;
     args.seen_stride = seen_stride;

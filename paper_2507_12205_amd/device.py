@@ -165,7 +165,7 @@ def kv_read(cache: KvCache, slots: torch.Tensor, k: torch.Tensor, v: torch.Tenso
 def kv_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, position: torch.Tensor, frequency: torch.Tensor,
               q: torch.Tensor = None, q_out: torch.Tensor = None, neighbours: bool = False, stream=None):
     """kv_write() of keys that are rotated by their tokens' positions, (tokens,) int32, on the way; queries q, (tokens, q_heads, head_dim) FP16 with
-    any strides, are rotated into q_out (q itself if not given), which is returned.  frequency: (pairs,) FP64 radians a position (rotary_frequency());
+    any strides, are rotated into q_out (q itself if not given; not one that is expand()ed), which is returned.  frequency: (pairs,) FP64 radians a position (rotary_frequency());
     pair i of a head is its values i and i + pairs, or with `neighbours` values 2 i and 2 i + 1; the values beyond 2 * pairs stay as they are."""
     device, shape = cache.device, k.shape
     assert k.dtype is v.dtype is torch.float16 and slots.dtype is torch.int64 and position.dtype is torch.int32 and frequency.dtype is torch.float64
@@ -194,11 +194,12 @@ def rotary_frequency(pairs: int, base: float = 10000.0, device="cuda:0") -> torc
 
 
 class KvCaches:
-    """The caches of a model's layers, alike but for their memory, for kv_keep()."""
+    """The caches of a model's layers, alike but for their memory, each of them once, for kv_keep()."""
 
     def __init__(self, caches):
         self.caches = list(caches)
         assert self.caches and all((c.bits, c.pages, c.heads, c.page_size, c.head_dim, c.device) == self._shape() for c in self.caches)
+        assert len({c.k.data_ptr() for c in self.caches}) == len({c.v.data_ptr() for c in self.caches}) == len(self.caches)          # each of them once
         self.device, self.descs = self.caches[0].device, B.cache_array([c.desc for c in self.caches])
 
     def _shape(self):

@@ -57,6 +57,8 @@ for name, o in arg["keep"]:
     out[name] = outcome(lambda: B.ecspmv_kv_keep(B.cache_array([cache()] * count), keep(**o), stream[0]))
 for name, o in arg["verify"]:
     out[name] = outcome(lambda: B.ecspmv_verify_tree(verify(**o), 0x900000, 1 << 20, stream[0]))
+for name, strides in arg["out"]:
+    out[name] = outcome(lambda: B.ecspmv_attention_tree(cache(), attention(out=view(0x710000, *strides)), 0xC00000, 1, 0x900000, 1 << 30, stream[0]))
 out["unlike"] = [outcome(lambda: B.ecspmv_kv_keep(B.cache_array([cache(), cache(**o)]), keep(), stream[0]))
                  for o in (dict(pages=5), dict(heads=3), dict(page_size=32), dict(head_dim=48), dict(bits=4), dict(k=0x900000))]
 # a later cache that is refused: nothing is launched for the ones before it
@@ -112,11 +114,14 @@ APPEND = [("p ok", {}), ("p none", dict(rotary_dim=0, frequency=0, position=0)),
           ("p position off", dict(position=0xB00002)), ("p no q_out", dict(q_out=0)), ("p q off", dict(q=0x700001)), ("p no k", dict(k=0)),
           ("p no slots", dict(slots=0)), ("p slots off", dict(slots=0x800004)), ("p tokens -1", dict(tokens=-1)),
           ("p nothing", dict(tokens=0, k=0, v=0, slots=0, q=0)), ("p tokens", dict(tokens=(1 << 27) + 1)), ("p rows", dict(tokens=1 << 20, q_heads=2048)),
-          ("p q heads", dict(q_heads=65536))]
+          ("p q heads", dict(q_heads=65536)),
+          ("p q_out of a token", dict(q_out_token_stride=0)), ("p q_out of a head", dict(q_out_head_stride=0)), ("p q_out of a value", dict(q_out_dim_stride=0)),
+          ("p one token", dict(tokens=1, q_out_token_stride=0)), ("p q of a token", dict(q_token_stride=0))]
 ATTENTION = [("a ok", {}), ("no seen", dict(seen=0)), ("seen off", dict(seen=0xC00002)), ("seen stride", dict(stride=0)),
              ("words", dict(tokens=100, max_new=65, stride=2)), ("words enough", dict(tokens=100, max_new=65, stride=3)),
              ("words of tokens", dict(tokens=32, max_new=1000, stride=1)), ("group", dict(q_heads=3)), ("no start", dict(q_start=0)),
              ("no table", dict(page_table=0)), ("nothing", dict(tokens=0)), ("no batch", dict(batch=0, seen=0)), ("no new", dict(max_new=0))]
+OUT = [("o token", (0, 64, 1)), ("o head", (256, 0, 1)), ("o value", (256, 64, 0)), ("o ok", (-256, 64, 1))]
 KEEP = [("k ok", {}), ("k nothing", dict(nodes=0, path=0, path_stride=0)), ("k no batch", dict(batch=0)), ("k no caches", dict(count=0)),
         ("k no pages", dict(max_pages=0, page_table=0)), ("k batch -1", dict(batch=-1)), ("k batch", dict(batch=65536)), ("k nodes -1", dict(nodes=-1)),
         ("k pages -1", dict(max_pages=-1)), ("k path stride", dict(path_stride=4)), ("k table stride", dict(table_stride=3)), ("k no path", dict(path=0)),
@@ -130,7 +135,7 @@ INVALID, UNSUPPORTED, HIP, SMALL = -1, -2, -4, -6
 
 
 def test_refusals(tmp_path):
-    got = standin.run(tmp_path, CODE, dict(cache=CACHE, append=APPEND, attention=ATTENTION, keep=KEEP, verify=VERIFY))
+    got = standin.run(tmp_path, CODE, dict(cache=CACHE, append=APPEND, attention=ATTENTION, keep=KEEP, verify=VERIFY, out=OUT))
 
     def holds(cases, right, unsupported=()):
         for name, _ in cases:
@@ -138,8 +143,9 @@ def test_refusals(tmp_path):
             assert got[name] == want, (name, got[name])
     holds(CACHE, {"ok": [1] * 3, "16 bits": [1] * 3, **{n: [[UNSUPPORTED, 0]] * 3 for n in ("bits", "page 48", "dim 72")},
                   **{n: [[INVALID, 0]] * 3 for n in ("no k", "v off", "no step", "step off", "no pages", "no heads")}})
-    holds(APPEND, {"p ok": 1, "p none": 1, "p no q": 1, "p nothing": 0}, ("p pairs", "p tokens", "p rows", "p q heads"))
+    holds(APPEND, {"p ok": 1, "p none": 1, "p no q": 1, "p nothing": 0, "p one token": 1, "p q of a token": 1}, ("p pairs", "p tokens", "p rows", "p q heads"))
     holds(ATTENTION, {"a ok": 1, "words enough": 1, "words of tokens": 1, "nothing": 0, "no batch": 0, "no new": 0})
+    holds(OUT, {"o ok": 1})
     holds(KEEP, {"k ok": 1, "k nothing": 0, "k no batch": 0, "k no caches": 0, "k no pages": 0}, ("k batch", "k pages"))
     holds(VERIFY, {"v ok": 1, "v all": 1, "no nodes": 1, "no sequences": 0}, ("vocab", "nodes", "v batch"))
     assert got["unlike"] == [[INVALID, 0]] * 5 + [1] and got["late"] == [INVALID, 0]

@@ -79,8 +79,10 @@ def test_keep(calls, devices):
     for other in ((9, 2, 16, 64), (8, 1, 16, 64), (8, 2, 32, 64), (8, 2, 16, 48)):
         with pytest.raises(AssertionError):
             D.KvCaches([at(), at(other)])
-    with pytest.raises(AssertionError):
-        D.KvCaches([])
+    twice = at()
+    for caches_of in ([], [twice, at(), twice]):
+        with pytest.raises(AssertionError):
+            D.KvCaches(caches_of)
     path, table = torch.zeros((2, 5), dtype=I32), torch.zeros((2, 4), dtype=I32)
     right = dict(caches=caches, first=torch.zeros(2, dtype=I32), path=path, accepted=torch.zeros(2, dtype=I32), page_table=table)
     D.kv_keep(**right)
