@@ -27,7 +27,7 @@ using ecs::Eight;
 using ecs::to_float;
 using ecs::to_half;
 
-constexpr uint32_t kThreads = 256;
+constexpr uint32_t kThreads = 256, kRun = 16;                            // tokens of a workgroup, if there are more than 8
 
 // Cosine and sine of x turns, by their series around the nearest quarter of a turn: |y| <= pi / 4, what is left out is below 3e-14
 __device__ __forceinline__ void turn(double x, float &c, float &s)
@@ -50,20 +50,47 @@ __device__ __forceinline__ float turned(float a, float c, float b, float s)
 }
 
 // The run of tokens of workgroup x of n: neighbouring runs, which share lines of memory where tokens lie in columns, on the same die (every eighth
-// workgroup) one after another: 8191 tokens, 64/8 heads of 128 in columns, 16 bits 240 us without, 176 with
+// workgroup) one after another: 8191 tokens, 64/8 heads of 128 in columns, 16 bits 240 us without, 174 with
 __device__ __forceinline__ uint32_t run_of(uint32_t x, uint32_t n)
 {
     const uint32_t die = x & 7u;
     return die * (n >> 3) + min(die, n & 7u) + (x >> 3);
 }
 
+// A value of 16 neighbouring tokens, of which there are `count`, where tokens lie after one another
+__device__ __forceinline__ void load_column(const uint16_t *p, uint32_t count, Eight (&e)[2])
+{
+    if (count >= kRun) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const uint4 w = *reinterpret_cast<const uint4 *>(p + 8 * k);
+            e[k] = Eight{{w.x, w.y, w.z, w.w}};
+        }
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < kRun; ++i)
+            if (i < count) e[i / 8].w[i % 8 / 2] |= (uint32_t)p[i] << (16 * (i & 1));
+    }
+}
+__device__ __forceinline__ void store_column(uint16_t *p, uint32_t count, const uint32_t (&w)[8])
+{
+    if (count >= kRun) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) *reinterpret_cast<uint4 *>(p + 8 * k) = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < kRun; ++i)
+            if (i < count) p[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+    }
+}
+
 // How the pairs of a head lie in a lane's pieces: halves of eight pairs, neighbours, or halves that begin anywhere (their partners are looked up)
 enum { kHalves, kNeighbours, kAnywhere };
 
-template <int BITS, int PAIRS>
+template <int BITS, int PAIRS, bool COLUMNS>
 __global__ __launch_bounds__(kThreads) void kv_append_kernel(const AppendArgs a)
 {
-    extern __shared__ float turns[];                                      // [token of the run][cos, sin][pair]
+    extern __shared__ __attribute__((aligned(16))) float turns[];                                      // [token of the run][cos, sin][pair]
     __shared__ uint4 rows_lds[PAIRS == kAnywhere ? 2 * kThreads : 1];     // two pieces of every lane
     const uint32_t tid = threadIdx.x, first = (a.q_wide && a.k_wide && a.v_wide ? blockIdx.x : run_of(blockIdx.x, gridDim.x)) << a.run_shift, run = min(1u << a.run_shift, a.tokens - first);
     // heads of q, or heads of k and then of v
@@ -77,6 +104,15 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(const AppendArgs a)
     uint32_t at[2] = {16u * lane, 16u * lane + 8u};
     if (PAIRS == kHalves && lane < pairs / 8u) at[0] = 8u * lane, at[1] = 8u * lane + pairs;
     const uint32_t pair0 = 8u * lane;
+
+    // Where tokens lie in columns, a thread brings one value of 16 tokens, and the rows of a pass are put together in LDS (rows of 16-byte pieces, one more
+    // than they need).  By rows, a lane reads its values one by one: 8184 tokens, 64/8 heads of 128, 16 bits 158 us, so 108, 4000 of 16/16 heads of 256 124
+    // and 62.  Columns that start off 16 bytes are read by rows (by columns all the same 263 for 176 with 8191 tokens).
+    const bool columns = COLUMNS && (of_q ? a.q_columns : a.kv_columns), columns_out = of_q && columns && a.q_out_columns;
+    const uint32_t tile_row = 32u << a.lanes_shift, tile_step = tile_row + 16u;         // bytes
+    uint8_t *tile = reinterpret_cast<uint8_t *>(turns + 2u * pad * (1u << a.run_shift));
+    const uint32_t column = tid & ((16u << a.lanes_shift) - 1u), column_head = tid >> (a.lanes_shift + 4u);
+    uint8_t *tile_column = tile + kRun * column_head * tile_step + 2u * column;
 
     struct Rows {
         uint32_t head, token;
@@ -94,6 +130,16 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(const AppendArgs a)
         r.of_v = !of_q && r.head >= a.cache.heads;
         if (r.of_v) r.head -= a.cache.heads;
         r.slot = of_q ? 0 : a.slots[r.token];
+        if (columns) {
+            r.e[0] = r.e[1] = Eight{};
+            const uint32_t of = pass * (per_pass / kRun) + column_head, head = head0 + of;
+            if (of < heads && column < dim) {
+                const bool of_v = !of_q && head >= a.cache.heads;
+                const ecs::View &v = of_q ? a.q : of_v ? a.v : a.k;
+                load_column(v.data + first + (int64_t)(of_v ? head - a.cache.heads : head) * v.head_stride + (int64_t)column * v.dim_stride, run, r.e);
+            }
+            return r;
+        }
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             r.e[k] = Eight{};
@@ -117,6 +163,17 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(const AppendArgs a)
 
     for (uint32_t pass = 0; pass * per_pass < rows; ++pass) {
         Rows r = next;
+        if (columns) {
+            __syncthreads();                                              // (what the last pass left has been read)
+#pragma unroll
+            for (uint32_t i = 0; i < kRun; ++i) *reinterpret_cast<uint16_t *>(tile_column + i * tile_step) = (uint16_t)r.e[i / 8].get(i % 8);
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const uint4 w = at[k] < dim ? *reinterpret_cast<const uint4 *>(tile + (tid >> a.lanes_shift) * tile_step + 2u * at[k]) : uint4{};
+                r.e[k] = Eight{{w.x, w.y, w.z, w.w}};
+            }
+        }
         if ((pass + 1u) * per_pass < rows) next = ask(pass + 1u);
         float x[16];
 #pragma unroll
@@ -165,10 +222,25 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(const AppendArgs a)
                 for (int i = 0; i < 4; ++i) e.w[i] = to_half(x[8 * k + 2 * i]) | to_half(x[8 * k + 2 * i + 1]) << 16;
                 if (r.of_v) e = r.e[k];                                   // (bit for bit, NaN too)
                 if (at[k] < dim) {
-                    if (of_q && r.inside) ecs::store_eight(a.q_out, a.q_out_wide, r.token, r.head, at[k], e);
+                    if (columns_out)
+                        *reinterpret_cast<uint4 *>(tile + (tid >> a.lanes_shift) * tile_step + 2u * at[k]) = make_uint4(e.w[0], e.w[1], e.w[2], e.w[3]);
+                    else if (of_q && r.inside)
+                        ecs::store_eight(a.q_out, a.q_out_wide, r.token, r.head, at[k], e);
                     if (valid) *reinterpret_cast<uint4 *>(codes + 2u * at[k]) = make_uint4(e.w[0], e.w[1], e.w[2], e.w[3]);
                 }
             }
+        }
+        if (columns_out) {
+            __syncthreads();
+            const uint32_t of = pass * (per_pass / kRun) + column_head;
+            uint32_t w[kRun / 2];
+#pragma unroll
+            for (uint32_t i = 0; i < kRun; ++i) {
+                const uint32_t h = *reinterpret_cast<const uint16_t *>(tile_column + i * tile_step);
+                w[i / 2] = (i & 1) ? w[i / 2] | h << 16 : h;
+            }
+            if (of < heads && column < dim)
+                store_column(a.q_out.data + first + (int64_t)(head0 + of) * a.q_out.head_stride + (int64_t)column * a.q_out.dim_stride, run, w);
         }
         if constexpr (BITS < 16)
             if (!of_q)
@@ -176,12 +248,17 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(const AppendArgs a)
     }
 }
 
-template <int BITS>
+template <int BITS, bool COLUMNS>
 int launch_pairs(const AppendArgs &a, uint32_t gx, uint32_t gy, uint32_t lds, void *stream)
 {
-    if (a.neighbours) return ecs::launch_args<kv_append_kernel<BITS, kNeighbours>>(a, gx, gy, 1, kThreads, stream, lds);
-    if (a.pairs % 8u == 0) return ecs::launch_args<kv_append_kernel<BITS, kHalves>>(a, gx, gy, 1, kThreads, stream, lds);
-    return ecs::launch_args<kv_append_kernel<BITS, kAnywhere>>(a, gx, gy, 1, kThreads, stream, lds);
+    if (a.neighbours) return ecs::launch_args<kv_append_kernel<BITS, kNeighbours, COLUMNS>>(a, gx, gy, 1, kThreads, stream, lds);
+    if (a.pairs % 8u == 0) return ecs::launch_args<kv_append_kernel<BITS, kHalves, COLUMNS>>(a, gx, gy, 1, kThreads, stream, lds);
+    return ecs::launch_args<kv_append_kernel<BITS, kAnywhere, COLUMNS>>(a, gx, gy, 1, kThreads, stream, lds);
+}
+template <int BITS>
+int launch_columns(const AppendArgs &a, uint32_t gx, uint32_t gy, uint32_t lds, void *stream)
+{
+    return a.q_columns || a.kv_columns ? launch_pairs<BITS, true>(a, gx, gy, lds, stream) : launch_pairs<BITS, false>(a, gx, gy, lds, stream);
 }
 
 }  // namespace
@@ -193,15 +270,27 @@ int launch_kv_append(AppendArgs &a, void *stream)
     a.lanes_shift = a.cache.dim <= 16u ? 0u : a.cache.dim <= 32u ? 1u : a.cache.dim <= 64u ? 2u : a.cache.dim <= 128u ? 3u : 4u;
     const uint32_t run = 1u << a.run_shift, runs = (a.tokens + run - 1u) / run, heads = a.q_heads + 2u * a.cache.heads;
     const uint32_t a_pass = std::max(1u, (kThreads >> a.lanes_shift) / run);
+    auto in_columns = [&](const View &v, uint32_t wide) {
+        return run == kRun && !wide && v.token_stride == 1 && v.head_stride % 8 == 0 && v.dim_stride % 8 == 0 && (uintptr_t)v.data % 16u == 0;
+    };
+    if (a.q_heads == 0) a.q_wide = 1u;                                    // (no queries: as good as rows)
+    a.q_columns = a.q_heads && in_columns(a.q, a.q_wide);
+    a.q_out_columns = a.q_heads && in_columns(a.q_out, a.q_out_wide);
+    a.kv_columns = in_columns(a.k, a.k_wide) && in_columns(a.v, a.v_wide);
+    // (in columns four runs share a line, and have to be at the same heads to share it in a die's cache: 8184 tokens, 64/8 heads of 128, 16 bits, with
+    // up to 32 heads 145.7 us, 16 118.5, 8 108.3, 4 114.3, 2 134.6; 8191 of them 174, 166, 158, 158)
+    const uint32_t most_heads = a.q_wide && a.k_wide && a.v_wide ? heads : 8u;
     // Some more workgroups than the chip holds at once, each with as many heads as that leaves it (8191 tokens, 64/8 heads, 16 bits: from 512 on 99.7 us,
     // 768 91.9, 1024 78.5, 1280 77.5, 2048 82.3, 8192 97.6)
-    a.heads_per_block = std::max({a_pass, heads / 32768u + 1u, (uint32_t)std::min<uint64_t>(heads, (uint64_t)runs * heads / 1280u)});
+    a.heads_per_block = std::max({a_pass, heads / 32768u + 1u, (uint32_t)std::min<uint64_t>(most_heads, (uint64_t)runs * heads / 1280u)});
     a.q_blocks = (a.q_heads + a.heads_per_block - 1u) / a.heads_per_block;
     const uint32_t gy = a.q_blocks + (2u * a.cache.heads + a.heads_per_block - 1u) / a.heads_per_block;
-    const uint32_t lds = 2u * run * ((a.pairs + 3u) & ~3u) * (uint32_t)sizeof(float);
-    return a.cache.bits == 16u ? launch_pairs<16>(a, runs, gy, lds, stream)
-           : a.cache.bits == 8u ? launch_pairs<8>(a, runs, gy, lds, stream)
-                                : launch_pairs<4>(a, runs, gy, lds, stream);
+    // a pass has 256 >> lanes_shift rows
+    const uint32_t tile = a.q_columns || a.kv_columns ? (kThreads >> a.lanes_shift) * ((32u << a.lanes_shift) + 16u) : 0u;
+    const uint32_t lds = 2u * run * ((a.pairs + 3u) & ~3u) * (uint32_t)sizeof(float) + tile;
+    return a.cache.bits == 16u ? launch_columns<16>(a, runs, gy, lds, stream)
+           : a.cache.bits == 8u ? launch_columns<8>(a, runs, gy, lds, stream)
+                                : launch_columns<4>(a, runs, gy, lds, stream);
 }
 
 }  // namespace ecs

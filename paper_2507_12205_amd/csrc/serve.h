@@ -42,8 +42,9 @@ struct AppendArgs {
     uint32_t lanes_shift, run_shift;      // as in KvArgs, but a lane has 16 values
     uint32_t heads_per_block, q_blocks;   // heads of q, or of k and v, that a workgroup takes; workgroups for q
     uint32_t q_wide, q_out_wide, k_wide, v_wide;
+    uint32_t q_columns, q_out_columns, kv_columns;              // tokens follow one another, from aligned places on: runs of 16 go through LDS
 };
-int launch_kv_append(AppendArgs &a, void *stream);                         // (chooses lanes_shift, heads_per_block, q_blocks)
+int launch_kv_append(AppendArgs &a, void *stream);                         // (chooses lanes_shift, heads_per_block, q_blocks, columns)
 
 constexpr uint32_t kKeepLayers = 64;      // of a launch
 struct KeepArgs {

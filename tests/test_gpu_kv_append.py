@@ -110,6 +110,42 @@ def test_against_64_bits(shape, kind, neighbours, bits):
         assert torch.equal(now.transpose(1, 2)[free], was.transpose(1, 2)[free])
 
 
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("tokens", [9, 16, 24, 72, 200, 328])
+@pytest.mark.parametrize("q_heads,heads,dim,rotary,neighbours", [(6, 3, 64, 64, False), (3, 5, 128, 64, True), (2, 1, 80, 36, False), (9, 2, 256, 256, False),
+                                                                 (1, 3, 16, 16, True), (0, 2, 240, 100, False), (20, 1, 32, 32, False)])
+def test_columns_give_the_same_bits(q_heads, heads, dim, rotary, neighbours, tokens, bits):
+    """Columns that start at multiples of 16 bytes and that do not, each of the tensors in them or not, tokens that are no multiple of 16: what rows give; and
+    nothing is written beside the tokens."""
+    import torch
+    from paper_2507_12205_amd import device as D
+    x = [values((tokens, n, dim), 3 + i, torch) for i, n in enumerate((heads, heads, q_heads))]
+    slots = torch.randperm(16 * 30, device="cuda")[:tokens]
+    position = torch.arange(tokens, dtype=torch.int32, device="cuda") * 1000
+    frequency = D.rotary_frequency(rotary // 2)
+
+    def wide(t, columns, pad):
+        """The tensor itself, or tokens after one another in columns of ceil8(tokens) + pad places, and all those places."""
+        if not columns:
+            return t, t
+        every = torch.full((t.shape[1], dim, -(-tokens // 8) * 8 + pad), 7.0, dtype=t.dtype, device=t.device)
+        every[:, :, :tokens] = t.permute(1, 2, 0)
+        return every[:, :, :tokens].permute(2, 0, 1), every
+
+    def run(columns, pad=0, in_place=False):
+        cache = D.kv_cache(30, heads, 16, dim, bits)
+        (k, _), (v, _), (q, all_q) = (wide(t.clone(), c, pad) for t, c in zip(x, columns))
+        out, all_out = (q, all_q) if in_place else wide(torch.zeros_like(x[2]), columns[3], pad)
+        D.kv_append(cache, k, v, slots, position, frequency, *((q, out) if q_heads else ()), neighbours=neighbours)
+        if q_heads and out is not x[2] and all_out.shape[-1] > tokens and all_out.dim() == 3 and all_out.shape[1] == dim:
+            assert (all_out[:, :, tokens:] == 7.0).all()
+        return [t for t in (cache.k, cache.v, cache.k_step, cache.v_step, out if q_heads else None) if t is not None]
+
+    want = run((False,) * 4)
+    for case in ([(True,) * 4], [(True,) * 4, 1], [(True,) * 4, 8, True], [(True, True, False, True)], [(False, False, True, False)], [(True, False, True, True), 8]):
+        assert all(torch.equal(a, b) for a, b in zip(run(*case), want)), case
+
+
 @pytest.mark.parametrize("bits", [16, 8])
 @pytest.mark.parametrize("rotary", [0, 64])
 def test_without_a_turn_it_is_kv_write(rotary, bits):
