@@ -90,9 +90,10 @@ enum { kHalves, kNeighbours, kAnywhere };
 template <int BITS, int PAIRS, bool COLUMNS>
 __global__ __launch_bounds__(kThreads) void kv_append_kernel(const AppendArgs a)
 {
-    extern __shared__ __attribute__((aligned(16))) float turns[];                                      // [token of the run][cos, sin][pair]
+    extern __shared__ __attribute__((aligned(16))) float turns[];            // [token of the run][cos, sin][pair]
     __shared__ uint4 rows_lds[PAIRS == kAnywhere ? 2 * kThreads : 1];     // two pieces of every lane
-    const uint32_t tid = threadIdx.x, first = (a.q_wide && a.k_wide && a.v_wide ? blockIdx.x : run_of(blockIdx.x, gridDim.x)) << a.run_shift, run = min(1u << a.run_shift, a.tokens - first);
+    const uint32_t tid = threadIdx.x, first = (a.q_wide && a.k_wide && a.v_wide ? blockIdx.x : run_of(blockIdx.x, gridDim.x)) << a.run_shift;
+    const uint32_t run = min(1u << a.run_shift, a.tokens - first);
     // heads of q, or heads of k and then of v
     const bool of_q = blockIdx.y < a.q_blocks;
     const uint32_t all = of_q ? a.q_heads : 2u * a.cache.heads, head0 = (blockIdx.y - (of_q ? 0u : a.q_blocks)) * a.heads_per_block;
@@ -106,8 +107,8 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(const AppendArgs a)
     const uint32_t pair0 = 8u * lane;
 
     // Where tokens lie in columns, a thread brings one value of 16 tokens, and the rows of a pass are put together in LDS (rows of 16-byte pieces, one more
-    // than they need).  By rows, a lane reads its values one by one: 8184 tokens, 64/8 heads of 128, 16 bits 158 us, so 108, 4000 of 16/16 heads of 256 124
-    // and 62.  Columns that start off 16 bytes are read by rows (by columns all the same 263 for 176 with 8191 tokens).
+    // than they need).  By rows, a lane reads its values one by one: 64/8 heads of 128, 16 bits, 8191 tokens so 158 us, 8184 by columns 108, 16/16 heads of 256,
+    // 4001 tokens 125, 4000 62.  Columns that start off 16 bytes are read by rows (by columns all the same 263 for 176: 8191 tokens, up to 32 heads).
     const bool columns = COLUMNS && (of_q ? a.q_columns : a.kv_columns), columns_out = of_q && columns && a.q_out_columns;
     const uint32_t tile_row = 32u << a.lanes_shift, tile_step = tile_row + 16u;         // bytes
     uint8_t *tile = reinterpret_cast<uint8_t *>(turns + 2u * pad * (1u << a.run_shift));
