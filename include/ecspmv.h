@@ -342,8 +342,9 @@ int ecspmv_attention(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *a
 /* The same for new tokens that are the nodes of a tree, or see one another in any other way: token t sees every key before the first new one,
  * and the i-th new token of its sequence, itself among them, where bit i % 32 of word i / 32 of its row of d_seen is set (device uint32, a row
  * for each token of q, rows seen_stride >= ceil(min(max_new, tokens) / 32) apart; bits of new tokens that there are none of count for
- * nothing).  Where kv_len is less than the number of new tokens, the first ones have no keys.  A stride of 0 from one value of out to another is
- * refused.  Long sequences of several are split by their
+ * nothing).  Where kv_len is less than the number of new tokens, the first ones have no keys.  Weights meet V in 22 bits where a head of the cache has
+ * up to 64 rows (max_new times the heads of its group) over 16 bits with a head_dim of up to 128, or 32 over the others, and beyond that in 11.  A stride
+ * of 0 from one value of out to another is refused.  Long sequences of several are split by their
  * lengths, and the workspace is another: _tree_workspace for one call; what ecspmv_attention_workspace_most says holds here too. */
 int ecspmv_attention_tree_workspace(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *a, size_t *bytes);
 int ecspmv_attention_tree(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *a, const uint32_t *d_seen, int64_t seen_stride, void *d_work,

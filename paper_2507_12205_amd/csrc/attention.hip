@@ -680,7 +680,10 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) :
 // error against 64 bits is 2.9e-4 of the result in place of the 2.1e-4 that its own rounding to FP16 makes.  Here the matrix instructions are
 // half of the time, and a second part costs what it takes (us by one / by two: 2048 tokens over 4096 keys, heads of 128, FP16 132 / 171, 8 bits 164 /
 // 194, 4 bits 168 / 202; 512 over 9098 108 / 133; five of up to 333 over 3000, heads of 80, 68 / 80, 4 bits 78 / 86).  With FP16 the sum of the weights is
-// that of the rounded ones.
+// that of the rounded ones.  Trees of up to 64 rows wait for the keys and values of FP16, so that a second part costs them nothing there, and they have it
+// (64 nodes of heads of 128, one tree over 32768 keys 131.3 / 132.5, four over 8000 112.2 / 111.1).  It is not free with 257 nodes (16000 keys, 32/8 heads, 95.5 /
+// 124.4), heads of 256 (192 nodes over 8000 45.9 / 50.3) and codes (four of 64 over 8000, 8 bits 83.5 / 93.9, 4 bits 77.6 / 87.4; sixteen of up to 16 over up to
+// 8192, 8 bits, 76.0 / 83.8), whose values are rounded to 2^-8 and 2^-5 of the largest of their row when they are written.
 //
 // 2048 tokens over 4096 keys, 32 heads of 128, FP16: 121 - 127 us, 810 - 850 TFLOP/s of the products that the mask leaves (a large matrix
 // product alone reaches 1140 - 1229 here).  A wavefront's products and its softmax follow one another, and those of the two wavefronts of a SIMD overlap only in
@@ -766,6 +769,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
 
     auto work = [&](auto shared_by) {                              // by how many wavefronts rows are shared
         constexpr int kShared = decltype(shared_by)::value, kHalves = KT / 32 / kShared;                           // halves of a tile: of a wavefront
+        constexpr int kParts = kShared == 2 && BITS == 16 && DP <= 128 ? 2 : 1;            // FP16 values that a weight goes to the second product as
         const uint32_t wave_row = row0 + 32u * (wave % (4u / kShared)), half0 = kHalves * (wave / (4u / kShared));     // first row, first half of a tile
         const uint32_t row = min(wave_row + n, rows - 1u), token = row / a.group;
         const int32_t seen = min(s.behind + (int32_t)token + 1, (int32_t)s.len);
@@ -1050,7 +1054,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
 #pragma unroll
             for (int i = 0; i < 16 * kHalves; ++i) {
                 w[i] = __builtin_amdgcn_exp2f(BITS == 16 ? fmaf(w[i], by, -base) : w[i] - base);
-                if constexpr (BITS < 16 && !kStepInExponent) sum += w[i];          // (with FP16 the rounded ones are added up, below)
+                if constexpr (kParts == 2 || (BITS < 16 && !kStepInExponent)) sum += w[i];  // (with FP16 in one part the rounded ones are added up, below)
             }
             if constexpr (BITS < 16) {
 #pragma unroll
@@ -1070,17 +1074,23 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
                             w[i + r] *= step[r];
                 }
             }
-            half8v weights[2 * kHalves];
+            half8v weights[2 * kHalves], rest[2 * kHalves];
 #pragma unroll
             for (int x = 0; x < 2 * kHalves; ++x) {
-                uint32_t o[4];
+                uint32_t o[4], e[4] = {};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const half2v p = {(_Float16)w[8 * x + 2 * i], (_Float16)w[8 * x + 2 * i + 1]};
-                    if constexpr (BITS == 16) sum = __builtin_amdgcn_fdot2(p, half2v{(_Float16)1.0f, (_Float16)1.0f}, sum, false);
-                    o[i] = as_word(p);
+                    o[i] = as_word(half2v{(_Float16)w[8 * x + 2 * i], (_Float16)w[8 * x + 2 * i + 1]});
+                    if constexpr (kParts == 2) {                   // what that leaves out, as in the kernel for few rows
+                        asm("" : "+v"(o[i]));
+                        const half2v p = as_half2(o[i]);
+                        e[i] = as_word(half2v{(_Float16)(w[8 * x + 2 * i] - (float)p[0]), (_Float16)(w[8 * x + 2 * i + 1] - (float)p[1])});
+                    } else if constexpr (BITS == 16) {
+                        sum = __builtin_amdgcn_fdot2(as_half2(o[i]), half2v{(_Float16)1.0f, (_Float16)1.0f}, sum, false);
+                    }
                 }
                 weights[x] = as_half8(o[0], o[1], o[2], o[3]);
+                rest[x] = as_half8(e[0], e[1], e[2], e[3]);
             }
             l += sum;
 #pragma unroll
@@ -1090,6 +1100,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
                     const int at = x * kTiles + y;
                     const uint2 lo = __builtin_bit_cast(uint2, vf[2 * at]), hi = __builtin_bit_cast(uint2, vf[2 * at + 1]);
                     acc[y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_half8(lo.x, lo.y, hi.x, hi.y), weights[x], acc[y], 0, 0, 0);
+                    if constexpr (kParts == 2) acc[y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_half8(lo.x, lo.y, hi.x, hi.y), rest[x], acc[y], 0, 0, 0);
                     if (2 * at + 1 + kReads / 2 < kReads) {
                         read_v(2 * at + kReads / 2);
                         read_v(2 * at + 1 + kReads / 2);

@@ -227,6 +227,28 @@ def test_values_of_very_different_sizes(new, total, bits):
     assert (np.abs(run(torch, D, *made, words_of(seen)) - 0.75) <= 0.75 * (2 ** -11 + 2 ** -14 + (2 ** -11 if bits == 8 else 0))).all()
 
 
+@pytest.mark.parametrize("new,heads,kv_heads,dim", [(5, 4, 1, 128), (33, 6, 6, 64), (64, 4, 4, 128), (16, 8, 2, 96), (9, 6, 2, 32)])
+@pytest.mark.parametrize("past", [1, 4, 40, 1500])
+def test_weights_of_up_to_64_rows(past, new, heads, kv_heads, dim):
+    """FP16, 17 to 64 rows of a head of the cache: a weight is two FP16 values, 2^-22 of it off and of the range below the normal one 2^-25 of the largest.  The
+    result is rounded to FP16 (2^-11 of it, 2^-25), scores are off by 2^-22 of scale times sum |q| times the largest |k| (sums of dim products), which the
+    weight has twice, and 2^-14 covers sums and exponentials, as in test_gpu_attention_codes."""
+    import torch
+    from paper_2507_12205_amd import device as D
+    rng, batch = np.random.default_rng(past + new), 6
+    cache, q, start, lens, table = made = make(torch, D, [new] * batch, [past + new] * batch, heads, kv_heads, dim, 16, 16, seed=past, stale=float("nan"))
+    seen = trees(rng, [new] * batch)
+    got = run(torch, D, *made, words_of(seen))
+    (k, v), x = values(cache), q.cpu().numpy().astype(np.float64)
+    want, size = tree.attention(x, k, v, start, lens, table, seen, dim ** -0.5)
+    keys = max(np.abs(ref.gather(k, table[b], n)).max() for b, n in enumerate(lens))
+    top = max(np.abs(ref.gather(v, table[b], n)).max() for b, n in enumerate(lens))
+    score = 2.0 ** -22 * dim ** -0.5 * np.abs(x).sum(-1, keepdims=True) * keys
+    bound = 2 ** -11 * np.abs(want) + (2 ** -22 + 2 ** -14 + 2 * score) * size + (past + new) * 2 ** -24 * top + 2 ** -25
+    worst = np.max(np.abs(got - want) / bound)
+    assert worst <= 1.0, worst
+
+
 @pytest.mark.parametrize("bits", [16, 8, 4])
 @pytest.mark.parametrize("new,total", [([4, 1], [2500, 900]), ([50, 70], [2500, 900])])
 def test_the_same_bits_every_time(new, total, bits):
