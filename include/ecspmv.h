@@ -383,7 +383,8 @@ int ecspmv_verify(const ecspmv_verify_t *a, void *d_work, size_t work_bytes, voi
  * however the tree was made; a tree without branches gives what ecspmv_verify gives without draft probabilities.  accepted[b] = n;
  * path[b][0 ... nodes - 1] (device int32) = the accepted nodes, then -1; tokens[b][0 ... nodes] = their tokens, the next token, then -1 (also in the
  * next token's place if p has nothing above 0).  A node whose token was refused at the same place already is not asked.  A drafted token
- * outside [0, vocab) is refused and takes nothing from S; a node whose parent is none before it is not reached. */
+ * outside [0, vocab) is refused and takes nothing from S; a node whose parent is none before it is not reached.  tokens, path and accepted may lie
+ * where drafted, parent, count and uniform do, and overlap nothing else. */
 typedef struct ecspmv_verify_tree_t {
     uint32_t struct_size;                   /* sizeof(ecspmv_verify_tree_t) as the caller compiled it */
     int32_t  batch, nodes, vocab;           /* nodes in [0, 1024]; vocab in [1, 2^20] */

@@ -9,9 +9,10 @@
 // for the children of the node that it is at.  Everything that the walk needs of p is asked for at once, before it starts.
 //
 // Two launches, as for drafts in a row (verify.hip): the first adds up tiles of the row that counts, each workgroup after a walk of its
-// own, one of which writes down what came of it; the second draws the token.  What bounds it are the trips to memory, one after the other: the
-// tree, its p, the row; the sums, the tile.  26 nodes over 32000 tokens 12.0 us, 32 sequences of up to 63 over 128256 16.9 (with a second walk
-// in the second launch instead of the first one's result 12.3 and 18.3).
+// own, one of which writes down in the workspace what came of it; the second draws the token and writes the outputs, which may so lie where
+// the tree and its random numbers do: all walks have ended by then, and the second launch reads none of these.  What bounds it are the trips
+// to memory, one after the other: the tree, its p, the row; the sums, the tile.  26 nodes over 32000 tokens 12.1 us, 32 sequences of up to 63
+// over 128256 16.6 (with a second walk in the second launch instead of the first one's result 12.3 and 18.3).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -120,11 +121,15 @@ __device__ __forceinline__ void walk_tree(const VerifyTreeArgs &a, uint32_t seq,
     __syncthreads();
 }
 
-// What a walk leaves for the second launch, behind a sequence's sums: accepted, refused, the row of p that counts; the refused tokens
+// What a walk leaves for the second launch, behind a sequence's sums: accepted, refused, the row of p that counts, the next token's random number; the
+// accepted nodes, each with its token in its last 20 bits, and then the refused tokens (no node is both, so that they are no more than the nodes)
 struct Left {
-    int32_t accepted, refused, row, pad;
-    int32_t gone[];
+    int32_t accepted, refused, row;
+    float u;
+    int32_t list[];
 };
+constexpr uint32_t kTokenBits = 20;
+static_assert(kMostNodes <= 1u << (31 - kTokenBits) && ecs::kMaxTiles * kTile <= 1u << kTokenBits, "a node and its token in one word");
 __device__ __forceinline__ uint32_t sequence_bytes(uint32_t nodes, uint32_t vocab)
 {
     return (vocab + kTile - 1u) / kTile * 8u + (uint32_t)sizeof(Left) + (nodes + 1u) / 2u * 8u;
@@ -150,30 +155,30 @@ __global__ __launch_bounds__(kThreads) void verify_tree_sums_kernel(const Verify
     Left *left = reinterpret_cast<Left *>(sums + tiles);
     if (tid == 0) {
         left->accepted = (int32_t)n, left->refused = (int32_t)refused, left->row = row;
-        a.accepted[seq] = (int32_t)n;
+        left->u = a.uniform[(size_t)seq * (a.nodes + 1u) + a.nodes];
     }
-    for (uint32_t i = tid; i < refused; i += kThreads) left->gone[i] = s.gone[i];
-    int32_t *tokens = a.tokens + (size_t)seq * (a.nodes + 1u), *path = a.path + (size_t)seq * a.nodes;
-    for (uint32_t i = tid; i <= a.nodes; i += kThreads) {
-        const int32_t node = i < n ? s.path[i] : -1;
-        if (i != n) tokens[i] = i < n ? s.token[node] : -1;
-        if (i < a.nodes) path[i] = node;
-    }
+    for (uint32_t i = tid; i < n + refused; i += kThreads)
+        left->list[i] = i < n ? s.path[i] << kTokenBits | s.token[s.path[i]] : s.gone[i - n];
 }
 
 __global__ __launch_bounds__(kThreads) void verify_tree_token_kernel(const VerifyTreeArgs a)
 {
-    __shared__ int32_t gone[kMostNodes];
+    __shared__ int32_t list[kMostNodes];
     __shared__ ecs::Drawing shared;
     const uint32_t seq = blockIdx.x, tid = threadIdx.x, tiles = (a.vocab + kTile - 1u) / kTile;
     const double *sums = reinterpret_cast<const double *>(a.work + (size_t)seq * sequence_bytes(a.nodes, a.vocab));
     const Left *left = reinterpret_cast<const Left *>(sums + tiles);
-    const double u = (double)a.uniform[(size_t)seq * (a.nodes + 1u) + a.nodes];
     const uint32_t n = (uint32_t)left->accepted, refused = (uint32_t)left->refused;
-    for (uint32_t i = tid; i < a.nodes; i += kThreads) gone[i] = left->gone[i];          // (all that there is room for: not waiting for how many)
-    Weights w = {a.target + seq * a.target_seq + left->row * a.target_row, gone, refused, a.vocab};
-    const int32_t token = ecs::draw_token(w, sums, u, a.vocab, shared);    // (a barrier before `gone` is read)
-    if (tid == 0) a.tokens[(size_t)seq * (a.nodes + 1u) + n] = token;
+    for (uint32_t i = tid; i < a.nodes; i += kThreads) list[i] = left->list[i];          // (all that there is room for: not waiting for how many)
+    Weights w = {a.target + seq * a.target_seq + left->row * a.target_row, list + n, refused, a.vocab};
+    const int32_t token = ecs::draw_token(w, sums, (double)left->u, a.vocab, shared);   // (a barrier before `list` is read)
+    int32_t *tokens = a.tokens + (size_t)seq * (a.nodes + 1u), *path = a.path + (size_t)seq * a.nodes;
+    for (uint32_t i = tid; i <= a.nodes; i += kThreads) {
+        const int32_t node = i < n ? list[i] : -1;
+        tokens[i] = i < n ? node & ((1 << kTokenBits) - 1) : i == n ? token : -1;
+        if (i < a.nodes) path[i] = i < n ? node >> kTokenBits : -1;
+    }
+    if (tid == 0) a.accepted[seq] = (int32_t)n;
 }
 
 }  // namespace

@@ -337,7 +337,7 @@ def verify_tree(target: torch.Tensor, drafted: torch.Tensor, parent: torch.Tenso
     """Which path of a tree of drafted tokens stands, and the token after it.  target: (batch, nodes + 1, vocab) probabilities, after the token before
     the tree and after each node, uniform: (batch, nodes + 1) random numbers in [0, 1), all FP32; drafted: (batch, nodes) and parent: (batch, nodes)
     int32, -1 for the token before the tree; count: (batch,) int32, how many nodes there are (None: all).  tokens: (batch, nodes + 1), path: (batch,
-    nodes), accepted: (batch,) int32.  workspace: of verify_tree_workspace(), or allocated here."""
+    nodes), accepted: (batch,) int32, which may be the memory of drafted, parent, count and uniform.  workspace: of verify_tree_workspace(), or allocated here."""
     device, (batch, rows, vocab), (seq, row, token) = target.get_device(), target.shape, target.stride()
     nodes = rows - 1
     assert target.dtype is uniform.dtype is torch.float32

@@ -137,3 +137,26 @@ def test_in_a_graph_and_on_another_stream(batch, nodes, vocab):
         side.synchronize()
         assert all(torch.equal(x, y) for x, y in zip(out, eager))
         equal([t.cpu().numpy() for t in out], tree.verify(*(t.cpu().numpy() for t in made), count.cpu().numpy()))
+
+
+@pytest.mark.parametrize("batch,nodes,vocab", [(1, 7, 50000), (40, 30, 40000), (3, 1024, 9000)])
+@pytest.mark.parametrize("outputs", ["count", "parent", "drafted", "all"])
+def test_outputs_in_the_inputs_memory(outputs, batch, nodes, vocab):
+    """Outputs are written when every walk has ended: they may lie where the tree and its random numbers lie."""
+    import torch
+    from paper_2507_12205_amd import device as D
+    a = make(batch, nodes, vocab, 17)
+    lengths = np.random.default_rng(3).integers(nodes // 2, nodes + 1, batch).astype(np.int32)
+    want = tree.verify(*a, lengths)
+    for turn in range(3):
+        target, drafted, parent, uniform, count = (torch.from_numpy(x.copy()).cuda() for x in (*a, lengths))
+        tokens, path, accepted = (torch.full(x.shape, 12345, dtype=torch.int32, device="cuda") for x in (uniform, drafted, count))
+        if outputs in ("count", "all"):
+            accepted = count
+        if outputs in ("parent", "all"):
+            path = parent
+        if outputs == "drafted":
+            path = drafted
+        if outputs == "all":
+            tokens = uniform.view(torch.int32)
+        equal([t.cpu().numpy() for t in D.verify_tree(target, drafted, parent, uniform, tokens, path, accepted, count)], want)
