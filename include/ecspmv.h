@@ -252,7 +252,8 @@ typedef struct ecspmv_view_t {
 /* A cache of keys and values in pages.  k, v: device, 16-byte aligned, [pages][heads][page_size][head_dim] values of
  *   bits = 16: FP16;
  *   bits = 8:  signed codes in [-127, 127], value = step * code, step = max|x| / 127 of the token and head;
- *              k_step, v_step: [pages][heads][page_size] float;
+ *              k_step, v_step: [pages][heads][page_size] float (of FP16 values 0 or at least 2^-31; attention may take a smaller step of
+ *              values for 2^-32, which moves no result by more than 2^-25);
  *   bits = 4:  codes in [0, 15], two to a byte, the earlier one in the low half, value = low + step * code, low = min x,
  *              step = (max x - min x) / 15, the next smaller FP16 value where low + 15 step would round to infinity; k_step, v_step:
  *              [pages][heads][page_size][2] FP16 (step, low).

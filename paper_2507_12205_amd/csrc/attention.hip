@@ -908,16 +908,18 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void attention_chunk_kernel(
                     }
                 }
                 const bool in = key0 + (lane & 15u) < end;
-                if constexpr (TREE)                                    // (a node that was left out may have a step that is none)
-                    if (!(BITS == 8 ? finite(__uint_as_float(raw_step)) : half_finite(raw_step) && half_finite(raw_step >> 16))) raw_step = 0u;
                 float step = !in ? 0.0f : BITS == 8 ? __uint_as_float(raw_step) : step_of(raw_step);
                 float low = !in || BITS == 8 ? 0.0f : low_of(raw_step);
                 float f = lane < 16u ? scale : 1.0f, reach = reach_of(step);
                 if constexpr (kStepInExponent)
                     if (lane >= 16u) {
-                        if (!(step > kLeastStep)) low += 8.0f * kLeastStep, step = kLeastStep;
-                        reach = __builtin_amdgcn_logf(step);
+                        // What is not finite goes into the exponent alone, and so to the rows that see the key: a node that was left out may have a
+                        // step that is none.  (8-bit steps below the least count as that: 127 of it are less than half of FP16's least value.)
+                        const bool none = !(finite(step) && finite(low));
+                        if (none || step < kLeastStep) low += 8.0f * kLeastStep, step = kLeastStep;
+                        reach = none ? __builtin_nanf("") : __builtin_amdgcn_logf(step);
                         f = __builtin_amdgcn_rcpf(step);
+                        if (none) low = 0.0f;
                         step = 1.0f;
                     }
                 if (lane < 32u) {

@@ -179,6 +179,33 @@ def test_nodes_that_were_left_out(new, total, bits):
         assert np.array_equal(run(torch, D, *made, words), clean)
 
 
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("new,total", [(6, 70), (30, 200), (40, 200), (200, 330), (7, 3000), (100, 3000)])
+def test_steps_that_are_none(new, total, bits):
+    """A step or lowest value that is NaN, or an infinity among those of the values, is the result of every row that sees its key, whichever kernel the number
+    of rows takes; the other rows have their bits.  A key before the tree, and a node."""
+    import torch
+    from paper_2507_12205_amd import device as D
+    cache, q, start, lens, table = made = make(torch, D, [new], [total], 4, 2, 128, 16, bits, seed=4)
+    seen = trees(np.random.default_rng(new), [new])
+    words = words_of(seen)
+    clean = run(torch, D, *made, words)
+    check(clean, made, seen)
+    parts = [()] if bits == 8 else [(0,), (1,)]
+    for at in (total - new - 20, total - new + new // 2):
+        page, off = int(table[0, at // 16]), at % 16
+        sees = seen[0][:, at - (total - new)] if at >= total - new else np.ones(new, bool)
+        assert sees.any()
+        for step, odd in ((cache.k_step, float("nan")), (cache.v_step, float("nan")), (cache.v_step, float("inf")), (cache.v_step, float("-inf"))):
+            for part in parts:
+                keep = step[(page, 1, off, *part)].clone()
+                step[(page, 1, off, *part)] = odd
+                got = run(torch, D, *made, words)
+                step[(page, 1, off, *part)] = keep
+                assert np.array_equal(got[~sees], clean[~sees]) and np.array_equal(got[:, :2], clean[:, :2])
+                assert not np.isfinite(got[sees][:, 2:]).any(), (at, odd, part)
+
+
 @pytest.mark.parametrize("bits", [16, 8, 4])
 @pytest.mark.parametrize("new", [2, 100])
 @pytest.mark.parametrize("scale", [0.0, -0.25])
