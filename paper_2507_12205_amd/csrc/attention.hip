@@ -1426,16 +1426,21 @@ int launch_chunk(const ArgsOf<kTree> &a, void *stream)
 #else
     const uint32_t gx = a.cache.heads, gy = a.row_tiles * a.splits, gz = a.batch;
 #endif
-    switch ((a.cache.dim + 31u) / 32u) {
+    const uint32_t width = (a.cache.dim + 31u) / 32u;
+    switch (width) {
     case 1: return ecs::launch_args<attention_chunk_kernel<BITS, 32, kTree, ON_KEYS>>(a, gx, gy, gz, 256, stream);
     case 2: return ecs::launch_args<attention_chunk_kernel<BITS, 64, kTree, ON_KEYS>>(a, gx, gy, gz, 256, stream);
     case 3: return ecs::launch_args<attention_chunk_kernel<BITS, 96, kTree, ON_KEYS>>(a, gx, gy, gz, 256, stream);
     case 4: return ecs::launch_args<attention_chunk_kernel<BITS, 128, kTree, ON_KEYS>>(a, gx, gy, gz, 256, stream);
-    case 5: return ecs::launch_args<attention_chunk_kernel<BITS, 160, kTree, ON_KEYS>>(a, gx, gy, gz, 256, stream);
-    case 6: return ecs::launch_args<attention_chunk_kernel<BITS, 192, kTree, ON_KEYS>>(a, gx, gy, gz, 256, stream);
-    case 7: return ecs::launch_args<attention_chunk_kernel<BITS, 224, kTree, ON_KEYS>>(a, gx, gy, gz, 256, stream);
-    default: return ecs::launch_args<attention_chunk_kernel<BITS, 256, kTree, ON_KEYS>>(a, gx, gy, gz, 256, stream);
+    default: break;
     }
+    if constexpr (!kTree || ON_KEYS == 2) {                        // (of trees, wider heads have 64 rows to a workgroup: plan_attention_tree)
+        if (width == 5u) return ecs::launch_args<attention_chunk_kernel<BITS, 160, kTree, ON_KEYS>>(a, gx, gy, gz, 256, stream);
+        if (width == 6u) return ecs::launch_args<attention_chunk_kernel<BITS, 192, kTree, ON_KEYS>>(a, gx, gy, gz, 256, stream);
+        if (width == 7u) return ecs::launch_args<attention_chunk_kernel<BITS, 224, kTree, ON_KEYS>>(a, gx, gy, gz, 256, stream);
+        return ecs::launch_args<attention_chunk_kernel<BITS, 256, kTree, ON_KEYS>>(a, gx, gy, gz, 256, stream);
+    }
+    return (int)hipErrorInvalidValue;
 }
 
 template <int BITS>

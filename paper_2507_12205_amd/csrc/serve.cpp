@@ -62,11 +62,12 @@ bool spread_out(const ecspmv_view_t &v, int64_t tokens, int64_t heads)
     return (v.token_stride != 0 || tokens <= 1) && (v.head_stride != 0 || heads <= 1) && v.dim_stride != 0;
 }
 
-// The lanes that share a row, and the neighbouring tokens of a head that follow one another
-void spread_rows(uint32_t dim, uint32_t tokens, uint32_t &lanes_shift, uint32_t &run_shift)
+// log2 of the neighbouring tokens of a head that follow one another
+uint32_t run_of_tokens(uint32_t tokens)
 {
-    while ((8u << lanes_shift) < dim) ++lanes_shift;
-    while ((1u << run_shift) < tokens && run_shift < 4u) ++run_shift;
+    uint32_t shift = 0;
+    while ((1u << shift) < tokens && shift < 4u) ++shift;
+    return shift;
 }
 
 int kv_call(const ecspmv_kv_cache_t *cache, const ecspmv_view_t *k, const ecspmv_view_t *v, const int64_t *d_slots, int64_t tokens,
@@ -83,7 +84,8 @@ int kv_call(const ecspmv_kv_cache_t *cache, const ecspmv_view_t *k, const ecspmv
     if (tokens > 0x7fffffff || ((uint64_t)tokens + 16u) * a.cache.heads > 0x7fffffffu) return ECSPMV_ERR_UNSUPPORTED;
     a.slots = d_slots;
     a.tokens = (uint32_t)tokens;
-    spread_rows(a.cache.dim, a.tokens, a.lanes_shift, a.run_shift);
+    while ((8u << a.lanes_shift) < a.cache.dim) ++a.lanes_shift;
+    a.run_shift = run_of_tokens(a.tokens);
     return ecs::hip_status(launch(a, stream));
 }
 
@@ -211,7 +213,7 @@ int ecspmv_kv_append(const ecspmv_kv_cache_t *cache, const ecspmv_view_t *k, con
     a.q_heads = (uint32_t)t.q_heads;
     a.pairs = (uint32_t)t.rotary_dim / 2u;
     a.neighbours = (uint32_t)t.neighbours;
-    spread_rows(a.cache.dim, a.tokens, a.lanes_shift, a.run_shift);
+    a.run_shift = run_of_tokens(a.tokens);
     return ecs::hip_status(ecs::launch_kv_append(a, stream));
 }
 

@@ -1,6 +1,7 @@
 """The Python calls of decoding with trees without a GPU: what they hand to the C ABI and what they refuse, on tensors of the CPU whose addresses
 nothing looks at; the bits of a tree; and the registers of the kernels."""
 import random
+import re
 
 import numpy as np
 import pytest
@@ -166,6 +167,12 @@ def test_frequencies():
 def test_no_scratch_memory():
     found = {n: v for n, v in kernels().items() if any(x in n for x in ("kv_append", "kv_keep", "verify_tree", "attention_rows_kernel", "attention_chunk_kernel"))}
     assert len(found) > 40 and not {n: v for n, v in found.items() if v[1]}
+
+
+def test_kernels_that_calls_reach():
+    """Trees in heads of more than 128 have 64 rows to a workgroup: the library holds no kernel of 128 for them."""
+    found = {tuple(map(int, m)) for n in kernels() for m in re.findall(r"attention_chunk_kernelILi(\d+)ELi(\d+)ELb1ELi(\d)EE", n)}
+    assert found == {(bits, dim, on_keys) for bits in (16, 8, 4) for dim in range(32, 257, 32) for on_keys in (1, 2) if dim <= 128 or on_keys == 2}
 
 
 @pytest.mark.parametrize("bits,heads,q_heads,dim", [(16, 32, 32, 128), (8, 8, 64, 128), (4, 2, 16, 96), (16, 1, 8, 256), (8, 1, 200, 64), (4, 40, 40, 64)])
