@@ -298,7 +298,7 @@ int ecspmv_kv_append(const ecspmv_kv_cache_t *cache, const ecspmv_view_t *k, con
  * page table.  All device int32: first (batch; the key of node 0), path (`nodes` to a row, rows path_stride apart), accepted (batch; counts
  * beyond 0 ... nodes as these), page_table (max_pages to a row, rows table_stride apart).  path[b][i] >= i, as it is on a path whose nodes
  * come after their parents; a row with a smaller one, or whose place or new place is in no page of the cache, stays where it is.  A page that
- * rows move in is one sequence's alone, and each cache is given once.
+ * rows move in is one sequence's alone, and no two caches share memory (rows of all of them move at the same time).
  * One launch per 64 caches (none for no sequences, nodes, pages or caches). */
 typedef struct ecspmv_keep_t {
     uint32_t struct_size;                   /* sizeof(ecspmv_keep_t) as the caller compiled it */

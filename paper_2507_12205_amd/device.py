@@ -194,12 +194,15 @@ def rotary_frequency(pairs: int, base: float = 10000.0, device="cuda:0") -> torc
 
 
 class KvCaches:
-    """The caches of a model's layers, alike but for their memory, each of them once, for kv_keep()."""
+    """The caches of a model's layers, alike but for their memory, which none shares with another, for kv_keep()."""
 
     def __init__(self, caches):
         self.caches = list(caches)
         assert self.caches and all((c.bits, c.pages, c.heads, c.page_size, c.head_dim, c.device) == self._shape() for c in self.caches)
-        assert len({c.k.data_ptr() for c in self.caches}) == len({c.v.data_ptr() for c in self.caches}) == len(self.caches)          # each of them once
+        # rows of different caches move at the same time: no two of their tensors, which are contiguous, overlap
+        tensors = [t for c in self.caches for t in ((c.k, c.v) if c.bits == 16 else (c.k, c.v, c.k_step, c.v_step))]
+        spans = sorted((t.data_ptr(), t.data_ptr() + t.nbytes) for t in tensors)
+        assert all(end <= start for (_, end), (start, _) in zip(spans, spans[1:]))
         self.device, self.descs = self.caches[0].device, B.cache_array([c.desc for c in self.caches])
 
     def _shape(self):

@@ -101,6 +101,29 @@ def test_keep(calls, devices):
     assert not calls
 
 
+def test_caches_that_share_memory(devices):
+    """Rows of different caches move at the same time: caches that overlap are refused, by whatever tensors; neighbours are not."""
+    def at(k, v, k_step=None, v_step=None):
+        c = cache(*k.shape)
+        c.device, c.k, c.v = 0, k, v
+        if k_step is not None:
+            c.bits, c.k_step, c.v_step = 8, k_step, v_step
+        return c
+    k, v = (torch.zeros((24, 2, 16, 64), dtype=F16) for _ in range(2))
+    D.KvCaches([at(k[:8], v[:8]), at(k[8:16], v[16:]), at(k[16:], v[8:16])])
+    D.KvCaches([at(k[8 * i:8 * i + 8], k[8 * j:8 * j + 8]) for i, j in ((0, 2),)])
+    for caches in ([at(k[:8], v[:8]), at(k[4:12], v[8:16])], [at(k[:8], v[:8]), at(k[8:16], v[7:15])], [at(k[:8], v[:8]), at(v[:8], k[8:16])],
+                   [at(k[:8], k[:8])], [at(k[:8], v[:8]), at(k[8:16], v[8:16]), at(k[16:], k[15:23])]):
+        with pytest.raises(AssertionError):
+            D.KvCaches(caches)
+    k, v = (torch.zeros((16, 2, 16, 64), dtype=torch.int8) for _ in range(2))
+    ks, vs = (torch.zeros((16, 2, 16)) for _ in range(2))
+    D.KvCaches([at(k[:8], v[:8], ks[:8], vs[:8]), at(k[8:], v[8:], ks[8:], vs[8:])])
+    for steps in ((ks[:8], vs[8:]), (ks[8:], ks[:8]), (ks[7:15], vs[8:]), (ks[8:], vs[1:9])):
+        with pytest.raises(AssertionError):
+            D.KvCaches([at(k[:8], v[:8], ks[:8], vs[:8]), at(k[8:], v[8:], *steps)])
+
+
 def test_attention(calls, devices, monkeypatch):
     monkeypatch.setattr(D.B, "ecspmv_attention_tree_workspace", lambda *a: 256)
     monkeypatch.setattr(D, "_workspace", lambda n, beside, stream: torch.zeros(n, dtype=torch.uint8))
