@@ -202,6 +202,8 @@ int ecspmv_kv_append(const ecspmv_kv_cache_t *cache, const ecspmv_view_t *k, con
     if ((s = check_view(k, a.k, a.k_wide)) || (s = check_view(v, a.v, a.v_wide))) return s;
     if (t.q_heads && ((s = check_view(&t.q, a.q, a.q_wide)) || (s = check_view(&t.q_out, a.q_out, a.q_out_wide)))) return s;
     if (t.q_heads && !spread_out(t.q_out, tokens, t.q_heads)) return ECSPMV_ERR_INVALID;
+    // (other workgroups read k and v while q_out is written)
+    if (t.q_heads && (t.q_out.data == k->data || t.q_out.data == v->data)) return ECSPMV_ERR_INVALID;
     if (!d_slots || !aligned(d_slots, 8)) return ECSPMV_ERR_INVALID;
     if (t.rotary_dim && (!t.frequency || !aligned(t.frequency, 8) || !t.position || !aligned(t.position, 4))) return ECSPMV_ERR_INVALID;
     if (tokens > 1 << 27 || t.q_heads > 65535 || ((uint64_t)tokens + 16u) * (2u * a.cache.heads + (uint32_t)t.q_heads) > 0x7fffffffu)

@@ -155,3 +155,27 @@ def test_refusals(tmp_path):
     assert got["verify work"] == [2 * (8 + 16 + 16), 1, [SMALL, 0], [INVALID, 0], [INVALID, 0]]
     assert got["stream"] == [[0x1000, 0x100], [0x2000, 0x200], [0, 0x100], HIP] * 4
     assert all(g < 1 << 32 for g in got["grid"])
+
+
+OVERLAP = r"""
+import ctypes
+c = B.KvCacheDesc(ctypes.sizeof(B.KvCacheDesc), bits=16, pages=4, heads=2, page_size=16, head_dim=64, k=0x100000, v=0x200000)
+def append(q, q_out, q_heads=2):
+    r = B.RotaryDesc(ctypes.sizeof(B.RotaryDesc), rotary_dim=64, neighbours=0, q_heads=q_heads, frequency=0xA00000, position=0xB00000, q=q, q_out=q_out)
+    for name in ("q", "q_out"):
+        for what, stride in (("token", 128), ("head", 64), ("dim", 1)):
+            setattr(r, f"{name}_{what}_stride", stride)
+    try:
+        B.ecspmv_kv_append(c, B.View(0x500000, 128, 64, 1), B.View(0x600000, 128, 64, 1), 0x800000, 5, r, 0x1000)
+    except B.EcspmvError as e:
+        return e.status
+    return 0
+print(json.dumps([append(*a) for a in arg]))
+"""
+
+
+def test_queries_do_not_go_where_keys_or_values_are_read(tmp_path):
+    """q_out is written while others still read k and v; q may lie there, q_out may be q, and without queries it is not looked at."""
+    k, v, q, out = 0x500000, 0x600000, 0x700000, 0x710000
+    calls = [(q, out), (q, q), (k, out), (v, out), (q, k), (q, v), (k, k), (v, v), (q, k, 0)]
+    assert standin.run(tmp_path, OVERLAP, calls) == [0, 0, 0, 0, INVALID, INVALID, INVALID, INVALID, 0]
