@@ -50,8 +50,9 @@ __device__ __forceinline__ void store_eight(const View &v, uint32_t wide, uint32
 }
 
 // The codes and the step of a row that 2^lanes_shift neighbouring lanes have, N values each in pieces of eight that start at at[...] of the row (a piece
-// that starts beyond it is none), to where they lie; `valid`: whether the row has a place.  All lanes of the row come here.  WIDE: values need not be FP16
-// values, so that the lowest one is rounded to what is kept of it; of FP16 values both give the same bits.
+// that starts beyond it is none), to where they lie; `valid`: whether the row has a place.  All lanes of the row come here.  WIDE: values are not FP16
+// values, so that the lowest one is rounded to what is kept of it; and a 4-bit step is the range times 1/15 in FP32, which may be its last
+// place away from the range divided by 15, and saves the division.
 template <int BITS, bool WIDE, int N>
 __device__ __forceinline__ void store_codes(float (&x)[N], uint8_t *codes, uint8_t *steps, const uint32_t (&at)[N / 8], uint32_t dim, uint32_t lanes_shift,
                                             bool valid)
@@ -85,11 +86,15 @@ __device__ __forceinline__ void store_codes(float (&x)[N], uint8_t *codes, uint8
         if (valid && at[0] == 0) *reinterpret_cast<float *>(steps) = step;
     } else {
         const uint32_t low_bits = to_half(low);
+        uint32_t step_bits;
         if constexpr (WIDE) {
             low = to_float(low_bits);
-            high = fmaxf(high, low);                                       // (rounded up, the lowest value may be above the largest)
+            float step = fmaxf(high - low, 0.0f) * (1.0f / 15.0f);         // (rounded up, the lowest value may be above the largest)
+            asm("" : "+v"(step));                                          // (a product in FP32: not one that is rounded to FP16 at once)
+            step_bits = to_half(step);
+        } else {
+            step_bits = to_half((high - low) / 15.0f);
         }
-        uint32_t step_bits = to_half((high - low) / 15.0f);
         if (fmaf(15.0f, to_float(step_bits), low) >= 65520.0f) --step_bits;  // (rounded up, and the last code would be infinity in FP16)
         const float step = to_float(step_bits), inv = step > 0.0f ? 1.0f / step : 0.0f;
 #pragma unroll
