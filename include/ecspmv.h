@@ -280,7 +280,8 @@ int ecspmv_kv_read(const ecspmv_kv_cache_t *cache, const int64_t *d_slots, int64
  *   (a cos t - b sin t, a sin t + b cos t),   t = position[token] * frequency[pair],
  * pair i being values i and i + rotary_dim / 2, or with `neighbours` values 2 i and 2 i + 1.  The angle is worked out in 64 bits, the
  * rotation in 32; what comes of it is rounded once, to FP16 or to a code (in 8 and 4 bits what is beyond FP16's largest value counts as
- * that).  Values go as they are; queries go to q_out, which may be q itself and overlaps nothing otherwise (a stride of 0
+ * that).  Values, and keys that are not rotated, become what ecspmv_kv_write makes of them; in 4 bits the step of a rotated key is its range times 1 / 15
+ * in FP32, which rounds to FP16 as the range divided by 15 does or, where that lies between two FP16 values, to the other one.  Queries go to q_out, which may be q itself and overlaps nothing otherwise (a stride of 0
  * from one of its values to another is refused, and so is a q_out that starts where k or v does), also those of tokens that d_slots leaves out.
  * rotary_dim: even, at most head_dim, 0 for no rotation; q_heads: 0 for no queries.  One launch (none for no tokens). */
 typedef struct ecspmv_rotary_t {

@@ -245,7 +245,7 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(const AppendArgs a)
         }
         if constexpr (BITS < 16)
             if (!of_q)
-                ecs::store_codes<BITS, true>(x, codes, (r.of_v ? a.cache.v_step : a.cache.k_step) + 4u * place, at, dim, a.lanes_shift, valid);
+                ecs::store_codes<BITS, true>(x, codes, (r.of_v ? a.cache.v_step : a.cache.k_step) + 4u * place, at, dim, a.lanes_shift, valid, !r.of_v && pairs != 0u);
     }
 }
 

@@ -50,12 +50,12 @@ __device__ __forceinline__ void store_eight(const View &v, uint32_t wide, uint32
 }
 
 // The codes and the step of a row that 2^lanes_shift neighbouring lanes have, N values each in pieces of eight that start at at[...] of the row (a piece
-// that starts beyond it is none), to where they lie; `valid`: whether the row has a place.  All lanes of the row come here.  WIDE: values are not FP16
-// values, so that the lowest one is rounded to what is kept of it; and a 4-bit step is the range times 1/15 in FP32, which may be its last
-// place away from the range divided by 15, and saves the division.
+// that starts beyond it is none), to where they lie; `valid`: whether the row has a place.  All lanes of the row come here.  WIDE: values need not be FP16
+// values, so that the lowest one is rounded to what is kept of it.  `turned`: a row that has been rotated; its 4-bit step is the range times 1/15, as a
+// program gets it that divides by a number in FP32 tensor operations (where the quotient lies between two FP16 values, it may be the other one).
 template <int BITS, bool WIDE, int N>
 __device__ __forceinline__ void store_codes(float (&x)[N], uint8_t *codes, uint8_t *steps, const uint32_t (&at)[N / 8], uint32_t dim, uint32_t lanes_shift,
-                                            bool valid)
+                                            bool valid, bool turned = false)
 {
     float low = 65504.0f, high = -65504.0f;
 #pragma unroll
@@ -89,9 +89,10 @@ __device__ __forceinline__ void store_codes(float (&x)[N], uint8_t *codes, uint8
         uint32_t step_bits;
         if constexpr (WIDE) {
             low = to_float(low_bits);
-            float step = fmaxf(high - low, 0.0f) * (1.0f / 15.0f);         // (rounded up, the lowest value may be above the largest)
-            asm("" : "+v"(step));                                          // (a product in FP32: not one that is rounded to FP16 at once)
-            step_bits = to_half(step);
+            const float range = fmaxf(high - low, 0.0f);                   // (rounded up, the lowest value may be above the largest)
+            float product = range * (1.0f / 15.0f);
+            asm("" : "+v"(product));                                       // (a product in FP32: not one that is rounded to FP16 at once)
+            step_bits = to_half(turned ? product : range / 15.0f);
         } else {
             step_bits = to_half((high - low) / 15.0f);
         }

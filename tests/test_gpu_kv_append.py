@@ -162,6 +162,37 @@ def test_without_a_turn_it_is_kv_write(rotary, bits):
     assert torch.equal(out, q)
 
 
+@pytest.mark.parametrize("rotary,neighbours", [(0, False), (16, False), (16, True), (10, False)])
+def test_without_a_turn_it_is_kv_write_in_4_bits(rotary, neighbours):
+    """The step is the range divided by 15 in FP32 and then rounded to FP16; of keys that are rotated, if by nothing, the range times 1/15.  Rows whose range is
+    15 times the middle of two FP16 values, for which the two differ in 439 of 1024 cases, and random ones."""
+    import torch
+    from paper_2507_12205_amd import device as D
+    n, rng = 4096, np.random.default_rng(1)
+    a, b = (D.kv_cache(n // 16, 4, 16, 16, 4) for _ in range(2))
+    x = rng.normal(size=(2, n, 4, 16)) * rng.choice([1e-3, 1.0, 30.0], size=(2, n, 4, 1))
+    spread = 15 * (2 * np.arange(1024, 2048) + 1)            # 16 bits: the ten upper ones above zero, the six lower ones below
+    high, low = (spread >> 6 << 6) * 2.0 ** -14, -(spread & 63) * 2.0 ** -14
+    ties = low[:, None, None] + (high - low)[:, None, None] * rng.random((1024, 4, 16))
+    ties[..., 3], ties[..., 11] = low[:, None], high[:, None]
+    x[0, :1024], x[1, 1024:2048] = ties, ties
+    k, v = (torch.from_numpy(t.astype(np.float16)).cuda() for t in x)
+    assert (k[:1024].float().amax(-1) - k[:1024].float().amin(-1) == torch.from_numpy(spread * 2.0 ** -14).cuda()[:, None]).all()
+    slots = torch.randperm(n, device="cuda")
+    D.kv_write(a, k, v, slots)
+    D.kv_append(b, k, v, slots, torch.zeros(n, dtype=torch.int32, device="cuda"), D.rotary_frequency(rotary // 2), neighbours=neighbours)
+    assert torch.equal(a.v, b.v) and torch.equal(a.v_step, b.v_step)
+    if rotary == 0:
+        assert torch.equal(a.k, b.k) and torch.equal(a.k_step, b.k_step)
+    else:
+        low, high = k.float().amin(-1), k.float().amax(-1)
+        step = ((high - low) * torch.tensor(1 / 15, device="cuda")).half()
+        want = torch.stack([step, low.half()], -1)[slots.argsort()].view(n // 16, 16, 4, 2).transpose(1, 2)
+        assert torch.equal(b.k_step, want)
+        apart = (a.k_step[..., 0].view(torch.int16) - b.k_step[..., 0].view(torch.int16)).abs()          # neighbouring FP16 values
+        assert apart.max() == 1 and torch.equal(a.k_step[..., 1], b.k_step[..., 1])
+
+
 @pytest.mark.parametrize("rotary,neighbours", [(64, False), (64, True), (20, False), (62, False)])
 @pytest.mark.parametrize("kind", ["plain", "columns"])
 def test_queries_in_place(kind, rotary, neighbours):
