@@ -347,8 +347,8 @@ int ecspmv_attention(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *a
  * for each token of q, rows seen_stride >= ceil(min(max_new, tokens) / 32) apart; bits of new tokens that there are none of count for
  * nothing).  Where kv_len is less than the number of new tokens, the first ones have no keys.  Weights meet V in 22 bits where a head of the cache has
  * up to 64 rows (max_new times the heads of its group) over 16 bits with a head_dim of up to 128, or 32 over the others, and beyond that in 11.  A stride
- * of 0 from one value of out to another is refused.  Long sequences of several are split by their
- * lengths, and the workspace is another: _tree_workspace for one call; what ecspmv_attention_workspace_most says holds here too. */
+ * of 0 from one value of out to another is refused.  Up to 64 sequences are split by their lengths, more of them all alike, and the workspace is
+ * another: _tree_workspace for one call; what ecspmv_attention_workspace_most says holds here too. */
 int ecspmv_attention_tree_workspace(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *a, size_t *bytes);
 int ecspmv_attention_tree(const ecspmv_kv_cache_t *cache, const ecspmv_attention_t *a, const uint32_t *d_seen, int64_t seen_stride, void *d_work,
                           size_t work_bytes, void *stream);
@@ -362,7 +362,7 @@ int ecspmv_attention_tree(const ecspmv_kv_cache_t *cache, const ecspmv_attention
  * w = max(target[n] - draft[n], 0) after a refusal (target[n] where that leaves nothing) and w = target[n] without one.
  * Differences and sums are in 64 bits.  accepted[b] = n; tokens[b][0 ... drafts] (device int32) = the accepted drafts, the next token,
  * then -1 (also in the next token's place if target[n] has nothing above 0).  A drafted token outside [0, vocab) is
- * refused.  *_seq, *_row: strides in elements from one sequence, resp. row, to the next. */
+ * refused.  accepted may be count; otherwise outputs overlap nothing.  *_seq, *_row: strides in elements from one sequence, resp. row, to the next. */
 typedef struct ecspmv_verify_t {
     uint32_t struct_size;                   /* sizeof(ecspmv_verify_t) as the caller compiled it */
     int32_t  batch, drafts, vocab;          /* drafts >= 0; vocab in [1, 2^20] */

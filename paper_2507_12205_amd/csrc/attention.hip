@@ -683,7 +683,7 @@ __global__ __launch_bounds__(256, BITS == 4 ? (DP > 128 ? 2 : DP > 64 ? 3 : 4) :
 // that of the rounded ones.  Trees of up to 64 rows wait for the keys and values of FP16, so that a second part costs them nothing there, and they have it
 // (64 nodes of heads of 128, one tree over 32768 keys 131.3 / 132.5, four over 8000 112.2 / 111.1).  It is not free with 257 nodes (16000 keys, 32/8 heads, 95.5 /
 // 124.4), heads of 256 (192 nodes over 8000 45.9 / 50.3) and codes (four of 64 over 8000, 8 bits 83.5 / 93.9, 4 bits 77.6 / 87.4; sixteen of up to 16 over up to
-// 8192, 8 bits, 76.0 / 83.8), whose values are rounded to 2^-8 and 2^-5 of the largest of their row when they are written.
+// 8192, 8 bits, 76.0 / 83.8), which are rounded by up to 2^-8 of their row's largest value, 2^-5 of its range in 4 bits, when they are written.
 //
 // 2048 tokens over 4096 keys, 32 heads of 128, FP16: 121 - 127 us, 810 - 850 TFLOP/s of the products that the mask leaves (a large matrix
 // product alone reaches 1140 - 1229 here).  A wavefront's products and its softmax follow one another, and those of the two wavefronts of a SIMD overlap only in

@@ -7,7 +7,9 @@
 // neighbouring tokens and some heads of them, in q the heads of a token after one another, as they lie, in k and v (and in q that lies as columns)
 // the tokens of a head, as they come to lie in the cache.  The turns of these tokens are worked out once, by all of its threads, and lie in LDS for all of
 // its rows.  What bounds it is memory: 8191 tokens, 64/8 heads of 128, 16 bits 77 us, 336 MB at 4.3 TB/s, 8 bits 81, 4 bits 79 (eight values a lane
-// with their partners' from another lane, q in the order of k and v: 95, 99, 99); 8 tokens, 12/12 heads of 64 as columns, 4.0.
+// with their partners' from another lane, q in the order of k and v: 95, 99, 99); 8 tokens, 12/12 heads of 64 as columns, 4.0.  In heads of 80 five of
+// a row's eight lanes have values: 8191 tokens, 32/32 heads, 16 bits 84 us, 252 MB at 3.0 TB/s; with 20 of the 40 pairs 98, as partners then come
+// through LDS, value by value (kAnywhere; where the pairs' number is no multiple of 8).
 //
 // An angle is a product in 64 bits (of position 10^6, 32 bits would leave 0.03 of an angle), and so are its cosine and sine, which are then
 // rounded to 32; the rotated values stay in 32 bits until they are rounded once, to FP16 or to a code.  The two products of a pair are
@@ -108,7 +110,9 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(const AppendArgs a)
 
     // Where tokens lie in columns, a thread brings one value of 16 tokens, and the rows of a pass are put together in LDS (rows of 16-byte pieces, one more
     // than they need).  By rows, a lane reads its values one by one: 64/8 heads of 128, 16 bits, 8191 tokens so 158 us, 8184 by columns 108, 16/16 heads of 256,
-    // 4001 tokens 125, 4000 62.  Columns that start off 16 bytes are read by rows (by columns all the same 263 for 176: 8191 tokens, up to 32 heads).
+    // 4001 tokens 125, 4000 62.  A run has 32 bytes of each line of 128, and three barriers to a pass: wavefronts wait for 56 % of their time (rows: 77 us; a
+    // run of 64 tokens would take whole lines, and four times the LDS for its turns).  Columns that start off 16 bytes are read by rows, value by value, 4.6
+    // times the memory instructions (by columns all the same 263 for 176: 8191 tokens, up to 32 heads).
     const bool columns = COLUMNS && (of_q ? a.q_columns : a.kv_columns), columns_out = of_q && columns && a.q_out_columns;
     const uint32_t tile_row = 32u << a.lanes_shift, tile_step = tile_row + 16u;         // bytes
     uint8_t *tile = reinterpret_cast<uint8_t *>(turns + 2u * pad * (1u << a.run_shift));

@@ -6,7 +6,7 @@
 // reads or writes these places, and there is nothing to wait for.  Bits are copied as they are.
 //
 // What bounds it are four trips to memory, one after the other (how many and where, pages, rows, their new places), and rows that lie apart: five
-// rows of 40 heads of 128 in 40 layers, 16 bits, 4.5 us (16 MB moved); four of 8 heads of 128 of 32 sequences in 32 layers, 4 bits, 7.9 (65536
+// rows of 40 heads of 128 in 40 layers, 16 bits, 4.5 us (4 MB read and 4 written); four of 8 heads of 128 of 32 sequences in 32 layers, 4 bits, 7.9 (65536
 // rows of 64 and 4 bytes; several rows at once in a workgroup, all read before any is written: 8.3).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
