@@ -179,6 +179,32 @@ def test_nodes_that_were_left_out(new, total, bits):
         assert np.array_equal(run(torch, D, *made, words), clean)
 
 
+@pytest.mark.parametrize("new,total", [(6, 90), (17, 90), (30, 400), (30, 3000), (60, 400)])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_infinities_that_rows_see(new, total, dim):
+    """A value's infinity is the result of the rows that see it, whatever its weight, zero in FP16 or with a second part below zero; the other values are a mean
+    of finite ones.  A key before the tree and a node, one that counts and one that does not."""
+    import torch
+    from paper_2507_12205_amd import device as D
+    cache, q, start, lens, table = made = make(torch, D, [new], [total], 4, 2, dim, 16, 16, seed=4)
+    seen = trees(np.random.default_rng(new), [new])
+    words = words_of(seen)
+    clean = run(torch, D, *made, words)
+    for at in (3, total - new - 1, total - new + new // 2):
+        page, off = int(table[0, at // 16]), at % 16
+        sees = seen[0][:, at - (total - new)] if at >= total - new else np.ones(new, bool)
+        assert sees.any()
+        for odd in (float("inf"), float("-inf"), float("nan")):
+            keep = cache.v[page, 1, off, 7].clone()
+            cache.v[page, 1, off, 7] = odd
+            got = run(torch, D, *made, words)
+            cache.v[page, 1, off, 7] = keep
+            assert np.array_equal(got[~sees], clean[~sees]) and np.array_equal(got[:, :2], clean[:, :2])
+            assert np.array_equal(got[sees][:, 2:, 7], np.full((sees.sum(), 2), odd), equal_nan=True)
+            rest = [d for d in range(dim) if d != 7]
+            assert np.array_equal(got[..., rest], clean[..., rest])
+
+
 @pytest.mark.parametrize("bits", [8, 4])
 @pytest.mark.parametrize("new,total", [(6, 70), (30, 200), (40, 200), (200, 330), (7, 3000), (100, 3000)])
 def test_steps_that_are_none(new, total, bits):
